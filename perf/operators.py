@@ -1,0 +1,635 @@
+"""Operators around one layer's attention: the calls, their plain forms and their definitions.
+
+Kinds:
+
+  norm      a block's output, normalised, gated and scaled, added to the residual
+            stream, and the norm with its modulation that feeds the next block
+  norm_grad its backward pass: gradients of the stream, of the block's output and of
+            every vector that took part
+  rotary    rotary positions on all heads of a tensor, or the transpose (its gradient)
+  append    new tokens of a batch of requests: their cache slots from the requests'
+            lengths, queries rotated, keys rotated into their slots, values beside them
+  shared    attention of a batch of requests over one shared prefix and each request's
+            own keys, with its log-sum-exp
+
+``own`` selects this package's kernels; otherwise elementary torch operations in fp32
+(angles in fp64), rounded once at the end.
+"""
+
+import math
+
+import torch
+
+own = False
+
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+DTYPES = {"bf16": BF16, "f32": F32}
+SIZE = {"bf16": 2, "f32": 4}
+EPS = 1e-6
+AXES = {128: (22, 21, 21), 64: (12, 10, 10)}  # pairs that turn with frame, height and width
+
+
+def listed():
+    return [
+        # a few tokens through a block with norms on both sides and a constant residual scale: all latency
+        {"name": "norm_tokens", "kind": "norm", "rows": 16, "cols": 5120, "x": "bf16", "y": "bf16", "h": "bf16",
+         "norm": "rms", "weight": True, "bias": False, "post": "rms", "gate": False, "modulate": False, "group": 0},
+        # a chunk of three latent frames at the 1.3B shape, one modulation per frame, the stream in fp32
+        {"name": "norm_chunk_1p3b", "kind": "norm", "rows": 4680, "cols": 1536, "x": "f32", "y": "bf16", "h": "bf16",
+         "norm": "layer", "weight": False, "bias": False, "post": "none", "gate": True, "modulate": True,
+         "group": 1560},
+        # the same chunk at the 14B shape, the stream in bf16, the block's output normalised before its gate
+        {"name": "norm_chunk_14b", "kind": "norm", "rows": 4680, "cols": 5120, "x": "bf16", "y": "bf16", "h": "bf16",
+         "norm": "layer", "weight": True, "bias": True, "post": "rms", "gate": True, "modulate": True, "group": 1560},
+        # the backward pass of the 1.3B chunk
+        {"name": "norm_grad_1p3b", "kind": "norm_grad", "rows": 4680, "cols": 1536, "x": "f32", "y": "bf16",
+         "h": "bf16", "norm": "layer", "weight": False, "bias": False, "post": "none", "gate": True,
+         "modulate": True, "group": 1560},
+        # the backward pass at the 14B shape of a layer with weights and norms on both sides
+        {"name": "norm_grad_14b", "kind": "norm_grad", "rows": 4680, "cols": 5120, "x": "bf16", "y": "bf16",
+         "h": "bf16", "norm": "rms", "weight": True, "bias": False, "post": "rms", "gate": True, "modulate": False,
+         "group": 0},
+        # the gradient of a 14B chunk's rotated queries: frame, height and width in interleaved pairs
+        {"name": "rotary_grad_14b", "kind": "rotary", "rows": 4680, "heads": 40, "head_dim": 128, "rotary_dim": 128,
+         "axes": 3, "interleaved": True, "scaling": "none", "x": "bf16", "inverse": True},
+        # one token each of 64 requests far into a long context, scaled, pairs in halves of the head
+        {"name": "append_tokens", "kind": "append", "requests": 64, "most": 1, "pad": 3, "capacity": 1024,
+         "sink": 0, "window": 0, "first": 1000003, "heads": 32, "kv_heads": 8, "head_dim": 128, "rotary_dim": 128,
+         "axes": 1, "interleaved": False, "scaling": "parts"},
+        # a latent frame of four forked rollouts into their rings of sink and recent keys
+        {"name": "append_frames", "kind": "append", "requests": 4, "most": 1560, "pad": 0, "capacity": 4680,
+         "sink": 1560, "window": 3120, "first": 0, "heads": 12, "kv_heads": 12, "head_dim": 128, "rotary_dim": 128,
+         "axes": 3, "interleaved": True, "scaling": "none"},
+        # the smallest batch of the parity tests' head shape: all latency
+        {"name": "shared_tiny", "kind": "shared", "requests": 2, "most": 1, "pad": 0, "prefix": 256, "capacity": 64,
+         "heads": 2, "kv_heads": 2, "head_dim": 64},
+        # single tokens of 64 requests behind one long prefix
+        {"name": "shared_tokens", "kind": "shared", "requests": 64, "most": 1, "pad": 0, "prefix": 32760,
+         "capacity": 1024, "heads": 12, "kv_heads": 12, "head_dim": 128},
+        # a few tokens each of 24 requests, four query heads to a key head, padded to a fixed count of rows
+        {"name": "shared_grouped", "kind": "shared", "requests": 24, "most": 5, "pad": 7, "prefix": 16381,
+         "capacity": 512, "heads": 32, "kv_heads": 8, "head_dim": 128},
+        # four rollouts forked from one history of seven chunks, a latent frame each
+        {"name": "shared_frames", "kind": "shared", "requests": 4, "most": 1560, "pad": 0, "prefix": 32760,
+         "capacity": 4680, "heads": 12, "kv_heads": 12, "head_dim": 128},
+    ]
+
+
+# a drawn case does at most the operations of the largest listed one, and its plain form's
+# weights take at most as much room
+MOST_ATTN = 4 * 4 * 1560 * (32760 + 4680) * 1536
+MOST_WEIGHTS = 4 * 1560 * 12 * (32760 + 4680)
+MOST_VALUES = 4680 * 5120
+MOST_KEYS = 40_000_000
+
+
+def _log(rng, lo, hi, step=1):
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return min(hi, max(lo, int(round(v / step)) * step))
+
+
+def _heads(rng):
+    kv = rng.choice((1, 2, 3, 4, 8, 12, 16))
+    return kv * rng.choice((1, 1, 2, 3, 4, 8) if kv < 8 else (1, 1, 2, 4)), kv
+
+
+def draw(rng):
+    kind = rng.choice(("norm", "norm_grad", "rotary", "append", "shared", "shared", "shared"))
+    if kind in ("norm", "norm_grad"):
+        while True:
+            rows, cols = _log(rng, 1, 4680), _log(rng, 64, 8192, 8)
+            if rows * cols <= MOST_VALUES:
+                break
+        gate, modulate = rng.random() < 0.6, rng.random() < 0.6
+        return {"kind": kind, "rows": rows, "cols": cols, "x": rng.choice(("bf16", "f32")),
+                "y": rng.choice(("bf16", "bf16", "f32", "none")), "h": rng.choice(("bf16", "bf16", "f32")),
+                "norm": rng.choice(("layer", "rms")), "weight": rng.random() < 0.5, "bias": rng.random() < 0.3,
+                "post": rng.choice(("none", "layer", "rms")), "gate": gate, "modulate": modulate,
+                "group": rng.choice((0, 1 + rows // 3, rng.randint(1, max(1, rows // 8)))) if gate or modulate else 0}
+    head_dim = rng.choice((64, 128, 128))
+    axes = rng.choice((1, 1, 3))
+    turned = {"head_dim": head_dim, "rotary_dim": head_dim if axes == 3 else rng.choice((head_dim, head_dim // 2)),
+              "axes": axes, "interleaved": rng.random() < 0.5,
+              "scaling": "none" if axes == 3 else rng.choice(("none", "linear", "base", "parts"))}
+    if kind == "rotary":
+        heads = rng.randint(1, 40)
+        rows = _log(rng, 1, min(16384, MOST_VALUES // (heads * head_dim)))
+        return {"kind": kind, "rows": rows, "heads": heads, **turned, "x": rng.choice(("bf16", "f32")),
+                "inverse": rng.random() < 0.5}
+    while True:
+        heads, kv = _heads(rng)
+        requests = _log(rng, 1, 128)
+        most = rng.choice((1, rng.randint(1, 8), _log(rng, 1, 1560)))
+        if kind == "append":
+            capacity = max(most, _log(rng, 16, 8192))
+            ring = rng.random() < 0.4
+            if (requests * most * heads * head_dim <= MOST_VALUES
+                    and requests * capacity * kv * head_dim <= 4 * MOST_KEYS):
+                sink = rng.randint(0, capacity // 4) if ring else 0
+                return {"kind": kind, "requests": requests, "most": most, "pad": rng.choice((0, 0, rng.randint(1, 9))),
+                        "capacity": capacity, "sink": sink, "window": capacity - sink if ring else 0,
+                        "first": 0 if axes == 3 else rng.choice((0, _log(rng, 1, 2000000))), "heads": heads,
+                        "kv_heads": kv, **turned}
+            continue
+        prefix = rng.choice((_log(rng, 64, 98280), _log(rng, 64, 98280), 0))
+        capacity = _log(rng, 16, 8192)
+        rows = requests * most
+        if (rows * heads * (prefix + capacity) <= MOST_WEIGHTS // 2
+                and 4 * rows * heads * head_dim * (prefix + capacity) <= MOST_ATTN // 2
+                and (prefix + requests * capacity) * kv * head_dim <= 4 * MOST_KEYS):
+            return {"kind": kind, "requests": requests, "most": most, "pad": rng.choice((0, 0, rng.randint(1, 9))),
+                    "prefix": prefix, "capacity": capacity, "heads": heads, "kv_heads": kv, "head_dim": head_dim}
+
+
+# ------------------------------------------------------------------ inputs
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1_000_003 * int(seed) + 29)
+    return g
+
+
+def _randn(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device="cuda", dtype=F32).to(dtype)
+
+
+def _randint(g, lo, hi, *shape):
+    return torch.randint(lo, hi, shape, generator=g, device="cuda", dtype=torch.int32)
+
+
+def _lengths(c, g):
+    """Rows of each request (the first one `most`, now and then none) and their running sum."""
+    n = _randint(g, 1 if c["most"] == 1 else 0, c["most"] + 1, c["requests"])
+    n[0] = c["most"]
+    start = torch.zeros(c["requests"] + 1, dtype=torch.int32, device="cuda")
+    start[1:] = torch.cumsum(n, 0)
+    return n, start
+
+
+def _rows(c):
+    """Rows of the batch's tensors: room for every request's most, and padding."""
+    return c["requests"] * c["most"] + c["pad"]
+
+
+def _frequencies(c):
+    """Each pair's radians per position (fp64), the pairs of each axis, the axis of each pair, the factor of cos and sin."""
+    half = c["rotary_dim"] // 2
+    axes = AXES[c["rotary_dim"]] if c["axes"] == 3 else (half,)
+    base, f = 10000.0, []
+    for n in axes:
+        j = torch.arange(n, dtype=F64)
+        b = base * 8.0 ** (n / (n - 1.0)) if c["scaling"] == "base" else base
+        f.append(b ** (-j / n))
+    f = torch.cat(f)
+    amplitude = 1.0
+    if c["scaling"] == "linear":
+        f = f / 4.0
+    if c["scaling"] == "parts":  # fast pairs as they are, slow ones slowed down, a ramp between
+        lo, hi = (half * math.log(4096 / (b * 2 * math.pi)) / math.log(base) for b in (32.0, 1.0))
+        lo, hi = max(0.0, math.floor(lo)), min(float(half - 1), math.ceil(hi))
+        ramp = ((torch.arange(half, dtype=F64) - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        f = f * (1 - ramp) + f / 16.0 * ramp
+        amplitude = 0.1 * math.log(16.0) + 1.0
+    axis = torch.tensor([k for k, n in enumerate(axes) for _ in range(n)])
+    return {"f": f.cuda(), "axes": axes, "axis": axis.cuda(), "amplitude": amplitude}
+
+
+def _positions(c, g, rows):
+    if c["axes"] == 3:  # frames of 30 x 52 places from some frame of a long video on
+        r = torch.arange(rows, device="cuda", dtype=torch.int32)
+        t0 = _randint(g, 0, 400, 1)
+        return torch.stack((t0 + r // 1560, r % 1560 // 52, r % 52), dim=1).contiguous()
+    return _randint(g, 0, 200000, rows, 1)
+
+
+def _norm_inputs(c, g):
+    n, d = c["rows"], c["cols"]
+    groups = -(-n // c["group"]) if c["group"] else 1
+    s = {"x": _randn(g, n, d, dtype=DTYPES[c["x"]]), "y": None, "gate": None, "post_weight": None, "weight": None,
+         "bias": None, "scale": None, "shift": None}
+    s["x"] += _randn(g, 1, d, dtype=s["x"].dtype)  # channels are not centred
+    if c["y"] != "none":
+        s["y"] = (_randn(g, n, d) * 0.7).to(DTYPES[c["y"]])
+        if c["gate"]:
+            s["gate"] = _randn(g, groups, d) * 0.5
+        if c["post"] != "none":
+            s["post_weight"] = 1 + 0.2 * _randn(g, d)
+    if c["weight"]:
+        s["weight"] = 1 + 0.2 * _randn(g, d)
+    if c["bias"]:
+        s["bias"] = 0.1 * _randn(g, d)
+    if c["modulate"]:
+        s["scale"], s["shift"] = _randn(g, groups, d) * 0.3, _randn(g, groups, d) * 0.3
+    s["alpha"] = 0.5
+    return s
+
+
+def prepare(case, seed):
+    c, g = case, _gen(seed)
+    if c["kind"] == "norm":
+        return {"c": c, **_norm_inputs(c, g)}
+    if c["kind"] == "norm_grad":
+        s = {"c": c, **_norm_inputs(c, g)}
+        s["d_h"] = _randn(g, c["rows"], c["cols"], dtype=DTYPES[c["h"]])
+        s["d_x"] = _randn(g, c["rows"], c["cols"], dtype=DTYPES[c["x"]])
+        return s
+    if c["kind"] == "rotary":
+        return {"c": c, **_frequencies(c), "positions": _positions(c, g, c["rows"]),
+                "x": _randn(g, c["rows"], c["heads"] * c["head_dim"], dtype=DTYPES[c["x"]])}
+    rows, hidden, kv_hidden = _rows(c), c["heads"] * c["head_dim"], c["kv_heads"] * c["head_dim"]
+    n, start = _lengths(c, g)
+    if c["kind"] == "append":
+        before = _randint(g, 0, 3 * c["capacity"], c["requests"]) if c["window"] else (
+            _randint(g, 0, 1 << 30, c["requests"]) % (c["capacity"] - n + 1).to(torch.int32))
+        positions = _positions(c, g, rows) if c["axes"] == 3 else None
+        return {"c": c, **_frequencies(c), "positions": positions, "start": start, "before": before,
+                "q": _randn(g, rows, hidden, dtype=BF16),
+                "k": _randn(g, rows, kv_hidden, dtype=BF16), "v": _randn(g, rows, kv_hidden, dtype=BF16),
+                "k_cache": torch.zeros(c["requests"], c["capacity"], kv_hidden, dtype=BF16, device="cuda"),
+                "v_cache": torch.zeros(c["requests"], c["capacity"], kv_hidden, dtype=BF16, device="cuda"),
+                "q_out": torch.zeros(rows, hidden, dtype=BF16, device="cuda")}
+    lens = _randint(g, 0, c["capacity"] + 1, c["requests"])  # own keys, none among them now and then
+    lens[0] = c["capacity"]
+    cache = [_randn(g, c["requests"], c["capacity"], kv_hidden, dtype=BF16) for _ in range(2)]
+    prefix = [_randn(g, c["prefix"], kv_hidden, dtype=BF16) for _ in range(2)]
+    return {"c": c, "start": start, "lens": lens, "q": _randn(g, rows, hidden, dtype=BF16),
+            "k_prefix": prefix[0], "v_prefix": prefix[1], "k_cache": cache[0], "v_cache": cache[1],
+            "out": torch.zeros(rows, hidden, dtype=BF16, device="cuda"),
+            "lse": torch.zeros(c["heads"], rows, dtype=F32, device="cuda")}
+
+
+# ------------------------------------------------------------------ plain forms
+def _normed(x, kind):
+    """The normalised rows and their reciprocal deviations."""
+    if kind == "layer":
+        x = x - x.mean(dim=1, keepdim=True)
+    r = torch.rsqrt((x * x).mean(dim=1, keepdim=True) + EPS)
+    return x * r, r
+
+
+def _spread(v, c, rows):
+    """Row r's vector of a [groups, cols] tensor."""
+    if not c["group"]:
+        return v
+    return v[torch.arange(rows, device=v.device) // c["group"]]
+
+
+def _sums(v, c):
+    """Sums of the rows of each group."""
+    if not c["group"]:
+        return v.sum(dim=0, keepdim=True)
+    groups = -(-c["rows"] // c["group"])
+    v = torch.nn.functional.pad(v, (0, 0, 0, groups * c["group"] - c["rows"]))
+    return v.view(groups, c["group"], -1).sum(dim=1)
+
+
+def _plain_norm(s):
+    c, x = s["c"], s["x"].float()
+    if s["y"] is not None:
+        z = s["y"].float()
+        if c["post"] != "none":
+            z = _normed(z, c["post"])[0] * s["post_weight"]
+        if s["gate"] is not None:
+            z = z * _spread(s["gate"], c, c["rows"])
+        x = x + s["alpha"] * z
+    h = _normed(x, c["norm"])[0]
+    if s["weight"] is not None:
+        h = h * s["weight"]
+    if s["bias"] is not None:
+        h = h + s["bias"]
+    if s["scale"] is not None:
+        h = h * (1 + _spread(s["scale"], c, c["rows"])) + _spread(s["shift"], c, c["rows"])
+    return x.to(s["x"].dtype), h.to(DTYPES[c["h"]])
+
+
+def _through(gx, xhat, r, kind):
+    """The gradient through x * r (centred first for `layer`)."""
+    d = gx - xhat * (gx * xhat).mean(dim=1, keepdim=True)
+    if kind == "layer":
+        d = d - gx.mean(dim=1, keepdim=True)
+    return d * r
+
+
+def _plain_norm_grad(s):
+    c, out = s["c"], {}
+    xhat, r = _normed(s["x"].float(), c["norm"])
+    dh = s["d_h"].float()
+    du = dh
+    if s["scale"] is not None:
+        u = xhat if s["weight"] is None else xhat * s["weight"]
+        u = u if s["bias"] is None else u + s["bias"]
+        out["shift"], out["scale"] = _sums(dh, c), _sums(dh * u, c)
+        du = dh * (1 + _spread(s["scale"], c, c["rows"]))
+    if s["weight"] is not None:
+        out["weight"] = (du * xhat).sum(dim=0)
+    if s["bias"] is not None:
+        out["bias"] = du.sum(dim=0)
+    d = s["d_x"].float() + _through(du if s["weight"] is None else du * s["weight"], xhat, r, c["norm"])
+    out["x"] = d.to(s["x"].dtype)
+    if s["y"] is not None:
+        y = s["y"].float()
+        yhat, ry = _normed(y, c["post"]) if c["post"] != "none" else (y, None)
+        z = yhat if s["post_weight"] is None else yhat * s["post_weight"]
+        dz = s["alpha"] * d
+        if s["gate"] is not None:
+            out["gate"] = _sums(dz * z, c)
+            dz = dz * _spread(s["gate"], c, c["rows"])
+        if s["post_weight"] is not None:
+            out["post_weight"] = (dz * yhat).sum(dim=0)
+            dz = dz * s["post_weight"]
+        out["y"] = (dz if c["post"] == "none" else _through(dz, yhat, ry, c["post"])).to(s["y"].dtype)
+    return out
+
+
+def _turn(x, positions, s, inverse=False):
+    """x [rows, heads * head_dim] with each head's first rotary_dim values turned, in fp32."""
+    c = s["c"]
+    angle = positions.double()[:, s["axis"]] * s["f"]
+    cos = (angle.cos() * s["amplitude"]).float()[:, None, :]
+    sin = (angle.sin() * (-s["amplitude"] if inverse else s["amplitude"])).float()[:, None, :]
+    x = x.float().view(x.shape[0], -1, c["head_dim"])
+    t, rest = x[..., :c["rotary_dim"]], x[..., c["rotary_dim"]:]
+    half = c["rotary_dim"] // 2
+    if c["interleaved"]:
+        a, b = t[..., 0::2], t[..., 1::2]
+        t = torch.stack((a * cos - b * sin, a * sin + b * cos), dim=-1).flatten(-2)
+    else:
+        a, b = t[..., :half], t[..., half:]
+        t = torch.cat((a * cos - b * sin, a * sin + b * cos), dim=-1)
+    return torch.cat((t, rest), dim=-1).flatten(1)
+
+
+def _plain_rotary(s):
+    return _turn(s["x"], s["positions"], s, s["c"]["inverse"]).to(s["x"].dtype)
+
+
+def _requests_of(start, rows):
+    """The request of each row (the count of requests for rows behind the last) and its place in it."""
+    r = torch.arange(rows, device="cuda", dtype=torch.int32)
+    b = (r[:, None] >= start[None, 1:]).sum(dim=1)
+    return b, r - start[b]
+
+
+def _plain_slots(s):
+    c, rows = s["c"], _rows(s["c"])
+    b, i = _requests_of(s["start"], rows)
+    new = s["start"][1:] - s["start"][:-1]
+    real = b < c["requests"]
+    bb = b.clamp(max=c["requests"] - 1)
+    at = s["before"][bb] + i
+    slot = at.long()
+    kept = real
+    if c["window"]:
+        slot = torch.where(slot < c["sink"], slot, c["sink"] + (slot - c["sink"]) % c["window"])
+        kept = kept & ((at < c["sink"]) | (new[bb] - i <= c["window"]))
+    slots = torch.where(kept, bb * c["capacity"] + slot, torch.full_like(slot, -1))
+    positions = torch.where(real, c["first"] + at, torch.zeros_like(at)).to(torch.int32)
+    return slots, positions, s["before"] + new
+
+
+def _plain_append(s):
+    slots, positions, lens = _plain_slots(s)
+    at = positions[:, None] if s["positions"] is None else s["positions"]
+    k, q = _turn(s["k"], at, s).to(BF16), _turn(s["q"], at, s).to(BF16)
+    kept = slots >= 0
+    s["k_cache"].view(-1, k.shape[1])[slots[kept]] = k[kept]
+    s["v_cache"].view(-1, k.shape[1])[slots[kept]] = s["v"][kept]
+    real = torch.arange(len(slots), device="cuda") < s["start"][-1]
+    s["q_out"][:] = torch.where(real[:, None], q, s["q_out"])
+    return slots, positions, lens
+
+
+def _plain_shared(s):
+    c, rows = s["c"], _rows(s["c"])
+    n, m, d, kv = c["requests"], c["most"], c["head_dim"], c["kv_heads"]
+    g = c["heads"] // kv
+    b, i = _requests_of(s["start"], rows)
+    at = torch.where(b < n, b * m + i, torch.full_like(b, n * m))
+    q = torch.zeros(n * m + 1, c["heads"] * d, device="cuda")
+    q[at] = s["q"].float()  # rows behind the last request meet in one more row
+    q = q[:-1].view(n, m, kv, g, d).permute(2, 0, 1, 3, 4).reshape(kv, n * m * g, d) * (1.0 / math.sqrt(d))
+    kp, vp = (s[x].float().view(c["prefix"], kv, d).permute(1, 0, 2) for x in ("k_prefix", "v_prefix"))
+    kc, vc = (s[x].float().view(n, c["capacity"], kv, d).permute(2, 0, 1, 3).reshape(kv * n, -1, d)
+              for x in ("k_cache", "v_cache"))
+    own_w = torch.matmul(q.reshape(kv * n, m * g, d), kc.transpose(1, 2).contiguous()).view(kv, n * m * g, -1)
+    w = torch.cat((torch.matmul(q, kp.transpose(1, 2).contiguous()), own_w), 2)
+    seen = torch.arange(c["capacity"], device="cuda")[None, :] < s["lens"][:, None]
+    w.view(kv, n, m * g, -1)[..., c["prefix"]:].masked_fill_(~seen[None, :, None, :], -math.inf)
+    top = w.amax(dim=2, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    w = w.sub_(top).exp_()
+    total = w.sum(dim=2, keepdim=True)
+    o = torch.matmul(w[..., :c["prefix"]], vp) + torch.matmul(
+        w[..., c["prefix"]:].reshape(kv * n, m * g, -1), vc).view(kv, n * m * g, d)
+    o = torch.where(total > 0, o / total, torch.zeros_like(o))
+    lse = (top + total.log())[..., 0]
+    o = o.view(kv, n * m, g, d).permute(1, 0, 2, 3).reshape(n * m, -1)
+    lse = lse.view(kv, n * m, g).permute(0, 2, 1).reshape(c["heads"], n * m)
+    real, at = b < n, at.clamp(max=n * m - 1)
+    s["out"][:] = torch.where(real[:, None], o[at].to(BF16), s["out"])
+    s["lse"][:] = torch.where(real[None, :], lse[:, at], s["lse"])
+    return s["out"], s["lse"]
+
+
+# ------------------------------------------------------------------ the calls
+def _own_norm(s):
+    import paper_2607_00712_amd as ispa
+    c = s["c"]
+    return ispa.norm_residual(s["x"], s["y"], norm=c["norm"], weight=s["weight"], bias=s["bias"], scale=s["scale"],
+                              shift=s["shift"], post=c["post"] if s["y"] is not None else "none",
+                              post_weight=s["post_weight"], gate=s["gate"], alpha=s["alpha"],
+                              group_rows=c["group"] or None, eps=EPS, h_dtype=DTYPES[c["h"]])
+
+
+def _own_norm_grad(s):
+    import paper_2607_00712_amd as ispa
+    c = s["c"]
+    return ispa.norm_residual_backward(s["d_h"], s["x"], s["y"], d_x_out=s["d_x"], norm=c["norm"], weight=s["weight"],
+                                       bias=s["bias"], scale=s["scale"], shift=s["shift"],
+                                       post=c["post"] if s["y"] is not None else "none",
+                                       post_weight=s["post_weight"], gate=s["gate"], alpha=s["alpha"],
+                                       group_rows=c["group"] or None, eps=EPS)
+
+
+def _own_rotary(s):
+    import paper_2607_00712_amd as ispa
+    c = s["c"]
+    return ispa.rotary(s["x"], s["positions"], s["f"], c["heads"], axes=s["axes"], interleaved=c["interleaved"],
+                       amplitude=s["amplitude"], inverse=c["inverse"])
+
+
+def _own_append(s):
+    import paper_2607_00712_amd as ispa
+    c = s["c"]
+    slots, positions, lens = ispa.slot_map(s["start"], s["before"], c["capacity"], _rows(c), sink=c["sink"],
+                                           window=c["window"], first_position=c["first"])
+    at = positions if s["positions"] is None else s["positions"]
+    ispa.rotary_append(s["q"], s["k"], s["v"], at, slots, s["f"], c["heads"], s["k_cache"], s["v_cache"],
+                       n_kv_heads=c["kv_heads"], axes=s["axes"], interleaved=c["interleaved"],
+                       amplitude=s["amplitude"], q_out=s["q_out"])
+    return slots, positions, lens
+
+
+def _own_shared(s):
+    import paper_2607_00712_amd as ispa
+    c = s["c"]
+    return ispa.attn_shared(s["q"], s["k_prefix"], s["v_prefix"], s["k_cache"], s["v_cache"], s["start"], s["lens"],
+                            c["heads"], n_kv_heads=c["kv_heads"], max_q=c["most"], out=s["out"], lse=s["lse"])
+
+
+def run(state):
+    s, kind = state, state["c"]["kind"]
+    if kind == "norm":
+        x, h = _own_norm(s) if own else _plain_norm(s)
+        return {"x": x, "h": h}
+    if kind == "norm_grad":
+        return _own_norm_grad(s) if own else _plain_norm_grad(s)
+    if kind == "rotary":
+        return {"x": _own_rotary(s) if own else _plain_rotary(s)}
+    if kind == "append":
+        slots, positions, lens = _own_append(s) if own else _plain_append(s)
+        return {"slots": slots, "positions": positions, "lens": lens, "q": s["q_out"], "k_cache": s["k_cache"],
+                "v_cache": s["v_cache"]}
+    out, lse = _own_shared(s) if own else _plain_shared(s)
+    return {"out": out, "lse": lse}
+
+
+# ------------------------------------------------------------------ definitions, in 64 bits
+def _exact_norm(x, kind):
+    if kind == "layer":
+        return (x - x.mean(1, keepdim=True)) / (x.var(1, unbiased=False, keepdim=True) + EPS).sqrt()
+    return x / (x.pow(2).mean(1, keepdim=True) + EPS).sqrt()
+
+
+def _wide(s):
+    return {k: v.double() if isinstance(v, torch.Tensor) and v.is_floating_point() else v for k, v in s.items()}
+
+
+def _exact_rows(v, c):
+    n = c["rows"]
+    return v.expand(n, -1) if not c["group"] else v.repeat_interleave(c["group"], dim=0)[:n]
+
+
+def _exact_branch(s):
+    """What is added to the stream."""
+    c, z = s["c"], s["y"]
+    if c["post"] != "none":
+        z = _exact_norm(z, c["post"]) * s["post_weight"]
+    return s["alpha"] * (z if s["gate"] is None else z * _exact_rows(s["gate"], c))
+
+
+def _exact_h(x, s):
+    c, h = s["c"], _exact_norm(x, s["c"]["norm"])
+    h = h if s["weight"] is None else h * s["weight"]
+    h = h if s["bias"] is None else h + s["bias"]
+    return h if s["scale"] is None else h * (1 + _exact_rows(s["scale"], c)) + _exact_rows(s["shift"], c)
+
+
+def _exact_norm_grad(s):
+    names = [k for k in ("x", "weight", "bias", "scale", "shift") if s[k] is not None]
+    for k in names:
+        s[k].requires_grad_(True)
+    out = dict(zip(names, torch.autograd.grad((_exact_h(s["x"], s) * s["d_h"]).sum(), [s[k] for k in names])))
+    out["x"] = out["x"] + s["d_x"]
+    if s["y"] is not None:
+        names = [k for k in ("y", "gate", "post_weight") if s[k] is not None]
+        for k in names:
+            s[k].requires_grad_(True)
+        out.update(zip(names, torch.autograd.grad((_exact_branch(s) * out["x"]).sum(), [s[k] for k in names])))
+    return {k: v.detach() for k, v in out.items()}
+
+
+def _exact_turn(x, positions, s, inverse=False):
+    c, half, f = s["c"], s["c"]["rotary_dim"] // 2, s["f"].cpu().tolist()
+    x = x.double().view(len(x), -1, c["head_dim"])
+    out = x.clone()
+    axis = [k for k, n in enumerate(s["axes"]) for _ in range(n)]
+    for j in range(half):
+        i, k = (2 * j, 2 * j + 1) if c["interleaved"] else (j, half + j)
+        z = torch.polar(torch.full((len(x), 1), s["amplitude"], dtype=F64, device="cuda"),
+                        (-1 if inverse else 1) * positions[:, axis[j], None].double() * f[j])
+        w = torch.complex(x[..., i], x[..., k]) * z
+        out[..., i], out[..., k] = w.real, w.imag
+    return out.flatten(1)
+
+
+def _exact_append(s):
+    c, start, before = s["c"], s["start"].tolist(), s["before"].tolist()
+    rows, slots, positions = _rows(c), [], []
+    for b in range(c["requests"]):
+        m = start[b + 1] - start[b]
+        for i in range(m):
+            at = before[b] + i
+            positions.append(c["first"] + at)
+            if c["window"] and at >= c["sink"]:
+                at = c["sink"] + (at - c["sink"]) % c["window"] if i >= m - c["window"] else None
+            slots.append(-1 if at is None else b * c["capacity"] + at)
+    real = len(slots)
+    slots += [-1] * (rows - real)
+    positions += [0] * (rows - real)
+    slots = torch.tensor(slots, device="cuda")
+    at = torch.tensor(positions, device="cuda")[:, None] if s["positions"] is None else s["positions"]
+    k, q = _exact_turn(s["k"], at, s), _exact_turn(s["q"], at, s)
+    q[real:] = 0
+    caches = [s[x].double().flatten(0, 1) for x in ("k_cache", "v_cache")]
+    for cache, new in zip(caches, (k, s["v"].double())):
+        cache[slots[slots >= 0]] = new[slots >= 0]
+    return {"slots": None, "positions": None, "lens": None, "q": q, "k_cache": caches[0].view(s["k_cache"].shape),
+            "v_cache": caches[1].view(s["v_cache"].shape)}
+
+
+def _exact_shared(s):
+    c, start, lens = s["c"], s["start"].tolist(), s["lens"].tolist()
+    d, g = c["head_dim"], c["heads"] // c["kv_heads"]
+    out, lse = s["out"].double(), s["lse"].double()
+    for h in range(c["heads"]):
+        at = slice(h // g * d, h // g * d + d)
+        kp, vp = s["k_prefix"][:, at].double(), s["v_prefix"][:, at].double()
+        for b in range(c["requests"]):
+            rows = slice(start[b], start[b + 1])
+            k = torch.cat((kp, s["k_cache"][b, :lens[b], at].double()))
+            v = torch.cat((vp, s["v_cache"][b, :lens[b], at].double()))
+            if not len(k):
+                out[rows, h * d:h * d + d], lse[h, rows] = 0, -math.inf
+                continue
+            w = s["q"][rows, h * d:h * d + d].double() @ k.t().contiguous() / math.sqrt(d)
+            lse[h, rows] = torch.logsumexp(w, 1)
+            out[rows, h * d:h * d + d] = torch.softmax(w, 1) @ v
+    return {"out": out, "lse": lse}
+
+
+def exact(case, seed):
+    s, kind = prepare(case, seed), case["kind"]
+    if kind == "norm":
+        w = _wide(s)
+        x = w["x"] if w["y"] is None else w["x"] + _exact_branch(w)
+        return {"x": x, "h": _exact_h(x, w)}
+    if kind == "norm_grad":
+        return _exact_norm_grad(_wide(s))
+    if kind == "rotary":
+        return {"x": _exact_turn(s["x"], s["positions"], s, case["inverse"])}
+    return _exact_append(s) if kind == "append" else _exact_shared(s)
+
+
+# ------------------------------------------------------------------ work
+def work(case):
+    c = case
+    if c["kind"] in ("norm", "norm_grad"):
+        n, d = c["rows"], c["cols"]
+        groups = -(-n // c["group"]) if c["group"] else 1
+        y = SIZE.get(c["y"], 0)
+        vectors = 4 * d * (c["weight"] + c["bias"] + 2 * groups * c["modulate"]
+                           + (groups * c["gate"] + (c["post"] != "none") if y else 0))
+        if c["kind"] == "norm":
+            return {"bytes": n * d * (SIZE[c["x"]] * (2 if y else 1) + y + SIZE[c["h"]]) + vectors, "flops": 20 * n * d}
+        return {"bytes": n * d * (3 * SIZE[c["x"]] + 2 * y + SIZE[c["h"]]) + 2 * vectors, "flops": 40 * n * d}
+    if c["kind"] == "rotary":
+        n = c["rows"] * c["heads"] * c["head_dim"]
+        return {"bytes": 2 * n * SIZE[c["x"]] + 4 * c["rows"] * c["axes"], "flops": 3 * n}
+    rows = c["requests"] * c["most"] / (1 if c["most"] == 1 else 2)  # the mean of the lengths
+    if c["kind"] == "append":
+        n = rows * (c["heads"] + 2 * c["kv_heads"]) * c["head_dim"]
+        return {"bytes": 4 * n + 12 * _rows(c) + 12 * c["requests"], "flops": 3 * n}
+    keys = c["capacity"] / 2
+    kv, hidden = c["kv_heads"] * c["head_dim"], c["heads"] * c["head_dim"]
+    return {"bytes": 4 * kv * (c["prefix"] + c["requests"] * keys) + 4 * rows * hidden + 4 * rows * c["heads"],
+            "flops": 4 * rows * hidden * (c["prefix"] + keys)}
