@@ -444,6 +444,220 @@ int ispa_quantize_rows(const void* x, int32_t x_dtype, int64_t rows, int32_t col
 int ispa_project_w8a8(const int8_t* q_a, const float* scale_a, const int8_t* q_w, const float* scale_w, int64_t n_rows,
                       int32_t d_in, int32_t d_out, void* y, int32_t y_dtype, hipStream_t stream);
 
+/* ---------------------------------------------------- norms around a block */
+/* kinds of norm: none; layer norm (x - mean) / sqrt(var + eps); RMS norm
+ * x / sqrt(mean(x^2) + eps) */
+#define ISPA_NORM_NONE  0
+#define ISPA_NORM_LAYER 1
+#define ISPA_NORM_RMS   2
+
+/*
+ * A block's output joins the residual stream and the next block's input leaves it,
+ * in one pass over the rows:
+ *   x_out = x + alpha * gate[g] * z,    z = y, or post(y) * post_weight
+ *   h     = (norm(x_out) * weight + bias) * (1 + scale[g]) + shift[g]
+ * with g = row / group_rows: rows share a modulation in groups of group_rows
+ * (a latent frame's tokens), the last group may be shorter.
+ *   x            device [rows, cols] of x_dtype, the residual stream
+ *   y            device [rows, cols] of y_dtype, the block's output, or NULL: the
+ *                stream is only normalised (x_out is then not written)
+ *   post         ISPA_NORM_*: the norm of y before it is added
+ *   post_weight  fp32 [cols] or NULL (needs post)
+ *   gate         fp32 [groups, cols] or NULL; alpha: the residual scale, finite
+ *   norm         ISPA_NORM_*; ISPA_NORM_NONE: h is not written (needs y)
+ *   weight, bias fp32 [cols] or NULL
+ *   scale, shift fp32 [groups, cols] or NULL
+ *   rows         0 .. 2^22 - 1 (0: nothing is done)
+ *   cols         a multiple of 8, 8 .. 16384
+ *   group_rows   rows of a group; <= 0: all rows are one group
+ *   eps          >= 0, finite; of both norms
+ *   x_out        device [rows, cols] of x_dtype; may be x; must not overlap
+ *                anything else
+ *   h            device [rows, cols] of h_dtype; must not overlap anything else
+ * Statistics and arithmetic are fp32, each output is rounded once; h is computed
+ * from the unrounded x_out. A row depends on no other row. Pointers 16-byte
+ * aligned. Asynchronous on `stream`.
+ */
+int ispa_norm_residual(const void* x, int32_t x_dtype, const void* y, int32_t y_dtype, int32_t post,
+                       const float* post_weight, const float* gate, float alpha, int32_t norm, const float* weight,
+                       const float* bias, const float* scale, const float* shift, int64_t rows, int32_t cols,
+                       int64_t group_rows, float eps, void* x_out, void* h, int32_t h_dtype, hipStream_t stream);
+
+/*
+ * The backward pass of ispa_norm_residual: from d_h, the gradient of h, and d_x_out,
+ * the gradient that reaches x_out from its other uses, the gradients of everything
+ * that took part.
+ *   d_h          device [rows, cols] of h_dtype; NULL iff norm is ISPA_NORM_NONE
+ *   d_x_out      device [rows, cols] of x_dtype or NULL (zero); needed without a norm
+ *   x_out        device [rows, cols] of x_dtype: x_out of the forward pass (x where
+ *                y is NULL); NULL iff norm is ISPA_NORM_NONE
+ *   y .. eps     as in the forward pass (shift is not needed)
+ *   d_x          device [rows, cols] of x_dtype: the gradient of x (and of x_out);
+ *                may be d_x_out
+ *   d_y          device [rows, cols] of y_dtype; NULL iff y is NULL
+ *   d_gate, d_scale, d_shift            fp32 [groups, cols] or NULL (not wanted)
+ *   d_post_weight, d_weight, d_bias     fp32 [cols] or NULL
+ *                (d_gate and d_post_weight need y; the others a norm;
+ *                d_post_weight needs post)
+ *   workspace    device, 256-byte aligned, at least
+ *                ispa_norm_residual_backward_workspace_bytes bytes; may be NULL where
+ *                no gradient of a vector is wanted. Used only during the call's
+ *                device work.
+ * Sums over rows are fp32, in an order that depends on the sizes alone: the same call
+ * gives the same bits. Asynchronous on `stream`.
+ */
+int ispa_norm_residual_backward(const void* d_h, int32_t h_dtype, const void* d_x_out, const void* x_out,
+                                int32_t x_dtype, const void* y, int32_t y_dtype, int32_t post,
+                                const float* post_weight, const float* gate, float alpha, int32_t norm,
+                                const float* weight, const float* bias, const float* scale, int64_t rows, int32_t cols,
+                                int64_t group_rows, float eps, void* d_x, void* d_y, float* d_gate,
+                                float* d_post_weight, float* d_weight, float* d_bias, float* d_scale, float* d_shift,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ispa_norm_residual_backward; 0 for invalid sizes or no rows. */
+size_t ispa_norm_residual_backward_workspace_bytes(int64_t rows, int32_t cols, int64_t group_rows);
+
+/* ------------------------------------------------------- rotary positions */
+/* Rules of ispa_rotary_frequencies for contexts longer than the trained one:
+ * none; linear (every frequency divided by factor); base (the base raised by
+ * factor^(n / (n - 1)) for an axis of n pairs, which divides its slowest frequency by
+ * factor and leaves its fastest); parts (frequencies that turn more than beta_fast
+ * times in original_length stay, those that turn less than beta_slow times are
+ * divided by factor, a linear ramp over the pairs between). */
+#define ISPA_ROTARY_NONE   0
+#define ISPA_ROTARY_LINEAR 1
+#define ISPA_ROTARY_BASE   2
+#define ISPA_ROTARY_PARTS  3
+
+/*
+ * Radians per position of each pair: pair i of an axis of n pairs turns by
+ * base^(-i / n) a position, the axes one after the other. Host-only.
+ *   axis_pairs  host [n_axes] pairs of each axis, 1 <= n_axes <= 4, at most 128 in all
+ *   base        > 1
+ *   scaling     ISPA_ROTARY_*; factor >= 1; original_length, beta_fast > beta_slow > 0:
+ *               ISPA_ROTARY_PARTS alone (one axis)
+ *   freqs       host double [sum of axis_pairs]
+ *   amplitude   host double or NULL: 0.1 ln(factor) + 1 for ISPA_ROTARY_PARTS, else 1:
+ *               the factor on cos and sin that goes with the frequencies
+ */
+int ispa_rotary_frequencies(const int32_t* axis_pairs, int32_t n_axes, double base, int32_t scaling, double factor,
+                            double original_length, double beta_fast, double beta_slow, double* freqs,
+                            double* amplitude);
+
+/*
+ * Rotary positions on every head of x: pair j of the first rotary_dim values of a head
+ * turns by positions[row, axis of j] * freqs[j]:
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos)
+ * a pair being values 2j, 2j + 1 (interleaved) or j, j + rotary_dim / 2. The angle is
+ * formed in fp64, so far positions keep their phase; the values behind rotary_dim
+ * pass through.
+ *   x           device [rows, n_heads * head_dim] of x_dtype, rows ld_x elements apart
+ *   out         device, of out_dtype, rows ld_out elements apart; may be x (same dtype
+ *               and row distance), else must not overlap it
+ *   positions   device int32 [rows, n_axes]
+ *   freqs       device double [rotary_dim / 2]
+ *   axis_pairs  host [n_axes]: pairs of each axis in order; their sum is rotary_dim / 2
+ *   rotary_dim  a multiple of 16, 16 .. head_dim
+ *   head_dim    a multiple of 16, 16 .. 256; n_heads * head_dim <= 2^20
+ *   inverse     != 0: the transpose (the opposite angle), which is the gradient
+ *   rows        0 .. 2^30 - 1; ld_x, ld_out multiples of 8, at least n_heads * head_dim
+ * x and out 16-byte aligned. Asynchronous on `stream`.
+ */
+int ispa_rotary(const void* x, int32_t x_dtype, int64_t ld_x, void* out, int32_t out_dtype, int64_t ld_out,
+                const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                int32_t rotary_dim, int32_t interleaved, float amplitude, int32_t inverse, int64_t rows,
+                int32_t n_heads, int32_t head_dim, hipStream_t stream);
+
+/*
+ * Where the rows of a batch go: request b's new tokens are rows q_start[b] ..
+ * q_start[b + 1] - 1, and before[b] tokens of its sequence came earlier. Its i-th new
+ * token is token t = before[b] + i and goes to place t of its cache; with window > 0
+ * the cache is a ring of sink + window places (as ispa_kv_ring_append keeps it): the
+ * places behind the sink are taken modulo window, and of more than `window` new tokens
+ * only the last `window` are kept there.
+ *   q_start     device int32 [n_req + 1], ascending
+ *   before      device int32 [n_req], >= 0
+ *   n_rows      rows of the batch's tensors, at least q_start[n_req] (rows behind it are
+ *               padding); 0 .. 2^31 - 1
+ *   capacity    places of each request's cache, >= 1; with window > 0 exactly
+ *               sink + window
+ *   slots       device int64 [n_rows]: b * capacity + place, or -1 for padding and for a
+ *               token without a place (not kept, or behind the capacity)
+ *   positions   device int32 [n_rows]: first_position + t, 0 for padding
+ *   lens        device int32 [n_req]: before[b] + new tokens; must not overlap before
+ * Asynchronous on `stream`.
+ */
+int ispa_slot_map(const int32_t* q_start, const int32_t* before, int32_t n_req, int64_t n_rows, int64_t capacity,
+                  int64_t sink, int64_t window, int64_t first_position, int64_t* slots, int32_t* positions,
+                  int32_t* lens, hipStream_t stream);
+
+/*
+ * New tokens into their caches in one launch: q rotated into q_out, k rotated into row
+ * slots[row] of k_cache, v into the same row of v_cache. Rows with a slot that is
+ * negative or at least cache_rows are left alone: neither q_out nor a cache is written
+ * for them. No slot may come twice.
+ *   q           device [rows, n_heads * head_dim], rows ld_q elements apart
+ *   k, v        device [rows, n_kv_heads * head_dim], ld_k and ld_v apart; all of x_dtype
+ *   q_out       device, of out_dtype, rows ld_out apart; may be q (same dtype and row
+ *               distance)
+ *   k_cache, v_cache  device bf16 [cache_rows, n_kv_heads * head_dim], contiguous; must
+ *               not overlap the inputs, q_out or each other
+ *   slots       device int64 [rows]
+ * Other arguments as for ispa_rotary. Asynchronous on `stream`.
+ */
+int ispa_rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                       int32_t x_dtype, void* q_out, int32_t out_dtype, int64_t ld_out, void* k_cache, void* v_cache,
+                       int64_t cache_rows, const int64_t* slots, const int32_t* positions, const double* freqs,
+                       const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                       float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                       hipStream_t stream);
+
+/* ---------------------------------------------- attention, shared prefix */
+/*
+ * Attention of a batch of requests that share a prefix (rollouts forked from one
+ * history): request b's queries see the keys of  prefix [0, prefix_len)  and of its own
+ * cache [0, cache_lens[b]), all of them (no mask inside a chunk, as in
+ * ispa_attn_chunk). The prefix is attended once for all requests and joined with each
+ * request's own result by Eq. 11-12.
+ *   q           bf16 [n_rows, n_heads * head_dim], rows ld_q elements apart; request b
+ *               has rows q_start[b] .. q_start[b + 1] - 1
+ *   k_prefix, v_prefix  bf16 [prefix_len, n_kv_heads * head_dim], rows ld_prefix apart;
+ *               may be NULL where prefix_len is 0; prefix_len <= 2^31 - 1
+ *   k_cache, v_cache    bf16: request b's row j at element b * ld_request + j * ld_cache;
+ *               capacity rows each; may be NULL where capacity is 0
+ *   q_start     device int32 [n_req + 1], ascending, from 0; q_start[n_req] <= n_rows:
+ *               rows behind it are padding, and out and lse are left as they are there
+ *   cache_lens  device int32 [n_req]; values outside [0, capacity] are taken as the
+ *               nearer end (a ring's count of tokens may stand for its filled rows)
+ *   n_req >= 1; n_rows >= 0 (0: nothing is done); n_rows * n_heads <= 2^26 and
+ *               n_req * n_kv_heads <= 2^20
+ *   max_q       >= 1: most rows of a request, as far as the host knows; the layout of
+ *               the work follows it, the result does not depend on it beyond rounding
+ *   n_heads     a multiple of n_kv_heads: query head i reads key head
+ *               i / (n_heads / n_kv_heads); head_dim in {64, 128}
+ *   scale       logit scale; <= 0 selects 1/sqrt(head_dim)
+ *   out         [n_rows, n_heads * head_dim] of out_dtype, rows ld_out apart; a query
+ *               without any key gets 0
+ *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
+ *   workspace   device, 256-byte aligned, at least ispa_attn_shared_workspace_bytes
+ *               bytes for the same sizes on the same device. Used only during the call's
+ *               device work.
+ * Row distances are multiples of 8 elements, pointers 16-byte aligned (lse 4). Keys and
+ * values behind a set's end are never used, whatever they hold. Outputs must not overlap
+ * the inputs or each other. The same call gives the same bits. Asynchronous on `stream`.
+ */
+int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const void* v_prefix, int64_t prefix_len,
+                     int64_t ld_prefix, const void* k_cache, const void* v_cache, int64_t capacity, int64_t ld_cache,
+                     int64_t ld_request, const int32_t* q_start, const int32_t* cache_lens, int32_t n_req,
+                     int32_t n_rows, int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                     void* out, int32_t out_dtype, int64_t ld_out, float* lse, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ispa_attn_shared on the current device; 0 for invalid sizes or no
+ * rows. */
+size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows,
+                                        int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+
 #ifdef __cplusplus
 }
 #endif

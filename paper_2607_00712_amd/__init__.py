@@ -14,6 +14,11 @@ works without the library, but every call raises if it is not built.
     project(a, weight, out_dtype) -> a @ weight^T  (the L-Layer's output projection)
     Stats(d_in, d_out, max_rows).accum(x, y_full, y_local)
     Stats.solve(lam) -> (delta_w, eps)
+    norm_residual(x, y, ...) -> (x_out, h);  norm_residual_backward(d_h, x_out, y, ...) -> gradients
+    rotary(x, positions, freqs, n_heads, ...);  rotary_frequencies(axis_pairs, ...) -> (freqs, amplitude)
+    slot_map(q_start, before, capacity, n_rows, ...) -> (slots, positions, lens)
+    rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, ...) -> q_out
+    attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_heads, ...) -> (out, lse)
 """
 
 import ctypes
@@ -24,6 +29,8 @@ import torch
 __all__ = ["IspaError", "NotSPDError", "lib", "attn_chunk", "attn_chunk_noalloc", "attn_ranges", "attn_merge", "Stats", "StatsBatch",
            "status_string",
            "select_layers", "inject_modulation", "LocalKV", "project", "quantize_rows", "project_w8a8",
+           "norm_residual", "norm_residual_backward", "rotary_frequencies", "rotary", "slot_map", "rotary_append",
+           "attn_shared",
            "LIB_PATH", "ISPA_OK", "ISPA_ERR_INVALID_ARG", "ISPA_ERR_UNSUPPORTED",
            "ISPA_ERR_NOT_SPD", "ISPA_ERR_HIP", "ISPA_ERR_STATE", "ISPA_ERR_SCRATCH",
            "ISPA_STATIC_SCRATCH_BYTES"]
@@ -43,6 +50,7 @@ DTYPE_BF16 = 0
 DTYPE_F32 = 1
 
 _c_i32, _c_i64, _c_f32, _c_p, _c_sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+_c_f64 = ctypes.c_double
 
 _SIGNATURES = {
     "ispa_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -66,6 +74,25 @@ _SIGNATURES = {
     "ispa_project": (ctypes.c_int, [_c_p, _c_p, _c_i64, _c_i32, _c_i32, _c_p, _c_i32, _c_p]),
     "ispa_quantize_rows": (ctypes.c_int, [_c_p, _c_i32, _c_i64, _c_i32, _c_p, _c_p, _c_p]),
     "ispa_project_w8a8": (ctypes.c_int, [_c_p, _c_p, _c_p, _c_p, _c_i64, _c_i32, _c_i32, _c_p, _c_i32, _c_p]),
+    "ispa_norm_residual": (ctypes.c_int, [_c_p, _c_i32, _c_p, _c_i32, _c_i32, _c_p, _c_p, _c_f32, _c_i32, _c_p, _c_p,
+                                          _c_p, _c_p, _c_i64, _c_i32, _c_i64, _c_f32, _c_p, _c_p, _c_i32, _c_p]),
+    "ispa_norm_residual_backward": (ctypes.c_int, [_c_p, _c_i32, _c_p, _c_p, _c_i32, _c_p, _c_i32, _c_i32, _c_p, _c_p,
+                                                   _c_f32, _c_i32, _c_p, _c_p, _c_p, _c_i64, _c_i32, _c_i64, _c_f32,
+                                                   _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "ispa_norm_residual_backward_workspace_bytes": (_c_sz, [_c_i64, _c_i32, _c_i64]),
+    "ispa_rotary_frequencies": (ctypes.c_int, [ctypes.POINTER(_c_i32), _c_i32, _c_f64, _c_i32, _c_f64, _c_f64, _c_f64,
+                                               _c_f64, ctypes.POINTER(_c_f64), ctypes.POINTER(_c_f64)]),
+    "ispa_rotary": (ctypes.c_int, [_c_p, _c_i32, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_p, ctypes.POINTER(_c_i32),
+                                   _c_i32, _c_i32, _c_i32, _c_f32, _c_i32, _c_i64, _c_i32, _c_i32, _c_p]),
+    "ispa_slot_map": (ctypes.c_int, [_c_p, _c_p, _c_i32, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
+                                     _c_p]),
+    "ispa_rotary_append": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i32, _c_i64, _c_p,
+                                          _c_p, _c_i64, _c_p, _c_p, _c_p, ctypes.POINTER(_c_i32), _c_i32, _c_i32,
+                                          _c_i32, _c_f32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p]),
+    "ispa_attn_shared": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64,
+                                        _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_f32, _c_p,
+                                        _c_i32, _c_i64, _c_p, _c_p, _c_sz, _c_p]),
+    "ispa_attn_shared_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
     "ispa_stats_workspace_bytes": (_c_sz, [_c_i32, _c_i32, _c_i64]),
     "ispa_stats_create": (ctypes.c_int, [ctypes.POINTER(_c_p), _c_p, _c_sz, _c_i32, _c_i32, _c_i64, _c_p]),
     "ispa_stats_reset": (ctypes.c_int, [_c_p]),
@@ -604,3 +631,360 @@ def project_w8a8(q_a, scale_a, q_w, scale_w, out=None, out_dtype=torch.float32):
                              _ptr(out), _DT[out.dtype], _stream(dev))
     _check(st, "ispa_project_w8a8")
     return out
+
+
+# ---- norms around a block, rotary positions, attention over a shared prefix ----
+_NORMS = {"none": 0, "layer": 1, "rms": 2}
+_ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def _on(dev, fn):
+    """fn() with dev the current device (the library works on the current one)."""
+    if torch.cuda.current_device() == dev.index:
+        return fn()
+    with torch.cuda.device(dev):
+        return fn()
+
+
+def _float_tensor(t, name, device=None):
+    """A contiguous 2-d bf16 or fp32 tensor; returns its dtype code."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DT:
+        raise TypeError(f"{name} must be a bf16 or fp32 torch.Tensor")
+    _require(t, name, t.dtype, device)
+    return _DT[t.dtype]
+
+
+def _strided_rows(t, name, device=None, dtype=None, width=None):
+    """A 2-d tensor of contiguous rows; returns its row distance in elements."""
+    if not isinstance(t, torch.Tensor) or (t.dtype != dtype if dtype is not None else t.dtype not in _DT):
+        raise TypeError(f"{name} must be a {dtype or 'bf16 or fp32'} torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a HIP device")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dim() != 2 or (width is not None and t.shape[1] != width):
+        raise ValueError(f"{name} must be 2-d" + (f" with {width} columns" if width is not None else ""))
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1 and rows > 0:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols or ld % 8:
+        raise ValueError(f"{name} must have rows a multiple of 8 elements apart that do not overlap")
+    return ld
+
+
+def _vector(t, name, device, shape):
+    if t is not None:
+        _require(t, name, torch.float32, device, ndim=len(shape))
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}")
+
+
+def _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate, group_rows):
+    """Checks what both directions of the norm take; returns (groups, group_rows)."""
+    if norm not in _NORMS or post not in _NORMS:
+        raise ValueError(f"norm and post must be one of {sorted(_NORMS)}")
+    _float_tensor(x, "x")
+    rows, cols = x.shape
+    if y is not None:
+        _float_tensor(y, "y", x.device)
+        if y.shape != x.shape:
+            raise ValueError("y must have the shape of x")
+    elif post != "none" or post_weight is not None or gate is not None:
+        raise ValueError("post, post_weight and gate need y")
+    if post == "none" and post_weight is not None:
+        raise ValueError("post_weight needs post")
+    if norm == "none" and (y is None or any(t is not None for t in (weight, bias, scale, shift))):
+        raise ValueError("without a norm there must be a y, and no weight, bias, scale or shift")
+    group_rows = int(group_rows) if group_rows is not None else max(rows, 1)
+    if group_rows < 1:
+        raise ValueError("group_rows must be positive")
+    groups = max(1, -(-rows // group_rows))
+    for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight)):
+        _vector(t, name, x.device, (cols,))
+    for name, t in (("scale", scale), ("shift", shift), ("gate", gate)):
+        _vector(t, name, x.device, (groups, cols))
+    return groups, group_rows
+
+
+def norm_residual(x, y=None, norm="layer", weight=None, bias=None, scale=None, shift=None, post="none",
+                  post_weight=None, gate=None, alpha=1.0, group_rows=None, eps=1e-6, x_out=None, h=None,
+                  h_dtype=torch.bfloat16):
+    """A block's output y joins the residual stream x and the next block's input h
+    leaves it (ispa_norm_residual): x_out = x + alpha * gate * z with z = y or
+    post(y) * post_weight, h = (norm(x_out) * weight + bias) * (1 + scale) + shift.
+
+    x, y [rows, cols] bf16 or fp32; weight, bias, post_weight fp32 [cols]; scale, shift,
+    gate fp32 [groups, cols], one for every group_rows rows (None: one for all). norm and
+    post: "layer", "rms" or "none". Returns (x_out, h): x_out is x itself where y is
+    None, h is None where norm is "none"; x_out=x updates the stream in place.
+    """
+    L = lib()
+    _, group_rows = _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate, group_rows)
+    dev = x.device
+    rows, cols = x.shape
+    if y is None:
+        if x_out is not None and x_out is not x:
+            raise ValueError("x_out needs y")
+        x_out = x
+    elif x_out is None:
+        x_out = torch.empty_like(x)
+    else:
+        _require(x_out, "x_out", x.dtype, dev)
+        if x_out.shape != x.shape:
+            raise ValueError("x_out must have the shape of x")
+    if norm == "none":
+        if h is not None:
+            raise ValueError("h needs a norm")
+    else:
+        if h is None:
+            h = x.new_empty((rows, cols), dtype=h_dtype)
+        _float_tensor(h, "h", dev)
+        if h.shape != x.shape:
+            raise ValueError("h must have the shape of x")
+    if rows == 0:
+        return x_out, h
+    st = _on(dev, lambda: L.ispa_norm_residual(
+        x.data_ptr(), _DT[x.dtype], _ptr(y), _DT[y.dtype] if y is not None else 0, _NORMS[post], _ptr(post_weight),
+        _ptr(gate), float(alpha), _NORMS[norm], _ptr(weight), _ptr(bias), _ptr(scale), _ptr(shift), rows, cols,
+        group_rows, float(eps), x_out.data_ptr() if y is not None else None, _ptr(h),
+        _DT[h.dtype] if h is not None else 0, _stream(dev)))
+    _check(st, "ispa_norm_residual")
+    return x_out, h
+
+
+def norm_residual_backward(d_h, x_out, y=None, d_x_out=None, norm="layer", weight=None, bias=None, scale=None,
+                           shift=None, post="none", post_weight=None, gate=None, alpha=1.0, group_rows=None, eps=1e-6):
+    """The gradients of norm_residual (ispa_norm_residual_backward), as a dict: "x", and
+    of "y", "weight", "bias", "scale", "shift", "post_weight", "gate" those that are
+    given. d_h is the gradient of h (None where norm is "none"), d_x_out what reaches
+    x_out from its other uses (None: nothing); x_out as the forward pass returned it.
+    """
+    L = lib()
+    x = x_out if x_out is not None else d_x_out
+    groups, group_rows = _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate, group_rows)
+    dev = x.device
+    rows, cols = x.shape
+    if norm == "none":
+        if d_h is not None or d_x_out is None:
+            raise ValueError("without a norm the gradient comes as d_x_out alone")
+    else:
+        _float_tensor(x_out, "x_out")
+        _float_tensor(d_h, "d_h", dev)
+        if d_h.shape != x.shape:
+            raise ValueError("d_h must have the shape of x_out")
+    if d_x_out is not None:
+        _require(d_x_out, "d_x_out", x.dtype, dev)
+        if d_x_out.shape != x.shape:
+            raise ValueError("d_x_out must have the shape of x_out")
+    new = torch.empty if rows else torch.zeros
+    out = {"x": torch.empty_like(x)}
+    if y is not None:
+        out["y"] = torch.empty_like(y)
+    for name, t, shape in (("weight", weight, (cols,)), ("bias", bias, (cols,)), ("scale", scale, (groups, cols)),
+                           ("shift", shift, (groups, cols)), ("post_weight", post_weight, (cols,)),
+                           ("gate", gate, (groups, cols))):
+        if t is not None:
+            out[name] = new(shape, dtype=torch.float32, device=dev)
+    if rows == 0:
+        return out
+    nbytes = L.ispa_norm_residual_backward_workspace_bytes(rows, cols, group_rows)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if len(out) > 1 + (y is not None) else None
+    grad = lambda name: _ptr(out.get(name))
+    st = _on(dev, lambda: L.ispa_norm_residual_backward(
+        _ptr(d_h), _DT[d_h.dtype] if d_h is not None else 0, _ptr(d_x_out), x.data_ptr() if norm != "none" else None,
+        _DT[x.dtype], _ptr(y), _DT[y.dtype] if y is not None else 0, _NORMS[post], _ptr(post_weight), _ptr(gate),
+        float(alpha), _NORMS[norm], _ptr(weight), _ptr(bias), _ptr(scale), rows, cols, group_rows, float(eps),
+        grad("x"), grad("y"), grad("gate"), grad("post_weight"), grad("weight"), grad("bias"), grad("scale"),
+        grad("shift"), _ptr(ws), nbytes, _stream(dev)))
+    _check(st, "ispa_norm_residual_backward")
+    return out
+
+
+def _pairs(axes, freqs):
+    axes = (freqs.shape[0],) if axes is None else tuple(int(n) for n in axes)
+    return (_c_i32 * len(axes))(*axes), len(axes)
+
+
+def rotary_frequencies(axis_pairs, base=10000.0, scaling="none", factor=1.0, original_length=0.0, beta_fast=32.0,
+                       beta_slow=1.0, device=None):
+    """Radians per position of each pair, fp64 on `device` (default: the current HIP
+    device), and the factor on cos and sin that goes with them (ispa_rotary_frequencies).
+    axis_pairs: the pairs of the one axis, or of each axis."""
+    if scaling not in _ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(_ROTARY_SCALINGS)}")
+    pairs = (int(axis_pairs),) if isinstance(axis_pairs, int) else tuple(int(n) for n in axis_pairs)
+    freqs = (_c_f64 * max(1, sum(max(0, n) for n in pairs)))()
+    amplitude = _c_f64(1.0)
+    _check(lib().ispa_rotary_frequencies((_c_i32 * max(1, len(pairs)))(*pairs), len(pairs), float(base),
+                                         _ROTARY_SCALINGS[scaling], float(factor), float(original_length),
+                                         float(beta_fast), float(beta_slow), freqs, ctypes.byref(amplitude)),
+           "ispa_rotary_frequencies")
+    return torch.tensor(list(freqs), dtype=torch.float64, device="cuda" if device is None else device), amplitude.value
+
+
+def _angles(positions, freqs, axes, dev, rows):
+    _require(positions, "positions", torch.int32, dev, ndim=positions.dim() if isinstance(positions, torch.Tensor) else 2)
+    _require(freqs, "freqs", torch.float64, dev, ndim=1)
+    pairs, n_axes = _pairs(axes, freqs)
+    if sum(pairs) != freqs.shape[0]:
+        raise ValueError("axes must add up to the pairs of freqs")
+    if tuple(positions.shape) != (rows, n_axes) and not (n_axes == 1 and tuple(positions.shape) == (rows,)):
+        raise ValueError(f"positions must have shape {(rows, n_axes)}")
+    return pairs, n_axes
+
+
+def rotary(x, positions, freqs, n_heads, axes=None, interleaved=True, amplitude=1.0, inverse=False, out=None):
+    """Rotary positions on the first 2 * len(freqs) values of every head (ispa_rotary).
+    x [rows, n_heads * head_dim] bf16 or fp32, rows may be apart (a slice of a wider
+    product); positions int32 [rows, n_axes] (or [rows]); freqs fp64 on the device; axes:
+    the pairs of each axis (None: one axis). inverse: the transpose, the gradient of the
+    forward call. out=x turns in place."""
+    L = lib()
+    ld = _strided_rows(x, "x")
+    dev = x.device
+    rows, hidden = x.shape
+    if n_heads < 1 or hidden % n_heads:
+        raise ValueError("hidden size is not a multiple of n_heads")
+    pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
+    if out is None:
+        out = x.new_empty((rows, hidden))
+    ld_out = _strided_rows(out, "out", dev, None, hidden)
+    if out.shape[0] != rows:
+        raise ValueError(f"out must have shape {(rows, hidden)}")
+    st = _on(dev, lambda: L.ispa_rotary(
+        x.data_ptr(), _DT[x.dtype], ld, out.data_ptr(), _DT[out.dtype], ld_out, positions.data_ptr(),
+        freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)), float(amplitude),
+        int(bool(inverse)), rows, int(n_heads), hidden // n_heads, _stream(dev)) if rows else ISPA_OK)
+    _check(st, "ispa_rotary")
+    return out
+
+
+def slot_map(q_start, before, capacity, n_rows, sink=0, window=0, first_position=0):
+    """Where the rows of a ragged batch go (ispa_slot_map): q_start int32 [n_req + 1] and
+    before int32 [n_req] on the device. Returns (slots int64 [n_rows], positions int32
+    [n_rows], lens int32 [n_req]); window > 0: caches that are rings of sink + window."""
+    L = lib()
+    _require(q_start, "q_start", torch.int32, ndim=1)
+    dev = q_start.device
+    _require(before, "before", torch.int32, dev, ndim=1)
+    if q_start.shape[0] != before.shape[0] + 1:
+        raise ValueError("q_start must have one entry more than before")
+    slots = q_start.new_empty((int(n_rows),), dtype=torch.int64)
+    positions = q_start.new_empty((int(n_rows),))
+    lens = torch.empty_like(before)
+    st = _on(dev, lambda: L.ispa_slot_map(
+        q_start.data_ptr(), before.data_ptr(), before.shape[0], int(n_rows), int(capacity), int(sink), int(window),
+        int(first_position), slots.data_ptr(), positions.data_ptr(), lens.data_ptr(), _stream(dev)))
+    _check(st, "ispa_slot_map")
+    return slots, positions, lens
+
+
+def rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, n_kv_heads=None, axes=None,
+                  interleaved=True, amplitude=1.0, q_out=None):
+    """New tokens into their caches in one launch (ispa_rotary_append): q rotated into
+    q_out, k rotated into row slots[row] of k_cache, v beside it; rows with slot -1 are
+    left alone. q [rows, n_heads * head_dim], k and v [rows, n_kv_heads * head_dim] of one
+    dtype; caches bf16, contiguous, their rows flattened over all leading dimensions.
+    Returns q_out (bf16 by default; q_out=q turns in place)."""
+    L = lib()
+    ld_q = _strided_rows(q, "q")
+    dev = q.device
+    rows, hidden = q.shape
+    n_kv_heads = n_heads if n_kv_heads is None else int(n_kv_heads)
+    if n_heads < 1 or hidden % n_heads or n_kv_heads < 1:
+        raise ValueError("hidden size is not a multiple of n_heads")
+    head_dim = hidden // n_heads
+    kv = n_kv_heads * head_dim
+    ld_k = _strided_rows(k, "k", dev, q.dtype, kv)
+    ld_v = _strided_rows(v, "v", dev, q.dtype, kv)
+    if k.shape[0] != rows or v.shape[0] != rows:
+        raise ValueError("q, k and v must have the same number of rows")
+    pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
+    _require(slots, "slots", torch.int64, dev, ndim=1)
+    if slots.shape[0] != rows:
+        raise ValueError("slots must have an entry for every row")
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _require(t, name, torch.bfloat16, dev, ndim=t.dim() if isinstance(t, torch.Tensor) and t.dim() > 1 else 2)
+        if t.shape[-1] != kv or t.shape != k_cache.shape:
+            raise ValueError(f"{name} must have rows of {kv} elements, and both caches one shape")
+    if q_out is None:
+        q_out = q.new_empty((rows, hidden), dtype=torch.bfloat16)
+    ld_out = _strided_rows(q_out, "q_out", dev, None, hidden)
+    if q_out.shape[0] != rows:
+        raise ValueError(f"q_out must have shape {(rows, hidden)}")
+    st = _on(dev, lambda: L.ispa_rotary_append(
+        q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[q.dtype], q_out.data_ptr(), _DT[q_out.dtype],
+        ld_out, k_cache.data_ptr(), v_cache.data_ptr(), k_cache.numel() // kv, slots.data_ptr(),
+        positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
+        float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _stream(dev)) if rows else ISPA_OK)
+    _check(st, "ispa_rotary_append")
+    return q_out
+
+
+def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_heads, n_kv_heads=None, prefix_len=None,
+                max_q=None, scale=0.0, out=None, lse=None, out_dtype=torch.bfloat16, need_lse=True):
+    """Attention of a batch of requests over a shared prefix and each request's own cache
+    (ispa_attn_shared).
+
+    q [n_rows, n_heads * d] bf16, request b's rows from q_start[b] on; k_prefix, v_prefix
+    [>= prefix_len, n_kv_heads * d] bf16 (prefix_len None: all rows); k_cache, v_cache
+    [n_req, capacity, n_kv_heads * d] bf16, cache_lens[b] rows filled; q_start int32
+    [n_req + 1] and cache_lens int32 [n_req] on the device. max_q: most rows of a request,
+    a hint (None: the mean). Returns (out, lse); rows behind q_start[n_req] are left as
+    they were (uninitialised where out or lse is not given).
+    """
+    L = lib()
+    ld_q = _strided_rows(q, "q", None, torch.bfloat16)
+    dev = q.device
+    rows, hidden = q.shape
+    n_kv_heads = n_heads if n_kv_heads is None else int(n_kv_heads)
+    if n_heads < 1 or hidden % n_heads or n_kv_heads < 1 or n_heads % n_kv_heads:
+        raise ValueError("hidden size must be a multiple of n_heads, and n_heads of n_kv_heads")
+    head_dim = hidden // n_heads
+    kv = n_kv_heads * head_dim
+    ld_p = _strided_rows(k_prefix, "k_prefix", dev, torch.bfloat16, kv)
+    if _strided_rows(v_prefix, "v_prefix", dev, torch.bfloat16, kv) != ld_p and k_prefix.shape[0] > 1:
+        raise ValueError("k_prefix and v_prefix must have the same row distance")
+    prefix_len = k_prefix.shape[0] if prefix_len is None else int(prefix_len)
+    if prefix_len > k_prefix.shape[0] or prefix_len > v_prefix.shape[0]:
+        raise ValueError("the prefix tensors hold fewer than prefix_len rows")
+    _require(q_start, "q_start", torch.int32, dev, ndim=1)
+    _require(cache_lens, "cache_lens", torch.int32, dev, ndim=1)
+    n_req = cache_lens.shape[0]
+    if n_req < 1 or q_start.shape[0] != n_req + 1:
+        raise ValueError("q_start must have one entry more than cache_lens, which must have one at least")
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be a bf16 torch.Tensor")
+        if t.device != dev or t.dim() != 3 or t.shape[0] != n_req or t.shape[2] != kv:
+            raise ValueError(f"{name} must be [n_req, capacity, {kv}] on {dev}")
+        if t.shape != k_cache.shape or t.stride() != k_cache.stride() or (kv > 1 and t.stride(2) != 1):
+            raise ValueError("k_cache and v_cache must have the same shape and distances, and contiguous rows")
+    capacity = k_cache.shape[1]
+    ld_c = k_cache.stride(1) if capacity > 1 else kv
+    ld_r = k_cache.stride(0) if n_req > 1 else 0
+    if max_q is None:
+        max_q = max(1, -(-rows // n_req))
+    if out is None:
+        out = q.new_empty((rows, hidden), dtype=out_dtype)
+    ld_out = _strided_rows(out, "out", dev, None, hidden)
+    if out.shape[0] != rows:
+        raise ValueError(f"out must have shape {(rows, hidden)}")
+    if lse is not None or need_lse:
+        lse = _output(lse, "lse", q, (n_heads, rows))
+    if rows == 0:
+        return out, lse
+
+    def call():
+        sizes = (prefix_len, capacity, n_req, rows, int(max_q), int(n_heads), n_kv_heads, head_dim)
+        nbytes = L.ispa_attn_shared_workspace_bytes(*sizes)
+        ws = q.new_empty(max(nbytes, 1), dtype=torch.uint8)
+        return L.ispa_attn_shared(
+            q.data_ptr(), ld_q, k_prefix.data_ptr(), v_prefix.data_ptr(), prefix_len, ld_p, k_cache.data_ptr(),
+            v_cache.data_ptr(), capacity, ld_c, ld_r, q_start.data_ptr(), cache_lens.data_ptr(), n_req, rows,
+            int(max_q), int(n_heads), n_kv_heads, head_dim, float(scale), out.data_ptr(), _DT[out.dtype], ld_out,
+            _ptr(lse), ws.data_ptr(), nbytes, _stream(dev))
+
+    _check(_on(dev, call), "ispa_attn_shared")
+    return out, lse

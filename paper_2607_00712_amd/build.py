@@ -14,7 +14,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libispa.so")
 
 SOURCES = ["ispa_abi.cpp", "attn_fast.cpp", "gram_fast.cpp", "proj_fast.cpp", "attn_chunk.hip", "stats.hip",
-           "solve.hip", "absorb.hip", "project.hip"]
+           "solve.hip", "absorb.hip", "project.hip", "norm.hip", "rotary.hip", "attn_shared.hip"]
 BUILD = os.path.join(PKG, "_build")
 LLVM_BIN = os.environ.get("ROCM_LLVM_BIN", "/opt/rocm/lib/llvm/bin")
 

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <math.h>
 #include <mutex>
 #include <new>
@@ -599,6 +600,430 @@ int ispa_project_w8a8(const int8_t* q_a, const float* scale_a, const int8_t* q_w
                                    ispa::attn_cu_count(), stream) == hipSuccess
              ? ISPA_OK
              : ISPA_ERR_HIP;
+}
+
+}  // extern "C"
+
+// ---- norms, rotary positions, shared-prefix attention ----
+namespace {
+
+bool bad_dtype(int32_t t) { return t != ISPA_DTYPE_BF16 && t != ISPA_DTYPE_F32; }
+size_t dtype_size(int32_t t) { return t == ISPA_DTYPE_F32 ? 4 : 2; }
+
+struct Span {
+  const void* p;
+  size_t n;
+};
+// out meets one of the other buffers (null ones meet nothing)
+bool meets(const Span& out, std::initializer_list<Span> others) {
+  if (!out.p) return false;
+  for (const Span& o : others)
+    if (o.p && overlaps(out.p, out.n, o.p, o.n)) return true;
+  return false;
+}
+bool any_misaligned(std::initializer_list<const void*> ps, uintptr_t mask = 15u) {
+  for (const void* p : ps)
+    if ((uintptr_t)p & mask) return true;
+  return false;
+}
+
+// The sizes, kinds and vectors that both directions of the norm share.
+int norm_common(int32_t x_dtype, const void* y, int32_t y_dtype, int32_t post, const float* post_weight,
+                const float* gate, float alpha, int32_t norm, const float* weight, const float* bias,
+                const float* scale, const float* shift, int64_t rows, int32_t cols, int64_t group_rows, float eps,
+                int32_t h_dtype, ispa::NormArgs* a) {
+  if (bad_dtype(x_dtype) || (y && bad_dtype(y_dtype)) || (norm != ISPA_NORM_NONE && bad_dtype(h_dtype)))
+    return ISPA_ERR_UNSUPPORTED;
+  if (norm < ISPA_NORM_NONE || norm > ISPA_NORM_RMS || post < ISPA_NORM_NONE || post > ISPA_NORM_RMS)
+    return ISPA_ERR_UNSUPPORTED;
+  if (rows < 0 || rows >= (1 << 22) || cols < 8 || cols % 8 != 0 || cols > kMaxDim) return ISPA_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || isinf(eps) || !(alpha == alpha) || isinf(alpha)) return ISPA_ERR_INVALID_ARG;
+  if (norm == ISPA_NORM_NONE && (!y || weight || bias || scale || shift)) return ISPA_ERR_INVALID_ARG;
+  if (!y && (post != ISPA_NORM_NONE || post_weight || gate)) return ISPA_ERR_INVALID_ARG;
+  if (post == ISPA_NORM_NONE && post_weight) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({y, post_weight, gate, weight, bias, scale, shift})) return ISPA_ERR_INVALID_ARG;
+  memset(a, 0, sizeof(*a));
+  a->y = y;
+  a->x_f32 = x_dtype == ISPA_DTYPE_F32;
+  a->y_f32 = y_dtype == ISPA_DTYPE_F32;
+  a->h_f32 = h_dtype == ISPA_DTYPE_F32;
+  a->norm = norm;
+  a->post = post;
+  a->post_weight = post_weight;
+  a->gate = gate;
+  a->weight = weight;
+  a->bias = bias;
+  a->scale = scale;
+  a->shift = shift;
+  a->alpha = alpha;
+  a->eps = eps;
+  a->rows = rows;
+  a->group_rows = group_rows > 0 && group_rows < rows ? group_rows : (rows > 0 ? rows : 1);
+  a->cols = cols;
+  return ISPA_OK;
+}
+
+// The angles' arguments that both rotary calls share.
+int rotary_common(const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                  int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                  int32_t n_kv_heads, int32_t head_dim, int32_t x_dtype, int32_t out_dtype, ispa::RotaryArgs* a) {
+  if (bad_dtype(x_dtype) || bad_dtype(out_dtype)) return ISPA_ERR_UNSUPPORTED;
+  if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0) return ISPA_ERR_UNSUPPORTED;
+  if (rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0) return ISPA_ERR_UNSUPPORTED;
+  if (!positions || !freqs || !axis_pairs || n_axes < 1 || n_axes > ispa::kRotaryAxes) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({positions}, 3u) || any_misaligned({freqs}, 7u)) return ISPA_ERR_INVALID_ARG;
+  if (rows < 0 || rows >= (1 << 30) || n_heads < 1 || n_kv_heads < 1) return ISPA_ERR_INVALID_ARG;
+  if ((int64_t)n_heads * head_dim > (1 << 20) || (int64_t)n_kv_heads * head_dim > (1 << 20))
+    return ISPA_ERR_INVALID_ARG;
+  if (!(amplitude == amplitude) || isinf(amplitude)) return ISPA_ERR_INVALID_ARG;
+  memset(a, 0, sizeof(*a));
+  int end = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    if (axis_pairs[i] < 1 || axis_pairs[i] > rotary_dim) return ISPA_ERR_INVALID_ARG;
+    end += axis_pairs[i];
+    if (i < ispa::kRotaryAxes - 1) a->axis_end[i] = i + 1 < n_axes ? end : rotary_dim;
+  }
+  if (end != rotary_dim / 2) return ISPA_ERR_INVALID_ARG;
+  for (int i = n_axes; i < ispa::kRotaryAxes; ++i)
+    if (i < ispa::kRotaryAxes - 1) a->axis_end[i] = rotary_dim;
+  a->positions = positions;
+  a->freqs = freqs;
+  a->n_axes = n_axes;
+  a->rotary_dim = rotary_dim;
+  a->head_dim = head_dim;
+  a->n_heads = n_heads;
+  a->n_kv_heads = n_kv_heads;
+  a->interleaved = interleaved != 0;
+  a->amplitude = amplitude;
+  a->rows = rows;
+  a->x_f32 = x_dtype == ISPA_DTYPE_F32;
+  a->out_f32 = out_dtype == ISPA_DTYPE_F32;
+  return ISPA_OK;
+}
+
+bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld % 8 != 0 || ld > ((int64_t)1 << 24); }
+// bytes from the first to behind the last value of rows ld apart
+size_t rows_bytes(int64_t rows, int64_t ld, int64_t width, size_t esz) {
+  return rows > 0 ? ((size_t)(rows - 1) * ld + width) * esz : 0;
+}
+
+bool shared_sizes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows, int32_t max_q, int32_t n_heads,
+                  int32_t n_kv_heads, int32_t head_dim, ispa::SharedArgs* a) {
+  if (head_dim != 64 && head_dim != 128) return false;
+  if (prefix_len < 0 || prefix_len > 0x7fffffff || capacity < 0 || capacity > 0x7fffffff) return false;
+  if (n_req < 1 || n_rows < 0 || max_q < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0) return false;
+  if ((int64_t)n_heads * head_dim > (1 << 20)) return false;
+  if ((int64_t)n_rows * n_heads > (1 << 26) || (int64_t)n_req * n_kv_heads > (1 << 20)) return false;
+  memset(a, 0, sizeof(*a));
+  a->prefix_len = prefix_len;
+  a->capacity = (int)capacity;
+  a->n_req = n_req;
+  a->n_rows = n_rows;
+  a->max_q = max_q;
+  a->n_heads = n_heads;
+  a->n_kv_heads = n_kv_heads;
+  a->group = n_heads / n_kv_heads;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ispa_norm_residual(const void* x, int32_t x_dtype, const void* y, int32_t y_dtype, int32_t post,
+                       const float* post_weight, const float* gate, float alpha, int32_t norm, const float* weight,
+                       const float* bias, const float* scale, const float* shift, int64_t rows, int32_t cols,
+                       int64_t group_rows, float eps, void* x_out, void* h, int32_t h_dtype, hipStream_t stream) {
+  ispa::NormArgs a;
+  const int st = norm_common(x_dtype, y, y_dtype, post, post_weight, gate, alpha, norm, weight, bias, scale, shift,
+                             rows, cols, group_rows, eps, h_dtype, &a);
+  if (st != ISPA_OK) return st;
+  if (!x || (y && !x_out) || ((norm != ISPA_NORM_NONE) != (h != nullptr))) return ISPA_ERR_INVALID_ARG;
+  if (!y) x_out = nullptr;
+  if (any_misaligned({x, x_out, h})) return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  const size_t n = (size_t)rows * cols, vec = (size_t)cols * 4,
+               mod = (size_t)((rows + a.group_rows - 1) / a.group_rows) * vec;
+  const Span sx{x, n * dtype_size(x_dtype)}, sy{y, n * dtype_size(y_dtype)}, sxo{x_out, sx.n},
+      sh{h, n * dtype_size(h_dtype)};
+  const Span pw{post_weight, vec}, g{gate, mod}, w{weight, vec}, b{bias, vec}, sc{scale, mod}, sf{shift, mod};
+  if (meets(sh, {sx, sy, sxo, pw, g, w, b, sc, sf}) || meets(sxo, {sy, pw, g, w, b, sc, sf})) return ISPA_ERR_INVALID_ARG;
+  if (x_out != x && meets(sxo, {sx})) return ISPA_ERR_INVALID_ARG;
+  a.x = x;
+  a.x_out = x_out;
+  a.h = h;
+  return ispa::launch_norm_residual(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+size_t ispa_norm_residual_backward_workspace_bytes(int64_t rows, int32_t cols, int64_t group_rows) {
+  if (rows < 1 || rows >= (1 << 22) || cols < 8 || cols % 8 != 0 || cols > kMaxDim) return 0;
+  if (group_rows <= 0 || group_rows > rows) group_rows = rows;
+  int block_rows;
+  const int64_t blocks = ispa::norm_group_blocks(rows, cols, group_rows, &block_rows);
+  return round_up((size_t)((rows + group_rows - 1) / group_rows * blocks) * 3 * cols * sizeof(float), kWsAlign);
+}
+
+int ispa_norm_residual_backward(const void* d_h, int32_t h_dtype, const void* d_x_out, const void* x_out,
+                                int32_t x_dtype, const void* y, int32_t y_dtype, int32_t post,
+                                const float* post_weight, const float* gate, float alpha, int32_t norm,
+                                const float* weight, const float* bias, const float* scale, int64_t rows, int32_t cols,
+                                int64_t group_rows, float eps, void* d_x, void* d_y, float* d_gate,
+                                float* d_post_weight, float* d_weight, float* d_bias, float* d_scale, float* d_shift,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  ispa::NormArgs a;
+  const int st = norm_common(x_dtype, y, y_dtype, post, post_weight, gate, alpha, norm, weight, bias, scale, nullptr,
+                             rows, cols, group_rows, eps, h_dtype, &a);
+  if (st != ISPA_OK) return st;
+  const bool has_norm = norm != ISPA_NORM_NONE;
+  if (has_norm != (d_h != nullptr) || has_norm != (x_out != nullptr) || (!has_norm && !d_x_out))
+    return ISPA_ERR_INVALID_ARG;
+  if (!d_x || ((y != nullptr) != (d_y != nullptr))) return ISPA_ERR_INVALID_ARG;
+  if (!y && (d_gate || d_post_weight)) return ISPA_ERR_INVALID_ARG;
+  if (!has_norm && (d_weight || d_bias || d_scale || d_shift)) return ISPA_ERR_INVALID_ARG;
+  if (post == ISPA_NORM_NONE && d_post_weight) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({d_h, d_x_out, x_out, d_x, d_y, d_gate, d_post_weight, d_weight, d_bias, d_scale, d_shift}))
+    return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  const bool sums = d_gate || d_post_weight || d_weight || d_bias || d_scale || d_shift;
+  const size_t need = sums ? ispa_norm_residual_backward_workspace_bytes(rows, cols, group_rows) : 0;
+  if (sums && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return ISPA_ERR_INVALID_ARG;
+  if (!sums) workspace = nullptr;
+  const size_t n = (size_t)rows * cols, vec = (size_t)cols * 4,
+               mod = (size_t)((rows + a.group_rows - 1) / a.group_rows) * vec;
+  const size_t nx = n * dtype_size(x_dtype), ny = n * dtype_size(y_dtype);
+  const Span in[] = {{d_h, n * dtype_size(h_dtype)}, {x_out, nx}, {y, ny}, {post_weight, vec}, {gate, mod},
+                     {weight, vec}, {bias, vec}, {scale, mod}};
+  const Span out[] = {{d_x, nx}, {d_y, ny}, {d_gate, mod}, {d_post_weight, vec}, {d_weight, vec}, {d_bias, vec},
+                      {d_scale, mod}, {d_shift, mod}, {workspace, need}};
+  constexpr int kOut = sizeof(out) / sizeof(out[0]);
+  for (int i = 0; i < kOut; ++i) {
+    for (const Span& s : in)
+      if (meets(out[i], {s})) return ISPA_ERR_INVALID_ARG;
+    for (int j = i + 1; j < kOut; ++j)
+      if (meets(out[i], {out[j]})) return ISPA_ERR_INVALID_ARG;
+    if (!(i == 0 && d_x == d_x_out) && meets(out[i], {{d_x_out, nx}})) return ISPA_ERR_INVALID_ARG;
+  }
+  a.x = x_out;
+  a.d_h = d_h;
+  a.d_x_in = d_x_out;
+  a.d_x = d_x;
+  a.d_y = d_y;
+  a.d_gate = d_gate;
+  a.d_post_weight = d_post_weight;
+  a.d_weight = d_weight;
+  a.d_bias = d_bias;
+  a.d_scale = d_scale;
+  a.d_shift = d_shift;
+  a.part = (float*)workspace;
+  return ispa::launch_norm_residual_backward(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+int ispa_rotary_frequencies(const int32_t* axis_pairs, int32_t n_axes, double base, int32_t scaling, double factor,
+                            double original_length, double beta_fast, double beta_slow, double* freqs,
+                            double* amplitude) {
+  if (scaling < ISPA_ROTARY_NONE || scaling > ISPA_ROTARY_PARTS) return ISPA_ERR_UNSUPPORTED;
+  if (!axis_pairs || !freqs || n_axes < 1 || n_axes > ispa::kRotaryAxes) return ISPA_ERR_INVALID_ARG;
+  if (!(base > 1.0) || isinf(base) || !(factor >= 1.0) || isinf(factor)) return ISPA_ERR_INVALID_ARG;
+  int total = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    if (axis_pairs[i] < 1 || axis_pairs[i] > 128) return ISPA_ERR_INVALID_ARG;
+    total += axis_pairs[i];
+  }
+  if (total > 128) return ISPA_ERR_INVALID_ARG;
+  const bool parts = scaling == ISPA_ROTARY_PARTS;
+  if (parts && (n_axes != 1 || !(original_length > 0.0) || isinf(original_length) || !(beta_slow > 0.0) ||
+                !(beta_fast > beta_slow) || isinf(beta_fast)))
+    return ISPA_ERR_INVALID_ARG;
+  int at = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    const int n = axis_pairs[i];
+    const double b = scaling == ISPA_ROTARY_BASE && n > 1 ? base * pow(factor, n / (n - 1.0)) : base;
+    // pairs whose count of turns in original_length is beta: n ln(length / (2 pi beta)) / ln(base)
+    const double two_pi = 6.283185307179586;
+    double lo = 0.0, hi = 0.0;
+    if (parts) {
+      lo = floor(n * log(original_length / (two_pi * beta_fast)) / log(base));
+      hi = ceil(n * log(original_length / (two_pi * beta_slow)) / log(base));
+      if (lo < 0.0) lo = 0.0;
+      if (hi > n - 1.0) hi = n - 1.0;
+    }
+    const double span = hi - lo > 1e-3 ? hi - lo : 1e-3;
+    for (int j = 0; j < n; ++j) {
+      double f = pow(b, -(double)j / n);
+      if (scaling == ISPA_ROTARY_LINEAR) f /= factor;
+      if (parts) {
+        double ramp = (j - lo) / span;
+        ramp = ramp < 0.0 ? 0.0 : ramp > 1.0 ? 1.0 : ramp;
+        f = f * (1.0 - ramp) + f / factor * ramp;
+      }
+      freqs[at++] = f;
+    }
+  }
+  if (amplitude) *amplitude = parts ? 0.1 * log(factor) + 1.0 : 1.0;
+  return ISPA_OK;
+}
+
+int ispa_rotary(const void* x, int32_t x_dtype, int64_t ld_x, void* out, int32_t out_dtype, int64_t ld_out,
+                const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                int32_t rotary_dim, int32_t interleaved, float amplitude, int32_t inverse, int64_t rows,
+                int32_t n_heads, int32_t head_dim, hipStream_t stream) {
+  ispa::RotaryArgs a;
+  const int st = rotary_common(positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows, n_heads,
+                               1, head_dim, x_dtype, out_dtype, &a);
+  if (st != ISPA_OK) return st;
+  const int64_t hidden = (int64_t)n_heads * head_dim;
+  if (!x || !out || any_misaligned({x, out})) return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_x, hidden) || bad_ld(ld_out, hidden)) return ISPA_ERR_INVALID_ARG;
+  const Span so{out, rows_bytes(rows, ld_out, hidden, dtype_size(out_dtype))};
+  if (!(out == x && x_dtype == out_dtype && ld_x == ld_out) &&
+      meets(so, {{x, rows_bytes(rows, ld_x, hidden, dtype_size(x_dtype))}}))
+    return ISPA_ERR_INVALID_ARG;
+  if (meets(so, {{positions, (size_t)rows * n_axes * 4}, {freqs, (size_t)rotary_dim * 4}})) return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.q = x;
+  a.ld_q = ld_x;
+  a.q_out = out;
+  a.ld_out = ld_out;
+  a.inverse = inverse != 0;
+  return ispa::launch_rotary(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+int ispa_slot_map(const int32_t* q_start, const int32_t* before, int32_t n_req, int64_t n_rows, int64_t capacity,
+                  int64_t sink, int64_t window, int64_t first_position, int64_t* slots, int32_t* positions,
+                  int32_t* lens, hipStream_t stream) {
+  if (!q_start || !before || !lens || (n_rows > 0 && (!slots || !positions))) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q_start, before, lens, positions}, 3u) || any_misaligned({slots}, 7u))
+    return ISPA_ERR_INVALID_ARG;
+  if (n_req < 1 || n_rows < 0 || n_rows > 0x7fffffff || capacity < 1 || capacity > ((int64_t)1 << 31))
+    return ISPA_ERR_INVALID_ARG;
+  if (sink < 0 || window < 0 || (window == 0 && sink != 0) || (window > 0 && (sink > capacity || sink + window != capacity)))
+    return ISPA_ERR_INVALID_ARG;
+  const Span in[] = {{q_start, ((size_t)n_req + 1) * 4}, {before, (size_t)n_req * 4}};
+  const Span out[] = {{slots, (size_t)n_rows * 8}, {positions, (size_t)n_rows * 4}, {lens, (size_t)n_req * 4}};
+  for (int i = 0; i < 3; ++i) {
+    if (meets(out[i], {in[0], in[1]})) return ISPA_ERR_INVALID_ARG;
+    for (int j = i + 1; j < 3; ++j)
+      if (meets(out[i], {out[j]})) return ISPA_ERR_INVALID_ARG;
+  }
+  ispa::SlotArgs a;
+  a.q_start = q_start;
+  a.before = before;
+  a.lens = lens;
+  a.positions = positions;
+  a.slots = slots;
+  a.n_req = n_req;
+  a.rows = n_rows;
+  a.capacity = capacity;
+  a.sink = sink;
+  a.window = window;
+  a.first_position = first_position;
+  return ispa::launch_slot_map(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+int ispa_rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                       int32_t x_dtype, void* q_out, int32_t out_dtype, int64_t ld_out, void* k_cache, void* v_cache,
+                       int64_t cache_rows, const int64_t* slots, const int32_t* positions, const double* freqs,
+                       const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                       float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                       hipStream_t stream) {
+  ispa::RotaryArgs a;
+  const int st = rotary_common(positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows, n_heads,
+                               n_kv_heads, head_dim, x_dtype, out_dtype, &a);
+  if (st != ISPA_OK) return st;
+  const int64_t hidden = (int64_t)n_heads * head_dim, kv = (int64_t)n_kv_heads * head_dim;
+  if (!q || !k || !v || !q_out || !k_cache || !v_cache || !slots) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q, k, v, q_out, k_cache, v_cache}) || any_misaligned({slots}, 7u)) return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_q, hidden) || bad_ld(ld_k, kv) || bad_ld(ld_v, kv) || bad_ld(ld_out, hidden))
+    return ISPA_ERR_INVALID_ARG;
+  if (cache_rows < 1 || cache_rows > ((int64_t)1 << 40) / kv) return ISPA_ERR_INVALID_ARG;
+  const size_t es = dtype_size(x_dtype), cache = (size_t)cache_rows * kv * 2;
+  const Span sq{q, rows_bytes(rows, ld_q, hidden, es)}, sk{k, rows_bytes(rows, ld_k, kv, es)},
+      sv{v, rows_bytes(rows, ld_v, kv, es)}, so{q_out, rows_bytes(rows, ld_out, hidden, dtype_size(out_dtype))},
+      kc{k_cache, cache}, vc{v_cache, cache}, sp{positions, (size_t)rows * n_axes * 4},
+      ss{slots, (size_t)rows * 8}, sf{freqs, (size_t)rotary_dim * 4};
+  if (meets(kc, {vc, sq, sk, sv, so, sp, ss, sf}) || meets(vc, {sq, sk, sv, so, sp, ss, sf}) ||
+      meets(so, {sk, sv, sp, ss, sf}))
+    return ISPA_ERR_INVALID_ARG;
+  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && meets(so, {sq})) return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.q_out = q_out;
+  a.ld_out = ld_out;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.cache_rows = cache_rows;
+  a.slots = slots;
+  return ispa::launch_rotary(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows,
+                                        int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  ispa::SharedArgs a;
+  if (!shared_sizes(prefix_len, capacity, n_req, n_rows, max_q, n_heads, n_kv_heads, head_dim, &a) || n_rows == 0)
+    return 0;
+  return round_up(ispa::attn_shared_plan(&a, head_dim), kWsAlign);
+}
+
+int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const void* v_prefix, int64_t prefix_len,
+                     int64_t ld_prefix, const void* k_cache, const void* v_cache, int64_t capacity, int64_t ld_cache,
+                     int64_t ld_request, const int32_t* q_start, const int32_t* cache_lens, int32_t n_req,
+                     int32_t n_rows, int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                     void* out, int32_t out_dtype, int64_t ld_out, float* lse, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream) {
+  if ((head_dim != 64 && head_dim != 128) || bad_dtype(out_dtype)) return ISPA_ERR_UNSUPPORTED;
+  ispa::SharedArgs a;
+  if (!shared_sizes(prefix_len, capacity, n_req, n_rows, max_q, n_heads, n_kv_heads, head_dim, &a))
+    return ISPA_ERR_INVALID_ARG;
+  if (!(scale == scale) || isinf(scale)) return ISPA_ERR_INVALID_ARG;
+  const int64_t hidden = (int64_t)n_heads * head_dim, kv = (int64_t)n_kv_heads * head_dim;
+  if (!q || !out || !q_start || !cache_lens) return ISPA_ERR_INVALID_ARG;
+  if ((prefix_len > 0 && (!k_prefix || !v_prefix)) || (capacity > 0 && (!k_cache || !v_cache)))
+    return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q, k_prefix, v_prefix, k_cache, v_cache, out}) ||
+      any_misaligned({q_start, cache_lens, lse}, 3u))
+    return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_q, hidden) || bad_ld(ld_out, hidden) || (prefix_len > 0 && bad_ld(ld_prefix, kv)) ||
+      (capacity > 0 && (bad_ld(ld_cache, kv) || ld_request < 0 || ld_request % 8 != 0)))
+    return ISPA_ERR_INVALID_ARG;
+  if (n_rows == 0) return ISPA_OK;
+  const size_t need = ispa_attn_shared_workspace_bytes(prefix_len, capacity, n_req, n_rows, max_q, n_heads, n_kv_heads,
+                                                       head_dim);
+  if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return ISPA_ERR_INVALID_ARG;
+  const size_t pre = rows_bytes(prefix_len, ld_prefix, kv, 2),
+               own = capacity > 0 ? ((size_t)(n_req - 1) * ld_request) * 2 + rows_bytes(capacity, ld_cache, kv, 2) : 0;
+  const Span in[] = {{q, rows_bytes(n_rows, ld_q, hidden, 2)}, {k_prefix, pre}, {v_prefix, pre}, {k_cache, own},
+                     {v_cache, own}, {q_start, ((size_t)n_req + 1) * 4}, {cache_lens, (size_t)n_req * 4}};
+  const Span so{out, rows_bytes(n_rows, ld_out, hidden, dtype_size(out_dtype))},
+      sl{lse, (size_t)n_heads * n_rows * 4}, sw{workspace, need};
+  for (const Span& s : in)
+    if (meets(so, {s}) || meets(sl, {s}) || meets(sw, {s})) return ISPA_ERR_INVALID_ARG;
+  if (meets(so, {sl, sw}) || meets(sl, {sw})) return ISPA_ERR_INVALID_ARG;
+  ispa::attn_shared_plan(&a, head_dim);
+  a.q = (const uint16_t*)q;
+  a.k_prefix = (const uint16_t*)k_prefix;
+  a.v_prefix = (const uint16_t*)v_prefix;
+  a.k_cache = (const uint16_t*)k_cache;
+  a.v_cache = (const uint16_t*)v_cache;
+  a.ld_q = ld_q;
+  a.ld_prefix = ld_prefix;
+  a.ld_cache = ld_cache;
+  a.ld_request = ld_request;
+  a.ld_out = ld_out;
+  a.q_start = q_start;
+  a.lens = cache_lens;
+  a.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)head_dim);
+  a.scale_log2 = a.scale * 1.4426950408889634f;
+  a.out = out;
+  a.out_bf16 = out_dtype == ISPA_DTYPE_BF16;
+  a.lse = lse;
+  a.part_o = (float*)workspace;
+  a.part_lse = (float*)((char*)workspace + a.lse_offset);
+  return ispa::launch_attn_shared(a, head_dim, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
 }
 
 }  // extern "C"

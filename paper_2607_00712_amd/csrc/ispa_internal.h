@@ -176,4 +176,79 @@ int solve_lookahead_check(int nblk, int n_cu);
 hipError_t launch_solve(const float* G, const float* C, int d, int d_out, float lambda,
                         float* delta_w, const SolveWork& w, hipStream_t stream);
 
+// ---- norms around a block (norm.hip) ----
+struct NormArgs {
+  const void* x;   // the stream before y (forward) or after it (backward)
+  const void* y;   // the block's output, or null
+  int x_f32, y_f32, h_f32;
+  int norm, post;  // ISPA_NORM_*
+  const float *post_weight, *gate, *weight, *bias, *scale, *shift;  // each may be null
+  float alpha, eps;
+  int64_t rows, group_rows;
+  int cols;
+  void *x_out, *h;  // forward
+  // backward
+  const void *d_h, *d_x_in;
+  void *d_x, *d_y;
+  float *d_gate, *d_post_weight, *d_weight, *d_bias, *d_scale, *d_shift;
+  float* part;  // sums of each workgroup, or null where no vector takes part
+  // set by the launch: lanes or waves to a row, rows of a workgroup at a time,
+  // workgroups to a group
+  int lanes, waves, block_rows, group_blocks;
+  int64_t n_groups;
+};
+hipError_t launch_norm_residual(NormArgs a, hipStream_t stream);
+// workgroups that share a group's rows in the backward pass
+int norm_group_blocks(int64_t rows, int cols, int64_t group_rows, int* block_rows);
+hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream);
+
+// ---- rotary positions (rotary.hip) ----
+constexpr int kRotaryAxes = 4;
+struct RotaryArgs {
+  const void *q, *k, *v;  // k and v null: q alone
+  void *q_out, *k_cache, *v_cache;
+  int x_f32, out_f32;
+  int64_t ld_q, ld_k, ld_v, ld_out;  // elements
+  const int32_t* positions;          // [rows, n_axes]
+  const int64_t* slots;              // [rows], cache rows
+  const double* freqs;               // [rotary_dim / 2], radians per position
+  int n_axes;
+  int axis_end[kRotaryAxes - 1];     // first pair behind each axis but the last
+  int rotary_dim, head_dim, n_heads, n_kv_heads;
+  int interleaved, inverse;
+  float amplitude;
+  int64_t rows, cache_rows;
+  int tokens;  // set by the launch: rows of a workgroup
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
+struct SlotArgs {
+  const int32_t *q_start, *before;
+  int32_t *lens, *positions;
+  int64_t* slots;
+  int n_req;
+  int64_t rows, capacity, sink, window, first_position;
+};
+hipError_t launch_slot_map(const SlotArgs& a, hipStream_t stream);
+
+// ---- attention over a shared prefix (attn_shared.hip) ----
+struct SharedArgs {
+  const uint16_t *q, *k_prefix, *v_prefix, *k_cache, *v_cache;
+  int64_t ld_q, ld_prefix, ld_cache, ld_request, ld_out;  // elements
+  int64_t prefix_len;
+  const int32_t *q_start, *lens;
+  int n_rows, n_req, max_q, capacity;
+  int n_heads, n_kv_heads, group;  // group = n_heads / n_kv_heads
+  float scale, scale_log2;
+  void* out;
+  int out_bf16;
+  float* lse;
+  // set by the plan: the layout of the work (attn_shared.hip), the partial results
+  int waves, prefix_kg, own_kg, prefix_tiles, own_tiles, prefix_splits, own_splits, prefix_blocks;
+  size_t lse_offset;
+  float *part_o, *part_lse;
+};
+// fills the plan and returns the workspace bytes
+size_t attn_shared_plan(SharedArgs* a, int head_dim);
+hipError_t launch_attn_shared(const SharedArgs& a, int head_dim, hipStream_t stream);
+
 }  // namespace ispa
