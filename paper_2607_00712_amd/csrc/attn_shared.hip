@@ -15,21 +15,22 @@
 // of the batch (or of one request) form one list of rows against that key head,
 // row r = token r / G, query head G h + r % G.
 //
-// Work items. A row tile (32 RG rows) of one key head against a segment of the
+// Work items. A row tile (32 RB RG rows) of one key head against a segment of the
 // prefix, or of one request's own keys (the device knows the lengths: an item takes
 // its even share of them). Each leaves a normalised partial output and its LSE for
 // every row in the workspace, [split][row][head], and a second launch joins a
 // row's splits, in order: the result does not depend on the order of execution.
 //
-// A workgroup of NW waves splits into RG groups of rows and KG groups of keys (RG
-// KG = NW): with few rows the waves share the keys of a step, with many rows they
-// share the rows. Keys come in blocks of 32, KG to a step, straight from HBM to
-// LDS (buffer loads to LDS) into a ring of 8 blocks, so that up to 7 blocks are in
-// flight while one is worked on; one barrier a step. A block's descriptor ends at
-// its last valid row: rows behind a set's end read as zero whatever the cache
-// holds there, and are masked.
+// A workgroup is 4 waves of up to 64 rows (RB blocks of 32): RG groups of rows times
+// KG groups of keys, RG KG = 4. With few rows the waves take different keys of a
+// step, with many rows they share them. 64 rows to a wave halve the LDS reads of an
+// operand a product; the registers (256 of accumulators and queries) allow one wave a
+// SIMD, which overlaps softmax and products itself.
+// Keys come in blocks of 32, KG to a step, straight from HBM to LDS into a ring of 8
+// blocks, one barrier a step. A block's descriptor ends at its last valid row: rows
+// behind a set's end read as zero whatever the cache holds there, and are masked.
 //
-// Per block and wave, 32 keys x 32 rows (bf16 MFMA 32x32x16, fp32 accumulation):
+// Per block and row block, 32 keys x 32 rows (bf16 MFMA 32x32x16, fp32 accumulation):
 //   S^T = K Q^T      A = K rows from LDS, B = Q^T in registers: a lane holds the
 //                    scores of one row (lane % 32) for 16 of the 32 keys
 //   O^T += V^T P^T   B = P^T straight from the score registers; the contraction
@@ -47,10 +48,15 @@
 namespace ispa {
 namespace {
 
-constexpr int kRingBlocks = 8;  // blocks of 32 keys in LDS
-constexpr int kBlk = 32;        // keys of a block, rows of a wave
+constexpr int kRingBlocks = 10;  // blocks of 32 keys in LDS (160 KB with 128 values a head)
+constexpr int kBlk = 32;        // keys of a block, rows of a row block
+constexpr int kShWaves = 4;
+constexpr int kShThreads = kShWaves * 64;
 constexpr int kShXcds = 8;
-constexpr float kShLazy = 8.f;  // rescale threshold of the softmax reference (log2)
+constexpr float kShLazy = 8.f;     // rescale threshold of the softmax reference (log2)
+constexpr float kShFar = 1024.f;   // and of a block's sum of weights of 16 keys
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 template <int D>
 struct SCfg {
@@ -60,6 +66,8 @@ struct SCfg {
   static constexpr int blockBytes = 2 * tileBytes;
   static constexpr int slices = D / 16;  // k steps of K Q^T
   static constexpr int dBlocks = D / 32;
+  static constexpr int loads = kBlk * chunks / kShThreads;  // direct loads of a thread for K (and V) of a block
+  static_assert(loads * kShThreads == kBlk * chunks, "block load split");
 };
 
 // Chunk swizzles of the LDS rows (a direct load fills consecutive 16-byte places, so
@@ -74,124 +82,229 @@ __device__ __forceinline__ int swizzle_v(int row) {
   return D == 128 ? ((4 * (row & 3)) ^ (2 * ((row >> 2) & 1))) : (row & (SCfg<D>::chunks - 1));
 }
 
-__device__ __forceinline__ uint32_t sh_lds_addr(const char* p) { return (uint32_t)(uintptr_t)(ISPA_LDS const char*)p; }
-
-__device__ __forceinline__ f32x16 sh_mfma(u32x4 a, bf16x8 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, c, 0, 0, 0);
+__device__ __forceinline__ f32x16 sh_mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// Four operand reads and their wait in one statement. (Through the builtin the
-// compiler takes a read as possibly behind the direct loads in flight and waits for
-// all of them.)
-__device__ __forceinline__ void read_k4(const uint32_t (&ad)[4], uint32_t off, u32x4 (&r)[4]) {
-  asm volatile(
-      "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
-      : "v"(ad[0] + off), "v"(ad[1] + off), "v"(ad[2] + off), "v"(ad[3] + off)
-      : "memory");
+// 64 x 16 bytes from HBM to LDS at `lds` + 16 lane (wave-uniform `lds`): lane i's from
+// byte voff of the descriptor, zero past its end. In assembly, so that the compiler's
+// LDS reads wait for LDS reads alone: through the builtin it takes every read as
+// possibly behind the loads in flight and waits for all of them. The statement has no
+// register outputs; arrival is waited for with arrived() below.
+__device__ __forceinline__ void load_to_lds(i32x4 desc, int voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(desc), "s"(lds)
+               : "memory");
 }
-// V^T operands of one 16-key slice, two 32-wide blocks of the head
-template <int IMM>
-__device__ __forceinline__ void read_v2(const uint32_t (&lo)[2], const uint32_t (&hi)[2], uint32_t off,
-                                        u32x4 (&r)[2]) {
-  u32x2 a0, a1, b0, b1;
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
-      "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1)
-      : "v"(lo[0] + off), "v"(hi[0] + off), "v"(lo[1] + off), "v"(hi[1] + off), "i"(IMM)
-      : "memory");
-  r[0] = u32x4{a0[0], a0[1], a1[0], a1[1]};
-  r[1] = u32x4{b0[0], b0[1], b1[0], b1[1]};
+// At most N of this wave's loads to LDS are in flight; then every wave is here.
+template <int N>
+__device__ __forceinline__ void arrived() {
+  static_assert(N >= 0 && N <= 63, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(N) : "memory");
+}
+__device__ __forceinline__ i32x4 descriptor(const uint16_t* p, int bytes) {
+  const uint64_t u = (uint64_t)(uintptr_t)p;
+  return i32x4{(int)(uint32_t)u, (int)(uint32_t)(u >> 32) & 0xffff, bytes, 0x00020000};
 }
 
 // The lane pair (l, l ^ 32) holds one row's scores of the two halves of a block's keys.
 __device__ __forceinline__ float pair_max32(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ __forceinline__ float pair_sum32(float x) { return x + __shfl_xor(x, 32); }
 
-template <int D>
+// A wave's state: RB blocks of 32 rows
+template <int D, int RB>
 struct SWave {
   using C = SCfg<D>;
-  f32x16 acc[C::dBlocks];       // O^T
-  float m, l, lr;               // reference (raw scores), sums of the weights and of the rounded weights
-  bf16x8 q[C::slices];          // Q^T operand
-  uint32_t kad[C::slices / 4][4];       // K operand addresses in a block
-  uint32_t vlo[C::dBlocks / 2][2], vhi[C::dBlocks / 2][2];  // V^T operand addresses in a block
+  f32x16 acc[RB][C::dBlocks];       // O^T
+  bf16x8 q[RB][C::slices];          // Q^T operand
+  float m[RB], l[RB], lr[RB];       // reference (raw scores), sums of the weights and of the rounded weights
+  int kad[C::slices];               // K operand offsets in a block
+  int vad[2][C::dBlocks];           // V^T operand offsets in a block (16-key slice 0)
 };
 
-// One block of 32 keys (nv > 0 of them valid) at LDS offset `off`.
-template <int D>
-__device__ __forceinline__ void block_step(const SharedArgs& a, SWave<D>& w, uint32_t off, int nv, int hh) {
+typedef ISPA_LDS const char lds_char;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// K operands of the block at `blk`
+template <int D, int RB>
+__device__ __forceinline__ void read_k(const SWave<D, RB>& w, lds_char* blk, bf16x8 (&k)[SCfg<D>::slices]) {
+#pragma unroll
+  for (int i = 0; i < SCfg<D>::slices; ++i) k[i] = *(ISPA_LDS const bf16x8*)(blk + w.kad[i]);
+}
+// S^T = K Q^T
+template <int D, int RB>
+__device__ __forceinline__ void scores(const SWave<D, RB>& w, const bf16x8 (&k)[SCfg<D>::slices], f32x16 (&sc)[RB]) {
+#pragma unroll
+  for (int i = 0; i < SCfg<D>::slices; ++i)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) sc[b] = sh_mfma(k[i], w.q[b][i], i == 0 ? f32x16{} : sc[b]);
+}
+
+// V^T operand o of the block at `blk`: 16-key slice o / dBlocks, values 32 (o % dBlocks) on
+constexpr int kVAhead = 3;  // operands read ahead of their use
+template <int D, int RB>
+__device__ __forceinline__ bf16x8 read_v1(const SWave<D, RB>& w, lds_char* blk, int o) {
   using C = SCfg<D>;
-  f32x16 sc = f32x16{};
+  union {
+    s16x4 half[2];
+    bf16x8 v;
+  } u;
 #pragma unroll
-  for (int g = 0; g < C::slices / 4; ++g) {
-    u32x4 k[4];
-    read_k4(w.kad[g], off, k);
+  for (int i = 0; i < 2; ++i)
+    u.half[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (ISPA_LDS s16x4*)(blk + w.vad[i][o % C::dBlocks] + C::tileBytes + 16 * (o / C::dBlocks) * C::rowBytes));
+  return u.v;
+}
+// O^T += V^T P^T of row block b
+template <int D, int RB>
+__device__ __forceinline__ void products(SWave<D, RB>& w, int b, const bf16x8 (&v)[2 * SCfg<D>::dBlocks],
+                                         const bf16x8 (&p)[2]) {
+  constexpr int n = SCfg<D>::dBlocks;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sc = sh_mfma(k[i], w.q[4 * g + i], sc);
+  for (int o = 0; o < 2 * n; ++o) w.acc[b][o % n] = sh_mfma(v[o], p[o / n], w.acc[b][o % n]);
+}
+
+// Keys from nv on are out of the set: register r holds key 4 hh + 8 (r / 4) + r % 4.
+template <int RB>
+__device__ __forceinline__ void mask(f32x16 (&sc)[RB], int nv, int hh) {
+  const int lim = nv - 4 * hh;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (8 * (r >> 2) + (r & 3) >= lim) {
+#pragma unroll
+      for (int b = 0; b < RB; ++b) sc[b][r] = -INFINITY;
+    }
+}
+
+// x *= alpha in the accumulation registers, for the rare rescale: left to the compiler
+// the multiplication pulls copies of every accumulator into the loop. (The first wait
+// states cover a product still being written, the last ones a product that follows.)
+__device__ __forceinline__ void scale_acc(f32x16& x, float alpha) {
+  float t;
+  asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float e = x[i];
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                 : "+a"(e), "=&v"(t)
+                 : "v"(alpha));
+    x[i] = e;
   }
-  u32x4 v[C::dBlocks / 2][2];
+  asm volatile("s_nop 7" ::);
+}
+
+template <int RB>
+__device__ __forceinline__ void maxima(const f32x16 (&sc)[RB], float (&top)[RB]) {
 #pragma unroll
-  for (int p = 0; p < C::dBlocks / 2; ++p) read_v2<C::tileBytes>(w.vlo[p], w.vhi[p], off, v[p]);
-  if (nv < kBlk) {
-    // register r holds key 4 hh + 8 (r / 4) + r % 4
-    const int lim = nv - 4 * hh;
+  for (int b = 0; b < RB; ++b) {
+    float t = fmaxf(fmaxf(sc[b][0], sc[b][1]), sc[b][2]);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (8 * (r >> 2) + (r & 3) >= lim) sc[r] = -INFINITY;
+    for (int r = 3; r < 15; r += 2) t = fmaxf(fmaxf(t, sc[b][r]), sc[b][r + 1]);
+    top[b] = pair_max32(fmaxf(t, sc[b][15]));
   }
-  float top = fmaxf(sc[0], sc[1]);
+}
+
+// The softmax reference follows the block's maxima; O and the sums are rescaled only
+// when some row's maximum is above its reference by more than `lazy` (log2).
+template <int D, int RB>
+__device__ __forceinline__ void follow(const SharedArgs& a, SWave<D, RB>& w, const float (&top)[RB], float lazy) {
+  bool far = false;
 #pragma unroll
-  for (int r = 2; r < 16; ++r) top = fmaxf(top, sc[r]);
-  top = pair_max32(top);
-  if (__any((top - w.m) * a.scale_log2 > kShLazy || w.m == -INFINITY)) {
-    const float m_new = fmaxf(w.m, top);
+  for (int b = 0; b < RB; ++b) far = far || (top[b] - w.m[b]) * a.scale_log2 > lazy || w.m[b] == -INFINITY;
+  if (!__any(far)) return;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const float m_new = fmaxf(w.m[b], top[b]);
     // (a row whose scores are all -inf so far keeps its zeros)
-    const float alpha = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m - m_new) * a.scale_log2);
-    w.l *= alpha;
-    w.lr *= alpha;
+    const float alpha = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m[b] - m_new) * a.scale_log2);
+    w.l[b] *= alpha;
+    w.lr[b] *= alpha;
 #pragma unroll
-    for (int d = 0; d < C::dBlocks; ++d) w.acc[d] *= alpha;
-    w.m = m_new;
+    for (int d = 0; d < SCfg<D>::dBlocks; ++d) scale_acc(w.acc[b][d], alpha);
+    w.m[b] = m_new;
   }
-  const float mc = w.m == -INFINITY ? 0.f : w.m * a.scale_log2;
+}
+
+// P^T of row block b, rounded to bf16, and its sums before and after the rounding
+template <int D, int RB>
+__device__ __forceinline__ void weights(const SharedArgs& a, const SWave<D, RB>& w, int b, const f32x16& sc,
+                                        bf16x8 (&p)[2], float& sum, float& rounded) {
+  const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+  const float mc = w.m[b] == -INFINITY ? 0.f : w.m[b] * a.scale_log2;
+  float s[2] = {0.f, 0.f}, r[2] = {0.f, 0.f};
 #pragma unroll
-  for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale_log2, -mc));
-  float s0 = sc[0] + sc[1], s1 = sc[2] + sc[3];
-#pragma unroll
-  for (int r = 4; r < 16; r += 4) {
-    s0 += sc[r] + sc[r + 1];
-    s1 += sc[r + 2] + sc[r + 3];
+  for (int i = 0; i < 16; i += 2) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -mc));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -mc));
+    const bf16x2 two = {(__bf16)e0, (__bf16)e1};
+    s[0] += e0;
+    s[1] += e1;
+    r[i / 2 % 2] = __builtin_amdgcn_fdot2_f32_bf16(two, one, r[i / 2 % 2], false);
+    p[i / 8][i % 8] = two[0];
+    p[i / 8][i % 8 + 1] = two[1];
   }
-  w.l += s0 + s1;
-  bf16x8 p0, p1;
+  sum = s[0] + s[1];
+  rounded = r[0] + r[1];
+}
+
+// One block of the pipelined loop, of three blocks in a row, as one straight run of
+// matrix instructions with the vector work between them (the order is pinned): the
+// products of block j - 1 (weights p, operands at `vblk`), then the scores of block
+// j + 1 (operands at `kblk`) into `next`, and beside them the softmax of block j (sc)
+// into p. The first V operands come in `v`, read before.
+template <int D, int RB>
+__device__ __forceinline__ void pipelined(const SharedArgs& a, SWave<D, RB>& w, lds_char* vblk, lds_char* kblk,
+                                          f32x16 (&sc)[RB], f32x16 (&next)[RB], bf16x8 (&p)[RB][2],
+                                          bf16x8 (&v)[2 * SCfg<D>::dBlocks], float (&sum)[RB], float (&rounded)[RB]) {
+  using C = SCfg<D>;
+  constexpr int kV = 2 * C::dBlocks, kK = C::slices;  // operands
+  constexpr int kSteps = RB * (kV + kK);              // matrix instructions
+  constexpr int kValues = 16 * RB;
+  const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+  bf16x8 k[kK], pn[RB][2];
+  float mc[RB], s1[RB], r1[RB], even = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p0[e] = (__bf16)sc[e];
-    p1[e] = (__bf16)sc[8 + e];
+  for (int b = 0; b < RB; ++b) {
+    mc[b] = w.m[b] == -INFINITY ? 0.f : w.m[b] * a.scale_log2;
+    sum[b] = s1[b] = rounded[b] = r1[b] = 0.f;
   }
-  {
-    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
-    float r0 = w.lr, r1 = 0.f;
-    r0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p0, p0, 0, 1), one, r0, false);
-    r1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p0, p0, 2, 3), one, r1, false);
-    r0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p0, p0, 4, 5), one, r0, false);
-    r1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p0, p0, 6, 7), one, r1, false);
-    r0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p1, p1, 0, 1), one, r0, false);
-    r1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p1, p1, 2, 3), one, r1, false);
-    r0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p1, p1, 4, 5), one, r0, false);
-    r1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p1, p1, 6, 7), one, r1, false);
-    w.lr = r0 + r1;
+#pragma unroll
+  for (int t = 0; t < kSteps; ++t) {
+    // operands three ahead
+    if (t < RB * kV && t % RB == 0 && t / RB + kVAhead < kV) v[t / RB + kVAhead] = read_v1<D, RB>(w, vblk, t / RB + kVAhead);
+    if (t >= RB * (kV - kVAhead) && t % RB == 0 && t / RB - (kV - kVAhead) < kK)
+      k[t / RB - (kV - kVAhead)] = *(ISPA_LDS const bf16x8*)(kblk + w.kad[t / RB - (kV - kVAhead)]);
+    if (t < RB * kV) {
+      const int o = t / RB, b = t % RB;
+      w.acc[b][o % C::dBlocks] = sh_mfma(v[o], p[b][o / C::dBlocks], w.acc[b][o % C::dBlocks]);
+    } else {
+      const int o = (t - RB * kV) / RB, b = t % RB;
+      next[b] = sh_mfma(k[o], w.q[b][o], o == 0 ? f32x16{} : next[b]);
+    }
+#pragma unroll
+    for (int i = t * kValues / kSteps; i < (t + 1) * kValues / kSteps; ++i) {
+      const int b = i / 16, r = i % 16;
+      const float e = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.scale_log2, -mc[b]));
+      if (r % 2 == 0) {
+        even = e;
+        sum[b] += e;
+      } else {
+        s1[b] += e;
+        const bf16x2 two = {(__bf16)even, (__bf16)e};
+        pn[b][r / 8][r % 8 - 1] = two[0];
+        pn[b][r / 8][r % 8] = two[1];
+        float& rs = r % 4 == 1 ? rounded[b] : r1[b];
+        rs = __builtin_amdgcn_fdot2_f32_bf16(two, one, rs, false);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
-  for (int d = 0; d < C::dBlocks; ++d) w.acc[d] = sh_mfma(v[d >> 1][d & 1], p0, w.acc[d]);
+  for (int b = 0; b < RB; ++b) {
+    sum[b] += s1[b];
+    rounded[b] += r1[b];
 #pragma unroll
-  for (int p = 0; p < C::dBlocks / 2; ++p)
-    read_v2<C::tileBytes + 16 * C::rowBytes>(w.vlo[p], w.vhi[p], off, v[p]);
-#pragma unroll
-  for (int d = 0; d < C::dBlocks; ++d) w.acc[d] = sh_mfma(v[d >> 1][d & 1], p1, w.acc[d]);
+    for (int h = 0; h < 2; ++h) p[b][h] = pn[b][h];
+  }
 }
 
 // Keys [begin, end) of one key head: rows of ld elements at kb / vb.
@@ -202,184 +315,297 @@ struct Keys {
   int64_t begin, end;
 };
 
-// 16-byte places of K (and of V) of a block, and direct loads of a thread for a
-// block: K's and V's, or with more threads than places either K's or V's
-template <int D, int NW>
-struct SLoads {
-  static constexpr int places = kBlk * SCfg<D>::chunks;
-  static constexpr int each = places / (NW * 64);  // 0: one load in all, of K or of V
-  static constexpr int block = each > 0 ? 2 * each : 1;
-  static_assert(each > 0 ? places % (NW * 64) == 0 : 2 * places == NW * 64, "block load split");
+// What is left to load: the next key's K and V rows, and the count of keys from there.
+struct Feed {
+  const uint16_t *k, *v;
+  int left;
+  int64_t block;       // elements of 32 rows
+  int row_bytes, pad;  // bytes from row to row, and of them behind the head's values
+  int qstride;         // bytes between the rows of a thread's successive loads
+  int voffk, voffv, wave;
 };
 
-// Direct loads of the KG blocks of step `step` into ring slot step % (8 / KG).
-// Thread t of load i fills 16-byte place i * NW * 64 + t of a block's K (or V) rows.
-template <int D, int NW, int KG>
-__device__ __forceinline__ void stage(const Keys& ks, int step, char* smem, int voffk, int voffv, int wave) {
+// Direct loads of the next N blocks into LDS at `to`: load i of thread t fills 16-byte
+// place i * 256 + t of a block's K (and V) rows.
+template <int D, int N>
+__device__ __forceinline__ void stage(Feed& f, uint32_t to) {
   using C = SCfg<D>;
-  constexpr int kLoads = SLoads<D, NW>::each;
-  constexpr int kSlots = kRingBlocks / KG;
-  char* slot = smem + (step % kSlots) * KG * C::blockBytes;
-  const int qstride = (int)(NW * 64 / C::chunks * ks.ld * 2);
+  to += f.wave * 1024;
 #pragma unroll
-  for (int b = 0; b < KG; ++b) {
-    const int64_t k0 = ks.begin + ((int64_t)step * KG + b) * kBlk;
-    const int64_t left = ks.end - k0;
-    const int nv = left >= kBlk ? kBlk : left > 0 ? (int)left : 0;
-    // nothing valid: an empty descriptor, the loads write zeros (every step issues the
-    // same number of loads, which the counted waits need)
-    const int bytes = nv > 0 ? (int)(((int64_t)(nv - 1) * ks.ld + D) * 2) : 0;
-    const int64_t base = nv > 0 ? k0 * ks.ld : 0;
-    if constexpr (kLoads == 0) {
-      const bool v = wave >= NW / 2;
-      const __amdgpu_buffer_rsrc_t rs =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>((v ? ks.vb : ks.kb) + base), 0, bytes, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ISPA_LDS void*)(slot + b * C::blockBytes + wave * 1024), 16,
-                                               v ? voffv : voffk, 0, 0, 0);
-      continue;
-    }
-    const __amdgpu_buffer_rsrc_t rk =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(ks.kb + base), 0, bytes, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rv =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(ks.vb + base), 0, bytes, 0x00020000);
+  for (int b = 0; b < N; ++b) {
+    // behind the last key: an empty descriptor, whose loads write zeros (every step
+    // issues the same number of loads, which the counted waits need)
+    const int nv = f.left < 0 ? 0 : f.left < kBlk ? f.left : kBlk;
+    const int bytes = nv > 0 ? nv * f.row_bytes - f.pad : 0;
+    const i32x4 dk = descriptor(f.k, bytes), dv = descriptor(f.v, bytes);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int place = (i * NW + wave) * 1024;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (ISPA_LDS void*)(slot + b * C::blockBytes + place), 16,
-                                               voffk + i * qstride, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (ISPA_LDS void*)(slot + b * C::blockBytes + C::tileBytes + place),
-                                               16, voffv + i * qstride, 0, 0, 0);
+    for (int i = 0; i < C::loads; ++i) {
+      load_to_lds(dk, f.voffk + i * f.qstride, to + b * C::blockBytes + i * kShWaves * 1024);
+      load_to_lds(dv, f.voffv + i * f.qstride, to + b * C::blockBytes + C::tileBytes + i * kShWaves * 1024);
     }
+    f.k += f.block;
+    f.v += f.block;
+    f.left -= kBlk;
   }
 }
 
-template <int N>
-__device__ __forceinline__ void sh_vm_wait() {
-  static_assert(N >= 0 && N <= 63, "vmcnt range");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
-}
-
-// One item: rows [row0, row0 + 32 RG) of n_item_rows (row r = token first + r / G)
-// against `ks`, into split `split`.
-template <int D, int NW, int KG>
+// One item: rows [row0, row0 + 32 RB RG) of n_item_rows (row r = token first + r / G)
+// against `ks`, into split `split`; RG = 4 / KG row groups.
+template <int D, int KG, int RB>
 __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const Keys& ks, int kv_head, int first,
                                          int64_t row0, int64_t n_item_rows, int split) {
   using C = SCfg<D>;
-  constexpr int kSlots = kRingBlocks / KG;
-  constexpr int kStepLoads = KG * SLoads<D, NW>::block;
+  constexpr int kStep = KG == 4 ? 4 : 2;          // blocks of a step
+  constexpr int kSlots = kRingBlocks / kStep;     // steps in LDS
+  constexpr int kStepLoads = 2 * kStep * C::loads;
+  constexpr int kStepBytes = kStep * C::blockBytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, ql = lane & 31;
   const int kg = wave % KG, rg = wave / KG;
-  const int64_t r = row0 + rg * kBlk + ql;
-  const bool live = r < n_item_rows;
-  const int64_t token = first + (live ? r / a.group : 0);
-  const int head = kv_head * a.group + (live ? (int)(r % a.group) : 0);
+  lds_char* ring = (lds_char*)smem;
 
-  SWave<D> w;
+  SWave<D, RB> w;
+  bool live[RB];
+  int token[RB], head[RB];
 #pragma unroll
-  for (int k = 0; k < C::slices; ++k)
-    w.q[k] = live ? *(const bf16x8*)(a.q + token * a.ld_q + head * D + 16 * k + 8 * hh) : bf16x8{};
+  for (int b = 0; b < RB; ++b) {
+    const int64_t r = row0 + (rg * RB + b) * kBlk + ql;
+    live[b] = r < n_item_rows;
+    token[b] = first + (live[b] ? (int)(r / a.group) : 0);
+    head[b] = kv_head * a.group + (live[b] ? (int)(r % a.group) : 0);
 #pragma unroll
-  for (int d = 0; d < C::dBlocks; ++d) w.acc[d] = f32x16{};
-  w.m = -INFINITY;
-  w.l = 0.f;
-  w.lr = 0.f;
-  const uint32_t lds0 = sh_lds_addr(smem);
+    for (int k = 0; k < C::slices; ++k)
+      w.q[b][k] = live[b] ? *(const bf16x8*)(a.q + token[b] * a.ld_q + head[b] * D + 16 * k + 8 * hh) : bf16x8{};
 #pragma unroll
-  for (int k = 0; k < C::slices; ++k)
-    w.kad[k >> 2][k & 3] = lds0 + ql * C::rowBytes + (((2 * k + hh) ^ swizzle_k<D>(ql)) << 4);
+    for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] = f32x16{};
+    w.m[b] = -INFINITY;
+    w.l[b] = 0.f;
+    w.lr[b] = 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < C::slices; ++k) w.kad[k] = ql * C::rowBytes + (((2 * k + hh) ^ swizzle_k<D>(ql)) << 4);
   {
     const int g16 = lane >> 4, sl = lane & 15;
 #pragma unroll
-    for (int d = 0; d < C::dBlocks; ++d) {
-      const int chunk = 4 * d + 2 * (g16 & 1) + ((sl & 3) >> 1);
-      const int row = 4 * (g16 >> 1) + (sl >> 2);
-      w.vlo[d >> 1][d & 1] = lds0 + row * C::rowBytes + ((chunk ^ swizzle_v<D>(row)) << 4) + ((sl & 1) << 3);
-      w.vhi[d >> 1][d & 1] = lds0 + (row + 8) * C::rowBytes + ((chunk ^ swizzle_v<D>(row + 8)) << 4) + ((sl & 1) << 3);
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 0; d < C::dBlocks; ++d) {
+        const int chunk = 4 * d + 2 * (g16 & 1) + ((sl & 3) >> 1);
+        const int row = 8 * i + 4 * (g16 >> 1) + (sl >> 2);
+        w.vad[i][d] = row * C::rowBytes + ((chunk ^ swizzle_v<D>(row)) << 4) + ((sl & 1) << 3);
+      }
   }
-  int voffk, voffv;
+  const int n_keys = (int)(ks.end - ks.begin);
+  Feed f;
+  f.k = ks.kb + ks.begin * ks.ld;
+  f.v = ks.vb + ks.begin * ks.ld;
+  f.block = ks.ld * kBlk;
+  f.row_bytes = (int)(ks.ld * 2);
+  f.pad = f.row_bytes - D * 2;
+  f.qstride = kShThreads / C::chunks * f.row_bytes;
+  f.wave = wave;
   {
-    const int row = tid % SLoads<D, NW>::places / C::chunks, stored = tid % C::chunks;
-    voffk = (int)((row * ks.ld + (stored ^ swizzle_k<D>(row)) * 8) * 2);
-    voffv = (int)((row * ks.ld + (stored ^ swizzle_v<D>(row)) * 8) * 2);
+    const int row = tid / C::chunks, stored = tid % C::chunks;
+    f.voffk = row * f.row_bytes + (stored ^ swizzle_k<D>(row)) * 16;
+    f.voffv = row * f.row_bytes + (stored ^ swizzle_v<D>(row)) * 16;
   }
-  const int n_steps = (int)((ks.end - ks.begin + KG * kBlk - 1) / (KG * kBlk));
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+  const int n_steps = (n_keys + kStep * kBlk - 1) / (kStep * kBlk);
+  f32x16 sc[RB];
+  float top[RB], sum[RB], rounded[RB];
+  bf16x8 v[2 * C::dBlocks], p[RB][2];
+  if constexpr (KG == 4) {
+    // bound by the bytes of the keys: a step at a time, each wave its own block of it
+    f.left = n_keys;
+    int left = n_keys - kg * kBlk;  // keys from this wave's block on
+    int slot = 0;
+    stage<D, kStep>(f, ring_at);
+    // the compiler's wait for the query loads stands here, not in the loop
 #pragma unroll
-  for (int s = 0; s < kSlots - 1; ++s) stage<D, NW, KG>(ks, s, smem, voffk, voffv, wave);
-  // the compiler's wait for the query loads stands here, not in the loop
+    for (int b = 0; b < RB; ++b)
 #pragma unroll
-  for (int k = 0; k < C::slices; ++k) asm volatile("" : "+v"(w.q[k]));
-  for (int s = 0; s < n_steps; ++s) {
-    // this step's loads have landed (the later steps' may be in flight), everywhere,
-    // and every wave is done with the step whose slot is filled next
-    sh_vm_wait<(kSlots - 2) * kStepLoads>();
-    __builtin_amdgcn_s_barrier();
-    stage<D, NW, KG>(ks, s + kSlots - 1, smem, voffk, voffv, wave);
-    const int64_t left = ks.end - (ks.begin + ((int64_t)s * KG + kg) * kBlk);
-    const int nv = left >= kBlk ? kBlk : (int)left;
-    if (nv > 0) block_step<D>(a, w, (uint32_t)(((s % kSlots) * KG + kg) * C::blockBytes), nv, hh);
-  }
-  sh_vm_wait<0>();  // the loads behind the end are done with the ring
-  __syncthreads();
-  float l = pair_sum32(w.l), lr = pair_sum32(w.lr);
-
-  // the key groups of a row group join in LDS, each lane its own values
-  if constexpr (KG > 1) {
-    constexpr int kVec = C::dBlocks * 4;  // f32x4 of a lane's accumulators
-    f32x4* dump = (f32x4*)smem;           // [(KG - 1) RG][kVec][64]
-    float* stat = (float*)(smem + (size_t)(NW - NW / KG) * kVec * 64 * 16);  // [(KG - 1) RG][3][64]
-    if (kg > 0) {
-      const int p = rg * (KG - 1) + kg - 1;
+      for (int k = 0; k < C::slices; ++k) asm volatile("" : "+v"(w.q[b][k]));
+#pragma unroll 1
+    for (int s = 0; s < n_steps; ++s) {
+      // this step's loads have landed and every wave is done with the step before
+      arrived<0>();
+      lds_char* blk = ring + slot * kStepBytes + kg * C::blockBytes;
+      slot ^= 1;
+      stage<D, kStep>(f, ring_at + slot * kStepBytes);
+      bf16x8 k[C::slices];
+      read_k<D, RB>(w, blk, k);
 #pragma unroll
-      for (int v = 0; v < kVec; ++v)
-        dump[(p * kVec + v) * 64 + lane] = f32x4{w.acc[v >> 2][4 * (v & 3)], w.acc[v >> 2][4 * (v & 3) + 1],
-                                                 w.acc[v >> 2][4 * (v & 3) + 2], w.acc[v >> 2][4 * (v & 3) + 3]};
-      stat[(p * 3 + 0) * 64 + lane] = w.m;
-      stat[(p * 3 + 1) * 64 + lane] = l;
-      stat[(p * 3 + 2) * 64 + lane] = lr;
+      for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, blk, o);
+      scores<D, RB>(w, k, sc);
+      if (left < kBlk) mask<RB>(sc, left, hh);
+      left -= kStep * kBlk;
+      maxima<RB>(sc, top);
+      follow<D, RB>(a, w, top, kShLazy);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
+        w.l[b] += sum[b];
+        w.lr[b] += rounded[b];
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
     }
-    __syncthreads();
-    if (kg == 0) {
-      float m = w.m;
+  } else {
+    constexpr int KB = kStep / KG;  // blocks of a step for this wave
+    int left = n_keys - kg * kBlk;
+    // a block of zeros before the first one, whose (zero) weights the first turn applies
+    f.left = 0;
+    stage<D, kStep>(f, ring_at + (kSlots - 1) * kStepBytes);
+    f.k = ks.kb + ks.begin * ks.ld;
+    f.v = ks.vb + ks.begin * ks.ld;
+    f.left = n_keys;
 #pragma unroll
-      for (int j = 0; j < KG - 1; ++j) m = fmaxf(m, stat[((rg * (KG - 1) + j) * 3) * 64 + lane]);
-      float e = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m - m) * a.scale_log2);
-      l *= e;
-      lr *= e;
+    for (int s = 0; s < kSlots - 2; ++s) stage<D, kStep>(f, ring_at + s * kStepBytes);
 #pragma unroll
-      for (int d = 0; d < C::dBlocks; ++d) w.acc[d] *= e;
+    for (int b = 0; b < RB; ++b) {
 #pragma unroll
-      for (int j = 0; j < KG - 1; ++j) {
-        const int p = rg * (KG - 1) + j;
-        const float mj = stat[(p * 3) * 64 + lane];
-        e = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mj - m) * a.scale_log2);
-        l = fmaf(e, stat[(p * 3 + 1) * 64 + lane], l);
-        lr = fmaf(e, stat[(p * 3 + 2) * 64 + lane], lr);
+      for (int k = 0; k < C::slices; ++k) asm volatile("" : "+v"(w.q[b][k]));
 #pragma unroll
-        for (int v = 0; v < kVec; ++v) {
-          const f32x4 o = dump[(p * kVec + v) * 64 + lane];
+      for (int h = 0; h < 2; ++h) p[b][h] = bf16x8{};
+    }
+    // the first block's scores give the first reference
+    arrived<(kSlots - 3) * kStepLoads>();
+    {
+      bf16x8 k[C::slices];
+      read_k<D, RB>(w, ring + kg * C::blockBytes, k);
+      scores<D, RB>(w, k, sc);
+      f32x16 first[RB];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w.acc[v >> 2][4 * (v & 3) + i] = fmaf(e, o[i], w.acc[v >> 2][4 * (v & 3) + i]);
+      for (int b = 0; b < RB; ++b) first[b] = sc[b];
+      if (left < kBlk) mask<RB>(first, left, hh);
+      maxima<RB>(first, top);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) w.m[b] = top[b];
+    }
+    int cur = 0, prev = kSlots - 1;  // this step's slot and the one before
+#pragma unroll 1
+    for (int s = 0; s < n_steps; ++s) {
+      const int nxt = cur + 1 == kSlots ? 0 : cur + 1;
+      lds_char* vblk = ring + prev * kStepBytes + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+#pragma unroll
+      for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+      // the next step's loads have landed, and every wave is done with the step before
+      // the last, whose slot is filled again
+      arrived<(kSlots - 4) * kStepLoads>();
+      stage<D, kStep>(f, ring_at + (prev == 0 ? kSlots - 1 : prev - 1) * kStepBytes);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        if (kb > 0) {
+          vblk = ring + cur * kStepBytes;
+#pragma unroll
+          for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+        }
+        lds_char* kblk = kb + 1 < KB ? ring + cur * kStepBytes + C::blockBytes
+                                     : ring + nxt * kStepBytes + (KB == 2 ? 0 : kg * C::blockBytes);
+        if (left < kBlk) mask<RB>(sc, left, hh);
+        left -= KG * kBlk;
+        f32x16 next[RB];
+        pipelined<D, RB>(a, w, vblk, kblk, sc, next, p, v, sum, rounded);
+        bool far = false;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) far = far || sum[b] > kShFar || w.m[b] == -INFINITY;
+        if (__any(far)) {
+          maxima<RB>(sc, top);
+          follow<D, RB>(a, w, top, 0.f);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          w.l[b] += sum[b];
+          w.lr[b] += rounded[b];
+          sc[b] = next[b];
         }
       }
-      w.m = m;
+      prev = cur;
+      cur = nxt;
+    }
+    lds_char* vblk = ring + prev * kStepBytes + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+#pragma unroll
+    for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
+  }
+  arrived<0>();  // the loads behind the end are done with the ring, and so is every wave
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    w.l[b] = pair_sum32(w.l[b]);
+    w.lr[b] = pair_sum32(w.lr[b]);
+  }
+
+  // the key groups of a row group join in LDS, one row block after the other, each
+  // lane its own values
+  if constexpr (KG > 1) {
+    constexpr int kVec = C::dBlocks * 4;                                      // f32x4 of a lane's accumulators
+    f32x4* dump = (f32x4*)smem;                                               // [(KG - 1) RG][kVec][64]
+    float* stat = (float*)(smem + (kShWaves - kShWaves / KG) * kVec * 1024);  // [(KG - 1) RG][3][64]
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      if (b > 0) __syncthreads();
+      if (kg > 0) {
+        const int p = rg * (KG - 1) + kg - 1;
+#pragma unroll
+        for (int v = 0; v < kVec; ++v) {
+          const f32x16& o = w.acc[b][v >> 2];
+          const int i = 4 * (v & 3);
+          dump[(p * kVec + v) * 64 + lane] = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+        }
+        stat[(p * 3 + 0) * 64 + lane] = w.m[b];
+        stat[(p * 3 + 1) * 64 + lane] = w.l[b];
+        stat[(p * 3 + 2) * 64 + lane] = w.lr[b];
+      }
+      __syncthreads();
+      if (kg == 0) {
+        float m = w.m[b];
+#pragma unroll
+        for (int j = 0; j < KG - 1; ++j) m = fmaxf(m, stat[((rg * (KG - 1) + j) * 3) * 64 + lane]);
+        float e = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m[b] - m) * a.scale_log2);
+        w.l[b] *= e;
+        w.lr[b] *= e;
+#pragma unroll
+        for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] *= e;
+#pragma unroll
+        for (int j = 0; j < KG - 1; ++j) {
+          const int p = rg * (KG - 1) + j;
+          const float mj = stat[(p * 3) * 64 + lane];
+          e = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mj - m) * a.scale_log2);
+          w.l[b] = fmaf(e, stat[(p * 3 + 1) * 64 + lane], w.l[b]);
+          w.lr[b] = fmaf(e, stat[(p * 3 + 2) * 64 + lane], w.lr[b]);
+#pragma unroll
+          for (int v = 0; v < kVec; ++v) {
+            const f32x4 o = dump[(p * kVec + v) * 64 + lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w.acc[b][v >> 2][4 * (v & 3) + i] = fmaf(e, o[i], w.acc[b][v >> 2][4 * (v & 3) + i]);
+          }
+        }
+        w.m[b] = m;
+      }
     }
   }
-  if (kg != 0 || !live) return;
-  // an empty segment (or scores of -inf alone) leaves LSE -inf, and its output is not read
-  const int64_t at = ((int64_t)split * a.n_rows + token) * a.n_heads + head;
-  if (hh == 0)
-    a.part_lse[((int64_t)split * a.n_heads + head) * a.n_rows + token] =
-        l > 0.f || l != l ? w.m * a.scale + logf(l) : -INFINITY;
-  const float inv = 1.0f / lr;
-  float* o = a.part_o + at * D + 4 * hh;
+  if (kg != 0) return;
 #pragma unroll
-  for (int d = 0; d < C::dBlocks; ++d)
+  for (int b = 0; b < RB; ++b) {
+    if (!live[b]) continue;
+    // an empty segment (or scores of -inf alone) leaves LSE -inf, and its output is not read
+    const int64_t at = ((int64_t)split * a.n_rows + token[b]) * a.n_heads + head[b];
+    if (hh == 0)
+      a.part_lse[((int64_t)split * a.n_heads + head[b]) * a.n_rows + token[b]] =
+          w.l[b] > 0.f || w.l[b] != w.l[b] ? w.m[b] * a.scale + logf(w.l[b]) : -INFINITY;
+    const float inv = 1.0f / w.lr[b];
+    float* o = a.part_o + at * D + 4 * hh;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *(f32x4*)(o + 32 * d + 8 * i) = f32x4{w.acc[d][4 * i] * inv, w.acc[d][4 * i + 1] * inv, w.acc[d][4 * i + 2] * inv,
-                                            w.acc[d][4 * i + 3] * inv};
+    for (int d = 0; d < C::dBlocks; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(o + 32 * d + 8 * i) = f32x4{w.acc[b][d][4 * i] * inv, w.acc[b][d][4 * i + 1] * inv,
+                                              w.acc[b][d][4 * i + 2] * inv, w.acc[b][d][4 * i + 3] * inv};
+  }
 }
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -388,8 +614,8 @@ __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo 
 // turn; the items that share keys (the row tiles of one segment) stay on one XCD.
 __device__ __forceinline__ int xcd_index(int bid, int n_padded) { return (bid % kShXcds) * (n_padded / kShXcds) + bid / kShXcds; }
 
-template <int D, int NW, int KGP, int KGO>
-__global__ __launch_bounds__(NW * 64) void attn_shared_kernel(SharedArgs a) {
+template <int D, int KGP, int RBP, int KGO, int RBO>
+__global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[kRingBlocks * SCfg<D>::blockBytes];
   const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);  // rows of the batch, without padding
   if ((int)blockIdx.x < a.prefix_blocks) {
@@ -399,7 +625,7 @@ __global__ __launch_bounds__(NW * 64) void attn_shared_kernel(SharedArgs a) {
     const int tile = i % a.prefix_tiles;
     i /= a.prefix_tiles;
     const int split = i % a.prefix_splits, head = i / a.prefix_splits;
-    constexpr int kRows = NW / KGP * kBlk;
+    constexpr int kRows = kShWaves / KGP * RBP * kBlk;
     const int64_t rows = (int64_t)total * a.group;
     if ((int64_t)tile * kRows >= rows) return;
     // even shares in whole blocks
@@ -407,7 +633,7 @@ __global__ __launch_bounds__(NW * 64) void attn_shared_kernel(SharedArgs a) {
     const int64_t b0 = blocks * split / a.prefix_splits * kBlk, b1 = blocks * (split + 1) / a.prefix_splits * kBlk;
     const Keys ks{a.k_prefix + head * D, a.v_prefix + head * D, a.ld_prefix, b0,
                   b1 < a.prefix_len ? b1 : a.prefix_len};
-    run_item<D, NW, KGP>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, split);
+    run_item<D, KGP, RBP>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, split);
     return;
   }
   int i = xcd_index(blockIdx.x - a.prefix_blocks, gridDim.x - a.prefix_blocks);
@@ -419,7 +645,7 @@ __global__ __launch_bounds__(NW * 64) void attn_shared_kernel(SharedArgs a) {
   i /= a.own_splits;
   const int head = i % a.n_kv_heads, b = i / a.n_kv_heads;
   const int first = clamp_int(a.q_start[b], 0, total), last = clamp_int(a.q_start[b + 1], first, total);
-  constexpr int kRows = NW / KGO * kBlk;
+  constexpr int kRows = kShWaves / KGO * RBO * kBlk;
   const int64_t rows = (int64_t)(last - first) * a.group;
   const int64_t len = clamp_int(a.lens[b], 0, a.capacity);
   const int64_t blocks = (len + kBlk - 1) / kBlk;
@@ -428,7 +654,7 @@ __global__ __launch_bounds__(NW * 64) void attn_shared_kernel(SharedArgs a) {
   const Keys ks{a.k_cache + base, a.v_cache + base, a.ld_cache, b0, b1 < len ? b1 : len};
   // (more than one turn only where a request has more rows than max_q tells)
   for (int64_t row0 = (int64_t)tile * kRows; row0 < rows; row0 += (int64_t)a.own_tiles * kRows) {
-    run_item<D, NW, KGO>(a, smem, ks, head, first, row0, rows, a.prefix_splits + split);
+    run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, a.prefix_splits + split);
     __syncthreads();
   }
 }
@@ -477,24 +703,39 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
   }
 }
 
-int key_groups(int64_t rows, int waves) {
-  // the fewest row groups that hold the rows, so that the other waves share the keys
-  return rows <= 32 * waves / 4 ? 4 : rows <= 32 * waves / 2 ? 2 : 1;
+// Row tiles: the fewest rows (32, 64, 128 or 256) that hold them all; the waves that
+// the rows do not need share the keys.
+constexpr int tile_rows(int shape) { return 32 << shape; }
+int tile_shape(int64_t rows) {
+  int s = 0;
+  while (s < 3 && rows > tile_rows(s)) ++s;
+  return s;
+}
+
+template <int D, int P, int O>
+void* kernel_of(int prefix, int own) {
+  // shape 0: 4 key groups x 32 rows; 1: 4 x 64; 2: 2 x 128; 3: 1 x 256
+  if constexpr (P < 0) {
+    return nullptr;
+  } else if constexpr (O < 0) {
+    return kernel_of<D, P - 1, P - 1>(prefix, own);
+  } else {
+    if (prefix == P && own == O)
+      return (void*)attn_shared_kernel<D, P < 2 ? 4 : P == 2 ? 2 : 1, P == 0 ? 1 : 2, O < 2 ? 4 : O == 2 ? 2 : 1,
+                                       O == 0 ? 1 : 2>;
+    return kernel_of<D, P, O - 1>(prefix, own);
+  }
 }
 
 template <int D>
 hipError_t launch_d(const SharedArgs& a, hipStream_t stream) {
   const int own = a.n_req * a.n_kv_heads * a.own_splits * a.own_tiles;
   const unsigned grid = (unsigned)(a.prefix_blocks + (own + kShXcds - 1) / kShXcds * kShXcds);
-  void (*kernel)(SharedArgs) = nullptr;
-#define ISPA_PICK(NW, P, O) \
-  if (a.waves == NW && a.prefix_kg == P && a.own_kg == O) kernel = attn_shared_kernel<D, NW, P, O>;
-  ISPA_PICK(4, 4, 4) ISPA_PICK(4, 2, 4) ISPA_PICK(4, 2, 2) ISPA_PICK(4, 1, 4) ISPA_PICK(4, 1, 2) ISPA_PICK(4, 1, 1)
-  ISPA_PICK(8, 1, 4) ISPA_PICK(8, 1, 2) ISPA_PICK(8, 1, 1)
-#undef ISPA_PICK
+  // (a request has no more rows than the batch: its tiles are no wider)
+  void (*kernel)(SharedArgs) = (void (*)(SharedArgs))kernel_of<D, 3, 3>(a.prefix_shape, a.own_shape);
   if (!kernel) return hipErrorInvalidConfiguration;
   if (grid > 0) {
-    kernel<<<grid, a.waves * 64, 0, stream>>>(a);
+    kernel<<<grid, kShThreads, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -510,12 +751,9 @@ size_t attn_shared_plan(SharedArgs* a, int head_dim) {
   const int64_t prefix_rows = (int64_t)a->n_rows * a->group;
   const int max_q = a->max_q < a->n_rows ? a->max_q : a->n_rows;
   const int64_t own_rows = (int64_t)max_q * a->group;
-  // more than 128 rows against the prefix are bound by the products: 256 rows share
-  // each staged key. Fewer are bound by the keys' bytes, and four waves keep up.
-  a->waves = prefix_rows > 128 ? 8 : 4;
-  a->prefix_kg = key_groups(prefix_rows, a->waves);
-  a->own_kg = key_groups(own_rows, a->waves);
-  const int prefix_tile = a->waves / a->prefix_kg * kBlk, own_tile = a->waves / a->own_kg * kBlk;
+  a->prefix_shape = tile_shape(prefix_rows);
+  a->own_shape = tile_shape(own_rows);
+  const int prefix_tile = tile_rows(a->prefix_shape), own_tile = tile_rows(a->own_shape);
   a->prefix_tiles = (int)((prefix_rows + prefix_tile - 1) / prefix_tile);
   a->own_tiles = (int)((own_rows + own_tile - 1) / own_tile);
   // segments of about an equal share of the keys for two workgroups a compute unit,

@@ -243,7 +243,7 @@ struct SharedArgs {
   int out_bf16;
   float* lse;
   // set by the plan: the layout of the work (attn_shared.hip), the partial results
-  int waves, prefix_kg, own_kg, prefix_tiles, own_tiles, prefix_splits, own_splits, prefix_blocks;
+  int prefix_shape, own_shape, prefix_tiles, own_tiles, prefix_splits, own_splits, prefix_blocks;
   size_t lse_offset;
   float *part_o, *part_lse;
 };
