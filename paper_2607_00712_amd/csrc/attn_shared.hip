@@ -53,8 +53,7 @@ constexpr int kBlk = 32;        // keys of a block, rows of a row block
 constexpr int kShWaves = 4;
 constexpr int kShThreads = kShWaves * 64;
 constexpr int kShXcds = 8;
-constexpr float kShLazy = 8.f;     // rescale threshold of the softmax reference (log2)
-constexpr float kShFar = 1024.f;   // and of a block's sum of weights of 16 keys
+constexpr float kShFar = 1024.f;  // a lane's sum of weights of a block (16 keys) that moves the softmax reference
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
@@ -203,14 +202,9 @@ __device__ __forceinline__ void maxima(const f32x16 (&sc)[RB], float (&top)[RB])
   }
 }
 
-// The softmax reference follows the block's maxima; O and the sums are rescaled only
-// when some row's maximum is above its reference by more than `lazy` (log2).
+// The softmax reference follows the block's maxima.
 template <int D, int RB>
-__device__ __forceinline__ void follow(const SharedArgs& a, SWave<D, RB>& w, const float (&top)[RB], float lazy) {
-  bool far = false;
-#pragma unroll
-  for (int b = 0; b < RB; ++b) far = far || (top[b] - w.m[b]) * a.scale_log2 > lazy || w.m[b] == -INFINITY;
-  if (!__any(far)) return;
+__device__ __forceinline__ void follow(const SharedArgs& a, SWave<D, RB>& w, const float (&top)[RB]) {
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const float m_new = fmaxf(w.m[b], top[b]);
@@ -349,33 +343,31 @@ __device__ __forceinline__ void stage(Feed& f, uint32_t to) {
   }
 }
 
-// One item: rows [row0, row0 + 32 RB RG) of n_item_rows (row r = token first + r / G)
-// against `ks`, into split `split`; RG = 4 / KG row groups.
-template <int D, int KG, int RB>
-__device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const Keys& ks, int kv_head, int first,
-                                         int64_t row0, int64_t n_item_rows, int split) {
-  using C = SCfg<D>;
-  constexpr int kStep = KG == 4 ? 4 : 2;          // blocks of a step
-  constexpr int kSlots = kRingBlocks / kStep;     // steps in LDS
-  constexpr int kStepLoads = 2 * kStep * C::loads;
-  constexpr int kStepBytes = kStep * C::blockBytes;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hh = lane >> 5, ql = lane & 31;
-  const int kg = wave % KG, rg = wave / KG;
-  lds_char* ring = (lds_char*)smem;
-
-  SWave<D, RB> w;
+// The rows of a wave's row blocks: lane l holds row l % 32 of each.
+template <int RB>
+struct SRows {
   bool live[RB];
   int token[RB], head[RB];
+};
+
+// A fresh state for rows row0 .. row0 + 32 RB - 1 of n_item_rows (row r = token first +
+// r / G, query head G kv_head + r % G).
+template <int D, int RB>
+__device__ __forceinline__ void start_rows(const SharedArgs& a, SWave<D, RB>& w, SRows<RB>& rows, int kv_head, int first,
+                                           int64_t row0, int64_t n_item_rows, int lane) {
+  using C = SCfg<D>;
+  const int hh = lane >> 5, ql = lane & 31;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    const int64_t r = row0 + (rg * RB + b) * kBlk + ql;
-    live[b] = r < n_item_rows;
-    token[b] = first + (live[b] ? (int)(r / a.group) : 0);
-    head[b] = kv_head * a.group + (live[b] ? (int)(r % a.group) : 0);
+    const int64_t r = row0 + b * kBlk + ql;
+    rows.live[b] = r < n_item_rows;
+    rows.token[b] = first + (rows.live[b] ? (int)((uint32_t)r / (uint32_t)a.group) : 0);
+    rows.head[b] = kv_head * a.group + (rows.live[b] ? (int)((uint32_t)r % (uint32_t)a.group) : 0);
 #pragma unroll
     for (int k = 0; k < C::slices; ++k)
-      w.q[b][k] = live[b] ? *(const bf16x8*)(a.q + token[b] * a.ld_q + head[b] * D + 16 * k + 8 * hh) : bf16x8{};
+      w.q[b][k] = rows.live[b]
+                      ? *(const bf16x8*)(a.q + rows.token[b] * a.ld_q + rows.head[b] * D + 16 * k + 8 * hh)
+                      : bf16x8{};
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] = f32x16{};
     w.m[b] = -INFINITY;
@@ -384,21 +376,68 @@ __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const 
   }
 #pragma unroll
   for (int k = 0; k < C::slices; ++k) w.kad[k] = ql * C::rowBytes + (((2 * k + hh) ^ swizzle_k<D>(ql)) << 4);
-  {
-    const int g16 = lane >> 4, sl = lane & 15;
+  const int g16 = lane >> 4, sl = lane & 15;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int d = 0; d < C::dBlocks; ++d) {
-        const int chunk = 4 * d + 2 * (g16 & 1) + ((sl & 3) >> 1);
-        const int row = 8 * i + 4 * (g16 >> 1) + (sl >> 2);
-        w.vad[i][d] = row * C::rowBytes + ((chunk ^ swizzle_v<D>(row)) << 4) + ((sl & 1) << 3);
-      }
+    for (int d = 0; d < C::dBlocks; ++d) {
+      const int chunk = 4 * d + 2 * (g16 & 1) + ((sl & 3) >> 1);
+      const int row = 8 * i + 4 * (g16 >> 1) + (sl >> 2);
+      w.vad[i][d] = row * C::rowBytes + ((chunk ^ swizzle_v<D>(row)) << 4) + ((sl & 1) << 3);
+    }
+}
+// The compiler's wait for the query loads stands where this does, not in a loop.
+template <int D, int RB>
+__device__ __forceinline__ void rows_here(SWave<D, RB>& w) {
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+#pragma unroll
+    for (int k = 0; k < SCfg<D>::slices; ++k) asm volatile("" : "+v"(w.q[b][k]));
+}
+
+// A block's weights are too large for the reference that they were formed with, or
+// there was none: the reference moves, and the weights are formed again.
+template <int D, int RB>
+__device__ __forceinline__ void check_reference(const SharedArgs& a, SWave<D, RB>& w, const f32x16 (&sc)[RB],
+                                                bf16x8 (&p)[RB][2], float (&sum)[RB], float (&rounded)[RB]) {
+  bool far = false;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) far = far || sum[b] > kShFar || w.m[b] == -INFINITY;
+  if (__any(far)) {
+    float top[RB];
+    maxima<RB>(sc, top);
+    follow<D, RB>(a, w, top);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
   }
+  // (the accumulators stay in the accumulation registers on both ways)
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+#pragma unroll
+    for (int d = 0; d < SCfg<D>::dBlocks; ++d) asm volatile("" : "+a"(w.acc[b][d]));
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    w.l[b] += sum[b];
+    w.lr[b] += rounded[b];
+  }
+}
+
+// The keys of an item, met by KG = 1 or 2 groups of waves: steps of two blocks that the
+// workgroup loads together. The next block's scores and the last block's products run
+// beside a block's softmax, so that the matrix cores run through it.
+template <int D, int KG, int RB>
+__device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w, lds_char* ring, const Keys& ks, int kg,
+                                            int wave, int tid) {
+  using C = SCfg<D>;
+  constexpr int kStep = 2;                     // blocks of a step
+  constexpr int kSlots = kRingBlocks / kStep;  // steps in LDS
+  constexpr int kStepLoads = 2 * kStep * C::loads;
+  constexpr int kStepBytes = kStep * C::blockBytes;
+  constexpr int KB = kStep / KG;  // blocks of a step for this wave
+  const int hh = (tid & 63) >> 5;
   const int n_keys = (int)(ks.end - ks.begin);
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
   Feed f;
-  f.k = ks.kb + ks.begin * ks.ld;
-  f.v = ks.vb + ks.begin * ks.ld;
   f.block = ks.ld * kBlk;
   f.row_bytes = (int)(ks.ld * 2);
   f.pad = f.row_bytes - D * 2;
@@ -409,203 +448,265 @@ __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const 
     f.voffk = row * f.row_bytes + (stored ^ swizzle_k<D>(row)) * 16;
     f.voffv = row * f.row_bytes + (stored ^ swizzle_v<D>(row)) * 16;
   }
-  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
-  const int n_steps = (n_keys + kStep * kBlk - 1) / (kStep * kBlk);
+  f.k = ks.kb + ks.begin * ks.ld;
+  f.v = ks.vb + ks.begin * ks.ld;
+  // a step of zeros before the first one, whose (zero) weights the first turn applies
+  f.left = 0;
+  stage<D, kStep>(f, ring_at + (kSlots - 1) * kStepBytes);
+  f.k = ks.kb + ks.begin * ks.ld;
+  f.v = ks.vb + ks.begin * ks.ld;
+  f.left = n_keys;
+#pragma unroll
+  for (int s = 0; s < kSlots - 2; ++s) stage<D, kStep>(f, ring_at + s * kStepBytes);
+  rows_here<D, RB>(w);
   f32x16 sc[RB];
-  float top[RB], sum[RB], rounded[RB];
+  float sum[RB], rounded[RB];
   bf16x8 v[2 * C::dBlocks], p[RB][2];
-  if constexpr (KG == 4) {
-    // bound by the bytes of the keys: a step at a time, each wave its own block of it
-    f.left = n_keys;
-    int left = n_keys - kg * kBlk;  // keys from this wave's block on
-    int slot = 0;
-    stage<D, kStep>(f, ring_at);
-    // the compiler's wait for the query loads stands here, not in the loop
 #pragma unroll
-    for (int b = 0; b < RB; ++b)
+  for (int b = 0; b < RB; ++b)
 #pragma unroll
-      for (int k = 0; k < C::slices; ++k) asm volatile("" : "+v"(w.q[b][k]));
+    for (int h = 0; h < 2; ++h) p[b][h] = bf16x8{};
+  arrived<(kSlots - 3) * kStepLoads>();
+  {
+    bf16x8 k[C::slices];
+    read_k<D, RB>(w, ring + kg * C::blockBytes, k);
+    scores<D, RB>(w, k, sc);
+    // the first block's maxima are the first reference
+    f32x16 first[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) first[b] = sc[b];
+    if (n_keys - kg * kBlk < kBlk) mask<RB>(first, n_keys - kg * kBlk, hh);
+    maxima<RB>(first, w.m);
+  }
+  const int n_steps = (n_keys + kStep * kBlk - 1) / (kStep * kBlk);
+  int left = n_keys - kg * kBlk;       // keys from this wave's block on
+  int cur = 0, prev = kSlots - 1;      // this step's slot and the one before
 #pragma unroll 1
-    for (int s = 0; s < n_steps; ++s) {
-      // this step's loads have landed and every wave is done with the step before
-      arrived<0>();
-      lds_char* blk = ring + slot * kStepBytes + kg * C::blockBytes;
-      slot ^= 1;
-      stage<D, kStep>(f, ring_at + slot * kStepBytes);
-      bf16x8 k[C::slices];
-      read_k<D, RB>(w, blk, k);
-#pragma unroll
-      for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, blk, o);
-      scores<D, RB>(w, k, sc);
-      if (left < kBlk) mask<RB>(sc, left, hh);
-      left -= kStep * kBlk;
-      maxima<RB>(sc, top);
-      follow<D, RB>(a, w, top, kShLazy);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
-        w.l[b] += sum[b];
-        w.lr[b] += rounded[b];
-      }
-#pragma unroll
-      for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
-    }
-  } else {
-    constexpr int KB = kStep / KG;  // blocks of a step for this wave
-    int left = n_keys - kg * kBlk;
-    // a block of zeros before the first one, whose (zero) weights the first turn applies
-    f.left = 0;
-    stage<D, kStep>(f, ring_at + (kSlots - 1) * kStepBytes);
-    f.k = ks.kb + ks.begin * ks.ld;
-    f.v = ks.vb + ks.begin * ks.ld;
-    f.left = n_keys;
-#pragma unroll
-    for (int s = 0; s < kSlots - 2; ++s) stage<D, kStep>(f, ring_at + s * kStepBytes);
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-#pragma unroll
-      for (int k = 0; k < C::slices; ++k) asm volatile("" : "+v"(w.q[b][k]));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) p[b][h] = bf16x8{};
-    }
-    // the first block's scores give the first reference
-    arrived<(kSlots - 3) * kStepLoads>();
-    {
-      bf16x8 k[C::slices];
-      read_k<D, RB>(w, ring + kg * C::blockBytes, k);
-      scores<D, RB>(w, k, sc);
-      f32x16 first[RB];
-#pragma unroll
-      for (int b = 0; b < RB; ++b) first[b] = sc[b];
-      if (left < kBlk) mask<RB>(first, left, hh);
-      maxima<RB>(first, top);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) w.m[b] = top[b];
-    }
-    int cur = 0, prev = kSlots - 1;  // this step's slot and the one before
-#pragma unroll 1
-    for (int s = 0; s < n_steps; ++s) {
-      const int nxt = cur + 1 == kSlots ? 0 : cur + 1;
-      lds_char* vblk = ring + prev * kStepBytes + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
-#pragma unroll
-      for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
-      // the next step's loads have landed, and every wave is done with the step before
-      // the last, whose slot is filled again
-      arrived<(kSlots - 4) * kStepLoads>();
-      stage<D, kStep>(f, ring_at + (prev == 0 ? kSlots - 1 : prev - 1) * kStepBytes);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        if (kb > 0) {
-          vblk = ring + cur * kStepBytes;
-#pragma unroll
-          for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
-        }
-        lds_char* kblk = kb + 1 < KB ? ring + cur * kStepBytes + C::blockBytes
-                                     : ring + nxt * kStepBytes + (KB == 2 ? 0 : kg * C::blockBytes);
-        if (left < kBlk) mask<RB>(sc, left, hh);
-        left -= KG * kBlk;
-        f32x16 next[RB];
-        pipelined<D, RB>(a, w, vblk, kblk, sc, next, p, v, sum, rounded);
-        bool far = false;
-#pragma unroll
-        for (int b = 0; b < RB; ++b) far = far || sum[b] > kShFar || w.m[b] == -INFINITY;
-        if (__any(far)) {
-          maxima<RB>(sc, top);
-          follow<D, RB>(a, w, top, 0.f);
-#pragma unroll
-          for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          w.l[b] += sum[b];
-          w.lr[b] += rounded[b];
-          sc[b] = next[b];
-        }
-      }
-      prev = cur;
-      cur = nxt;
-    }
+  for (int s = 0; s < n_steps; ++s) {
+    const int nxt = cur + 1 == kSlots ? 0 : cur + 1;
     lds_char* vblk = ring + prev * kStepBytes + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
 #pragma unroll
-    for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+    for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+    // the next step's loads have landed, and every wave is done with the step before
+    // the last, whose slot is filled again
+    arrived<(kSlots - 4) * kStepLoads>();
+    stage<D, kStep>(f, ring_at + (prev == 0 ? kSlots - 1 : prev - 1) * kStepBytes);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      if (kb > 0) {
+        vblk = ring + cur * kStepBytes;
+#pragma unroll
+        for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+      }
+      lds_char* kblk = kb + 1 < KB ? ring + cur * kStepBytes + C::blockBytes
+                                   : ring + nxt * kStepBytes + (KB == 2 ? 0 : kg * C::blockBytes);
+      if (left < kBlk) mask<RB>(sc, left, hh);
+      left -= KG * kBlk;
+      f32x16 next[RB];
+      pipelined<D, RB>(a, w, vblk, kblk, sc, next, p, v, sum, rounded);
+      check_reference<D, RB>(a, w, sc, p, sum, rounded);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) sc[b] = next[b];
+    }
+    prev = cur;
+    cur = nxt;
+  }
+  lds_char* vblk = ring + prev * kStepBytes + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+#pragma unroll
+  for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
+}
+
+// A wave's own keys, in a ring of its own: K and V tiles of 32 keys in turn, each loaded
+// again as soon as it has been read, so that all but one tile of the ring are in flight
+// at any time and no wave waits for another. Bound by the bytes of the keys.
+template <int D, int RB>
+__device__ __forceinline__ void private_keys(const SharedArgs& a, SWave<D, RB>& w, lds_char* ring, const Keys& ks,
+                                             int lane) {
+  using C = SCfg<D>;
+  constexpr int kTiles = 2 * kRingBlocks * C::tileBytes / kShWaves / C::tileBytes;  // tiles of the wave's ring
+  constexpr int kLoads = C::tileBytes / 1024;                                       // loads of a tile
+  constexpr int kRowsPer = 64 / C::chunks;                                          // rows of a load
+  // loads after which the swizzles come again
+  constexpr int kNk = D == 128 ? 4 : 1, kNv = D == 128 ? 2 : 1;
+  const int hh = lane >> 5;
+  const int row_bytes = (int)(ks.ld * 2), pad = row_bytes - D * 2;
+  const int64_t block = ks.ld * kBlk;
+  const uint16_t *kp = ks.kb + ks.begin * ks.ld, *vp = ks.vb + ks.begin * ks.ld;
+  const int n_keys = (int)(ks.end - ks.begin);
+  int k_left = n_keys, v_left = n_keys, left = n_keys;
+  int voffk[kNk], voffv[kNv];
+#pragma unroll
+  for (int i = 0; i < kNk; ++i) {
+    const int row = i * kRowsPer + lane / C::chunks;
+    voffk[i] = row * row_bytes + ((lane % C::chunks) ^ swizzle_k<D>(row)) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < kNv; ++i) {
+    const int row = i * kRowsPer + lane / C::chunks;
+    voffv[i] = row * row_bytes + ((lane % C::chunks) ^ swizzle_v<D>(row)) * 16;
+  }
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+  auto load = [&](bool is_v, int slot) __attribute__((always_inline)) {
+    int& n = is_v ? v_left : k_left;
+    const uint16_t*& at = is_v ? vp : kp;
+    const int nv = n < 0 ? 0 : n < kBlk ? n : kBlk;
+    const i32x4 d = descriptor(at, nv > 0 ? nv * row_bytes - pad : 0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int nk = is_v ? kNv : kNk;
+      load_to_lds(d, (is_v ? voffv[i % kNv] : voffk[i % kNk]) + i / nk * nk * kRowsPer * row_bytes,
+                  ring_at + slot * C::tileBytes + i * 1024);
+    }
+    n -= kBlk;
+    at += block;
+  };
+#pragma unroll
+  for (int u = 0; u < kTiles; ++u) load(u & 1, u);
+  rows_here<D, RB>(w);
+  f32x16 sc[RB];
+  float sum[RB], rounded[RB];
+  bf16x8 v[2 * C::dBlocks], p[RB][2];
+  int slot = 0;
+#pragma unroll 1
+  while (left > 0) {
+    // tiles land in order: this one has when at most the ring's others are in flight
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"((kTiles - 1) * kLoads) : "memory");
+    lds_char* tile = ring + slot * C::tileBytes;
+    {
+      bf16x8 k[C::slices];
+      read_k<D, RB>(w, tile, k);
+      scores<D, RB>(w, k, sc);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
+    load(kTiles & 1, slot);
+    slot = slot + 1 == kTiles ? 0 : slot + 1;
+    if (left < kBlk) mask<RB>(sc, left, hh);
+    left -= kBlk;
+#pragma unroll
+    for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
+    check_reference<D, RB>(a, w, sc, p, sum, rounded);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"((kTiles - 1) * kLoads) : "memory");
+    tile = ring + slot * C::tileBytes - C::tileBytes;  // (V operand offsets are those behind a K tile)
+#pragma unroll
+    for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, tile, o);
 #pragma unroll
     for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    load(!(kTiles & 1), slot);
+    slot = slot + 1 == kTiles ? 0 : slot + 1;
   }
-  arrived<0>();  // the loads behind the end are done with the ring, and so is every wave
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads behind the end are done with the ring
+}
+
+// The key groups of a row group join in LDS, one row block after the other, each lane
+// its own values; the result is kg 0's.
+template <int D, int KG, int RB>
+__device__ __forceinline__ void join_groups(const SharedArgs& a, SWave<D, RB>& w, char* smem, int kg, int rg, int lane) {
+  using C = SCfg<D>;
+  constexpr int kVec = C::dBlocks * 4;                                      // f32x4 of a lane's accumulators
+  f32x4* dump = (f32x4*)smem;                                               // [(KG - 1) RG][kVec][64]
+  float* stat = (float*)(smem + (kShWaves - kShWaves / KG) * kVec * 1024);  // [(KG - 1) RG][3][64]
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    w.l[b] = pair_sum32(w.l[b]);
-    w.lr[b] = pair_sum32(w.lr[b]);
-  }
-
-  // the key groups of a row group join in LDS, one row block after the other, each
-  // lane its own values
-  if constexpr (KG > 1) {
-    constexpr int kVec = C::dBlocks * 4;                                      // f32x4 of a lane's accumulators
-    f32x4* dump = (f32x4*)smem;                                               // [(KG - 1) RG][kVec][64]
-    float* stat = (float*)(smem + (kShWaves - kShWaves / KG) * kVec * 1024);  // [(KG - 1) RG][3][64]
+    if (b > 0) __syncthreads();
+    if (kg > 0) {
+      const int p = rg * (KG - 1) + kg - 1;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      if (b > 0) __syncthreads();
-      if (kg > 0) {
-        const int p = rg * (KG - 1) + kg - 1;
+      for (int v = 0; v < kVec; ++v) {
+        const f32x16& o = w.acc[b][v >> 2];
+        const int i = 4 * (v & 3);
+        dump[(p * kVec + v) * 64 + lane] = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+      }
+      stat[(p * 3 + 0) * 64 + lane] = w.m[b];
+      stat[(p * 3 + 1) * 64 + lane] = w.l[b];
+      stat[(p * 3 + 2) * 64 + lane] = w.lr[b];
+    }
+    __syncthreads();
+    if (kg == 0) {
+      float m = w.m[b];
+#pragma unroll
+      for (int j = 0; j < KG - 1; ++j) m = fmaxf(m, stat[((rg * (KG - 1) + j) * 3) * 64 + lane]);
+      float e = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m[b] - m) * a.scale_log2);
+      w.l[b] *= e;
+      w.lr[b] *= e;
+#pragma unroll
+      for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] *= e;
+#pragma unroll
+      for (int j = 0; j < KG - 1; ++j) {
+        const int p = rg * (KG - 1) + j;
+        const float mj = stat[(p * 3) * 64 + lane];
+        e = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mj - m) * a.scale_log2);
+        w.l[b] = fmaf(e, stat[(p * 3 + 1) * 64 + lane], w.l[b]);
+        w.lr[b] = fmaf(e, stat[(p * 3 + 2) * 64 + lane], w.lr[b]);
 #pragma unroll
         for (int v = 0; v < kVec; ++v) {
-          const f32x16& o = w.acc[b][v >> 2];
-          const int i = 4 * (v & 3);
-          dump[(p * kVec + v) * 64 + lane] = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+          const f32x4 o = dump[(p * kVec + v) * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w.acc[b][v >> 2][4 * (v & 3) + i] = fmaf(e, o[i], w.acc[b][v >> 2][4 * (v & 3) + i]);
         }
-        stat[(p * 3 + 0) * 64 + lane] = w.m[b];
-        stat[(p * 3 + 1) * 64 + lane] = w.l[b];
-        stat[(p * 3 + 2) * 64 + lane] = w.lr[b];
       }
-      __syncthreads();
-      if (kg == 0) {
-        float m = w.m[b];
-#pragma unroll
-        for (int j = 0; j < KG - 1; ++j) m = fmaxf(m, stat[((rg * (KG - 1) + j) * 3) * 64 + lane]);
-        float e = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m[b] - m) * a.scale_log2);
-        w.l[b] *= e;
-        w.lr[b] *= e;
-#pragma unroll
-        for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] *= e;
-#pragma unroll
-        for (int j = 0; j < KG - 1; ++j) {
-          const int p = rg * (KG - 1) + j;
-          const float mj = stat[(p * 3) * 64 + lane];
-          e = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mj - m) * a.scale_log2);
-          w.l[b] = fmaf(e, stat[(p * 3 + 1) * 64 + lane], w.l[b]);
-          w.lr[b] = fmaf(e, stat[(p * 3 + 2) * 64 + lane], w.lr[b]);
-#pragma unroll
-          for (int v = 0; v < kVec; ++v) {
-            const f32x4 o = dump[(p * kVec + v) * 64 + lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w.acc[b][v >> 2][4 * (v & 3) + i] = fmaf(e, o[i], w.acc[b][v >> 2][4 * (v & 3) + i]);
-          }
-        }
-        w.m[b] = m;
-      }
+      w.m[b] = m;
     }
   }
-  if (kg != 0) return;
+}
+
+// The rows' normalised output and LSE into split `split`.
+template <int D, int RB>
+__device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, RB>& w, const SRows<RB>& rows, int split,
+                                           int lane) {
+  const int hh = lane >> 5;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    if (!live[b]) continue;
+    if (!rows.live[b]) continue;
+    const int token = rows.token[b], head = rows.head[b];
     // an empty segment (or scores of -inf alone) leaves LSE -inf, and its output is not read
-    const int64_t at = ((int64_t)split * a.n_rows + token[b]) * a.n_heads + head[b];
     if (hh == 0)
-      a.part_lse[((int64_t)split * a.n_heads + head[b]) * a.n_rows + token[b]] =
+      a.part_lse[((int64_t)split * a.n_heads + head) * a.n_rows + token] =
           w.l[b] > 0.f || w.l[b] != w.l[b] ? w.m[b] * a.scale + logf(w.l[b]) : -INFINITY;
     const float inv = 1.0f / w.lr[b];
-    float* o = a.part_o + at * D + 4 * hh;
+    float* o = a.part_o + (((int64_t)split * a.n_rows + token) * a.n_heads + head) * D + 4 * hh;
 #pragma unroll
-    for (int d = 0; d < C::dBlocks; ++d)
+    for (int d = 0; d < SCfg<D>::dBlocks; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *(f32x4*)(o + 32 * d + 8 * i) = f32x4{w.acc[b][d][4 * i] * inv, w.acc[b][d][4 * i + 1] * inv,
                                               w.acc[b][d][4 * i + 2] * inv, w.acc[b][d][4 * i + 3] * inv};
   }
+}
+
+// A workgroup's item: rows [row0, row0 + 32 RB RG) of n_item_rows against `ks`, into
+// split `split`; RG = 4 / KG row groups.
+template <int D, int KG, int RB>
+__device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const Keys& ks, int kv_head, int first,
+                                         int64_t row0, int64_t n_item_rows, int split) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = wave % KG, rg = wave / KG;
+  SWave<D, RB> w;
+  SRows<RB> rows;
+  start_rows<D, RB>(a, w, rows, kv_head, first, row0 + rg * RB * kBlk, n_item_rows, lane);
+  lds_char* ring = (lds_char*)smem;
+  if constexpr (KG == kShWaves) {
+    // even shares of the blocks
+    const int64_t n = (ks.end - ks.begin + kBlk - 1) / kBlk;
+    Keys own = ks;
+    own.begin = ks.begin + n * wave / kShWaves * kBlk;
+    own.end = ks.begin + n * (wave + 1) / kShWaves * kBlk;
+    if (own.end > ks.end) own.end = ks.end;
+    private_keys<D, RB>(a, w, ring + wave * (kRingBlocks * SCfg<D>::blockBytes / kShWaves), own, lane);
+  } else {
+    shared_keys<D, KG, RB>(a, w, ring, ks, kg, wave, tid);
+  }
+  arrived<0>();  // the ring is free
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    w.l[b] = pair_sum32(w.l[b]);
+    w.lr[b] = pair_sum32(w.lr[b]);
+  }
+  if constexpr (KG > 1) join_groups<D, KG, RB>(a, w, smem, kg, rg, lane);
+  if (kg == 0) write_part<D, RB>(a, w, rows, split, lane);
 }
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -637,6 +738,10 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
     return;
   }
   int i = xcd_index(blockIdx.x - a.prefix_blocks, gridDim.x - a.prefix_blocks);
+  // up to 32 rows: every wave an item of its own
+  constexpr bool kWaveItems = KGO == kShWaves && RBO == 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (kWaveItems) i = i * kShWaves + wave;
   const int n = a.n_req * a.n_kv_heads * a.own_splits * a.own_tiles;
   if (i >= n) return;
   const int tile = i % a.own_tiles;
@@ -645,7 +750,7 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   i /= a.own_splits;
   const int head = i % a.n_kv_heads, b = i / a.n_kv_heads;
   const int first = clamp_int(a.q_start[b], 0, total), last = clamp_int(a.q_start[b + 1], first, total);
-  constexpr int kRows = kShWaves / KGO * RBO * kBlk;
+  constexpr int kRows = kWaveItems ? kBlk : kShWaves / KGO * RBO * kBlk;
   const int64_t rows = (int64_t)(last - first) * a.group;
   const int64_t len = clamp_int(a.lens[b], 0, a.capacity);
   const int64_t blocks = (len + kBlk - 1) / kBlk;
@@ -654,8 +759,19 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   const Keys ks{a.k_cache + base, a.v_cache + base, a.ld_cache, b0, b1 < len ? b1 : len};
   // (more than one turn only where a request has more rows than max_q tells)
   for (int64_t row0 = (int64_t)tile * kRows; row0 < rows; row0 += (int64_t)a.own_tiles * kRows) {
-    run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, a.prefix_splits + split);
-    __syncthreads();
+    if constexpr (kWaveItems) {
+      const int lane = threadIdx.x & 63;
+      SWave<D, 1> w;
+      SRows<1> r;
+      start_rows<D, 1>(a, w, r, head, first, row0, rows, lane);
+      private_keys<D, 1>(a, w, (lds_char*)smem + wave * (kRingBlocks * SCfg<D>::blockBytes / kShWaves), ks, lane);
+      w.l[0] = pair_sum32(w.l[0]);
+      w.lr[0] = pair_sum32(w.lr[0]);
+      write_part<D, 1>(a, w, r, a.prefix_splits + split, lane);
+    } else {
+      run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, a.prefix_splits + split);
+      __syncthreads();
+    }
   }
 }
 
@@ -663,6 +779,7 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
 template <int D>
 __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
   constexpr int kLanes = D / 4;
+  constexpr float kLog2e = 1.4426950408889634f;
   const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const int c = threadIdx.x % kLanes;
@@ -674,18 +791,36 @@ __global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
   const int64_t lstep = (int64_t)a.n_heads * a.n_rows;
   const float* os = a.part_o + (token * a.n_heads + head) * D + 4 * c;
   const int64_t ostep = (int64_t)a.n_rows * a.n_heads * D;
-  float m = -INFINITY;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, ls[s * lstep]);
-  float sum = 0.f;
+  // a batch of splits at a time, its loads in flight together, with a running maximum
+  constexpr int kBatch = 8;
+  float m = -INFINITY, sum = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const float l = ls[s * lstep];
-    if (l == -INFINITY) continue;
-    const float e = __builtin_amdgcn_exp2f((l - m) * 1.4426950408889634f);
-    sum += e;
-    const f32x4 v = *(const f32x4*)(os + s * ostep);
+  for (int s0 = 0; s0 < splits; s0 += kBatch) {
+    float l[kBatch];
+    f32x4 v[kBatch];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = fmaf(e, v[k], o[k]);
+    for (int j = 0; j < kBatch; ++j) {
+      const bool in = s0 + j < splits;
+      l[j] = in ? ls[(s0 + j) * lstep] : -INFINITY;
+      v[j] = in ? *(const f32x4*)(os + (s0 + j) * ostep) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, l[j]);
+    const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * kLog2e);
+    sum *= old;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] *= old;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      // (a split without keys has no output: what lies there is not used)
+      const bool empty = l[j] == -INFINITY;
+      const float e = empty ? 0.f : __builtin_amdgcn_exp2f((l[j] - top) * kLog2e);
+      sum += e;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = fmaf(e, empty ? 0.f : v[j][k], o[k]);
+    }
+    m = top;
   }
   // no key at all: out = 0, lse = -inf
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
@@ -729,7 +864,8 @@ void* kernel_of(int prefix, int own) {
 
 template <int D>
 hipError_t launch_d(const SharedArgs& a, hipStream_t stream) {
-  const int own = a.n_req * a.n_kv_heads * a.own_splits * a.own_tiles;
+  int own = a.n_req * a.n_kv_heads * a.own_splits * a.own_tiles;
+  if (a.own_shape == 0) own = (own + kShWaves - 1) / kShWaves;  // an item to a wave
   const unsigned grid = (unsigned)(a.prefix_blocks + (own + kShXcds - 1) / kShXcds * kShXcds);
   // (a request has no more rows than the batch: its tiles are no wider)
   void (*kernel)(SharedArgs) = (void (*)(SharedArgs))kernel_of<D, 3, 3>(a.prefix_shape, a.own_shape);
@@ -745,6 +881,55 @@ hipError_t launch_d(const SharedArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// How many segments the prefix and the own keys are cut into. In units of one key's K
+// and V rows streamed by a compute unit at its share of the HBM rate (24 ns of 512
+// bytes), a launch takes about
+//   max(rounds x keys of a segment, all keys / slots) + rounds x kStart + kJoin x segments
+// where `slots` workgroups run at a time, kStart is a workgroup's start and end (6 us),
+// and kJoin a split's part of the join. A row tile of 256 rows is bound by its products
+// (1.45 units a key); narrower ones by the stream, and a workgroup may take more than
+// its share of that while others are done. Measured at 128 values a head: 64 rows of 32
+// heads against 32768 keys 115 us in 8 segments (one round), 133 in 16, 184 in 32; 3900
+// rows of 12 heads against 32760 keys 911 us in 4 segments (three full rounds), 1001 in
+// 2, 1015 in 1.
+void choose_splits(SharedArgs* a, int head_dim) {
+  constexpr int kStart = 250, kJoin = 4;
+  const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
+  const int64_t prefix_items = (int64_t)a->n_kv_heads * a->prefix_tiles;
+  const int64_t own_items = (int64_t)a->n_req * a->n_kv_heads * a->own_tiles;
+  const bool wide = a->prefix_shape == 3;
+  const double per_prefix = wide ? 1.45 : 1.0, per_own = a->own_shape == 3 ? 1.45 : 1.0;
+  const double alone = wide ? 1.0 : 1.5;  // a workgroup's rate over its share, when others leave it
+  const int slots = wide && head_dim == 64 ? 2 * n_cu : n_cu;
+  // half of the caches' capacity stands for the lengths, which the device knows
+  const double total =
+      (prefix_items * a->prefix_len * per_prefix + own_items * (a->capacity / 2.0) * per_own) / slots;
+  a->prefix_splits = 0;
+  if (a->prefix_len > 0) {
+    double best = 0.0;
+    for (int64_t n = 1; n == 1 || (n <= 128 && n * 256 <= a->prefix_len); ++n) {
+      const int64_t rounds = (prefix_items * n + slots - 1) / slots;
+      const double chain = rounds * ((double)a->prefix_len / n) * per_prefix / alone;
+      const double cost = (chain > total ? chain : total) + rounds * kStart + kJoin * n;
+      if (n == 1 || cost < best) {
+        best = cost;
+        a->prefix_splits = (int)n;
+      }
+    }
+  }
+  // no own item's stream outlasts the whole. (Up to 32 rows an item is a wave's: four run
+  // in a slot, and one alone streams at less than half of the slot's share.)
+  a->own_splits = 0;
+  if (a->capacity > 0) {
+    const int64_t least = a->own_shape == 0 ? 128 : 256;
+    const double share = total > least ? total : (double)least;
+    int64_t n = (int64_t)ceil((a->own_shape == 0 ? 1.4 : 1.0) * a->capacity * per_own / share);
+    if (n * least > a->capacity) n = a->capacity / least;
+    if (n > 128) n = 128;
+    a->own_splits = n > 1 ? (int)n : 1;
+  }
+}
+
 }  // namespace
 
 size_t attn_shared_plan(SharedArgs* a, int head_dim) {
@@ -756,20 +941,11 @@ size_t attn_shared_plan(SharedArgs* a, int head_dim) {
   const int prefix_tile = tile_rows(a->prefix_shape), own_tile = tile_rows(a->own_shape);
   a->prefix_tiles = (int)((prefix_rows + prefix_tile - 1) / prefix_tile);
   a->own_tiles = (int)((own_rows + own_tile - 1) / own_tile);
-  // segments of about an equal share of the keys for two workgroups a compute unit,
-  // and of at least 256 keys
-  const int64_t prefix_items = (int64_t)a->n_kv_heads * a->prefix_tiles;
-  const int64_t own_items = (int64_t)a->n_req * a->n_kv_heads * a->own_tiles;
-  const int64_t keys = prefix_items * a->prefix_len + own_items * a->capacity;
-  const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
-  int64_t seg = keys / (2 * n_cu);
-  if (seg < 256) seg = 256;
-  a->prefix_splits = (int)((a->prefix_len + seg - 1) / seg);
-  a->own_splits = (int)((a->capacity + seg - 1) / seg);
+  choose_splits(a, head_dim);
   // a grid of bounded size whatever max_q tells: the tiles of a request take turns
   const int64_t most = ((int64_t)1 << 21) / ((int64_t)a->n_req * a->n_kv_heads * (a->own_splits > 0 ? a->own_splits : 1));
   if (a->own_tiles > most) a->own_tiles = most > 1 ? (int)most : 1;
-  const int64_t blocks = prefix_items * a->prefix_splits;
+  const int64_t blocks = (int64_t)a->n_kv_heads * a->prefix_tiles * a->prefix_splits;
   a->prefix_blocks = (int)((blocks + kShXcds - 1) / kShXcds * kShXcds);
   const int64_t splits = a->prefix_splits + a->own_splits;
   const size_t o = (size_t)splits * a->n_rows * a->n_heads * head_dim * sizeof(float);
