@@ -18,17 +18,18 @@
 // Work items. A row tile (32 RB RG rows) of one key head against a segment of the
 // prefix, or of one request's own keys (the device knows the lengths: an item takes
 // its even share of them). Each leaves a normalised partial output and its LSE for
-// every row in the workspace, [split][row][head], and a second launch joins a
-// row's splits, in order: the result does not depend on the order of execution.
+// every row in the workspace, and a second launch joins a row's splits, in order: the
+// result does not depend on the order of execution.
 //
 // A workgroup is 4 waves of up to 64 rows (RB blocks of 32): RG groups of rows times
 // KG groups of keys, RG KG = 4. With few rows the waves take different keys of a
 // step, with many rows they share them. 64 rows to a wave halve the LDS reads of an
 // operand a product; the registers (256 of accumulators and queries) allow one wave a
 // SIMD, which overlaps softmax and products itself.
-// Keys come in blocks of 32, KG to a step, straight from HBM to LDS into a ring of 8
-// blocks, one barrier a step. A block's descriptor ends at its last valid row: rows
-// behind a set's end read as zero whatever the cache holds there, and are masked.
+// Keys come in blocks of 32 straight from HBM to LDS, into a ring that the workgroup
+// fills together (KG 1 and 2: one barrier to two blocks) or into a ring for each wave
+// (KG 4: no barrier). A block's descriptor ends at its last valid row: rows behind a
+// set's end read as zero whatever the cache holds there, and are masked.
 //
 // Per block and row block, 32 keys x 32 rows (bf16 MFMA 32x32x16, fp32 accumulation):
 //   S^T = K Q^T      A = K rows from LDS, B = Q^T in registers: a lane holds the
@@ -37,10 +38,10 @@
 //                    index is permuted (4h..4h+3, 8+4h..8+4h+3 for lane half h) and
 //                    the V^T operand is read with the same permutation by LDS
 //                    transpose reads
-// The softmax reference trails the running maximum by at most 8 (log2), so that
-// almost every block skips the rescaling. P is rounded to bf16 for the product, and
-// O is divided by the sum of the rounded weights (the rounding of a dominant weight
-// cancels); the LSE takes the unrounded sum, in fp32.
+// The softmax reference is the first block's maximum, until a block's weights sum to
+// more than 2^10 in a lane: then it moves to that block's maximum and the block's
+// weights are formed again, so that almost every block needs neither maxima nor
+// rescaling. The LSE takes the unrounded sum, in fp32.
 #include "ispa_internal.h"
 
 #include <math.h>
@@ -49,7 +50,7 @@ namespace ispa {
 namespace {
 
 constexpr int kRingBlocks = 10;  // blocks of 32 keys in LDS (160 KB with 128 values a head)
-constexpr int kBlk = 32;        // keys of a block, rows of a row block
+constexpr int kBlk = 32;         // keys of a block, rows of a row block
 constexpr int kShWaves = 4;
 constexpr int kShThreads = kShWaves * 64;
 constexpr int kShXcds = 8;
@@ -153,13 +154,39 @@ __device__ __forceinline__ bf16x8 read_v1(const SWave<D, RB>& w, lds_char* blk, 
         (ISPA_LDS s16x4*)(blk + w.vad[i][o % C::dBlocks] + C::tileBytes + 16 * (o / C::dBlocks) * C::rowBytes));
   return u.v;
 }
+// The weights of a block as product operands: rounded to bf16, and (F = 2) what the
+// rounding left, rounded again. Up to 128 rows the keys' bytes bound the work and the
+// second product is free: the weights then keep 16 bits, and an output's error is that of
+// its own rounding. Wider tiles are bound by the products and take the rounded weights
+// alone (2^-9 each, a relative error of about that of a bf16 output, as in chunk
+// attention), normalised by the sum of the rounded weights.
+template <int F>
+struct SWeights {
+  bf16x8 p[F][2];
+};
+template <int F>
+__device__ __forceinline__ void put_pair(SWeights<F>& p, int i, float e0, float e1, float& rounded) {
+  const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
+  p.p[0][i / 8][i % 8] = hi[0];
+  p.p[0][i / 8][i % 8 + 1] = hi[1];
+  if constexpr (F == 2) {
+    p.p[1][i / 8][i % 8] = (__bf16)(e0 - (float)hi[0]);
+    p.p[1][i / 8][i % 8 + 1] = (__bf16)(e1 - (float)hi[1]);
+  } else {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    rounded = __builtin_amdgcn_fdot2_f32_bf16(hi, one, rounded, false);
+  }
+}
+
 // O^T += V^T P^T of row block b
-template <int D, int RB>
+template <int D, int RB, int F>
 __device__ __forceinline__ void products(SWave<D, RB>& w, int b, const bf16x8 (&v)[2 * SCfg<D>::dBlocks],
-                                         const bf16x8 (&p)[2]) {
+                                         const SWeights<F>& p) {
   constexpr int n = SCfg<D>::dBlocks;
 #pragma unroll
-  for (int o = 0; o < 2 * n; ++o) w.acc[b][o % n] = sh_mfma(v[o], p[o / n], w.acc[b][o % n]);
+  for (int o = 0; o < 2 * n; ++o)
+#pragma unroll
+    for (int f = 0; f < F; ++f) w.acc[b][o % n] = sh_mfma(v[o], p.p[f][o / n], w.acc[b][o % n]);
 }
 
 // Keys from nv on are out of the set: register r holds key 4 hh + 8 (r / 4) + r % 4.
@@ -218,23 +245,19 @@ __device__ __forceinline__ void follow(const SharedArgs& a, SWave<D, RB>& w, con
   }
 }
 
-// P^T of row block b, rounded to bf16, and its sums before and after the rounding
-template <int D, int RB>
+// P^T of row block b and its sums, of the weights and (F = 1) of the rounded ones
+template <int D, int RB, int F>
 __device__ __forceinline__ void weights(const SharedArgs& a, const SWave<D, RB>& w, int b, const f32x16& sc,
-                                        bf16x8 (&p)[2], float& sum, float& rounded) {
-  const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+                                        SWeights<F>& p, float& sum, float& rounded) {
   const float mc = w.m[b] == -INFINITY ? 0.f : w.m[b] * a.scale_log2;
   float s[2] = {0.f, 0.f}, r[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 16; i += 2) {
     const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -mc));
     const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -mc));
-    const bf16x2 two = {(__bf16)e0, (__bf16)e1};
     s[0] += e0;
     s[1] += e1;
-    r[i / 2 % 2] = __builtin_amdgcn_fdot2_f32_bf16(two, one, r[i / 2 % 2], false);
-    p[i / 8][i % 8] = two[0];
-    p[i / 8][i % 8 + 1] = two[1];
+    put_pair<F>(p, i, e0, e1, r[i / 2 % 2]);
   }
   sum = s[0] + s[1];
   rounded = r[0] + r[1];
@@ -245,17 +268,18 @@ __device__ __forceinline__ void weights(const SharedArgs& a, const SWave<D, RB>&
 // products of block j - 1 (weights p, operands at `vblk`), then the scores of block
 // j + 1 (operands at `kblk`) into `next`, and beside them the softmax of block j (sc)
 // into p. The first V operands come in `v`, read before.
-template <int D, int RB>
+template <int D, int RB, int F>
 __device__ __forceinline__ void pipelined(const SharedArgs& a, SWave<D, RB>& w, lds_char* vblk, lds_char* kblk,
-                                          f32x16 (&sc)[RB], f32x16 (&next)[RB], bf16x8 (&p)[RB][2],
+                                          const f32x16 (&sc)[RB], f32x16 (&next)[RB], SWeights<F> (&p)[RB],
                                           bf16x8 (&v)[2 * SCfg<D>::dBlocks], float (&sum)[RB], float (&rounded)[RB]) {
   using C = SCfg<D>;
   constexpr int kV = 2 * C::dBlocks, kK = C::slices;  // operands
-  constexpr int kSteps = RB * (kV + kK);              // matrix instructions
-  constexpr int kValues = 16 * RB;
-  const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
-  bf16x8 k[kK], pn[RB][2];
-  float mc[RB], s1[RB], r1[RB], even = 0.f;
+  constexpr int kEach = RB * F;                       // products of a V operand
+  constexpr int kSteps = kEach * kV + RB * kK;        // matrix instructions
+  constexpr int kPairs = 8 * RB;
+  bf16x8 k[kK];
+  SWeights<F> pn[RB];
+  float mc[RB], s1[RB], r1[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     mc[b] = w.m[b] == -INFINITY ? 0.f : w.m[b] * a.scale_log2;
@@ -264,31 +288,26 @@ __device__ __forceinline__ void pipelined(const SharedArgs& a, SWave<D, RB>& w, 
 #pragma unroll
   for (int t = 0; t < kSteps; ++t) {
     // operands three ahead
-    if (t < RB * kV && t % RB == 0 && t / RB + kVAhead < kV) v[t / RB + kVAhead] = read_v1<D, RB>(w, vblk, t / RB + kVAhead);
-    if (t >= RB * (kV - kVAhead) && t % RB == 0 && t / RB - (kV - kVAhead) < kK)
-      k[t / RB - (kV - kVAhead)] = *(ISPA_LDS const bf16x8*)(kblk + w.kad[t / RB - (kV - kVAhead)]);
-    if (t < RB * kV) {
-      const int o = t / RB, b = t % RB;
-      w.acc[b][o % C::dBlocks] = sh_mfma(v[o], p[b][o / C::dBlocks], w.acc[b][o % C::dBlocks]);
+    if (t < kEach * kV) {
+      const int o = t / kEach, f = t / RB % F, b = t % RB, ahead = o + kVAhead;
+      if (t % kEach == 0) {
+        if (ahead < kV) v[ahead] = read_v1<D, RB>(w, vblk, ahead);
+        else if (ahead - kV < kK) k[ahead - kV] = *(ISPA_LDS const bf16x8*)(kblk + w.kad[ahead - kV]);
+      }
+      w.acc[b][o % C::dBlocks] = sh_mfma(v[o], p[b].p[f][o / C::dBlocks], w.acc[b][o % C::dBlocks]);
     } else {
-      const int o = (t - RB * kV) / RB, b = t % RB;
+      const int o = (t - kEach * kV) / RB, b = t % RB, ahead = o + kVAhead;
+      if (b == 0 && ahead < kK) k[ahead] = *(ISPA_LDS const bf16x8*)(kblk + w.kad[ahead]);
       next[b] = sh_mfma(k[o], w.q[b][o], o == 0 ? f32x16{} : next[b]);
     }
 #pragma unroll
-    for (int i = t * kValues / kSteps; i < (t + 1) * kValues / kSteps; ++i) {
-      const int b = i / 16, r = i % 16;
-      const float e = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.scale_log2, -mc[b]));
-      if (r % 2 == 0) {
-        even = e;
-        sum[b] += e;
-      } else {
-        s1[b] += e;
-        const bf16x2 two = {(__bf16)even, (__bf16)e};
-        pn[b][r / 8][r % 8 - 1] = two[0];
-        pn[b][r / 8][r % 8] = two[1];
-        float& rs = r % 4 == 1 ? rounded[b] : r1[b];
-        rs = __builtin_amdgcn_fdot2_f32_bf16(two, one, rs, false);
-      }
+    for (int i = t * kPairs / kSteps; i < (t + 1) * kPairs / kSteps; ++i) {
+      const int b = i / 8, r = 2 * (i % 8);
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[b][r], a.scale_log2, -mc[b]));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[b][r + 1], a.scale_log2, -mc[b]));
+      sum[b] += e0;
+      s1[b] += e1;
+      put_pair<F>(pn[b], r, e0, e1, i % 2 == 0 ? rounded[b] : r1[b]);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -296,8 +315,7 @@ __device__ __forceinline__ void pipelined(const SharedArgs& a, SWave<D, RB>& w, 
   for (int b = 0; b < RB; ++b) {
     sum[b] += s1[b];
     rounded[b] += r1[b];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) p[b][h] = pn[b][h];
+    p[b] = pn[b];
   }
 }
 
@@ -397,9 +415,9 @@ __device__ __forceinline__ void rows_here(SWave<D, RB>& w) {
 
 // A block's weights are too large for the reference that they were formed with, or
 // there was none: the reference moves, and the weights are formed again.
-template <int D, int RB>
+template <int D, int RB, int F>
 __device__ __forceinline__ void check_reference(const SharedArgs& a, SWave<D, RB>& w, const f32x16 (&sc)[RB],
-                                                bf16x8 (&p)[RB][2], float (&sum)[RB], float (&rounded)[RB]) {
+                                                SWeights<F> (&p)[RB], float (&sum)[RB], float (&rounded)[RB]) {
   bool far = false;
 #pragma unroll
   for (int b = 0; b < RB; ++b) far = far || sum[b] > kShFar || w.m[b] == -INFINITY;
@@ -408,7 +426,7 @@ __device__ __forceinline__ void check_reference(const SharedArgs& a, SWave<D, RB
     maxima<RB>(sc, top);
     follow<D, RB>(a, w, top);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
+    for (int b = 0; b < RB; ++b) weights<D, RB, F>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
   }
   // (the accumulators stay in the accumulation registers on both ways)
 #pragma unroll
@@ -418,7 +436,7 @@ __device__ __forceinline__ void check_reference(const SharedArgs& a, SWave<D, RB
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     w.l[b] += sum[b];
-    w.lr[b] += rounded[b];
+    w.lr[b] += F == 2 ? sum[b] : rounded[b];
   }
 }
 
@@ -433,7 +451,8 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
   constexpr int kSlots = kRingBlocks / kStep;  // steps in LDS
   constexpr int kStepLoads = 2 * kStep * C::loads;
   constexpr int kStepBytes = kStep * C::blockBytes;
-  constexpr int KB = kStep / KG;  // blocks of a step for this wave
+  constexpr int KB = kStep / KG;     // blocks of a step for this wave
+  constexpr int F = KG > 1 ? 2 : 1;  // (up to 128 rows: exact weights)
   const int hh = (tid & 63) >> 5;
   const int n_keys = (int)(ks.end - ks.begin);
   const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
@@ -461,11 +480,14 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
   rows_here<D, RB>(w);
   f32x16 sc[RB];
   float sum[RB], rounded[RB];
-  bf16x8 v[2 * C::dBlocks], p[RB][2];
+  bf16x8 v[2 * C::dBlocks];
+  SWeights<F> p[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) p[b][h] = bf16x8{};
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) p[b].p[f][h] = bf16x8{};
   arrived<(kSlots - 3) * kStepLoads>();
   {
     bf16x8 k[C::slices];
@@ -503,8 +525,8 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
       if (left < kBlk) mask<RB>(sc, left, hh);
       left -= KG * kBlk;
       f32x16 next[RB];
-      pipelined<D, RB>(a, w, vblk, kblk, sc, next, p, v, sum, rounded);
-      check_reference<D, RB>(a, w, sc, p, sum, rounded);
+      pipelined<D, RB, F>(a, w, vblk, kblk, sc, next, p, v, sum, rounded);
+      check_reference<D, RB, F>(a, w, sc, p, sum, rounded);
 #pragma unroll
       for (int b = 0; b < RB; ++b) sc[b] = next[b];
     }
@@ -515,7 +537,7 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
 #pragma unroll
   for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
 #pragma unroll
-  for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
+  for (int b = 0; b < RB; ++b) products<D, RB, F>(w, b, v, p[b]);
 }
 
 // A wave's own keys, in a ring of its own: K and V tiles of 32 keys in turn, each loaded
@@ -567,7 +589,9 @@ __device__ __forceinline__ void private_keys(const SharedArgs& a, SWave<D, RB>& 
   rows_here<D, RB>(w);
   f32x16 sc[RB];
   float sum[RB], rounded[RB];
-  bf16x8 v[2 * C::dBlocks], p[RB][2];
+  bf16x8 v[2 * C::dBlocks];
+  constexpr int F = 2;
+  SWeights<F> p[RB];
   int slot = 0;
 #pragma unroll 1
   while (left > 0) {
@@ -585,14 +609,14 @@ __device__ __forceinline__ void private_keys(const SharedArgs& a, SWave<D, RB>& 
     if (left < kBlk) mask<RB>(sc, left, hh);
     left -= kBlk;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) weights<D, RB>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
-    check_reference<D, RB>(a, w, sc, p, sum, rounded);
+    for (int b = 0; b < RB; ++b) weights<D, RB, F>(a, w, b, sc[b], p[b], sum[b], rounded[b]);
+    check_reference<D, RB, F>(a, w, sc, p, sum, rounded);
     asm volatile("s_waitcnt vmcnt(%0)" ::"i"((kTiles - 1) * kLoads) : "memory");
     tile = ring + slot * C::tileBytes - C::tileBytes;  // (V operand offsets are those behind a K tile)
 #pragma unroll
     for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, tile, o);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) products<D, RB>(w, b, v, p[b]);
+    for (int b = 0; b < RB; ++b) products<D, RB, F>(w, b, v, p[b]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     load(!(kTiles & 1), slot);
     slot = slot + 1 == kTiles ? 0 : slot + 1;
@@ -653,10 +677,11 @@ __device__ __forceinline__ void join_groups(const SharedArgs& a, SWave<D, RB>& w
   }
 }
 
-// The rows' normalised output and LSE into split `split`.
+// The rows' normalised output and LSE into the partial rows part + token: outputs
+// [partial row][head][D], LSEs [head][part_rows] behind part * n_heads.
 template <int D, int RB>
-__device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, RB>& w, const SRows<RB>& rows, int split,
-                                           int lane) {
+__device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, RB>& w, const SRows<RB>& rows,
+                                           int64_t part, int part_rows, int lane) {
   const int hh = lane >> 5;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -664,10 +689,10 @@ __device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, R
     const int token = rows.token[b], head = rows.head[b];
     // an empty segment (or scores of -inf alone) leaves LSE -inf, and its output is not read
     if (hh == 0)
-      a.part_lse[((int64_t)split * a.n_heads + head) * a.n_rows + token] =
+      a.part_lse[part * a.n_heads + (int64_t)head * part_rows + token] =
           w.l[b] > 0.f || w.l[b] != w.l[b] ? w.m[b] * a.scale + logf(w.l[b]) : -INFINITY;
     const float inv = 1.0f / w.lr[b];
-    float* o = a.part_o + (((int64_t)split * a.n_rows + token) * a.n_heads + head) * D + 4 * hh;
+    float* o = a.part_o + ((part + token) * a.n_heads + head) * D + 4 * hh;
 #pragma unroll
     for (int d = 0; d < SCfg<D>::dBlocks; ++d)
 #pragma unroll
@@ -677,11 +702,11 @@ __device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, R
   }
 }
 
-// A workgroup's item: rows [row0, row0 + 32 RB RG) of n_item_rows against `ks`, into
-// split `split`; RG = 4 / KG row groups.
+// A workgroup's item: rows [row0, row0 + 32 RB RG) of n_item_rows against `ks`, into the
+// partial rows from `part` on; RG = 4 / KG row groups.
 template <int D, int KG, int RB>
 __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const Keys& ks, int kv_head, int first,
-                                         int64_t row0, int64_t n_item_rows, int split) {
+                                         int64_t row0, int64_t n_item_rows, int64_t part, int part_rows) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wave % KG, rg = wave / KG;
   SWave<D, RB> w;
@@ -706,43 +731,60 @@ __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const 
     w.lr[b] = pair_sum32(w.lr[b]);
   }
   if constexpr (KG > 1) join_groups<D, KG, RB>(a, w, smem, kg, rg, lane);
-  if (kg == 0) write_part<D, RB>(a, w, rows, split, lane);
+  if (kg == 0) write_part<D, RB>(a, w, rows, part, part_rows, lane);
 }
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// Logical index of a workgroup in a section of n items: the 8 XCDs take workgroups in
-// turn; the items that share keys (the row tiles of one segment) stay on one XCD.
-__device__ __forceinline__ int xcd_index(int bid, int n_padded) { return (bid % kShXcds) * (n_padded / kShXcds) + bid / kShXcds; }
+// Logical index of a workgroup in a section of n items, -1 behind them: the 8 XCDs take
+// workgroups in turn; the items that share keys (the row tiles of one segment) stay on
+// one XCD.
+__device__ __forceinline__ int xcd_index(int bid, int n) {
+  const int per = (n + kShXcds - 1) / kShXcds;
+  const int i = bid % kShXcds * per + bid / kShXcds;
+  return bid / kShXcds < per && i < n ? i : -1;
+}
+
+// The batch's row tiles against the prefix, and the segments that the prefix is cut into
+// for so many (the host knows only the padded count of rows, so the plan holds them for
+// every count of tiles).
+struct Prefix {
+  int tiles, splits;
+};
+__device__ __forceinline__ Prefix prefix_of(const SharedArgs& a, int total, int tile_rows) {
+  const int tiles = (int)(((int64_t)total * a.group + tile_rows - 1) / tile_rows);
+  const int i = tiles < 1 ? 0 : tiles > kSharedPlans ? kSharedPlans - 1 : tiles - 1;
+  return {tiles, a.prefix_len > 0 ? a.prefix_splits[i] : 0};
+}
 
 template <int D, int KGP, int RBP, int KGO, int RBO>
 __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[kRingBlocks * SCfg<D>::blockBytes];
   const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);  // rows of the batch, without padding
   if ((int)blockIdx.x < a.prefix_blocks) {
-    int i = xcd_index(blockIdx.x, a.prefix_blocks);
-    const int n = a.n_kv_heads * a.prefix_splits * a.prefix_tiles;
-    if (i >= n) return;
-    const int tile = i % a.prefix_tiles;
-    i /= a.prefix_tiles;
-    const int split = i % a.prefix_splits, head = i / a.prefix_splits;
     constexpr int kRows = kShWaves / KGP * RBP * kBlk;
     const int64_t rows = (int64_t)total * a.group;
-    if ((int64_t)tile * kRows >= rows) return;
+    const Prefix pre = prefix_of(a, total, kRows);
+    int i = xcd_index(blockIdx.x, a.n_kv_heads * pre.splits * pre.tiles);
+    if (i < 0) return;
+    const int tile = i % pre.tiles;
+    i /= pre.tiles;
+    const int split = i % pre.splits, head = i / pre.splits;
     // even shares in whole blocks
     const int64_t blocks = (a.prefix_len + kBlk - 1) / kBlk;
-    const int64_t b0 = blocks * split / a.prefix_splits * kBlk, b1 = blocks * (split + 1) / a.prefix_splits * kBlk;
+    const int64_t b0 = blocks * split / pre.splits * kBlk, b1 = blocks * (split + 1) / pre.splits * kBlk;
     const Keys ks{a.k_prefix + head * D, a.v_prefix + head * D, a.ld_prefix, b0,
                   b1 < a.prefix_len ? b1 : a.prefix_len};
-    run_item<D, KGP, RBP>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, split);
+    run_item<D, KGP, RBP>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, (int64_t)split * total, total);
     return;
   }
-  int i = xcd_index(blockIdx.x - a.prefix_blocks, gridDim.x - a.prefix_blocks);
   // up to 32 rows: every wave an item of its own
   constexpr bool kWaveItems = KGO == kShWaves && RBO == 1;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (kWaveItems) i = i * kShWaves + wave;
   const int n = a.n_req * a.n_kv_heads * a.own_splits * a.own_tiles;
+  int i = xcd_index(blockIdx.x - a.prefix_blocks, kWaveItems ? (n + kShWaves - 1) / kShWaves : n);
+  if (i < 0) return;
+  if (kWaveItems) i = i * kShWaves + wave;
   if (i >= n) return;
   const int tile = i % a.own_tiles;
   i /= a.own_tiles;
@@ -757,6 +799,7 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   const int64_t b0 = blocks * split / a.own_splits * kBlk, b1 = blocks * (split + 1) / a.own_splits * kBlk;
   const int64_t base = (int64_t)b * a.ld_request + head * D;
   const Keys ks{a.k_cache + base, a.v_cache + base, a.ld_cache, b0, b1 < len ? b1 : len};
+  const int64_t part = a.own_part + (int64_t)split * a.n_rows;
   // (more than one turn only where a request has more rows than max_q tells)
   for (int64_t row0 = (int64_t)tile * kRows; row0 < rows; row0 += (int64_t)a.own_tiles * kRows) {
     if constexpr (kWaveItems) {
@@ -767,67 +810,79 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
       private_keys<D, 1>(a, w, (lds_char*)smem + wave * (kRingBlocks * SCfg<D>::blockBytes / kShWaves), ks, lane);
       w.l[0] = pair_sum32(w.l[0]);
       w.lr[0] = pair_sum32(w.lr[0]);
-      write_part<D, 1>(a, w, r, a.prefix_splits + split, lane);
+      write_part<D, 1>(a, w, r, part, a.n_rows, lane);
     } else {
-      run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, a.prefix_splits + split);
+      run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, part, a.n_rows);
       __syncthreads();
     }
   }
 }
 
-// Eq. 11-12 over a row's splits: D / 4 lanes to a row of a head.
-template <int D>
-__global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a) {
-  constexpr int kLanes = D / 4;
-  constexpr float kLog2e = 1.4426950408889634f;
-  const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
-  const int c = threadIdx.x % kLanes;
-  const int64_t token = i / a.n_heads;
-  const int head = (int)(i - token * a.n_heads);
-  if (token >= total) return;
-  const int splits = a.prefix_splits + a.own_splits;
-  const float* ls = a.part_lse + (int64_t)head * a.n_rows + token;
-  const int64_t lstep = (int64_t)a.n_heads * a.n_rows;
-  const float* os = a.part_o + (token * a.n_heads + head) * D + 4 * c;
-  const int64_t ostep = (int64_t)a.n_rows * a.n_heads * D;
-  // a batch of splits at a time, its loads in flight together, with a running maximum
+// A row's running join: maximum of the LSEs, sum of the weights, weighted outputs.
+struct Joined {
+  float m, sum;
+  f32x4 o;
+};
+// Joins n splits, `ls` and `os` the row's first LSE and output, ls_step and os_step from
+// split to split: a batch at a time, its loads in flight together.
+__device__ __forceinline__ void join_splits(Joined& r, int n, const float* ls, int64_t ls_step, const float* os,
+                                            int64_t os_step) {
   constexpr int kBatch = 8;
-  float m = -INFINITY, sum = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < splits; s0 += kBatch) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  for (int s0 = 0; s0 < n; s0 += kBatch) {
     float l[kBatch];
     f32x4 v[kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      const bool in = s0 + j < splits;
-      l[j] = in ? ls[(s0 + j) * lstep] : -INFINITY;
-      v[j] = in ? *(const f32x4*)(os + (s0 + j) * ostep) : f32x4{0.f, 0.f, 0.f, 0.f};
+      const bool in = s0 + j < n;
+      l[j] = in ? *ls : -INFINITY;
+      v[j] = in ? *(const f32x4*)os : f32x4{0.f, 0.f, 0.f, 0.f};
+      ls += ls_step;
+      os += os_step;
     }
-    float top = m;
+    float top = r.m;
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) top = fmaxf(top, l[j]);
-    const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * kLog2e);
-    sum *= old;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] *= old;
+    const float old = r.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.m - top) * kLog2e);
+    r.sum *= old;
+    r.o *= old;
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       // (a split without keys has no output: what lies there is not used)
       const bool empty = l[j] == -INFINITY;
       const float e = empty ? 0.f : __builtin_amdgcn_exp2f((l[j] - top) * kLog2e);
-      sum += e;
+      r.sum += e;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = fmaf(e, empty ? 0.f : v[j][k], o[k]);
+      for (int k = 0; k < 4; ++k) r.o[k] = fmaf(e, empty ? 0.f : v[j][k], r.o[k]);
     }
-    m = top;
+    r.m = top;
   }
+}
+
+// Eq. 11-12 over a row's splits (the prefix's segments, then its own keys'): D / 4 lanes
+// to a row of a head.
+template <int D>
+__global__ __launch_bounds__(256) void attn_shared_join_kernel(SharedArgs a, int tile_rows) {
+  constexpr int kLanes = D / 4;
+  const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);
+  const uint32_t i = (blockIdx.x * 256 + threadIdx.x) / kLanes;
+  const int c = threadIdx.x % kLanes;
+  const int token = (int)(i / (uint32_t)a.n_heads), head = (int)(i % (uint32_t)a.n_heads);
+  if (token >= total) return;
+  Joined r{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+  const int64_t row = (int64_t)a.n_heads * D, at_row = (int64_t)token * row + head * D + 4 * c;
+  join_splits(r, prefix_of(a, total, tile_rows).splits, a.part_lse + (int64_t)head * total + token,
+              (int64_t)a.n_heads * total, a.part_o + at_row, (int64_t)total * row);
+  join_splits(r, a.own_splits, a.part_lse + a.own_part * a.n_heads + (int64_t)head * a.n_rows + token,
+              (int64_t)a.n_heads * a.n_rows, a.part_o + a.own_part * row + at_row, (int64_t)a.n_rows * row);
+  const float m = r.m, sum = r.sum;
+  f32x4 o = r.o;
   // no key at all: out = 0, lse = -inf
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
   for (int k = 0; k < 4; ++k) o[k] *= inv;
   if (a.lse && c == 0) a.lse[(int64_t)head * a.n_rows + token] = sum == 0.f ? -INFINITY : m + logf(sum);
-  const int64_t at = token * a.ld_out + head * D + 4 * c;
+  const int64_t at = (int64_t)token * a.ld_out + head * D + 4 * c;
   if (a.out_bf16) {
     bf16x4 r;
 #pragma unroll
@@ -877,50 +932,68 @@ hipError_t launch_d(const SharedArgs& a, hipStream_t stream) {
   }
   const int64_t rows = (int64_t)a.n_rows * a.n_heads;
   constexpr int kPer = 256 / (D / 4);
-  attn_shared_join_kernel<D><<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, stream>>>(a);
+  attn_shared_join_kernel<D><<<(unsigned)((rows + kPer - 1) / kPer), 256, 0, stream>>>(a, tile_rows(a.prefix_shape));
   return hipGetLastError();
 }
 
-// How many segments the prefix and the own keys are cut into. In units of one key's K
-// and V rows streamed by a compute unit at its share of the HBM rate (24 ns of 512
-// bytes), a launch takes about
+// How many segments the prefix (for every count of row tiles) and the own keys are cut
+// into. In units of one key's K and V rows streamed by a compute unit at its share of
+// the HBM rate (24 ns of 512 bytes), a launch takes about
 //   max(rounds x keys of a segment, all keys / slots) + rounds x kStart + kJoin x segments
 // where `slots` workgroups run at a time, kStart is a workgroup's start and end (6 us),
 // and kJoin a split's part of the join. A row tile of 256 rows is bound by its products
-// (1.45 units a key); narrower ones by the stream, and a workgroup may take more than
-// its share of that while others are done. Measured at 128 values a head: 64 rows of 32
-// heads against 32768 keys 115 us in 8 segments (one round), 133 in 16, 184 in 32; 3900
-// rows of 12 heads against 32760 keys 911 us in 4 segments (three full rounds), 1001 in
-// 2, 1015 in 1.
-void choose_splits(SharedArgs* a, int head_dim) {
+// (1.45 units a key); narrower ones by the stream, of which a workgroup may take a
+// little more than its share while others are done. Measured at 128 values a head: 64
+// rows of 32 heads against 32768 keys 115 us in 8 segments (one round), 133 in 16, 184
+// in 32; 3900 rows of 12 heads against 32760 keys 911 us in 4 segments (three full
+// rounds), 1001 in 2, 1015 in 1.
+void choose_splits(SharedArgs* a, int head_dim, int prefix_tiles) {
   constexpr int kStart = 250, kJoin = 4;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
-  const int64_t prefix_items = (int64_t)a->n_kv_heads * a->prefix_tiles;
-  const int64_t own_items = (int64_t)a->n_req * a->n_kv_heads * a->own_tiles;
   const bool wide = a->prefix_shape == 3;
   const double per_prefix = wide ? 1.45 : 1.0, per_own = a->own_shape == 3 ? 1.45 : 1.0;
-  const double alone = wide ? 1.0 : 1.5;  // a workgroup's rate over its share, when others leave it
+  const double alone = wide ? 1.0 : 1.1;
   const int slots = wide && head_dim == 64 ? 2 * n_cu : n_cu;
   // half of the caches' capacity stands for the lengths, which the device knows
-  const double total =
-      (prefix_items * a->prefix_len * per_prefix + own_items * (a->capacity / 2.0) * per_own) / slots;
-  a->prefix_splits = 0;
-  if (a->prefix_len > 0) {
+  const double own = (double)a->n_req * a->n_kv_heads * a->own_tiles * (a->capacity / 2.0) * per_own / slots;
+  const int64_t own_items = (int64_t)a->n_req * a->n_kv_heads * a->own_tiles;
+  const int64_t own_groups = a->capacity == 0 ? 0 : a->own_shape == 0 ? own_items / kShWaves : own_items;
+  const int tile = tile_rows(a->prefix_shape);
+  int64_t blocks = 0, part = 0;
+  for (int t = 1; t <= kSharedPlans; ++t) {
+    // the last plan stands for its count of tiles and all above it
+    const int tiles = t == kSharedPlans && prefix_tiles > t ? prefix_tiles : t;
+    a->prefix_splits[t - 1] = t > 1 ? a->prefix_splits[t - 2] : 1;
+    if (tiles > prefix_tiles || a->prefix_len == 0) continue;
+    const int64_t items = (int64_t)a->n_kv_heads * tiles;
+    const double total = own + items * a->prefix_len * per_prefix / slots;
     double best = 0.0;
-    for (int64_t n = 1; n == 1 || (n <= 128 && n * 256 <= a->prefix_len); ++n) {
-      const int64_t rounds = (prefix_items * n + slots - 1) / slots;
+    const int64_t most = a->prefix_len / 256 < 1 ? 1 : a->prefix_len / 256 > 128 ? 128 : a->prefix_len / 256;
+    for (int j = 0; j < 12; ++j) {  // the fewest segments; parts of a round, and whole ones
+      int64_t n = j < 4 ? j + 1 : j < 9 ? j * slots / (8 * items) : (j - 7) * slots / items;
+      n = n < 1 ? 1 : n > most ? most : n;
+      const int64_t rounds = (items * n + slots - 1) / slots;
+      const int64_t starts = (items * n + own_groups + slots - 1) / slots;  // the own items' rounds too
       const double chain = rounds * ((double)a->prefix_len / n) * per_prefix / alone;
-      const double cost = (chain > total ? chain : total) + rounds * kStart + kJoin * n;
-      if (n == 1 || cost < best) {
+      const double cost = (chain > total ? chain : total) + starts * kStart + kJoin * n;
+      if (best == 0.0 || cost < best) {
         best = cost;
-        a->prefix_splits = (int)n;
+        a->prefix_splits[t - 1] = (uint8_t)n;
       }
     }
+    // (the last plan's blocks cover all counts of tiles from kSharedPlans on)
+    const int64_t rows = (int64_t)tiles * tile / a->group + 1;
+    if (items * a->prefix_splits[t - 1] > blocks) blocks = items * a->prefix_splits[t - 1];
+    const int64_t p = a->prefix_splits[t - 1] * (rows < a->n_rows ? rows : a->n_rows);
+    if (p > part) part = p;
   }
+  a->prefix_blocks = (int)((blocks + kShXcds - 1) / kShXcds * kShXcds);
+  a->own_part = part;
   // no own item's stream outlasts the whole. (Up to 32 rows an item is a wave's: four run
   // in a slot, and one alone streams at less than half of the slot's share.)
   a->own_splits = 0;
   if (a->capacity > 0) {
+    const double total = own + (double)a->n_kv_heads * prefix_tiles * a->prefix_len * per_prefix / slots;
     const int64_t least = a->own_shape == 0 ? 128 : 256;
     const double share = total > least ? total : (double)least;
     int64_t n = (int64_t)ceil((a->own_shape == 0 ? 1.4 : 1.0) * a->capacity * per_own / share);
@@ -939,18 +1012,15 @@ size_t attn_shared_plan(SharedArgs* a, int head_dim) {
   a->prefix_shape = tile_shape(prefix_rows);
   a->own_shape = tile_shape(own_rows);
   const int prefix_tile = tile_rows(a->prefix_shape), own_tile = tile_rows(a->own_shape);
-  a->prefix_tiles = (int)((prefix_rows + prefix_tile - 1) / prefix_tile);
   a->own_tiles = (int)((own_rows + own_tile - 1) / own_tile);
-  choose_splits(a, head_dim);
+  choose_splits(a, head_dim, (int)((prefix_rows + prefix_tile - 1) / prefix_tile));
   // a grid of bounded size whatever max_q tells: the tiles of a request take turns
   const int64_t most = ((int64_t)1 << 21) / ((int64_t)a->n_req * a->n_kv_heads * (a->own_splits > 0 ? a->own_splits : 1));
   if (a->own_tiles > most) a->own_tiles = most > 1 ? (int)most : 1;
-  const int64_t blocks = (int64_t)a->n_kv_heads * a->prefix_tiles * a->prefix_splits;
-  a->prefix_blocks = (int)((blocks + kShXcds - 1) / kShXcds * kShXcds);
-  const int64_t splits = a->prefix_splits + a->own_splits;
-  const size_t o = (size_t)splits * a->n_rows * a->n_heads * head_dim * sizeof(float);
+  const int64_t parts = a->own_part + (int64_t)a->own_splits * a->n_rows;
+  const size_t o = (size_t)parts * a->n_heads * head_dim * sizeof(float);
   a->lse_offset = (o + 255) / 256 * 256;
-  return a->lse_offset + (size_t)splits * a->n_rows * a->n_heads * sizeof(float);
+  return a->lse_offset + (size_t)parts * a->n_heads * sizeof(float);
 }
 
 hipError_t launch_attn_shared(const SharedArgs& a, int head_dim, hipStream_t stream) {

@@ -231,6 +231,7 @@ struct SlotArgs {
 hipError_t launch_slot_map(const SlotArgs& a, hipStream_t stream);
 
 // ---- attention over a shared prefix (attn_shared.hip) ----
+constexpr int kSharedPlans = 64;
 struct SharedArgs {
   const uint16_t *q, *k_prefix, *v_prefix, *k_cache, *v_cache;
   int64_t ld_q, ld_prefix, ld_cache, ld_request, ld_out;  // elements
@@ -243,7 +244,9 @@ struct SharedArgs {
   int out_bf16;
   float* lse;
   // set by the plan: the layout of the work (attn_shared.hip), the partial results
-  int prefix_shape, own_shape, prefix_tiles, own_tiles, prefix_splits, own_splits, prefix_blocks;
+  int prefix_shape, own_shape, own_tiles, own_splits, prefix_blocks;
+  uint8_t prefix_splits[kSharedPlans];  // by the count of row tiles
+  int64_t own_part;                     // partial rows of the prefix's segments
   size_t lse_offset;
   float *part_o, *part_lse;
 };
