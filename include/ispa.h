@@ -498,7 +498,7 @@ int ispa_norm_residual(const void* x, int32_t x_dtype, const void* y, int32_t y_
  *   d_gate, d_scale, d_shift            fp32 [groups, cols] or NULL (not wanted)
  *   d_post_weight, d_weight, d_bias     fp32 [cols] or NULL
  *                (d_gate and d_post_weight need y; the others a norm;
- *                d_post_weight needs post)
+ *                d_post_weight needs post); groups * cols <= 2^31
  *   workspace    device, 256-byte aligned, at least
  *                ispa_norm_residual_backward_workspace_bytes bytes; may be NULL where
  *                no gradient of a vector is wanted. Used only during the call's

@@ -781,6 +781,7 @@ int ispa_norm_residual_backward(const void* d_h, int32_t h_dtype, const void* d_
   if (!y && (d_gate || d_post_weight)) return ISPA_ERR_INVALID_ARG;
   if (!has_norm && (d_weight || d_bias || d_scale || d_shift)) return ISPA_ERR_INVALID_ARG;
   if (post == ISPA_NORM_NONE && d_post_weight) return ISPA_ERR_INVALID_ARG;
+  if ((rows + a.group_rows - 1) / a.group_rows * cols > ((int64_t)1 << 31)) return ISPA_ERR_INVALID_ARG;
   if (any_misaligned({d_h, d_x_out, x_out, d_x, d_y, d_gate, d_post_weight, d_weight, d_bias, d_scale, d_shift}))
     return ISPA_ERR_INVALID_ARG;
   if (rows == 0) return ISPA_OK;

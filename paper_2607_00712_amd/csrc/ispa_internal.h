@@ -196,6 +196,7 @@ struct NormArgs {
   // workgroups to a group
   int lanes, waves, block_rows, group_blocks;
   int64_t n_groups;
+  int group_vectors, shared_vectors;  // gradients wanted of the groups' own and of shared vectors
 };
 hipError_t launch_norm_residual(NormArgs a, hipStream_t stream);
 // workgroups that share a group's rows in the backward pass

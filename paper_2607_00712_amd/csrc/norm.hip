@@ -23,15 +23,27 @@
 // part. The statistics are computed again from x' and y, which the pass reads
 // anyway: nothing but the tensors themselves is kept for it.
 //
-// Both are bound by bytes: each tensor is read once and written once. A row stays
-// in registers between its reductions; a variance is the mean of the centred
-// squares (no cancellation). All arithmetic is fp32, rounded once at the store.
+// Both are bound by bytes: each tensor is read once and written once, and a row stays in
+// registers between its reductions. Forward, a row to a workgroup (or to a wave) and no
+// loop: the many workgroups of a compute unit are what keeps loads in flight, and rows of
+// one's own for each workgroup, fetched ahead of the reductions, came out slower (4680 rows
+// of 5120, fp32 stream: 80 us against 65). Backward, where the columns' sums stay with a
+// workgroup over its rows, the next row is on its way while this one is reduced, as it lies
+// in memory (a bf16 chunk takes 4 registers). A variance is the mean of the centred squares
+// (no cancellation). All arithmetic is fp32, rounded once at the store.
+//
+// Measured at 4680 rows, bf16 block output, gate, scale and shift (us, and TB/s of the
+// tensors read and written once; a copy of 48 MB runs at 5.0):
+//   cols        1536 fp32   1536 bf16   5120 fp32   5120 bf16, RMS norm of y too
+//   forward      17 (5.0)    13 (4.5)    62 (4.7)    50 (3.8)
+//   backward     38 (3.4)    29 (3.0)   115 (3.8)   104 (2.8)
 #include "ispa_internal.h"
 
 namespace ispa {
 namespace {
 
-constexpr int kNMaxWaves = 16;
+constexpr int kNMaxWaves = 16;  // of a workgroup
+constexpr int kNMaxSums = 3;    // sums taken together
 
 struct alignas(16) F8 {
   float v[8];
@@ -72,28 +84,97 @@ __device__ __forceinline__ void store8(void* p, bool f32, int64_t e, const F8& x
   }
 }
 
-// Sums over the lanes of a row: `lanes` (a power of two up to 64) neighbouring
-// lanes, or `waves` whole waves of a workgroup that work on one row. Every lane gets
-// the same bits. Successive calls use the two halves of `part` in turn, so one
-// barrier each is enough: a wave writes a half again only after a barrier that
-// every wave reaches after reading it.
+// Eight values of a bf16 or fp32 tensor as they lie in memory (zeros where not `here`):
+// fetched early, unpacked at their use, so that nothing waits in between. The types are
+// the kernel's template arguments: a branch on them around each load costs more than the
+// row's arithmetic.
+template <bool F32>
+struct Raw8 {
+  u32x4 d[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> fetch8(const void* p, int64_t e, bool here) {
+  Raw8<F32> r;
+#pragma unroll
+  for (int i = 0; i < (F32 ? 2 : 1); ++i)
+    r.d[i] = here ? *(const u32x4*)((const char*)p + e * (F32 ? 4 : 2) + 16 * i) : u32x4{0, 0, 0, 0};
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ F8 unpack8(const Raw8<F32>& r) {
+  F8 x;
+  if constexpr (F32) {
+    const f32x4 lo = __builtin_bit_cast(f32x4, r.d[0]), hi = __builtin_bit_cast(f32x4, r.d[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x.v[i] = lo[i];
+      x.v[4 + i] = hi[i];
+    }
+  } else {
+    const bf16x8 b = __builtin_bit_cast(bf16x8, r.d[0]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.v[i] = (float)b[i];
+  }
+  return x;
+}
+
+// One step of a sum over lanes within a row of 16 (DPP, no trip through LDS).
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(
+                 float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+}
+
+// Sums over the lanes of a row: `lanes` (8, 16, 32 or 64) neighbouring lanes, or `waves`
+// whole waves of a workgroup that work on one row. Every lane gets the same bits.
+// Successive calls use the two halves of `part` in turn, so one barrier each is enough: a
+// wave writes a half again only after a barrier that every wave reaches after reading it.
 struct RowSum {
-  float* part;  // [2][2][kNMaxWaves]
-  int lanes, waves, wave, turn;
+  float* part;  // [2][kNMaxSums][kNMaxWaves]
+  int lanes, waves, wave, turn;  // wave: of the workgroup; its row's are wave / waves * waves on
+
+  // over the row's lanes of this wave
+  template <int N>
+  __device__ __forceinline__ void over_lanes(float (&s)[N]) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      s[n] = dpp_add<0xB1>(s[n]);   // lane ^ 1
+      s[n] = dpp_add<0x4E>(s[n]);   // lane ^ 2
+      s[n] = dpp_add<0x141>(s[n]);  // the other quad of 8
+    }
+    if (lanes > 8) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = dpp_add<0x140>(s[n]);  // the other half of 16
+    }
+    if (lanes == 32) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] += __shfl_xor(s[n], 16);
+    } else if (lanes == 64) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        s[n] = dpp_add<0x142, 0xa>(s[n]);  // rows 1 and 3 take rows 0 and 2
+        s[n] = dpp_add<0x143, 0xc>(s[n]);  // rows 2 and 3 take row 1
+        s[n] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s[n]), 63));
+      }
+    }
+  }
+  // the waves' values to every wave: [n * kNMaxWaves + w], w from the row's first wave on
+  template <int N>
+  __device__ __forceinline__ const float* exchange(const float (&s)[N]) {
+    float* p = part + turn * kNMaxSums * kNMaxWaves;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) p[n * kNMaxWaves + wave] = s[n];
+    }
+    __syncthreads();
+    return p + wave / waves * waves;
+  }
   template <int N>
   __device__ __forceinline__ void operator()(float (&s)[N]) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] += __shfl_xor(s[n], o);
-    }
+    over_lanes(s);
     if (waves > 1) {
-      float* p = part + turn * 2 * kNMaxWaves;
-      turn ^= 1;
-      if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) p[n * kNMaxWaves + wave] = s[n];
-      }
-      __syncthreads();
+      const float* p = exchange(s);
 #pragma unroll
       for (int n = 0; n < N; ++n) s[n] = 0.f;
       for (int w = 0; w < waves; ++w) {
@@ -109,365 +190,403 @@ struct Row {
   F8 c[K];
 };
 
-// x -> its normalised values (the lanes past the row's end stay zero); returns
-// the reciprocal deviation
+// A row's mean (0 for the RMS norm) and reciprocal deviation. The variance is the mean of
+// the centred squares; over several waves each centres on its own mean, and the parts join
+// as
+//   sum (x - mean)^2 = sum_w M2_w + n_w (mean_w - mean)^2
+// so that one exchange is enough.
+struct Moments {
+  float mean, r;
+};
 template <int K>
-__device__ __forceinline__ float normalise(Row<K>& x, const bool (&in)[K], int kind, float inv_n, float eps,
+__device__ __forceinline__ Moments moments(const Row<K>& x, const bool (&in)[K], int kind, float inv_n, float eps,
                                            RowSum& sum) {
-  if (kind == ISPA_NORM_LAYER) {
-    float s[1] = {0.f};
+  float mean = 0.f, m2[1] = {0.f};
+  if (kind != ISPA_NORM_LAYER) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m2[0] = fmaf(x.c[k].v[i], x.c[k].v[i], m2[0]);
+    sum(m2);
+  } else {
+    float s[1] = {0.f}, n = 0.f, inv = inv_n;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] += x.c[k].v[i];
-    sum(s);
-    const float mean = s[0] * inv_n;
+    sum.over_lanes(s);
+    if (sum.waves > 1) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) n += 8.0f * __popcll(__ballot(in[k]));
+      inv = 1.0f / fmaxf(n, 1.0f);
+    }
+    mean = s[0] * inv;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x.c[k].v[i] = in[k] ? x.c[k].v[i] - mean : 0.f;
+      for (int i = 0; i < 8; ++i) {
+        const float v = in[k] ? x.c[k].v[i] - mean : 0.f;
+        m2[0] = fmaf(v, v, m2[0]);
+      }
+    sum.over_lanes(m2);
+    if (sum.waves > 1) {
+      const float mine[3] = {mean, m2[0], n};
+      const float* p = sum.exchange(mine);
+      mean = 0.f;
+      for (int w = 0; w < sum.waves; ++w) mean = fmaf(p[2 * kNMaxWaves + w], p[w], mean);
+      mean *= inv_n;
+      m2[0] = 0.f;
+      for (int w = 0; w < sum.waves; ++w) {
+        const float d = p[w] - mean;
+        m2[0] += fmaf(p[2 * kNMaxWaves + w] * d, d, p[kNMaxWaves + w]);
+      }
+    }
   }
-  float s[1] = {0.f};
+  return {mean, 1.0f / sqrtf(m2[0] * inv_n + eps)};
+}
+// A row's normalised values in place of it (the chunks outside stay zero); returns the
+// reciprocal deviation
+template <int K>
+__device__ __forceinline__ float normalise(Row<K>& x, const bool (&in)[K], int kind, float inv_n, float eps,
+                                           RowSum& sum) {
+  const Moments m = moments<K>(x, in, kind, inv_n, eps, sum);
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[0] += x.c[k].v[i] * x.c[k].v[i];
-  sum(s);
-  const float r = 1.0f / sqrtf(s[0] * inv_n + eps);
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x.c[k].v[i] *= r;
-  return r;
+    for (int i = 0; i < 8; ++i) x.c[k].v[i] = in[k] ? (x.c[k].v[i] - m.mean) * m.r : 0.f;
+  return m.r;
 }
 
-// This thread's place: `lanes` lanes or `waves` waves to a row, K chunks of 8
-// columns to a lane, chunk k at (k * lanes-of-the-row + lane).
+// This thread's place: a slot of `lanes` lanes or `waves` waves to a row, K chunks of 8
+// columns to a lane, chunk k at (k * threads of the slot + place in it).
 struct Place {
-  int lane, stride, row_in_block;
+  int lane, stride, slot;
 };
 __device__ __forceinline__ Place place_of(const NormArgs& a) {
   Place p;
-  const int t = threadIdx.x;
-  if (a.waves > 1) {
-    p.stride = a.waves * 64;
-    p.row_in_block = 0;
-    p.lane = t;
-  } else {
-    p.stride = a.lanes;
-    p.row_in_block = t / a.lanes;
-    p.lane = t % a.lanes;
-  }
+  p.stride = a.waves > 1 ? a.waves * 64 : a.lanes;
+  p.slot = threadIdx.x / p.stride;
+  p.lane = threadIdx.x - p.slot * p.stride;
   return p;
 }
+// The rows [first, end) of workgroup blockIdx.x: an equal run of the rows of its group.
+struct Run {
+  int64_t group;
+  int first, end;
+};
+__device__ __forceinline__ Run run_of(const NormArgs& a) {
+  Run r;
+  r.group = blockIdx.x / a.group_blocks;
+  const int part = (int)(blockIdx.x - r.group * a.group_blocks);
+  const int64_t g0 = r.group * a.group_rows;
+  const int64_t n = (g0 + a.group_rows < a.rows ? g0 + a.group_rows : a.rows) - g0;
+  r.first = (int)(g0 + n * part / a.group_blocks);
+  r.end = (int)(g0 + n * (part + 1) / a.group_blocks);
+  return r;
+}
 
-template <int K>
-__global__ void norm_residual_kernel(NormArgs a) {
-  __shared__ float part[2 * 2 * kNMaxWaves];
+// f of every value of the row and of a vector
+template <int K, class F>
+__device__ __forceinline__ void with_vector(const float* v, int64_t base, Row<K>& x, const bool (&in)[K],
+                                            const int (&col)[K], F f) {
+  if (!v) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (!in[k]) continue;
+    const F8 w = load8(v, true, base + col[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.c[k].v[i] = f(x.c[k].v[i], w.v[i]);
+  }
+}
+
+// Forward: a row to a slot. XF: the stream is fp32; Y: 0 no block output, 1 bf16, 2 fp32.
+template <int K, bool XF, int Y>
+__global__ __launch_bounds__(64 * kNMaxWaves) void norm_residual_kernel(NormArgs a) {
+  __shared__ float part[2 * kNMaxSums * kNMaxWaves];
   const Place pl = place_of(a);
-  const int64_t row = (int64_t)blockIdx.x * a.block_rows + pl.row_in_block;
-  const bool live = row < a.rows;  // (a workgroup of several waves to a row has one live row)
+  const Run run = run_of(a);
   RowSum sum{part, a.lanes, a.waves, (int)threadIdx.x >> 6, 0};
   const int chunks = a.cols >> 3;
   const float inv_n = 1.0f / (float)a.cols;
-  const int64_t base = row * a.cols, gbase = live ? row / a.group_rows * a.cols : 0;
+  const int row = run.first + pl.slot;
+  const int64_t base = (int64_t)row * a.cols, gbase = run.group * a.cols;
   bool in[K];
   int col[K];
   Row<K> x, z;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = pl.lane + k * pl.stride;
-    in[k] = live && c < chunks;
-    col[k] = c * 8;
-    x.c[k] = in[k] ? load8(a.x, a.x_f32, base + col[k]) : zero8();
-    if (a.y) z.c[k] = in[k] ? load8(a.y, a.y_f32, base + col[k]) : zero8();
-  }
-  if (a.y) {
-    if (a.post != ISPA_NORM_NONE) normalise<K>(z, in, a.post, inv_n, a.eps, sum);
+  {
+    Raw8<XF> rx[K];
+    Raw8<Y == 2> ry[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!in[k]) continue;
-      if (a.post_weight) {
-        const F8 w = load8(a.post_weight, true, col[k]);
+      const int c = pl.lane + k * pl.stride;
+      in[k] = c < chunks && pl.slot < a.block_rows && row < run.end;
+      col[k] = c * 8;
+      rx[k] = fetch8<XF>(a.x, base + col[k], in[k]);
+      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, base + col[k], in[k]);
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z.c[k].v[i] *= w.v[i];
-      }
-      if (a.gate) {
-        const F8 w = load8(a.gate, true, gbase + col[k]);
+    for (int k = 0; k < K; ++k) {
+      x.c[k] = unpack8<XF>(rx[k]);
+      if constexpr (Y > 0) z.c[k] = unpack8<Y == 2>(ry[k]);
+    }
+  }
+  if constexpr (Y > 0) {
+    if (a.post != ISPA_NORM_NONE) normalise<K>(z, in, a.post, inv_n, a.eps, sum);
+    with_vector<K>(a.post_weight, 0, z, in, col, [](float u, float w) { return u * w; });
+    with_vector<K>(a.gate, gbase, z, in, col, [](float u, float w) { return u * w; });
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z.c[k].v[i] *= w.v[i];
-      }
+    for (int k = 0; k < K; ++k) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x.c[k].v[i] = fmaf(a.alpha, z.c[k].v[i], x.c[k].v[i]);
-      store8(a.x_out, a.x_f32, base + col[k], x.c[k]);
+      if (in[k]) store8(a.x_out, XF, base + col[k], x.c[k]);
     }
   }
   if (a.norm == ISPA_NORM_NONE) return;
   normalise<K>(x, in, a.norm, inv_n, a.eps, sum);
+  with_vector<K>(a.weight, 0, x, in, col, [](float u, float w) { return u * w; });
+  with_vector<K>(a.bias, 0, x, in, col, [](float u, float w) { return u + w; });
+  with_vector<K>(a.scale, gbase, x, in, col, [](float u, float w) { return fmaf(u, w, u); });
+  with_vector<K>(a.shift, gbase, x, in, col, [](float u, float w) { return u + w; });
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    if (!in[k]) continue;
-    F8& u = x.c[k];
-    if (a.weight) {
-      const F8 w = load8(a.weight, true, col[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u.v[i] *= w.v[i];
-    }
-    if (a.bias) {
-      const F8 w = load8(a.bias, true, col[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u.v[i] += w.v[i];
-    }
-    if (a.scale) {
-      const F8 w = load8(a.scale, true, gbase + col[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u.v[i] *= 1.0f + w.v[i];
-    }
-    if (a.shift) {
-      const F8 w = load8(a.shift, true, gbase + col[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u.v[i] += w.v[i];
-    }
-    store8(a.h, a.h_f32, base + col[k], u);
-  }
+  for (int k = 0; k < K; ++k)
+    if (in[k]) store8(a.h, a.h_f32, base + col[k], x.c[k]);
 }
 
-// Backward: workgroup blockIdx.x takes an equal run of the rows of one group and
-// leaves its sums A, B, P of every column in part[blockIdx.x][3][cols]. The rows
-// of its `slots` (waves or parts of waves to a row each) add up in LDS, in order.
-template <int K>
-__global__ void norm_backward_kernel(NormArgs a) {
-  extern __shared__ float lds[];  // [2][2][kNMaxWaves], then [3][cols] where a workgroup has several slots
+// Backward: a workgroup takes its run of rows a row to a slot at a time, and leaves the
+// sums A, B, P of every column in part[blockIdx.x][3][cols]; the slots' sums meet in LDS
+// and add up in order.
+template <int K, bool XF, int Y, bool HF, int T>
+__global__ __launch_bounds__(T) void norm_backward_kernel(NormArgs a) {
+  extern __shared__ float lds[];  // [2][kNMaxSums][kNMaxWaves], then [block_rows][cols]
   const Place pl = place_of(a);
+  const Run run = run_of(a);
   RowSum sum{lds, a.lanes, a.waves, (int)threadIdx.x >> 6, 0};
   const int chunks = a.cols >> 3;
   const float inv_n = 1.0f / (float)a.cols;
-  const int64_t group = blockIdx.x / a.group_blocks;
-  const int part = (int)(blockIdx.x - group * a.group_blocks);
-  const int64_t g0 = group * a.group_rows;
-  const int64_t n = (g0 + a.group_rows < a.rows ? g0 + a.group_rows : a.rows) - g0;
-  const int64_t r0 = g0 + n * part / a.group_blocks, r1 = g0 + n * (part + 1) / a.group_blocks;
-  const int64_t gbase = group * a.cols;
+  const int64_t gbase = run.group * a.cols;
+  const bool has_norm = a.norm != ISPA_NORM_NONE;
+  bool in[K];
+  int col[K];
   Row<K> sa, sb, sp;
+  Raw8<XF> rx[K], rg[K];
+  Raw8<HF> rd[K];
+  Raw8<Y == 2> ry[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k) sa.c[k] = sb.c[k] = sp.c[k] = zero8();
-  // every slot makes the same number of turns (the reductions of a row of several
-  // waves meet at barriers)
-  for (int64_t rb = r0; rb < r1; rb += a.block_rows) {
-    const int64_t row = rb + pl.row_in_block;
-    const bool live = row < r1;
-    const int64_t base = row * a.cols;
-    bool in[K];
-    int col[K];
-    Row<K> x, d, y;
+  for (int k = 0; k < K; ++k) {
+    const int c = pl.lane + k * pl.stride;
+    in[k] = c < chunks && pl.slot < a.block_rows;
+    col[k] = c * 8;
+    sa.c[k] = sb.c[k] = sp.c[k] = zero8();
+  }
+  auto fetch = [&](int row) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = pl.lane + k * pl.stride;
-      in[k] = live && c < chunks;
-      col[k] = c * 8;
-      x.c[k] = in[k] && a.norm != ISPA_NORM_NONE ? load8(a.x, a.x_f32, base + col[k]) : zero8();
-      d.c[k] = in[k] && a.norm != ISPA_NORM_NONE ? load8(a.d_h, a.h_f32, base + col[k]) : zero8();
-      if (a.y) y.c[k] = in[k] ? load8(a.y, a.y_f32, base + col[k]) : zero8();
+      const bool here = in[k] && row < run.end;
+      const int64_t e = (int64_t)row * a.cols + col[k];
+      rx[k] = fetch8<XF>(a.x, e, here && has_norm);
+      rd[k] = fetch8<HF>(a.d_h, e, here && has_norm);
+      rg[k] = fetch8<XF>(a.d_x_in, e, here && a.d_x_in);
+      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, e, here);
     }
-    if (a.norm != ISPA_NORM_NONE) {
-      const float r = normalise<K>(x, in, a.norm, inv_n, a.eps, sum);
-      float s[2] = {0.f, 0.f};
+  };
+  fetch(run.first + pl.slot);
+  for (int r0 = run.first; r0 < run.end; r0 += a.block_rows) {
+    const int row = r0 + pl.slot;
+    const int64_t base = (int64_t)row * a.cols;
+    Row<K> x, d, y, g;
+    float s[2] = {0.f, 0.f};
+    bool here[K];  // (what is outside stays zero and adds nothing to the sums)
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (!in[k]) continue;
+    for (int k = 0; k < K; ++k) {
+      here[k] = in[k] && row < run.end;
+      x.c[k] = unpack8<XF>(rx[k]);
+      d.c[k] = unpack8<HF>(rd[k]);
+      g.c[k] = unpack8<XF>(rg[k]);
+      if constexpr (Y > 0) y.c[k] = unpack8<Y == 2>(ry[k]);
+    }
+    fetch(row + a.block_rows);
+    if (has_norm) {
+      const float r = normalise<K>(x, here, a.norm, inv_n, a.eps, sum);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sa.c[k].v[i] += d.c[k].v[i];
           sb.c[k].v[i] = fmaf(d.c[k].v[i], x.c[k].v[i], sb.c[k].v[i]);
         }
-        if (a.scale) {
-          const F8 w = load8(a.scale, true, gbase + col[k]);
+      with_vector<K>(a.scale, gbase, d, here, col, [](float u, float w) { return u * (1.0f + w); });
+      with_vector<K>(a.weight, 0, d, here, col, [](float u, float w) { return u * w; });
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d.c[k].v[i] *= 1.0f + w.v[i];
-        }
-        if (a.weight) {
-          const F8 w = load8(a.weight, true, col[k]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) d.c[k].v[i] *= w.v[i];
-        }
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           s[0] += d.c[k].v[i];
           s[1] = fmaf(d.c[k].v[i], x.c[k].v[i], s[1]);
         }
-      }
       sum(s);
       const float m1 = a.norm == ISPA_NORM_LAYER ? s[0] * inv_n : 0.f, m2 = s[1] * inv_n;
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d.c[k].v[i] = r * (d.c[k].v[i] - m1 - x.c[k].v[i] * m2);
+        for (int i = 0; i < 8; ++i)
+          g.c[k].v[i] = here[k] ? fmaf(r, d.c[k].v[i] - m1 - x.c[k].v[i] * m2, g.c[k].v[i]) : 0.f;
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (!in[k]) continue;
-      if (a.d_x_in) {
-        const F8 w = load8(a.d_x_in, a.x_f32, base + col[k]);
+    for (int k = 0; k < K; ++k)
+      if (here[k]) store8(a.d_x, XF, base + col[k], g.c[k]);
+    if constexpr (Y > 0) {
+      float ry1 = 1.f;
+      if (a.post != ISPA_NORM_NONE) ry1 = normalise<K>(y, here, a.post, inv_n, a.eps, sum);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d.c[k].v[i] += w.v[i];
-      }
-      store8(a.d_x, a.x_f32, base + col[k], d.c[k]);
-    }
-    if (a.y) {
-      float ry = 1.f;
-      if (a.post != ISPA_NORM_NONE) ry = normalise<K>(y, in, a.post, inv_n, a.eps, sum);
-      float s[2] = {0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (!in[k]) continue;
+      for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          sp.c[k].v[i] = fmaf(d.c[k].v[i], y.c[k].v[i], sp.c[k].v[i]);
-          d.c[k].v[i] *= a.alpha;
+          sp.c[k].v[i] = fmaf(g.c[k].v[i], y.c[k].v[i], sp.c[k].v[i]);
+          g.c[k].v[i] *= a.alpha;
         }
-        if (a.gate) {
-          const F8 w = load8(a.gate, true, gbase + col[k]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) d.c[k].v[i] *= w.v[i];
-        }
-        if (a.post_weight) {
-          const F8 w = load8(a.post_weight, true, col[k]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) d.c[k].v[i] *= w.v[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s[0] += d.c[k].v[i];
-          s[1] = fmaf(d.c[k].v[i], y.c[k].v[i], s[1]);
-        }
-      }
+      with_vector<K>(a.gate, gbase, g, here, col, [](float u, float w) { return u * w; });
+      with_vector<K>(a.post_weight, 0, g, here, col, [](float u, float w) { return u * w; });
       float m1 = 0.f, m2 = 0.f;
       if (a.post != ISPA_NORM_NONE) {
+        s[0] = s[1] = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            s[0] += g.c[k].v[i];
+            s[1] = fmaf(g.c[k].v[i], y.c[k].v[i], s[1]);
+          }
         sum(s);
         m1 = a.post == ISPA_NORM_LAYER ? s[0] * inv_n : 0.f;
         m2 = s[1] * inv_n;
       }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        if (!in[k]) continue;
+        if (!here[k]) continue;
         F8 o;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o.v[i] = ry * (d.c[k].v[i] - m1 - y.c[k].v[i] * m2);
-        store8(a.d_y, a.y_f32, base + col[k], o);
+        for (int i = 0; i < 8; ++i) o.v[i] = ry1 * (g.c[k].v[i] - m1 - y.c[k].v[i] * m2);
+        store8(a.d_y, Y == 2, base + col[k], o);
       }
     }
   }
   if (!a.part) return;
-  // this workgroup's sums: slot after slot adds its own in LDS
   float* out = a.part + (int64_t)blockIdx.x * 3 * a.cols;
-  float* acc = lds + 2 * 2 * kNMaxWaves;
-  for (int s = 0; s < a.block_rows; ++s) {
-    if (pl.row_in_block == s) {
+  float* slots = lds + 2 * kNMaxSums * kNMaxWaves;
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int c = pl.lane + k * pl.stride;
-        if (c >= chunks) continue;
+  for (int v = 0; v < 3; ++v) {
+    const Row<K>& m = v == 0 ? sa : v == 1 ? sb : sp;
+    if (a.block_rows == 1) {
 #pragma unroll
-        for (int v = 0; v < 3; ++v) {
-          F8 w = v == 0 ? sa.c[k] : v == 1 ? sb.c[k] : sp.c[k];
-          if (s > 0) {
-            const F8 o = load8(acc, true, v * a.cols + c * 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w.v[i] += o.v[i];
-          }
-          if (s + 1 < a.block_rows)
-            store8(acc, true, v * a.cols + c * 8, w);
-          else
-            store8(out, true, v * a.cols + c * 8, w);
-        }
-      }
+      for (int k = 0; k < K; ++k)
+        if (in[k]) store8(out, true, (int64_t)v * a.cols + col[k], m.c[k]);
+      continue;
     }
-    if (s + 1 < a.block_rows) __syncthreads();
+    if (v > 0) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (in[k]) store8(slots, true, (int64_t)pl.slot * a.cols + col[k], m.c[k]);
+    __syncthreads();
+    for (int c = threadIdx.x * 4; c < a.cols; c += blockDim.x * 4) {
+      f32x4 t = *(const f32x4*)(slots + c);
+      for (int s = 1; s < a.block_rows; ++s) t += *(const f32x4*)(slots + s * a.cols + c);
+      *(f32x4*)(out + (int64_t)v * a.cols + c) = t;
+    }
   }
 }
 
-// The gradients of the vectors from part[n_groups * group_blocks][3][cols]: 32
-// columns to a workgroup; its 16 slices of threads take a group's parts in turn
-// and add up in LDS in order. With many groups (at least a slice's worth) every
-// slice takes whole groups of its own instead, and no barrier stands between them.
-constexpr int kFCols = 32, kFSlices = 16;
+// The gradients of the vectors from part[n_groups * group_blocks][3][cols]. A workgroup
+// takes 32 columns of a group (several groups where a group has few parts), its 16 slices
+// of threads the group's parts in turn, added up in LDS in order; the last row of
+// workgroups adds all parts for the vectors that the groups share.
+constexpr int kFCols = 32, kFSlices = 16, kFAhead = 4;
 
-__global__ __launch_bounds__(kFCols* kFSlices) void norm_backward_vectors_kernel(NormArgs a) {
+__global__ __launch_bounds__(kFCols* kFSlices) void norm_backward_vectors_kernel(NormArgs a, int spg) {
   __shared__ float s[kFSlices][3][kFCols];
   const int cx = threadIdx.x % kFCols, sl = threadIdx.x / kFCols;
-  const int c = blockIdx.x * kFCols + cx;
+  const int col_blocks = (a.cols + kFCols - 1) / kFCols;
+  const int by = blockIdx.x / col_blocks;
+  const int c = (blockIdx.x - by * col_blocks) * kFCols + cx;
   const bool in = c < a.cols;
   const int cc = in ? c : 0;
-  const float w = a.weight ? a.weight[cc] : 1.f, b = a.bias ? a.bias[cc] : 0.f;
-  const float pw = a.post_weight ? a.post_weight[cc] : 1.f;
-  const bool own_group = a.n_groups >= kFSlices;
-  float dw = 0.f, db = 0.f, dpw = 0.f;
-  for (int64_t g0 = 0; g0 < a.n_groups; g0 += own_group ? kFSlices : 1) {
-    const int64_t g = own_group ? g0 + sl : g0;
-    float v[3] = {0.f, 0.f, 0.f};
-    if (g < a.n_groups) {
-      const float* p = a.part + (g * a.group_blocks) * 3 * a.cols + cc;
-      for (int j = own_group ? 0 : sl; j < a.group_blocks; j += own_group ? 1 : kFSlices)
+  const bool all = a.shared_vectors && (by + 1) * col_blocks == (int)gridDim.x;
+  const int slices = all ? kFSlices : spg;  // slices that share a group
+  const int64_t g = all ? 0 : (int64_t)by * (kFSlices / spg) + sl / spg;
+  const int64_t n = all ? a.n_groups * a.group_blocks : g < a.n_groups ? a.group_blocks : 0;
+  const float* p = a.part + g * a.group_blocks * 3 * a.cols + cc;
+  float v[3] = {0.f, 0.f, 0.f};
+  for (int64_t j0 = sl % slices; j0 < n; j0 += slices * kFAhead) {
+    float u[kFAhead][3], sc[kFAhead], gt[kFAhead];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) v[i] += p[((int64_t)j * 3 + i) * a.cols];
-    }
-    if (!own_group) {
+    for (int q = 0; q < kFAhead; ++q) {
+      const int64_t j = j0 + q * slices;
+      const bool here = j < n;
 #pragma unroll
-      for (int i = 0; i < 3; ++i) s[sl][i][cx] = v[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        v[i] = 0.f;
-        for (int j = 0; j < kFSlices; ++j) v[i] += s[j][i][cx];
+      for (int i = 0; i < 3; ++i) u[q][i] = here ? p[(j * 3 + i) * a.cols] : 0.f;
+      sc[q] = gt[q] = 1.f;
+      if (all && here) {
+        const int64_t o = j / a.group_blocks * a.cols + cc;
+        if (a.scale) sc[q] = 1.0f + a.scale[o];
+        if (a.gate) gt[q] = a.gate[o];
       }
-      __syncthreads();
     }
-    if (in && g < a.n_groups && (own_group || sl == 0)) {
-      const int64_t o = g * a.cols + c;
-      const float sc = a.scale ? 1.0f + a.scale[o] : 1.f, gt = a.gate ? a.gate[o] : 1.f;
-      if (a.d_shift) a.d_shift[o] = v[0];
-      if (a.d_scale) a.d_scale[o] = w * v[1] + b * v[0];
-      if (a.d_gate) a.d_gate[o] = a.alpha * pw * v[2];
-      dw += sc * v[1];
-      db += sc * v[0];
-      dpw += a.alpha * gt * v[2];
+#pragma unroll
+    for (int q = 0; q < kFAhead; ++q) {
+      v[0] = fmaf(sc[q], u[q][0], v[0]);
+      v[1] = fmaf(sc[q], u[q][1], v[1]);
+      v[2] = fmaf(gt[q], u[q][2], v[2]);
     }
   }
-  if (own_group) {
-    s[sl][0][cx] = dw;
-    s[sl][1][cx] = db;
-    s[sl][2][cx] = dpw;
+  if (slices > 1) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s[sl][i][cx] = v[i];
     __syncthreads();
-    dw = db = dpw = 0.f;
-    for (int j = 0; j < kFSlices; ++j) {
-      dw += s[j][0][cx];
-      db += s[j][1][cx];
-      dpw += s[j][2][cx];
+    if (sl % slices == 0) {
+      for (int j = 1; j < slices; ++j)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) v[i] += s[sl + j][i][cx];
     }
   }
-  if (in && sl == 0) {
-    if (a.d_weight) a.d_weight[c] = dw;
-    if (a.d_bias) a.d_bias[c] = db;
-    if (a.d_post_weight) a.d_post_weight[c] = dpw;
+  if (!in || sl % slices != 0) return;
+  if (all) {
+    if (a.d_weight) a.d_weight[c] = v[1];
+    if (a.d_bias) a.d_bias[c] = v[0];
+    if (a.d_post_weight) a.d_post_weight[c] = a.alpha * v[2];
+  } else if (g < a.n_groups) {
+    const int64_t o = g * a.cols + c;
+    if (a.d_shift) a.d_shift[o] = v[0];
+    if (a.d_scale) a.d_scale[o] = (a.weight ? a.weight[c] : 1.f) * v[1] + (a.bias ? a.bias[c] : 0.f) * v[0];
+    if (a.d_gate) a.d_gate[o] = a.alpha * (a.post_weight ? a.post_weight[c] : 1.f) * v[2];
   }
 }
 
-// Lanes or waves to a row: rows of up to 64 chunks of 8 columns share a wave (a
-// power of two of lanes each); wider ones take up to k_max chunks a lane.
-int norm_shape(NormArgs* a, int k_max) {
+// Lanes or waves to a row, and the chunks of 8 columns of a lane (returned): rows of up to
+// 64 chunks share a wave (8 to 64 lanes each), wider ones have as many waves as give a
+// lane at most `most` chunks, up to 16.
+int norm_shape(NormArgs* a, int most) {
   const int chunks = a->cols / 8;
   a->waves = 1;
   a->lanes = 64;
-  int k = 1;
   if (chunks <= 64) {
     a->lanes = 8;
     while (a->lanes < chunks) a->lanes *= 2;
-  } else {
-    k = k_max;
-    while (k > 1 && (chunks + 63) / 64 <= k - 1) --k;
-    a->waves = (chunks + 64 * k - 1) / (64 * k);
+    return 1;
   }
-  return k;
+  if (chunks > 64 * kNMaxWaves * most) most = (chunks + 64 * kNMaxWaves - 1) / (64 * kNMaxWaves);
+  a->waves = (chunks + 64 * most - 1) / (64 * most);
+  return (chunks + 64 * a->waves - 1) / (64 * a->waves);
+}
+// Threads of a workgroup
+int norm_threads(const NormArgs& a) {
+  const int n = a.block_rows * (a.waves > 1 ? a.waves * 64 : a.lanes);
+  return (n + 63) / 64 * 64;
+}
+// Workgroups to a group of rows: about `target` in all, each with the same turns.
+int norm_blocks(int64_t rows, int64_t group_rows, int block_rows, int64_t target) {
+  const int64_t groups = (rows + group_rows - 1) / group_rows;
+  const int64_t turns = (group_rows + block_rows - 1) / block_rows;  // of a group
+  const int64_t each = (groups * turns + target - 1) / target;
+  return (int)((turns + each - 1) / each);
 }
 
 }  // namespace
@@ -475,43 +594,80 @@ int norm_shape(NormArgs* a, int k_max) {
 int norm_group_blocks(int64_t rows, int cols, int64_t group_rows, int* block_rows) {
   NormArgs a;
   a.cols = cols;
-  norm_shape(&a, 2);
-  *block_rows = a.waves > 1 ? 1 : 256 / a.lanes;
-  const int64_t groups = (rows + group_rows - 1) / group_rows;
-  int64_t n = (512 + groups - 1) / groups;  // about two workgroups to a compute unit
-  const int64_t most = (group_rows + *block_rows - 1) / *block_rows;
-  if (n > most) n = most;
-  return (int)(n < 1 ? 1 : n);
+  norm_shape(&a, 1);
+  // twelve waves fill a compute unit's registers; a workgroup's sums are written once
+  // (those of three vectors are as long as a few rows)
+  const int slots = a.waves > 1 ? 12 / a.waves : 512 / a.lanes;
+  *block_rows = slots < 1 ? 1 : slots;
+  return norm_blocks(rows, group_rows, *block_rows, 256);
 }
 
-hipError_t launch_norm_residual(NormArgs a, hipStream_t stream) {
-  int k = norm_shape(&a, 4);
-  a.block_rows = a.waves > 1 ? 1 : 256 / a.lanes;
-  const int threads = a.waves > 1 ? a.waves * 64 : 256;
-  const dim3 grid((unsigned)((a.rows + a.block_rows - 1) / a.block_rows));
-  switch (k) {
-    case 1: norm_residual_kernel<1><<<grid, threads, 0, stream>>>(a); break;
-    case 2: norm_residual_kernel<2><<<grid, threads, 0, stream>>>(a); break;
-    case 3: norm_residual_kernel<3><<<grid, threads, 0, stream>>>(a); break;
-    default: norm_residual_kernel<4><<<grid, threads, 0, stream>>>(a); break;
+namespace {
+template <int K>
+void forward_k(const NormArgs& a, unsigned grid, int threads, hipStream_t stream) {
+#define ISPA_NORM(XF, Y)                                    \
+  if ((a.x_f32 != 0) == XF && (a.y ? 1 + a.y_f32 : 0) == Y) \
+    norm_residual_kernel<K, XF, Y><<<grid, threads, 0, stream>>>(a);
+  ISPA_NORM(false, 0) ISPA_NORM(false, 1) ISPA_NORM(false, 2) ISPA_NORM(true, 0) ISPA_NORM(true, 1) ISPA_NORM(true, 2)
+#undef ISPA_NORM
+}
+template <int K, int T>
+void backward_k(const NormArgs& a, unsigned grid, int threads, size_t lds, hipStream_t stream) {
+#define ISPA_NORM(XF, Y)                                    \
+  if ((a.x_f32 != 0) == XF && (a.y ? 1 + a.y_f32 : 0) == Y) { \
+    if (a.h_f32)                                            \
+      norm_backward_kernel<K, XF, Y, true, T><<<grid, threads, lds, stream>>>(a);  \
+    else                                                    \
+      norm_backward_kernel<K, XF, Y, false, T><<<grid, threads, lds, stream>>>(a); \
   }
+  ISPA_NORM(false, 0) ISPA_NORM(false, 1) ISPA_NORM(false, 2) ISPA_NORM(true, 0) ISPA_NORM(true, 1) ISPA_NORM(true, 2)
+#undef ISPA_NORM
+}
+}  // namespace
+
+hipError_t launch_norm_residual(NormArgs a, hipStream_t stream) {
+  // A row of up to 192 chunks stays in one wave, whose reductions need no exchange (4680
+  // rows of 1536: 17.0 us, bf16 12.7; with two waves to a row 19.0 and 13.9). A wider one
+  // has two chunks to a lane: three take as long in many rows and longer in few (1000 rows
+  // of 8192 bf16: 17.4 against 13.9), one is slower with a norm of the block output, whose
+  // exchanges grow with the waves (4680 of 5120 bf16: 65 against 57).
+  const int k = norm_shape(&a, a.cols <= 8 * 64 * 3 ? 3 : 2);
+  a.block_rows = a.waves > 1 ? (a.waves >= 4 ? 1 : 4 / a.waves) : 256 / a.lanes;
+  a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
+  a.group_blocks = (int)((a.group_rows + a.block_rows - 1) / a.block_rows);
+  const int threads = norm_threads(a);
+  const unsigned grid = (unsigned)(a.n_groups * a.group_blocks);
+  if (k == 1)
+    forward_k<1>(a, grid, threads, stream);
+  else if (k == 2)
+    forward_k<2>(a, grid, threads, stream);
+  else
+    forward_k<3>(a, grid, threads, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream) {
-  const int k = norm_shape(&a, 2);
+  const int k = norm_shape(&a, 1);
   a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
   a.group_blocks = norm_group_blocks(a.rows, a.cols, a.group_rows, &a.block_rows);
-  const int threads = a.waves > 1 ? a.waves * 64 : 256;
-  const size_t lds = (2 * 2 * kNMaxWaves + (a.block_rows > 1 ? 3 * (size_t)a.cols : 0)) * sizeof(float);
-  const dim3 grid((unsigned)(a.n_groups * a.group_blocks));
-  if (k == 1)
-    norm_backward_kernel<1><<<grid, threads, lds, stream>>>(a);
+  const int threads = norm_threads(a);
+  const size_t lds =
+      (2 * kNMaxSums * kNMaxWaves + (a.block_rows > 1 ? (size_t)a.block_rows * a.cols : 0)) * sizeof(float);
+  const unsigned grid = (unsigned)(a.n_groups * a.group_blocks);
+  if (k == 1 && threads <= 768)
+    backward_k<1, 768>(a, grid, threads, lds, stream);
+  else if (k == 1)
+    backward_k<1, 1024>(a, grid, threads, lds, stream);
   else
-    norm_backward_kernel<2><<<grid, threads, lds, stream>>>(a);
+    backward_k<2, 1024>(a, grid, threads, lds, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
-  norm_backward_vectors_kernel<<<(a.cols + kFCols - 1) / kFCols, kFCols * kFSlices, 0, stream>>>(a);
+  a.group_vectors = a.d_gate || a.d_scale || a.d_shift;
+  a.shared_vectors = a.d_weight || a.d_bias || a.d_post_weight;
+  int spg = 1;
+  while (spg < kFSlices && spg < a.group_blocks) spg *= 2;
+  const int64_t y = (a.group_vectors ? (a.n_groups + kFSlices / spg - 1) / (kFSlices / spg) : 0) + a.shared_vectors;
+  norm_backward_vectors_kernel<<<(unsigned)(y * ((a.cols + kFCols - 1) / kFCols)), kFCols * kFSlices, 0, stream>>>(a, spg);
   return hipGetLastError();
 }
 

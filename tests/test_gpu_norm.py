@@ -238,6 +238,24 @@ def test_backward(case, direct):
         check(got[k], v, tol, k)
 
 
+@pytest.mark.parametrize("cols", [64, 1024, 2056])
+def test_backward_without_eps(cols):
+    # eps 0 is allowed where no row is constant; slots without a row must not reach the sums
+    c, t, _ = make(5, cols, norm="rms", post="layer", post_weight=True, weight=True, gate=True, scale=True, group=2)
+    c["eps"] = 0.0
+    gpu = to_gpu(t)
+    d_h = torch.randn(5, cols, generator=torch.Generator().manual_seed(cols)).to(BF16)
+    x_gpu = gpu.pop("x")
+    got = ispa.norm_residual_backward(d_h.to(DEV), x_gpu, **gpu, **c)
+    w = wide(t, grad=True)
+    want = torch.autograd.grad((head(c, w, w["x"]) * d_h.double()).sum(), [w["weight"], w["scale"], w["x"]])
+    branch = stream(c, {**w, "x": torch.zeros(5, cols, dtype=torch.float64)})
+    gate, pw = torch.autograd.grad((branch * want[2]).sum(), [w["gate"], w["post_weight"]])
+    # sums of at most five terms of order ten: 2^-18 of their magnitudes
+    for name, v in (("weight", want[0]), ("scale", want[1]), ("gate", gate), ("post_weight", pw)):
+        check(got[name], v.detach(), 2.0 ** -12 * (1 + v.detach().abs()), name)
+
+
 def test_gradient_against_differences():
     # the backward pass against central differences of the forward pass in fp32: a step of
     # 2^-6 leaves a relative second-order error below 2^-8 and a rounding of 2^-18 / 2^-6
