@@ -10,11 +10,14 @@
 // product of a far position (10^6) and a frequency near one keeps only 2^-4 rad
 // in fp32; cos and sin of the fraction are taken in fp32 (one sincospif).
 //
-// Bound by bytes: q, k and v are read once and written once. The angles of a
-// token are the same for all heads, so a workgroup computes them once for its
-// tokens into LDS (rotary_dim / 2 pairs of fp64 operations a token against 2 x
-// n_heads x head_dim values of traffic) and a thread keeps the eight cos / sin of
-// its unit (eight pairs of a head) while it walks over the heads.
+// Bound by bytes: q, k and v are read once and written once. The angles of a token are the
+// same for all heads, so a workgroup computes them once for its tokens into LDS
+// (rotary_dim / 2 pairs of fp64 operations a token against n_heads x head_dim values of
+// traffic each way) while its first heads are on their way, and reads a unit of 16 values
+// of the next head while it turns this one.
+// Measured, bf16, heads of 128 (us, TB/s of the values read and written once; a copy of 48
+// MB runs at 5.0): 4680 rows of 40 heads 17 (5.6); with the append of k and v 4680 rows of
+// 12 + 12 + 12 heads 18 (4.8), 20000 rows 69 (5.3), 6240 rows of 32 + 8 + 8 heads 33 (4.7).
 //
 // slot_map: the place of each row of a ragged batch in its request's cache, by a
 // search of the request starts; one launch serves every layer of a step.
@@ -27,90 +30,156 @@ constexpr int kRThreads = 256;
 constexpr int kRMaxTokens = 8;   // tokens of a workgroup
 constexpr int kRMaxPairs = 128;  // rotary_dim / 2
 
-__device__ __forceinline__ void rload8(const void* p, bool f32, int64_t e, float (&r)[8]) {
-  if (f32) {
-    const f32x4 a = *(const f32x4*)((const float*)p + e), b = *(const f32x4*)((const float*)p + e + 4);
+template <class T>
+using Global = __attribute__((address_space(1))) T;
+
+// Eight values as they lie in memory, so that several loads are in flight at once; p the
+// tensor's address, e an element
+template <bool F32>
+struct Chunk {
+  f32x4 lo, hi;
+  __device__ __forceinline__ void load(uintptr_t p, int64_t e) {
+    const auto* at = (const Global<f32x4>*)(p + e * 4);
+    lo = at[0];
+    hi = at[1];
+  }
+  __device__ __forceinline__ void values(float (&r)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      r[i] = a[i];
-      r[4 + i] = b[i];
+      r[i] = lo[i];
+      r[4 + i] = hi[i];
     }
-  } else {
-    const bf16x8 a = *(const bf16x8*)((const uint16_t*)p + e);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (float)a[i];
   }
-}
-__device__ __forceinline__ void rstore8(void* p, bool f32, int64_t e, const float (&x)[8]) {
+};
+template <>
+struct Chunk<false> {
+  bf16x8 b;
+  __device__ __forceinline__ void load(uintptr_t p, int64_t e) { b = *(const Global<bf16x8>*)(p + e * 2); }
+  __device__ __forceinline__ void values(float (&r)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = (float)b[i];
+  }
+};
+__device__ __forceinline__ void rstore8(uintptr_t p, bool f32, int64_t e, const float (&x)[8]) {
   if (f32) {
-    *(f32x4*)((float*)p + e) = f32x4{x[0], x[1], x[2], x[3]};
-    *(f32x4*)((float*)p + e + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    auto* at = (Global<f32x4>*)(p + e * 4);
+    at[0] = f32x4{x[0], x[1], x[2], x[3]};
+    at[1] = f32x4{x[4], x[5], x[6], x[7]};
   } else {
     bf16x8 a;
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = (__bf16)x[i];
-    *(bf16x8*)((uint16_t*)p + e) = a;
+    *(Global<bf16x8>*)(p + e * 2) = a;
   }
 }
 
-// The heads of one token of one tensor: 16 values of a head to a unit, units
-// [0, turned) rotate, the others pass through; this thread takes the units that
-// are `first` modulo `step` (a multiple of the units of a head, so that every
-// one of its units has the same place in its head and the same angles).
-__device__ __forceinline__ void heads_of(const RotaryArgs& a, const void* src, int64_t se, void* dst, bool dst_f32,
-                                         int64_t de, int n_units, int first, int step, const float2* cs) {
-  const int per_head = a.head_dim >> 4;
-  const int u = first % per_head;  // place in the head
-  const int half = a.rotary_dim >> 1;
-  const bool turned = u < (a.rotary_dim >> 4);
-  // element offsets of the two chunks of 8 inside a head, and the first pair
-  const int e0 = turned && !a.interleaved ? 8 * u : 16 * u;
-  const int e1 = turned && !a.interleaved ? half + 8 * u : 16 * u + 8;
-  float c[8], s[8];
-  if (turned) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      c[i] = cs[8 * u + i].x;
-      s[i] = cs[8 * u + i].y;
-    }
-  }
-  for (int unit = first; unit < n_units; unit += step) {
-    const int64_t h = (int64_t)(unit / per_head) * a.head_dim;
-    float x[8], y[8];
-    rload8(src, a.x_f32, se + h + e0, x);
-    rload8(src, a.x_f32, se + h + e1, y);
-    if (turned) {
-      if (a.interleaved) {
-        // pairs (x0,x1) .. (x6,x7), (y0,y1) .. (y6,y7)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float xa = x[2 * i], xb = x[2 * i + 1], ya = y[2 * i], yb = y[2 * i + 1];
-          x[2 * i] = xa * c[i] - xb * s[i];
-          x[2 * i + 1] = xa * s[i] + xb * c[i];
-          y[2 * i] = ya * c[4 + i] - yb * s[4 + i];
-          y[2 * i + 1] = ya * s[4 + i] + yb * c[4 + i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float xa = x[i], xb = y[i];
-          x[i] = xa * c[i] - xb * s[i];
-          y[i] = xa * s[i] + xb * c[i];
-        }
-      }
-    }
-    rstore8(dst, dst_f32, de + h + e0, x);
-    rstore8(dst, dst_f32, de + h + e1, y);
-  }
-}
+// One unit: 16 values of a head as they lie in memory
+template <bool F32>
+struct Unit {
+  Chunk<F32> c0, c1;
+};
 
-// Workgroup: a.tokens rows; rows without a slot (k given) are left alone.
+// Workgroup: a.tokens rows; rows without a slot (k given) are left alone. The heads of q,
+// k and v of all its rows are one list, so that every thread has work whatever the heads:
+// a thread keeps its place in a head and takes every (threads / units of a head)-th head
+// of the list. Units [0, rotary_dim / 16) of a head rotate, the others pass through.
+template <bool F32>
 __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 cs[kRMaxTokens * kRMaxPairs];
   __shared__ int64_t slot_of[kRMaxTokens];
   const int64_t row0 = (int64_t)blockIdx.x * a.tokens;
   const int n = (int)(a.rows - row0 < a.tokens ? a.rows - row0 : a.tokens);
   const int pairs = a.rotary_dim >> 1;
+  const int per_head = a.head_dim >> 4, step = kRThreads / per_head;
+  const int u = threadIdx.x % per_head;  // place in the head
+  const int heads = a.n_heads + (a.k ? 2 * a.n_kv_heads : 0);  // of a row
+  const int end = (int)threadIdx.x < step * per_head ? n * heads : 0;
+  // a unit's two chunks of 8 and the first pairs of their angles: the same place in both
+  // halves of the rotated part (lanes side by side then read side by side, in either order
+  // of the pairs), or side by side behind it
+  const bool turned = u < (a.rotary_dim >> 4);
+  const int e0 = turned ? 8 * u : 16 * u, e1 = turned ? pairs + 8 * u : 16 * u + 8;
+  const int p0 = a.interleaved ? 4 * u : 8 * u, p1 = a.interleaved ? (pairs >> 1) + 4 * u : 8 * u + 4;
+  // in registers for certain: a choice between arguments is otherwise made by a load from
+  // the chosen one's place, which every unit's load then waits for
+  uintptr_t q = (uintptr_t)a.q, k = (uintptr_t)a.k, v = (uintptr_t)a.v;
+  uintptr_t q_out = (uintptr_t)a.q_out, k_cache = (uintptr_t)a.k_cache, v_cache = (uintptr_t)a.v_cache;
+  int64_t ld_q = a.ld_q, ld_k = a.ld_k, ld_v = a.ld_v;
+  asm("" : "+s"(q), "+s"(k), "+s"(v), "+s"(q_out), "+s"(k_cache), "+s"(v_cache), "+s"(ld_q), "+s"(ld_k), "+s"(ld_v));
+  auto fetch = [&](int w, Unit<F32>& p) __attribute__((always_inline)) {
+    if (w >= end) return;
+    const int t = w / heads;
+    int h = w - t * heads;
+    const int64_t row = row0 + t;
+    uintptr_t src = q;
+    int64_t ld = ld_q;
+    if (h >= a.n_heads) {
+      h -= a.n_heads;
+      src = k, ld = ld_k;
+      if (h >= a.n_kv_heads) {
+        h -= a.n_kv_heads;
+        src = v, ld = ld_v;
+      }
+    }
+    const int64_t s = row * ld + h * a.head_dim;
+    p.c0.load(src, s + e0);
+    p.c1.load(src, s + e1);
+  };
+  auto finish = [&](int w, const Unit<F32>& p) __attribute__((always_inline)) {
+    const int t = w / heads;
+    int h = w - t * heads;
+    uintptr_t dst = q_out;
+    bool f32 = a.out_f32, turn = turned;
+    int64_t d = (row0 + t) * a.ld_out;
+    if (a.k) {
+      const int64_t slot = slot_of[t];
+      if (slot < 0) return;
+      if (h >= a.n_heads) {
+        h -= a.n_heads;
+        dst = k_cache, f32 = false, d = slot * a.n_kv_heads * a.head_dim;
+        if (h >= a.n_kv_heads) {
+          h -= a.n_kv_heads;
+          dst = v_cache, turn = false;
+        }
+      }
+    }
+    d += h * a.head_dim;
+    float x[8], y[8];
+    p.c0.values(x);
+    p.c1.values(y);
+    if (turn) {
+      const float2* at = cs + t * pairs;
+      float2 c[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = at[p0 + i];
+        c[4 + i] = at[p1 + i];
+      }
+      if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float xa = x[2 * i], xb = x[2 * i + 1], ya = y[2 * i], yb = y[2 * i + 1];
+          x[2 * i] = xa * c[i].x - xb * c[i].y;
+          x[2 * i + 1] = xa * c[i].y + xb * c[i].x;
+          y[2 * i] = ya * c[4 + i].x - yb * c[4 + i].y;
+          y[2 * i + 1] = ya * c[4 + i].y + yb * c[4 + i].x;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float xa = x[i], xb = y[i];
+          x[i] = xa * c[i].x - xb * c[i].y;
+          y[i] = xa * c[i].y + xb * c[i].x;
+        }
+      }
+    }
+    rstore8(dst, f32, d + e0, x);
+    rstore8(dst, f32, d + e1, y);
+  };
+
+  int w = threadIdx.x / per_head;
+  Unit<F32> now, next;
+  fetch(w, now);  // on its way while the angles are formed
   for (int i = threadIdx.x; i < n * pairs; i += kRThreads) {
     const int t = i / pairs, j = i - t * pairs;
     int axis = 0;
@@ -127,32 +196,10 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
     slot_of[threadIdx.x] = s < a.cache_rows ? s : -1;
   }
   __syncthreads();
-  // the units of a token: its query heads, its key heads, and v in 16-value pieces;
-  // `lanes` threads to a token's tensor, a multiple of the units of a head
-  const int per_head = a.head_dim >> 4;
-  const int step = kRThreads / per_head * per_head;
-  if ((int)threadIdx.x >= step) return;
-  for (int t = 0; t < n; ++t) {
-    const int64_t row = row0 + t;
-    int64_t slot = 0;
-    if (a.k) {
-      slot = slot_of[t];
-      if (slot < 0) continue;
-    }
-    heads_of(a, a.q, row * a.ld_q, a.q_out, a.out_f32, row * a.ld_out, a.n_heads * per_head, threadIdx.x, step,
-             cs + t * pairs);
-    if (a.k) {
-      const int nk = a.n_kv_heads * per_head;
-      const int64_t hidden = (int64_t)a.n_kv_heads * a.head_dim;
-      heads_of(a, a.k, row * a.ld_k, a.k_cache, false, slot * hidden, nk, threadIdx.x, step, cs + t * pairs);
-      for (int u = threadIdx.x; u < nk; u += step) {
-        float x[8], y[8];
-        rload8(a.v, a.x_f32, row * a.ld_v + 16 * u, x);
-        rload8(a.v, a.x_f32, row * a.ld_v + 16 * u + 8, y);
-        rstore8(a.v_cache, false, slot * hidden + 16 * u, x);
-        rstore8(a.v_cache, false, slot * hidden + 16 * u + 8, y);
-      }
-    }
+  for (; w < end; w += step) {
+    fetch(w + step, next);
+    finish(w, now);
+    now = next;
   }
 }
 
@@ -198,8 +245,20 @@ __global__ __launch_bounds__(256) void slot_map_kernel(SlotArgs a) {
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
   // four tokens to a workgroup share its start; few tokens spread over the chip
-  a.tokens = a.rows >= 4096 ? 4 : a.rows >= 2048 ? 2 : 1;
-  rotary_kernel<<<(unsigned)((a.rows + a.tokens - 1) / a.tokens), kRThreads, 0, stream>>>(a);
+  // Tokens to a workgroup: about three rounds of its threads, and at least four workgroups
+  // to a compute unit. 4680 rows of 12 heads of 128 take 9.6 us with four tokens and 11.5
+  // with one, which has more starts; of 40 + 40 + 40 heads 81 with four and 64 with one
+  // (before the addresses came from registers: 59 now).
+  const int units = (a.head_dim >> 4) * (a.n_heads + (a.k ? 2 * a.n_kv_heads : 0));
+  const int64_t most = a.rows / 1024;
+  a.tokens = 3 * kRThreads / units;
+  if (a.tokens > most) a.tokens = (int)most;
+  a.tokens = a.tokens < 1 ? 1 : a.tokens > kRMaxTokens ? kRMaxTokens : a.tokens;
+  const unsigned grid = (unsigned)((a.rows + a.tokens - 1) / a.tokens);
+  if (a.x_f32)
+    rotary_kernel<true><<<grid, kRThreads, 0, stream>>>(a);
+  else
+    rotary_kernel<false><<<grid, kRThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
