@@ -638,9 +638,12 @@ _NORMS = {"none": 0, "layer": 1, "rms": 2}
 _ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _on(dev, fn):
     """fn() with dev the current device (the library works on the current one)."""
-    if torch.cuda.current_device() == dev.index:
+    if _current_device() == dev.index:  # (a tensor there: the runtime is up)
         return fn()
     with torch.cuda.device(dev):
         return fn()
@@ -656,6 +659,13 @@ def _float_tensor(t, name, device=None):
 
 def _strided_rows(t, name, device=None, dtype=None, width=None):
     """A 2-d tensor of contiguous rows; returns its row distance in elements."""
+    # one expression for the usual case; the reasons only when it fails
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2
+            and (t.dtype == dtype if dtype is not None else t.dtype in _DT) and (device is None or t.device == device)):
+        rows, cols = t.shape
+        ld, one = t.stride()
+        if rows > 1 and one == 1 and ld >= cols and ld % 8 == 0 and (width is None or cols == width):
+            return ld
     if not isinstance(t, torch.Tensor) or (t.dtype != dtype if dtype is not None else t.dtype not in _DT):
         raise TypeError(f"{name} must be a {dtype or 'bf16 or fp32'} torch.Tensor")
     if not t.is_cuda:
@@ -674,10 +684,9 @@ def _strided_rows(t, name, device=None, dtype=None, width=None):
 
 
 def _vector(t, name, device, shape):
-    if t is not None:
-        _require(t, name, torch.float32, device, ndim=len(shape))
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must have shape {shape}")
+    _require(t, name, torch.float32, device, ndim=len(shape))
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}")
 
 
 def _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate, group_rows):
@@ -700,10 +709,13 @@ def _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate
     if group_rows < 1:
         raise ValueError("group_rows must be positive")
     groups = max(1, -(-rows // group_rows))
+    dev = x.device
     for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight)):
-        _vector(t, name, x.device, (cols,))
+        if t is not None:
+            _vector(t, name, dev, (cols,))
     for name, t in (("scale", scale), ("shift", shift), ("gate", gate)):
-        _vector(t, name, x.device, (groups, cols))
+        if t is not None:
+            _vector(t, name, dev, (groups, cols))
     return groups, group_rows
 
 
@@ -801,9 +813,13 @@ def norm_residual_backward(d_h, x_out, y=None, d_x_out=None, norm="layer", weigh
     return out
 
 
+_axis_types = [_c_i32 * n for n in range(1, 5)]
+
+
 def _pairs(axes, freqs):
     axes = (freqs.shape[0],) if axes is None else tuple(int(n) for n in axes)
-    return (_c_i32 * len(axes))(*axes), len(axes)
+    n = len(axes)
+    return (_axis_types[n - 1] if 0 < n <= 4 else _c_i32 * n)(*axes), n
 
 
 def rotary_frequencies(axis_pairs, base=10000.0, scaling="none", factor=1.0, original_length=0.0, beta_fast=32.0,
@@ -827,9 +843,9 @@ def _angles(positions, freqs, axes, dev, rows):
     _require(positions, "positions", torch.int32, dev, ndim=positions.dim() if isinstance(positions, torch.Tensor) else 2)
     _require(freqs, "freqs", torch.float64, dev, ndim=1)
     pairs, n_axes = _pairs(axes, freqs)
-    if sum(pairs) != freqs.shape[0]:
+    if axes is not None and sum(pairs) != freqs.shape[0]:
         raise ValueError("axes must add up to the pairs of freqs")
-    if tuple(positions.shape) != (rows, n_axes) and not (n_axes == 1 and tuple(positions.shape) == (rows,)):
+    if positions.shape != (rows, n_axes) and not (n_axes == 1 and positions.shape == (rows,)):
         raise ValueError(f"positions must have shape {(rows, n_axes)}")
     return pairs, n_axes
 
@@ -959,13 +975,15 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
             raise TypeError(f"{name} must be a bf16 torch.Tensor")
         if t.device != dev or t.dim() != 3 or t.shape[0] != n_req or t.shape[2] != kv:
             raise ValueError(f"{name} must be [n_req, capacity, {kv}] on {dev}")
-        if t.shape != k_cache.shape or t.stride() != k_cache.stride() or (kv > 1 and t.stride(2) != 1):
-            raise ValueError("k_cache and v_cache must have the same shape and distances, and contiguous rows")
     capacity = k_cache.shape[1]
-    ld_c = k_cache.stride(1) if capacity > 1 else kv
-    ld_r = k_cache.stride(0) if n_req > 1 else 0
-    if max_q is None:
-        max_q = max(1, -(-rows // n_req))
+    ld_r, ld_c, one = k_cache.stride()
+    if v_cache.shape[1] != capacity or v_cache.stride() != (ld_r, ld_c, one) or one != 1:
+        raise ValueError("k_cache and v_cache must have the same shape and distances, and contiguous rows")
+    if capacity <= 1:
+        ld_c = kv
+    if n_req <= 1:
+        ld_r = 0
+    max_q = int(max_q) if max_q is not None else max(1, -(-rows // n_req))
     if out is None:
         out = q.new_empty((rows, hidden), dtype=out_dtype)
     ld_out = _strided_rows(out, "out", dev, None, hidden)
@@ -977,13 +995,13 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
         return out, lse
 
     def call():
-        sizes = (prefix_len, capacity, n_req, rows, int(max_q), int(n_heads), n_kv_heads, head_dim)
-        nbytes = L.ispa_attn_shared_workspace_bytes(*sizes)
+        nbytes = L.ispa_attn_shared_workspace_bytes(prefix_len, capacity, n_req, rows, max_q, n_heads, n_kv_heads,
+                                                    head_dim)
         ws = q.new_empty(max(nbytes, 1), dtype=torch.uint8)
         return L.ispa_attn_shared(
             q.data_ptr(), ld_q, k_prefix.data_ptr(), v_prefix.data_ptr(), prefix_len, ld_p, k_cache.data_ptr(),
             v_cache.data_ptr(), capacity, ld_c, ld_r, q_start.data_ptr(), cache_lens.data_ptr(), n_req, rows,
-            int(max_q), int(n_heads), n_kv_heads, head_dim, float(scale), out.data_ptr(), _DT[out.dtype], ld_out,
+            max_q, n_heads, n_kv_heads, head_dim, scale, out.data_ptr(), _DT[out.dtype], ld_out,
             _ptr(lse), ws.data_ptr(), nbytes, _stream(dev))
 
     _check(_on(dev, call), "ispa_attn_shared")

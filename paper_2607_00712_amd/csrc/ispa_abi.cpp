@@ -992,8 +992,7 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
       (capacity > 0 && (bad_ld(ld_cache, kv) || ld_request < 0 || ld_request % 8 != 0)))
     return ISPA_ERR_INVALID_ARG;
   if (n_rows == 0) return ISPA_OK;
-  const size_t need = ispa_attn_shared_workspace_bytes(prefix_len, capacity, n_req, n_rows, max_q, n_heads, n_kv_heads,
-                                                       head_dim);
+  const size_t need = round_up(ispa::attn_shared_plan(&a, head_dim), kWsAlign);
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return ISPA_ERR_INVALID_ARG;
   const size_t pre = rows_bytes(prefix_len, ld_prefix, kv, 2),
                own = capacity > 0 ? ((size_t)(n_req - 1) * ld_request) * 2 + rows_bytes(capacity, ld_cache, kv, 2) : 0;
@@ -1004,7 +1003,6 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
   for (const Span& s : in)
     if (meets(so, {s}) || meets(sl, {s}) || meets(sw, {s})) return ISPA_ERR_INVALID_ARG;
   if (meets(so, {sl, sw}) || meets(sl, {sw})) return ISPA_ERR_INVALID_ARG;
-  ispa::attn_shared_plan(&a, head_dim);
   a.q = (const uint16_t*)q;
   a.k_prefix = (const uint16_t*)k_prefix;
   a.v_prefix = (const uint16_t*)v_prefix;
