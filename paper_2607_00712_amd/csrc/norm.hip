@@ -29,14 +29,15 @@
 // one's own for each workgroup, fetched ahead of the reductions, came out slower (4680 rows
 // of 5120, fp32 stream: 80 us against 65). Backward, where the columns' sums stay with a
 // workgroup over its rows, the next row is on its way while this one is reduced, as it lies
-// in memory (a bf16 chunk takes 4 registers). A variance is the mean of the centred squares
-// (no cancellation). All arithmetic is fp32, rounded once at the store.
+// in memory (a bf16 chunk takes 4 registers): 4680 rows of 4096 bf16 take 54 us, and 77 where
+// each row waits for its own loads. A variance is the mean of the centred squares (no
+// cancellation). All arithmetic is fp32, rounded once at the store.
 //
 // Measured at 4680 rows, bf16 block output, gate, scale and shift (us, and TB/s of the
 // tensors read and written once; a copy of 48 MB runs at 5.0):
 //   cols        1536 fp32   1536 bf16   5120 fp32   5120 bf16, RMS norm of y too
-//   forward      17 (5.0)    13 (4.5)    62 (4.7)    50 (3.8)
-//   backward     38 (3.4)    29 (3.0)   115 (3.8)   104 (2.8)
+//   forward      17 (5.0)    13 (4.5)    62 (4.7)    49 (3.9)
+//   backward     33 (3.9)    26 (3.3)   102 (4.2)    85 (3.4)
 #include "ispa_internal.h"
 
 namespace ispa {
@@ -84,25 +85,32 @@ __device__ __forceinline__ void store8(void* p, bool f32, int64_t e, const F8& x
   }
 }
 
-// Eight values of a bf16 or fp32 tensor as they lie in memory (zeros where not `here`):
-// fetched early, unpacked at their use, so that nothing waits in between. The types are
-// the kernel's template arguments: a branch on them around each load costs more than the
-// row's arithmetic.
+// Eight values of a bf16 or fp32 tensor as they lie in memory: fetched early, unpacked at
+// their use, so that nothing waits in between. The types are the kernel's template
+// arguments (a branch on them around each load costs more than the row's arithmetic), and
+// every lane loads, from a place inside the tensor, whether it keeps the values or not: a
+// load that only some lanes make joins its values with the others' zeros, and the compiler
+// waits for it there.
 template <bool F32>
 struct Raw8 {
   u32x4 d[F32 ? 2 : 1];
 };
 template <bool F32>
-__device__ __forceinline__ Raw8<F32> fetch8(const void* p, int64_t e, bool here) {
+__device__ __forceinline__ Raw8<F32> fetch8(const void* p, int64_t e) {
   Raw8<F32> r;
 #pragma unroll
   for (int i = 0; i < (F32 ? 2 : 1); ++i)
-    r.d[i] = here ? *(const u32x4*)((const char*)p + e * (F32 ? 4 : 2) + 16 * i) : u32x4{0, 0, 0, 0};
+    r.d[i] = *(const u32x4*)((const char*)p + e * (F32 ? 4 : 2) + 16 * i);
   return r;
 }
+// the values, or zeros
 template <bool F32>
-__device__ __forceinline__ F8 unpack8(const Raw8<F32>& r) {
+__device__ __forceinline__ F8 unpack8(Raw8<F32> r, bool here) {
   F8 x;
+#pragma unroll
+  for (int i = 0; i < (F32 ? 2 : 1); ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.d[i][j] = here ? r.d[i][j] : 0u;
   if constexpr (F32) {
     const f32x4 lo = __builtin_bit_cast(f32x4, r.d[0]), hi = __builtin_bit_cast(f32x4, r.d[1]);
 #pragma unroll
@@ -133,19 +141,29 @@ struct RowSum {
   float* part;  // [2][kNMaxSums][kNMaxWaves]
   int lanes, waves, wave, turn;  // wave: of the workgroup; its row's are wave / waves * waves on
 
-  // over the row's lanes of this wave
   template <int N>
-  __device__ __forceinline__ void over_lanes(float (&s)[N]) const {
+  static __device__ __forceinline__ void over8(float (&s)[N]) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       s[n] = dpp_add<0xB1>(s[n]);   // lane ^ 1
       s[n] = dpp_add<0x4E>(s[n]);   // lane ^ 2
       s[n] = dpp_add<0x141>(s[n]);  // the other quad of 8
     }
-    if (lanes > 8) {
+  }
+  template <int N>
+  static __device__ __forceinline__ void over16(float (&s)[N]) {
+    over8(s);
 #pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = dpp_add<0x140>(s[n]);  // the other half of 16
+    for (int n = 0; n < N; ++n) s[n] = dpp_add<0x140>(s[n]);  // the other half of 16
+  }
+  // over the row's lanes of this wave
+  template <int N>
+  __device__ __forceinline__ void over_lanes(float (&s)[N]) const {
+    if (lanes == 8) {
+      over8(s);
+      return;
     }
+    over16(s);
     if (lanes == 32) {
 #pragma unroll
       for (int n = 0; n < N; ++n) s[n] += __shfl_xor(s[n], 16);
@@ -158,29 +176,31 @@ struct RowSum {
       }
     }
   }
-  // the waves' values to every wave: [n * kNMaxWaves + w], w from the row's first wave on
+  // the values of the row's waves to every wave: that of its wave (lane & 15) to a lane,
+  // zero behind the last
   template <int N>
-  __device__ __forceinline__ const float* exchange(const float (&s)[N]) {
+  __device__ __forceinline__ void exchange(float (&s)[N]) {
     float* p = part + turn * kNMaxSums * kNMaxWaves;
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
+    const int lane = threadIdx.x & 63, w = lane & 15;
+    if (lane == 0) {
 #pragma unroll
       for (int n = 0; n < N; ++n) p[n * kNMaxWaves + wave] = s[n];
     }
     __syncthreads();
-    return p + wave / waves * waves;
+    p += wave / waves * waves + (w < waves ? w : 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float v = p[n * kNMaxWaves];
+      s[n] = w < waves ? v : 0.f;
+    }
   }
   template <int N>
   __device__ __forceinline__ void operator()(float (&s)[N]) {
     over_lanes(s);
     if (waves > 1) {
-      const float* p = exchange(s);
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = 0.f;
-      for (int w = 0; w < waves; ++w) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) s[n] += p[n * kNMaxWaves + w];
-      }
+      exchange(s);
+      over16(s);
     }
   }
 };
@@ -230,16 +250,14 @@ __device__ __forceinline__ Moments moments(const Row<K>& x, const bool (&in)[K],
       }
     sum.over_lanes(m2);
     if (sum.waves > 1) {
-      const float mine[3] = {mean, m2[0], n};
-      const float* p = sum.exchange(mine);
-      mean = 0.f;
-      for (int w = 0; w < sum.waves; ++w) mean = fmaf(p[2 * kNMaxWaves + w], p[w], mean);
-      mean *= inv_n;
-      m2[0] = 0.f;
-      for (int w = 0; w < sum.waves; ++w) {
-        const float d = p[w] - mean;
-        m2[0] += fmaf(p[2 * kNMaxWaves + w] * d, d, p[kNMaxWaves + w]);
-      }
+      float w[3] = {mean, m2[0], n};
+      sum.exchange(w);
+      s[0] = w[2] * w[0];
+      sum.over16(s);
+      mean = s[0] * inv_n;
+      const float d = w[0] - mean;
+      m2[0] = fmaf(w[2] * d, d, w[1]);
+      sum.over16(m2);
     }
   }
   return {mean, 1.0f / sqrtf(m2[0] * inv_n + eps)};
@@ -321,13 +339,14 @@ __global__ __launch_bounds__(64 * kNMaxWaves) void norm_residual_kernel(NormArgs
       const int c = pl.lane + k * pl.stride;
       in[k] = c < chunks && pl.slot < a.block_rows && row < run.end;
       col[k] = c * 8;
-      rx[k] = fetch8<XF>(a.x, base + col[k], in[k]);
-      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, base + col[k], in[k]);
+      const int64_t e = in[k] ? base + col[k] : 0;
+      rx[k] = fetch8<XF>(a.x, e);
+      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, e);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x.c[k] = unpack8<XF>(rx[k]);
-      if constexpr (Y > 0) z.c[k] = unpack8<Y == 2>(ry[k]);
+      x.c[k] = unpack8<XF>(rx[k], in[k]);
+      if constexpr (Y > 0) z.c[k] = unpack8<Y == 2>(ry[k], in[k]);
     }
   }
   if constexpr (Y > 0) {
@@ -378,33 +397,55 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(NormArgs a) {
     col[k] = c * 8;
     sa.c[k] = sb.c[k] = sp.c[k] = zero8();
   }
+  // What is absent is read from the stream and left out when the row's turn comes.
+  const void *px = has_norm ? a.x : a.d_x_in, *pd = has_norm ? a.d_h : px, *pg = a.d_x_in ? a.d_x_in : px;
   auto fetch = [&](int row) __attribute__((always_inline)) {
+    if (row >= a.rows) row = (int)a.rows - 1;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool here = in[k] && row < run.end;
-      const int64_t e = (int64_t)row * a.cols + col[k];
-      rx[k] = fetch8<XF>(a.x, e, here && has_norm);
-      rd[k] = fetch8<HF>(a.d_h, e, here && has_norm);
-      rg[k] = fetch8<XF>(a.d_x_in, e, here && a.d_x_in);
-      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, e, here);
+      const int64_t e = (int64_t)row * a.cols + (in[k] ? col[k] : 0);
+      rx[k] = fetch8<XF>(px, e);
+      rd[k] = fetch8<HF>(pd, e);
+      rg[k] = fetch8<XF>(pg, e);
+      if constexpr (Y > 0) ry[k] = fetch8<Y == 2>(a.y, e);
     }
   };
-  fetch(run.first + pl.slot);
+  // With a chunk to a lane, a row is fetched while the one before it is reduced; and what d_h
+  // and d_z are multiplied by, the same for all rows of the run, is read ahead of the loop,
+  // since a load between two rows' would be waited for with the next row's. Two chunks (rows
+  // behind 8192 columns) have no registers for either.
+  constexpr bool kAhead = K == 1;
+  Row<K> wd, wz;
+  if constexpr (kAhead) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      wd.c[0].v[i] = 1.f;
+      wz.c[0].v[i] = a.alpha;
+    }
+    with_vector<K>(a.scale, gbase, wd, in, col, [](float u, float w) { return u + w; });
+    with_vector<K>(a.weight, 0, wd, in, col, [](float u, float w) { return u * w; });
+    if constexpr (Y > 0) {
+      with_vector<K>(a.gate, gbase, wz, in, col, [](float u, float w) { return u * w; });
+      with_vector<K>(a.post_weight, 0, wz, in, col, [](float u, float w) { return u * w; });
+    }
+    fetch(run.first + pl.slot);
+  }
   for (int r0 = run.first; r0 < run.end; r0 += a.block_rows) {
     const int row = r0 + pl.slot;
     const int64_t base = (int64_t)row * a.cols;
     Row<K> x, d, y, g;
     float s[2] = {0.f, 0.f};
+    if constexpr (!kAhead) fetch(row);
     bool here[K];  // (what is outside stays zero and adds nothing to the sums)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       here[k] = in[k] && row < run.end;
-      x.c[k] = unpack8<XF>(rx[k]);
-      d.c[k] = unpack8<HF>(rd[k]);
-      g.c[k] = unpack8<XF>(rg[k]);
-      if constexpr (Y > 0) y.c[k] = unpack8<Y == 2>(ry[k]);
+      x.c[k] = unpack8<XF>(rx[k], here[k]);
+      d.c[k] = unpack8<HF>(rd[k], here[k]);
+      g.c[k] = unpack8<XF>(rg[k], here[k] && a.d_x_in);
+      if constexpr (Y > 0) y.c[k] = unpack8<Y == 2>(ry[k], here[k]);
     }
-    fetch(row + a.block_rows);
+    if constexpr (kAhead) fetch(row + a.block_rows);
     if (has_norm) {
       const float r = normalise<K>(x, here, a.norm, inv_n, a.eps, sum);
 #pragma unroll
@@ -413,9 +454,12 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(NormArgs a) {
         for (int i = 0; i < 8; ++i) {
           sa.c[k].v[i] += d.c[k].v[i];
           sb.c[k].v[i] = fmaf(d.c[k].v[i], x.c[k].v[i], sb.c[k].v[i]);
+          if constexpr (kAhead) d.c[k].v[i] *= wd.c[k].v[i];
         }
-      with_vector<K>(a.scale, gbase, d, here, col, [](float u, float w) { return u * (1.0f + w); });
-      with_vector<K>(a.weight, 0, d, here, col, [](float u, float w) { return u * w; });
+      if constexpr (!kAhead) {
+        with_vector<K>(a.scale, gbase, d, here, col, [](float u, float w) { return u * (1.0f + w); });
+        with_vector<K>(a.weight, 0, d, here, col, [](float u, float w) { return u * w; });
+      }
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -442,10 +486,12 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sp.c[k].v[i] = fmaf(g.c[k].v[i], y.c[k].v[i], sp.c[k].v[i]);
-          g.c[k].v[i] *= a.alpha;
+          g.c[k].v[i] *= kAhead ? wz.c[k].v[i] : a.alpha;
         }
-      with_vector<K>(a.gate, gbase, g, here, col, [](float u, float w) { return u * w; });
-      with_vector<K>(a.post_weight, 0, g, here, col, [](float u, float w) { return u * w; });
+      if constexpr (!kAhead) {
+        with_vector<K>(a.gate, gbase, g, here, col, [](float u, float w) { return u * w; });
+        with_vector<K>(a.post_weight, 0, g, here, col, [](float u, float w) { return u * w; });
+      }
       float m1 = 0.f, m2 = 0.f;
       if (a.post != ISPA_NORM_NONE) {
         s[0] = s[1] = 0.f;
@@ -648,6 +694,7 @@ hipError_t launch_norm_residual(NormArgs a, hipStream_t stream) {
 
 hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream) {
   const int k = norm_shape(&a, 1);
+  if (a.norm == ISPA_NORM_NONE) a.h_f32 = 0;  // (the pass reads the stream in place of d_h)
   a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
   a.group_blocks = norm_group_blocks(a.rows, a.cols, a.group_rows, &a.block_rows);
   const int threads = norm_threads(a);
@@ -658,6 +705,8 @@ hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream) {
     backward_k<1, 768>(a, grid, threads, lds, stream);
   else if (k == 1)
     backward_k<1, 1024>(a, grid, threads, lds, stream);
+  else if (threads <= 768)
+    backward_k<2, 768>(a, grid, threads, lds, stream);
   else
     backward_k<2, 1024>(a, grid, threads, lds, stream);
   hipError_t e = hipGetLastError();
