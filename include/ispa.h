@@ -553,14 +553,15 @@ int ispa_rotary_frequencies(const int32_t* axis_pairs, int32_t n_axes, double ba
  * pass through.
  *   x           device [rows, n_heads * head_dim] of x_dtype, rows ld_x elements apart
  *   out         device, of out_dtype, rows ld_out elements apart; may be x (same dtype
- *               and row distance), else must not overlap it
+ *               and row distance), else must not overlap it (other columns of the same
+ *               wider rows do not)
  *   positions   device int32 [rows, n_axes]
  *   freqs       device double [rotary_dim / 2]
  *   axis_pairs  host [n_axes]: pairs of each axis in order; their sum is rotary_dim / 2
  *   rotary_dim  a multiple of 16, 16 .. head_dim
  *   head_dim    a multiple of 16, 16 .. 256; n_heads * head_dim <= 2^20
  *   inverse     != 0: the transpose (the opposite angle), which is the gradient
- *   rows        0 .. 2^30 - 1; ld_x, ld_out multiples of 8, at least n_heads * head_dim
+ *   rows        0 .. 2^24 - 1; ld_x, ld_out multiples of 8, at least n_heads * head_dim
  * x and out 16-byte aligned. Asynchronous on `stream`.
  */
 int ispa_rotary(const void* x, int32_t x_dtype, int64_t ld_x, void* out, int32_t out_dtype, int64_t ld_out,
@@ -599,7 +600,7 @@ int ispa_slot_map(const int32_t* q_start, const int32_t* before, int32_t n_req, 
  *   q           device [rows, n_heads * head_dim], rows ld_q elements apart
  *   k, v        device [rows, n_kv_heads * head_dim], ld_k and ld_v apart; all of x_dtype
  *   q_out       device, of out_dtype, rows ld_out apart; may be q (same dtype and row
- *               distance)
+ *               distance), also where q, k and v are columns of the same wider rows
  *   k_cache, v_cache  device bf16 [cache_rows, n_kv_heads * head_dim], contiguous; must
  *               not overlap the inputs, q_out or each other
  *   slots       device int64 [rows]

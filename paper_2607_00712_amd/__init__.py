@@ -954,6 +954,7 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
     ld_q = _strided_rows(q, "q", None, torch.bfloat16)
     dev = q.device
     rows, hidden = q.shape
+    n_heads = int(n_heads)
     n_kv_heads = n_heads if n_kv_heads is None else int(n_kv_heads)
     if n_heads < 1 or hidden % n_heads or n_kv_heads < 1 or n_heads % n_kv_heads:
         raise ValueError("hidden size must be a multiple of n_heads, and n_heads of n_kv_heads")
@@ -1001,7 +1002,7 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
         return L.ispa_attn_shared(
             q.data_ptr(), ld_q, k_prefix.data_ptr(), v_prefix.data_ptr(), prefix_len, ld_p, k_cache.data_ptr(),
             v_cache.data_ptr(), capacity, ld_c, ld_r, q_start.data_ptr(), cache_lens.data_ptr(), n_req, rows,
-            max_q, n_heads, n_kv_heads, head_dim, scale, out.data_ptr(), _DT[out.dtype], ld_out,
+            max_q, n_heads, n_kv_heads, head_dim, float(scale), out.data_ptr(), _DT[out.dtype], ld_out,
             _ptr(lse), ws.data_ptr(), nbytes, _stream(dev))
 
     _check(_on(dev, call), "ispa_attn_shared")

@@ -672,7 +672,7 @@ int rotary_common(const int32_t* positions, const double* freqs, const int32_t* 
   if (rotary_dim < 16 || rotary_dim > head_dim || rotary_dim % 16 != 0) return ISPA_ERR_UNSUPPORTED;
   if (!positions || !freqs || !axis_pairs || n_axes < 1 || n_axes > ispa::kRotaryAxes) return ISPA_ERR_INVALID_ARG;
   if (any_misaligned({positions}, 3u) || any_misaligned({freqs}, 7u)) return ISPA_ERR_INVALID_ARG;
-  if (rows < 0 || rows >= (1 << 30) || n_heads < 1 || n_kv_heads < 1) return ISPA_ERR_INVALID_ARG;
+  if (rows < 0 || rows >= (1 << 24) || n_heads < 1 || n_kv_heads < 1) return ISPA_ERR_INVALID_ARG;
   if ((int64_t)n_heads * head_dim > (1 << 20) || (int64_t)n_kv_heads * head_dim > (1 << 20))
     return ISPA_ERR_INVALID_ARG;
   if (!(amplitude == amplitude) || isinf(amplitude)) return ISPA_ERR_INVALID_ARG;
@@ -705,6 +705,23 @@ bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld % 8 != 0 || ld 
 // bytes from the first to behind the last value of rows ld apart
 size_t rows_bytes(int64_t rows, int64_t ld, int64_t width, size_t esz) {
   return rows > 0 ? ((size_t)(rows - 1) * ld + width) * esz : 0;
+}
+
+// Rows of `width` elements of esz bytes, ld elements apart
+struct Rows {
+  const void* p;
+  int64_t rows, ld, width;
+  size_t esz;
+};
+// Two tensors of rows meet: their spans do, and they are not different columns of rows the
+// same distance apart (slices of one wider product).
+bool rows_meet(const Rows& a, const Rows& b) {
+  if (!meets({a.p, rows_bytes(a.rows, a.ld, a.width, a.esz)}, {{b.p, rows_bytes(b.rows, b.ld, b.width, b.esz)}}))
+    return false;
+  const int64_t l = a.ld * (int64_t)a.esz;
+  if (l != b.ld * (int64_t)b.esz) return true;
+  const int64_t d = (((intptr_t)b.p - (intptr_t)a.p) % l + l) % l;
+  return d < a.width * (int64_t)a.esz || d + b.width * (int64_t)b.esz > l;
 }
 
 bool shared_sizes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows, int32_t max_q, int32_t n_heads,
@@ -877,7 +894,7 @@ int ispa_rotary(const void* x, int32_t x_dtype, int64_t ld_x, void* out, int32_t
   if (bad_ld(ld_x, hidden) || bad_ld(ld_out, hidden)) return ISPA_ERR_INVALID_ARG;
   const Span so{out, rows_bytes(rows, ld_out, hidden, dtype_size(out_dtype))};
   if (!(out == x && x_dtype == out_dtype && ld_x == ld_out) &&
-      meets(so, {{x, rows_bytes(rows, ld_x, hidden, dtype_size(x_dtype))}}))
+      rows_meet({out, rows, ld_out, hidden, dtype_size(out_dtype)}, {x, rows, ld_x, hidden, dtype_size(x_dtype)}))
     return ISPA_ERR_INVALID_ARG;
   if (meets(so, {{positions, (size_t)rows * n_axes * 4}, {freqs, (size_t)rotary_dim * 4}})) return ISPA_ERR_INVALID_ARG;
   if (rows == 0) return ISPA_OK;
@@ -943,9 +960,12 @@ int ispa_rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k,
       kc{k_cache, cache}, vc{v_cache, cache}, sp{positions, (size_t)rows * n_axes * 4},
       ss{slots, (size_t)rows * 8}, sf{freqs, (size_t)rotary_dim * 4};
   if (meets(kc, {vc, sq, sk, sv, so, sp, ss, sf}) || meets(vc, {sq, sk, sv, so, sp, ss, sf}) ||
-      meets(so, {sk, sv, sp, ss, sf}))
+      meets(so, {sp, ss, sf}))
     return ISPA_ERR_INVALID_ARG;
-  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && meets(so, {sq})) return ISPA_ERR_INVALID_ARG;
+  const Rows to{q_out, rows, ld_out, hidden, dtype_size(out_dtype)};
+  if (rows_meet(to, {k, rows, ld_k, kv, es}) || rows_meet(to, {v, rows, ld_v, kv, es})) return ISPA_ERR_INVALID_ARG;
+  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && rows_meet(to, {q, rows, ld_q, hidden, es}))
+    return ISPA_ERR_INVALID_ARG;
   if (rows == 0) return ISPA_OK;
   a.q = q;
   a.k = k;
@@ -996,13 +1016,16 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return ISPA_ERR_INVALID_ARG;
   const size_t pre = rows_bytes(prefix_len, ld_prefix, kv, 2),
                own = capacity > 0 ? ((size_t)(n_req - 1) * ld_request) * 2 + rows_bytes(capacity, ld_cache, kv, 2) : 0;
-  const Span in[] = {{q, rows_bytes(n_rows, ld_q, hidden, 2)}, {k_prefix, pre}, {v_prefix, pre}, {k_cache, own},
-                     {v_cache, own}, {q_start, ((size_t)n_req + 1) * 4}, {cache_lens, (size_t)n_req * 4}};
+  const Span sq{q, rows_bytes(n_rows, ld_q, hidden, 2)};
+  const Span in[] = {{k_prefix, pre}, {v_prefix, pre}, {k_cache, own}, {v_cache, own},
+                     {q_start, ((size_t)n_req + 1) * 4}, {cache_lens, (size_t)n_req * 4}};
   const Span so{out, rows_bytes(n_rows, ld_out, hidden, dtype_size(out_dtype))},
       sl{lse, (size_t)n_heads * n_rows * 4}, sw{workspace, need};
   for (const Span& s : in)
     if (meets(so, {s}) || meets(sl, {s}) || meets(sw, {s})) return ISPA_ERR_INVALID_ARG;
-  if (meets(so, {sl, sw}) || meets(sl, {sw})) return ISPA_ERR_INVALID_ARG;
+  if (meets(so, {sl, sw}) || meets(sl, {sw, sq}) || meets(sw, {sq}) ||
+      rows_meet({out, n_rows, ld_out, hidden, dtype_size(out_dtype)}, {q, n_rows, ld_q, hidden, 2}))
+    return ISPA_ERR_INVALID_ARG;
   a.q = (const uint16_t*)q;
   a.k_prefix = (const uint16_t*)k_prefix;
   a.v_prefix = (const uint16_t*)v_prefix;

@@ -244,6 +244,20 @@ def test_strides():
         ispa.attn_shared(**make_wrong_head_dim(), n_heads=2)
 
 
+def test_output_beside_the_queries():
+    # the output takes other columns of the rows that hold q; over q's own columns it is refused
+    t = make([3, 9], [20, 33], 75, 40, 4, 2, 64)
+    gpu = on_gpu(t)
+    want, want_lse = ispa.attn_shared(**gpu, n_heads=4, n_kv_heads=2)
+    wide = torch.cat((gpu["q"], gpu["q"] * 0), 1)
+    args = {**gpu, "q": wide[:, :256]}
+    _, lse = ispa.attn_shared(**args, n_heads=4, n_kv_heads=2, out=wide[:, 256:])
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, 256:], want) and torch.equal(lse, want_lse) and torch.equal(wide[:, :256], gpu["q"])
+    with pytest.raises(ispa.IspaError):
+        ispa.attn_shared(**args, n_heads=4, n_kv_heads=2, out=wide[:, 248:504])
+
+
 def make_wrong_head_dim():
     return on_gpu(make([1], [2], 5, 3, 2, 2, 96))
 

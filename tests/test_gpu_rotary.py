@@ -205,6 +205,35 @@ def test_rotary_append(heads, kv_heads, head_dim, axes, interleaved, dtype, out_
     assert (flat[0][untouched] == 3).all() and (flat[1][untouched] == 3).all()
 
 
+@pytest.mark.parametrize("rows", [1, 2, 21])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_append_and_turn_inside_one_wide_product(rows, dtype):
+    # q turned in place between k and v of the same rows, and into other columns of them:
+    # what is beside it stays as it was
+    heads, kv_heads, head_dim = 6, 2, 64
+    nq, nk = heads * head_dim, kv_heads * head_dim
+    g = torch.Generator().manual_seed(rows)
+    x = torch.randn(rows, 2 * nq + 2 * nk, generator=g).to(dtype)
+    p = torch.randint(0, 5000, (rows, 1), generator=g, dtype=torch.int32)
+    f, _ = ispa.rotary_frequencies(32, device="cpu")
+    wide = x.to(DEV)
+    k, q, v, spare = wide.split((nk, nq, nk, nq), 1)
+    caches = [torch.zeros(rows, nk, dtype=BF16, device=DEV) for _ in range(2)]
+    slots = torch.arange(rows, device=DEV)
+    assert ispa.rotary_append(q, k, v, p.to(DEV), slots, f.to(DEV), heads, *caches, n_kv_heads=kv_heads, q_out=q) is q
+    want, size = turned(x[:, nk:nk + nq], p, f, (32,), head_dim, True, 1.0)
+    check(q, want, size, "q")
+    want, size = turned(x[:, :nk], p, f, (32,), head_dim, True, 1.0)
+    check(caches[0], want, size, "k")
+    assert torch.equal(caches[1].cpu(), x[:, nk + nq:2 * nk + nq].to(BF16))
+    assert torch.equal(k.cpu(), x[:, :nk]) and torch.equal(wide[:, nk + nq:].cpu(), x[:, nk + nq:])
+    before = wide.clone()
+    ispa.rotary(q, p.to(DEV), f.to(DEV), heads, inverse=True, out=spare)
+    want, size = turned(before[:, nk:nk + nq].cpu(), p, f, (32,), head_dim, True, 1.0, inverse=True)
+    check(spare, want, size, "spare")
+    assert torch.equal(wide[:, :2 * nk + nq], before[:, :2 * nk + nq])
+
+
 def test_append_behind_32_bits_and_graph():
     # a cache of more than 2^32 bytes: slots at its end; the step captured once and replayed
     # with new tokens and lengths

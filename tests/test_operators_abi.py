@@ -117,6 +117,19 @@ def test_rotary_append_refusals(want, kw):
     assert call("ispa_rotary_append", APPEND, **kw) == want
 
 
+@pytest.mark.parametrize("kw", [
+    dict(q_out=MB + 128, ld_out=64, ld_q=64),               # q's own rows, the second head
+    dict(q_out=MB + 2 * 96, ld_out=96, ld_q=96, k=MB + 2 * 64, ld_k=96),   # over q one row down, beside k
+    dict(q_out=MB, ld_out=96, ld_q=96, k=MB + 2 * 56, ld_k=96),            # in place, but k begins inside
+    dict(q_out=MB, ld_out=96, ld_q=96, k=MB + 2 * 72, ld_k=96),            # k runs into the next row
+    dict(q_out=MB, ld_out=64, k=MB + 2 * 64, ld_k=96),                     # other distances
+    dict(q_out=MB, ld_out=96, ld_q=96, v=MB + 2 * 32, ld_v=96),
+    dict(rows=1 << 24),
+])
+def test_rotary_append_refuses_overlapping_columns(kw):
+    assert call("ispa_rotary_append", APPEND, **kw) == E
+
+
 SLOT = dict(q_start=MB, before=2 * MB, n_req=3, n_rows=10, capacity=20, sink=0, window=0, first_position=0,
             slots=3 * MB, positions=4 * MB, lens=5 * MB, stream=0)
 
