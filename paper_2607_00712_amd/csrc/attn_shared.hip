@@ -90,7 +90,8 @@ __device__ __forceinline__ f32x16 sh_mfma(bf16x8 a, bf16x8 b, f32x16 c) {
 // byte voff of the descriptor, zero past its end. In assembly, so that the compiler's
 // LDS reads wait for LDS reads alone: through the builtin it takes every read as
 // possibly behind the loads in flight and waits for all of them. The statement has no
-// register outputs; arrival is waited for with arrived() below.
+// register outputs; arrival is waited for with arrived() below. (m0 is written here alone:
+// nothing that the compiler makes of these kernels uses it.)
 __device__ __forceinline__ void load_to_lds(i32x4 desc, int voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(desc), "s"(lds)
                : "memory");

@@ -542,10 +542,11 @@ __global__ __launch_bounds__(T) void norm_backward_kernel(NormArgs a) {
 }
 
 // The gradients of the vectors from part[n_groups * group_blocks][3][cols]. A workgroup
-// takes 32 columns of a group (several groups where a group has few parts), its 16 slices
+// takes 32 columns of a group (several groups where a group has few parts), its 32 slices
 // of threads the group's parts in turn, added up in LDS in order; the last row of
-// workgroups adds all parts for the vectors that the groups share.
-constexpr int kFCols = 32, kFSlices = 16, kFAhead = 4;
+// workgroups adds all parts for the vectors that the groups share (one group's own sums
+// serve for both).
+constexpr int kFCols = 32, kFSlices = 32, kFAhead = 4;
 
 __global__ __launch_bounds__(kFCols* kFSlices) void norm_backward_vectors_kernel(NormArgs a, int spg) {
   __shared__ float s[kFSlices][3][kFCols];
@@ -555,7 +556,8 @@ __global__ __launch_bounds__(kFCols* kFSlices) void norm_backward_vectors_kernel
   const int c = (blockIdx.x - by * col_blocks) * kFCols + cx;
   const bool in = c < a.cols;
   const int cc = in ? c : 0;
-  const bool all = a.shared_vectors && (by + 1) * col_blocks == (int)gridDim.x;
+  const bool one = a.n_groups == 1;
+  const bool all = !one && a.shared_vectors && (by + 1) * col_blocks == (int)gridDim.x;
   const int slices = all ? kFSlices : spg;  // slices that share a group
   const int64_t g = all ? 0 : (int64_t)by * (kFSlices / spg) + sl / spg;
   const int64_t n = all ? a.n_groups * a.group_blocks : g < a.n_groups ? a.group_blocks : 0;
@@ -594,11 +596,13 @@ __global__ __launch_bounds__(kFCols* kFSlices) void norm_backward_vectors_kernel
     }
   }
   if (!in || sl % slices != 0) return;
-  if (all) {
-    if (a.d_weight) a.d_weight[c] = v[1];
-    if (a.d_bias) a.d_bias[c] = v[0];
-    if (a.d_post_weight) a.d_post_weight[c] = a.alpha * v[2];
-  } else if (g < a.n_groups) {
+  if (all || (one && g == 0)) {
+    const float sc = one && a.scale ? 1.0f + a.scale[c] : 1.f, gt = one && a.gate ? a.gate[c] : 1.f;
+    if (a.d_weight) a.d_weight[c] = sc * v[1];
+    if (a.d_bias) a.d_bias[c] = sc * v[0];
+    if (a.d_post_weight) a.d_post_weight[c] = a.alpha * gt * v[2];
+  }
+  if (!all && g < a.n_groups) {
     const int64_t o = g * a.cols + c;
     if (a.d_shift) a.d_shift[o] = v[0];
     if (a.d_scale) a.d_scale[o] = (a.weight ? a.weight[c] : 1.f) * v[1] + (a.bias ? a.bias[c] : 0.f) * v[0];
@@ -715,7 +719,9 @@ hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream) {
   a.shared_vectors = a.d_weight || a.d_bias || a.d_post_weight;
   int spg = 1;
   while (spg < kFSlices && spg < a.group_blocks) spg *= 2;
-  const int64_t y = (a.group_vectors ? (a.n_groups + kFSlices / spg - 1) / (kFSlices / spg) : 0) + a.shared_vectors;
+  const int64_t y = a.n_groups == 1 ? 1
+                                    : (a.group_vectors ? (a.n_groups + kFSlices / spg - 1) / (kFSlices / spg) : 0) +
+                                          a.shared_vectors;
   norm_backward_vectors_kernel<<<(unsigned)(y * ((a.cols + kFCols - 1) / kFCols)), kFCols * kFSlices, 0, stream>>>(a, spg);
   return hipGetLastError();
 }

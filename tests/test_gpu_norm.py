@@ -165,6 +165,10 @@ BACKWARD = [
     make(10, 96, scale=True, gate=True, group=1), make(11, 96, scale=True, weight=True, bias=True, group=5),
     make(900, 96, scale=True, shift=True, weight=True, bias=True, gate=True, group=7),
     make(5, 1024), make(700, 1536, x=BF16, y=F32, h=F32, gate=True, scale=True, group=300),
+    # every vector over one group: of few rows, of many, and with a group length behind them
+    make(3, 40, post="rms", post_weight=True, gate=True, weight=True, bias=True, scale=True, shift=True),
+    make(700, 1536, post="layer", post_weight=True, gate=True, weight=True, bias=True, scale=True, shift=True),
+    make(2000, 64, x=BF16, y=F32, norm="rms", post="rms", post_weight=True, gate=True, weight=True, scale=True, group=4000),
 ]
 
 
