@@ -169,6 +169,10 @@ BACKWARD = [
     make(3, 40, post="rms", post_weight=True, gate=True, weight=True, bias=True, scale=True, shift=True),
     make(700, 1536, post="layer", post_weight=True, gate=True, weight=True, bias=True, scale=True, shift=True),
     make(2000, 64, x=BF16, y=F32, norm="rms", post="rms", post_weight=True, gate=True, weight=True, scale=True, group=4000),
+    # twelve waves to a row, sixteen, and two chunks to a lane of ten, of thirteen and sixteen waves
+    make(600, 6144, post="rms", post_weight=True, scale=True, group=150), make(520, 8192, gate=True, weight=True, bias=True),
+    make(300, 10240, x=BF16, y=F32, scale=True, group=200), make(270, 13000, norm="rms", post="layer", weight=True),
+    make(260, 16376, x=BF16, h=F32, gate=True, shift=True),
 ]
 
 

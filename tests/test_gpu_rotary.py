@@ -48,6 +48,8 @@ CASES = [
     (2, 40, 256, (32, 32, 32, 32), False, 1.0, BF16, 1), (2050, 2, 64, (32,), True, 1.0, BF16, 1),
     (4099, 1, 128, (64,), False, 1.0, BF16, 1), (9, 2, 128, (64,), True, 1.0, F32, 2000003),
     (9, 2, 128, (64,), False, 1.0, F32, 2 ** 31 - 40), (4, 300, 64, (32,), True, 1.0, F32, -5000),
+    # eight tokens to a workgroup, the last ones fewer
+    (8195, 1, 48, (8, 16), True, 0.5, BF16, 1), (8200, 2, 80, (24,), False, 1.0, F32, 1),
 ]
 
 
@@ -232,6 +234,32 @@ def test_append_and_turn_inside_one_wide_product(rows, dtype):
     want, size = turned(before[:, nk:nk + nq].cpu(), p, f, (32,), head_dim, True, 1.0, inverse=True)
     check(spare, want, size, "spare")
     assert torch.equal(wide[:, :2 * nk + nq], before[:, :2 * nk + nq])
+
+
+def test_append_of_many_rows():
+    # several tokens to a workgroup, rows without a slot among them, a head of 80 values of
+    # which 48 turn
+    rows, heads, kv_heads, head_dim = 8203, 3, 1, 80
+    g = torch.Generator().manual_seed(8)
+    q, k, v = (torch.randn(rows, n * head_dim, generator=g).to(BF16) for n in (heads, kv_heads, kv_heads))
+    p = torch.randint(0, 100000, (rows, 1), generator=g, dtype=torch.int32)
+    f, _ = ispa.rotary_frequencies(24, device="cpu")
+    slots = torch.randperm(9000, generator=g)[:rows].clone()
+    slots[torch.randperm(rows, generator=g)[:700]] = -1
+    caches = [torch.full((9000, head_dim), 3.0, dtype=BF16, device=DEV) for _ in range(2)]
+    out = torch.full((rows, heads * head_dim), 9.0, dtype=BF16, device=DEV)
+    ispa.rotary_append(q.to(DEV), k.to(DEV), v.to(DEV), p.to(DEV), slots.to(DEV), f.to(DEV), heads, *caches,
+                       n_kv_heads=kv_heads, interleaved=False, q_out=out)
+    kept = slots >= 0
+    want, size = turned(q, p, f, (24,), head_dim, False, 1.0)
+    check(out[kept.to(DEV)], want[kept], size[kept], "q")
+    assert (out.cpu()[~kept] == 9).all()
+    want, size = turned(k, p, f, (24,), head_dim, False, 1.0)
+    check(caches[0][slots[kept].to(DEV)], want[kept], size[kept], "k")
+    assert torch.equal(caches[1].cpu()[slots[kept]], v[kept])
+    free = torch.ones(9000, dtype=torch.bool)
+    free[slots[kept]] = False
+    assert (caches[0].cpu()[free] == 3).all() and (caches[1].cpu()[free] == 3).all()
 
 
 def test_append_behind_32_bits_and_graph():
