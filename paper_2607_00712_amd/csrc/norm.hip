@@ -676,11 +676,13 @@ void backward_k(const NormArgs& a, unsigned grid, int threads, size_t lds, hipSt
 }  // namespace
 
 hipError_t launch_norm_residual(NormArgs a, hipStream_t stream) {
-  // A row of up to 192 chunks stays in one wave, whose reductions need no exchange (4680
-  // rows of 1536: 17.0 us, bf16 12.7; with two waves to a row 19.0 and 13.9). A wider one
-  // has two chunks to a lane: three take as long in many rows and longer in few (1000 rows
-  // of 8192 bf16: 17.4 against 13.9), one is slower with a norm of the block output, whose
-  // exchanges grow with the waves (4680 of 5120 bf16: 65 against 57).
+  // A row of up to 192 chunks stays in one wave, whose reductions need no exchange: 4680 bf16
+  // rows of 1032, 1280 and 1536 columns with two norms take 12.5, 13.3 and 14.2 us, and 14.5,
+  // 15.1 and 16.0 with two waves to a row. Four chunks to a lane gain nothing more (1792 and
+  // 2048 columns: 17.4 and 18.0 against 17.8 and 18.9, without y 16.3 and 17.9 against 14.8
+  // and 16.3). A wider row has two chunks to a lane: three take as long in many rows and
+  // longer in few (1000 rows of 8192 bf16: 17.4 against 13.9), one is slower with a norm of
+  // the block output, whose exchanges grow with the waves (4680 of 5120 bf16: 65 against 57).
   const int k = norm_shape(&a, a.cols <= 8 * 64 * 3 ? 3 : 2);
   a.block_rows = a.waves > 1 ? (a.waves >= 4 ? 1 : 4 / a.waves) : 256 / a.lanes;
   a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
