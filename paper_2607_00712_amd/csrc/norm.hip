@@ -645,8 +645,11 @@ int norm_group_blocks(int64_t rows, int cols, int64_t group_rows, int* block_row
   NormArgs a;
   a.cols = cols;
   norm_shape(&a, 1);
-  // twelve waves fill a compute unit's registers; a workgroup's sums are written once
-  // (those of three vectors are as long as a few rows)
+  // One workgroup to a compute unit, of the twelve waves that fill its registers: every
+  // workgroup writes its sums once, which are as long as three fp32 rows. 4680 rows of 1536
+  // with an fp32 stream take 33.1 us, with half the waves in 512 workgroups 37.5, a quarter in
+  // 1024 36.1; 5120 bf16 85.9 against 97.1 and 119. (Rows behind 8192 columns alone gain from
+  // 512: 2000 of 16384 294 against 269.)
   const int slots = a.waves > 1 ? 12 / a.waves : 512 / a.lanes;
   *block_rows = slots < 1 ? 1 : slots;
   return norm_blocks(rows, group_rows, *block_rows, 256);
