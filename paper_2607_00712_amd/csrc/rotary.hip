@@ -20,7 +20,8 @@
 // 12 + 12 + 12 heads 18 (4.8), 20000 rows 69 (5.3), 6240 rows of 32 + 8 + 8 heads 33 (4.7).
 //
 // slot_map: the place of each row of a ragged batch in its request's cache, by a
-// search of the request starts; one launch serves every layer of a step.
+// search of the request starts; one launch serves every layer of a step (2.2 us for
+// 64 requests of a token, 3 for four of 1560).
 #include "ispa_internal.h"
 
 namespace ispa {
