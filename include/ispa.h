@@ -596,7 +596,8 @@ int ispa_slot_map(const int32_t* q_start, const int32_t* before, int32_t n_req, 
  * New tokens into their caches in one launch: q rotated into q_out, k rotated into row
  * slots[row] of k_cache, v into the same row of v_cache. Rows with a slot that is
  * negative or at least cache_rows are left alone: neither q_out nor a cache is written
- * for them. No slot may come twice.
+ * for them, as is right for padding; tokens without a place that attend all the same need
+ * ispa_rotary_append_batch. No slot may come twice.
  *   q           device [rows, n_heads * head_dim], rows ld_q elements apart
  *   k, v        device [rows, n_kv_heads * head_dim], ld_k and ld_v apart; all of x_dtype
  *   q_out       device, of out_dtype, rows ld_out apart; may be q (same dtype and row
@@ -612,6 +613,22 @@ int ispa_rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k,
                        const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
                        float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                        hipStream_t stream);
+
+/*
+ * ispa_rotary_append for a batch with tokens that have no place in their cache (more new
+ * ones than a ring's window, or behind the capacity: slot -1 from ispa_slot_map). Their
+ * keys and values are stored nowhere, but they attend: q is turned into q_out for every
+ * real row, whatever its slot, and for every row with a slot.
+ *   n_real      device int32, the count of real rows, those of padding are behind them
+ *               (q_start + n_req of ispa_slot_map), or NULL: all rows are real
+ * n_real must not overlap the outputs.
+ */
+int ispa_rotary_append_batch(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             int32_t x_dtype, void* q_out, int32_t out_dtype, int64_t ld_out, void* k_cache,
+                             void* v_cache, int64_t cache_rows, const int64_t* slots, const int32_t* n_real,
+                             const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                             int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                             int32_t n_kv_heads, int32_t head_dim, hipStream_t stream);
 
 /* ---------------------------------------------- attention, shared prefix */
 /*

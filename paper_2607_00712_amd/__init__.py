@@ -17,7 +17,7 @@ works without the library, but every call raises if it is not built.
     norm_residual(x, y, ...) -> (x_out, h);  norm_residual_backward(d_h, x_out, y, ...) -> gradients
     rotary(x, positions, freqs, n_heads, ...);  rotary_frequencies(axis_pairs, ...) -> (freqs, amplitude)
     slot_map(q_start, before, capacity, n_rows, ...) -> (slots, positions, lens)
-    rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, ...) -> q_out
+    rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, q_start=..., ...) -> q_out
     attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_heads, ...) -> (out, lse)
 """
 
@@ -89,6 +89,9 @@ _SIGNATURES = {
     "ispa_rotary_append": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i32, _c_i64, _c_p,
                                           _c_p, _c_i64, _c_p, _c_p, _c_p, ctypes.POINTER(_c_i32), _c_i32, _c_i32,
                                           _c_i32, _c_f32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p]),
+    "ispa_rotary_append_batch": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i32, _c_i64,
+                                                _c_p, _c_p, _c_i64, _c_p, _c_p, _c_p, _c_p, ctypes.POINTER(_c_i32),
+                                                _c_i32, _c_i32, _c_i32, _c_f32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p]),
     "ispa_attn_shared": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64,
                                         _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_f32, _c_p,
                                         _c_i32, _c_i64, _c_p, _c_p, _c_sz, _c_p]),
@@ -897,12 +900,18 @@ def slot_map(q_start, before, capacity, n_rows, sink=0, window=0, first_position
 
 
 def rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, n_kv_heads=None, axes=None,
-                  interleaved=True, amplitude=1.0, q_out=None):
-    """New tokens into their caches in one launch (ispa_rotary_append): q rotated into
-    q_out, k rotated into row slots[row] of k_cache, v beside it; rows with slot -1 are
-    left alone. q [rows, n_heads * head_dim], k and v [rows, n_kv_heads * head_dim] of one
-    dtype; caches bf16, contiguous, their rows flattened over all leading dimensions.
-    Returns q_out (bf16 by default; q_out=q turns in place)."""
+                  interleaved=True, amplitude=1.0, q_out=None, q_start=None):
+    """New tokens into their caches in one launch (ispa_rotary_append_batch): q rotated into
+    q_out, k rotated into row slots[row] of k_cache, v beside it. q [rows, n_heads *
+    head_dim], k and v [rows, n_kv_heads * head_dim] of one dtype; caches bf16, contiguous,
+    their rows flattened over all leading dimensions. Returns q_out (bf16 by default;
+    q_out=q turns in place).
+
+    A row with slot -1 reaches no cache. It is padding, or a token that its cache does not
+    keep (slot_map), whose query attends all the same: a new q_out holds every row turned,
+    and with q_start (slot_map's, int32 [n_req + 1]) a given one the rows before
+    q_start[n_req], the padding behind them left alone. A given q_out without q_start
+    takes every row with slot -1 for padding (ispa_rotary_append)."""
     L = lib()
     ld_q = _strided_rows(q, "q")
     dev = q.device
@@ -924,16 +933,26 @@ def rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, n
         _require(t, name, torch.bfloat16, dev, ndim=t.dim() if isinstance(t, torch.Tensor) and t.dim() > 1 else 2)
         if t.shape[-1] != kv or t.shape != k_cache.shape:
             raise ValueError(f"{name} must have rows of {kv} elements, and both caches one shape")
+    n_real = None  # (a new q_out has nothing to keep: every row turns)
+    if q_start is not None:
+        _require(q_start, "q_start", torch.int32, dev, ndim=1)
+        if q_start.shape[0] < 2:
+            raise ValueError("q_start must have an entry more than there are requests")
+        if q_out is not None:
+            n_real = q_start.data_ptr() + 4 * (q_start.shape[0] - 1)
+    batch = q_out is None or n_real is not None
     if q_out is None:
         q_out = q.new_empty((rows, hidden), dtype=torch.bfloat16)
     ld_out = _strided_rows(q_out, "q_out", dev, None, hidden)
     if q_out.shape[0] != rows:
         raise ValueError(f"q_out must have shape {(rows, hidden)}")
-    st = _on(dev, lambda: L.ispa_rotary_append(
+    fn = L.ispa_rotary_append_batch if batch else L.ispa_rotary_append
+    st = _on(dev, lambda: fn(
         q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[q.dtype], q_out.data_ptr(), _DT[q_out.dtype],
         ld_out, k_cache.data_ptr(), v_cache.data_ptr(), k_cache.numel() // kv, slots.data_ptr(),
-        positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
-        float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _stream(dev)) if rows else ISPA_OK)
+        *((n_real,) if batch else ()), positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0],
+        int(bool(interleaved)), float(amplitude), rows, int(n_heads), n_kv_heads, head_dim,
+        _stream(dev)) if rows else ISPA_OK)
     _check(st, "ispa_rotary_append")
     return q_out
 

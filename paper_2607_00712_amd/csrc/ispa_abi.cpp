@@ -724,6 +724,54 @@ bool rows_meet(const Rows& a, const Rows& b) {
   return d < a.width * (int64_t)a.esz || d + b.width * (int64_t)b.esz > l;
 }
 
+int rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                  int32_t x_dtype, void* q_out, int32_t out_dtype, int64_t ld_out, void* k_cache, void* v_cache,
+                  int64_t cache_rows, const int64_t* slots, bool unplaced, const int32_t* n_real,
+                  const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                  int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                  int32_t n_kv_heads, int32_t head_dim, hipStream_t stream) {
+  ispa::RotaryArgs a;
+  const int st = rotary_common(positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows, n_heads,
+                               n_kv_heads, head_dim, x_dtype, out_dtype, &a);
+  if (st != ISPA_OK) return st;
+  const int64_t hidden = (int64_t)n_heads * head_dim, kv = (int64_t)n_kv_heads * head_dim;
+  if (!q || !k || !v || !q_out || !k_cache || !v_cache || !slots) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q, k, v, q_out, k_cache, v_cache}) || any_misaligned({slots}, 7u) ||
+      any_misaligned({n_real}, 3u))
+    return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_q, hidden) || bad_ld(ld_k, kv) || bad_ld(ld_v, kv) || bad_ld(ld_out, hidden))
+    return ISPA_ERR_INVALID_ARG;
+  if (cache_rows < 1 || cache_rows > ((int64_t)1 << 40) / kv) return ISPA_ERR_INVALID_ARG;
+  const size_t es = dtype_size(x_dtype), cache = (size_t)cache_rows * kv * 2;
+  const Span sq{q, rows_bytes(rows, ld_q, hidden, es)}, sk{k, rows_bytes(rows, ld_k, kv, es)},
+      sv{v, rows_bytes(rows, ld_v, kv, es)}, so{q_out, rows_bytes(rows, ld_out, hidden, dtype_size(out_dtype))},
+      kc{k_cache, cache}, vc{v_cache, cache}, sp{positions, (size_t)rows * n_axes * 4},
+      ss{slots, (size_t)rows * 8}, sf{freqs, (size_t)rotary_dim * 4}, sn{n_real, 4};
+  if (meets(kc, {vc, sq, sk, sv, so, sp, ss, sf, sn}) || meets(vc, {sq, sk, sv, so, sp, ss, sf, sn}) ||
+      meets(so, {sp, ss, sf, sn}))
+    return ISPA_ERR_INVALID_ARG;
+  const Rows to{q_out, rows, ld_out, hidden, dtype_size(out_dtype)};
+  if (rows_meet(to, {k, rows, ld_k, kv, es}) || rows_meet(to, {v, rows, ld_v, kv, es})) return ISPA_ERR_INVALID_ARG;
+  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && rows_meet(to, {q, rows, ld_q, hidden, es}))
+    return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.q_out = q_out;
+  a.ld_out = ld_out;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.cache_rows = cache_rows;
+  a.slots = slots;
+  a.n_real = n_real;
+  a.unplaced = unplaced;
+  return ispa::launch_rotary(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
 bool shared_sizes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows, int32_t max_q, int32_t n_heads,
                   int32_t n_kv_heads, int32_t head_dim, ispa::SharedArgs* a) {
   if (head_dim != 64 && head_dim != 128) return false;
@@ -944,42 +992,20 @@ int ispa_rotary_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k,
                        const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
                        float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                        hipStream_t stream) {
-  ispa::RotaryArgs a;
-  const int st = rotary_common(positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows, n_heads,
-                               n_kv_heads, head_dim, x_dtype, out_dtype, &a);
-  if (st != ISPA_OK) return st;
-  const int64_t hidden = (int64_t)n_heads * head_dim, kv = (int64_t)n_kv_heads * head_dim;
-  if (!q || !k || !v || !q_out || !k_cache || !v_cache || !slots) return ISPA_ERR_INVALID_ARG;
-  if (any_misaligned({q, k, v, q_out, k_cache, v_cache}) || any_misaligned({slots}, 7u)) return ISPA_ERR_INVALID_ARG;
-  if (bad_ld(ld_q, hidden) || bad_ld(ld_k, kv) || bad_ld(ld_v, kv) || bad_ld(ld_out, hidden))
-    return ISPA_ERR_INVALID_ARG;
-  if (cache_rows < 1 || cache_rows > ((int64_t)1 << 40) / kv) return ISPA_ERR_INVALID_ARG;
-  const size_t es = dtype_size(x_dtype), cache = (size_t)cache_rows * kv * 2;
-  const Span sq{q, rows_bytes(rows, ld_q, hidden, es)}, sk{k, rows_bytes(rows, ld_k, kv, es)},
-      sv{v, rows_bytes(rows, ld_v, kv, es)}, so{q_out, rows_bytes(rows, ld_out, hidden, dtype_size(out_dtype))},
-      kc{k_cache, cache}, vc{v_cache, cache}, sp{positions, (size_t)rows * n_axes * 4},
-      ss{slots, (size_t)rows * 8}, sf{freqs, (size_t)rotary_dim * 4};
-  if (meets(kc, {vc, sq, sk, sv, so, sp, ss, sf}) || meets(vc, {sq, sk, sv, so, sp, ss, sf}) ||
-      meets(so, {sp, ss, sf}))
-    return ISPA_ERR_INVALID_ARG;
-  const Rows to{q_out, rows, ld_out, hidden, dtype_size(out_dtype)};
-  if (rows_meet(to, {k, rows, ld_k, kv, es}) || rows_meet(to, {v, rows, ld_v, kv, es})) return ISPA_ERR_INVALID_ARG;
-  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && rows_meet(to, {q, rows, ld_q, hidden, es}))
-    return ISPA_ERR_INVALID_ARG;
-  if (rows == 0) return ISPA_OK;
-  a.q = q;
-  a.k = k;
-  a.v = v;
-  a.ld_q = ld_q;
-  a.ld_k = ld_k;
-  a.ld_v = ld_v;
-  a.q_out = q_out;
-  a.ld_out = ld_out;
-  a.k_cache = k_cache;
-  a.v_cache = v_cache;
-  a.cache_rows = cache_rows;
-  a.slots = slots;
-  return ispa::launch_rotary(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+  return rotary_append(q, ld_q, k, ld_k, v, ld_v, x_dtype, q_out, out_dtype, ld_out, k_cache, v_cache, cache_rows, slots,
+                       false, nullptr, positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows,
+                       n_heads, n_kv_heads, head_dim, stream);
+}
+
+int ispa_rotary_append_batch(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             int32_t x_dtype, void* q_out, int32_t out_dtype, int64_t ld_out, void* k_cache,
+                             void* v_cache, int64_t cache_rows, const int64_t* slots, const int32_t* n_real,
+                             const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                             int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                             int32_t n_kv_heads, int32_t head_dim, hipStream_t stream) {
+  return rotary_append(q, ld_q, k, ld_k, v, ld_v, x_dtype, q_out, out_dtype, ld_out, k_cache, v_cache, cache_rows, slots,
+                       true, n_real, positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows,
+                       n_heads, n_kv_heads, head_dim, stream);
 }
 
 size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows,

@@ -212,6 +212,8 @@ struct RotaryArgs {
   int64_t ld_q, ld_k, ld_v, ld_out;  // elements
   const int32_t* positions;          // [rows, n_axes]
   const int64_t* slots;              // [rows], cache rows
+  const int32_t* n_real;             // count of real rows on the device; null: all
+  int unplaced;                      // real rows without a slot turn their queries
   const double* freqs;               // [rotary_dim / 2], radians per position
   int n_axes;
   int axis_end[kRotaryAxes - 1];     // first pair behind each axis but the last

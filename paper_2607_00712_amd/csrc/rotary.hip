@@ -80,10 +80,14 @@ struct Unit {
   Chunk<F32> c0, c1;
 };
 
-// Workgroup: a.tokens rows; rows without a slot (k given) are left alone. The heads of q,
-// k and v of all its rows are one list, so that every thread has work whatever the heads:
-// a thread keeps its place in a head and takes every (threads / units of a head)-th head
-// of the list. Units [0, rotary_dim / 16) of a head rotate, the others pass through.
+// What stands in place of a row's slot where it has none: its query turns all the same (a
+// token that its cache does not keep attends like the others), or the row is left alone.
+constexpr int64_t kQuery = -2, kNone = -1;
+
+// Workgroup: a.tokens rows. The heads of q, k and v of all its rows are one list, so that
+// every thread has work whatever the heads: a thread keeps its place in a head and takes
+// every (threads / units of a head)-th head of the list. Units [0, rotary_dim / 16) of a
+// head rotate, the others pass through.
 template <bool F32>
 __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 cs[kRMaxTokens * kRMaxPairs];
@@ -134,7 +138,7 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
     int64_t d = (row0 + t) * a.ld_out;
     if (a.k) {
       const int64_t slot = slot_of[t];
-      if (slot < 0) return;
+      if (slot < 0 && (h >= a.n_heads || slot == kNone)) return;
       if (h >= a.n_heads) {
         h -= a.n_heads;
         dst = k_cache, f32 = false, d = slot * a.n_kv_heads * a.head_dim;
@@ -193,8 +197,9 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
     cs[t * pairs + j] = make_float2(c * a.amplitude, s * (a.inverse ? -a.amplitude : a.amplitude));
   }
   if (a.k && threadIdx.x < (unsigned)n) {
-    const int64_t s = a.slots[row0 + threadIdx.x];
-    slot_of[threadIdx.x] = s < a.cache_rows ? s : -1;
+    const int64_t row = row0 + threadIdx.x, s = a.slots[row];
+    const bool query = a.unplaced && (!a.n_real || row < *a.n_real);
+    slot_of[threadIdx.x] = s >= 0 && s < a.cache_rows ? s : query ? kQuery : kNone;
   }
   __syncthreads();
   for (; w < end; w += step) {

@@ -226,3 +226,17 @@ def test_binding_refuses_host_tensors_and_names():
             fn()
     with pytest.raises(TypeError):
         ispa.norm_residual(x.double())
+
+
+@pytest.mark.parametrize("want, kw", [
+    (E, dict(n_real=10 * MB + 2)), (E, dict(q_out=10 * MB)), (E, dict(n_real=4 * MB + 252)), (E, dict(k_cache=10 * MB - 64)),
+    (E, dict(v_cache=10 * MB)), (E, dict(slots=0)), (E, dict(q=0)), (U, dict(head_dim=8)), (E, dict(q_out=2 * MB)),
+    (E, dict(rows=-1)), (OK, dict(rows=0)), (OK, dict(rows=0, n_real=0)),
+])
+def test_rotary_append_batch_refusals(want, kw):
+    args = {}
+    for name, value in APPEND.items():
+        args[name] = value
+        if name == "slots":
+            args["n_real"] = 10 * MB
+    assert call("ispa_rotary_append_batch", args, **kw) == want
