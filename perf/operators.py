@@ -465,7 +465,7 @@ def _own_append(s):
     at = positions if s["positions"] is None else s["positions"]
     ispa.rotary_append(s["q"], s["k"], s["v"], at, slots, s["f"], c["heads"], s["k_cache"], s["v_cache"],
                        n_kv_heads=c["kv_heads"], axes=s["axes"], interleaved=c["interleaved"],
-                       amplitude=s["amplitude"], q_out=s["q_out"])
+                       amplitude=s["amplitude"], q_out=s["q_out"], q_start=s["start"])
     return slots, positions, lens
 
 
