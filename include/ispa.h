@@ -523,7 +523,9 @@ size_t ispa_norm_residual_backward_workspace_bytes(int64_t rows, int32_t cols, i
  * factor^(n / (n - 1)) for an axis of n pairs, which divides its slowest frequency by
  * factor and leaves its fastest); parts (frequencies that turn more than beta_fast
  * times in original_length stay, those that turn less than beta_slow times are
- * divided by factor, a linear ramp over the pairs between). */
+ * divided by factor, a linear ramp over the pairs between: from the whole pair before
+ * that of beta_fast, or the first one, to the whole pair behind that of beta_slow, which
+ * may lie behind the last one). */
 #define ISPA_ROTARY_NONE   0
 #define ISPA_ROTARY_LINEAR 1
 #define ISPA_ROTARY_BASE   2

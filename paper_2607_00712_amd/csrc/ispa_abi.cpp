@@ -906,20 +906,19 @@ int ispa_rotary_frequencies(const int32_t* axis_pairs, int32_t n_axes, double ba
     const double b = scaling == ISPA_ROTARY_BASE && n > 1 ? base * pow(factor, n / (n - 1.0)) : base;
     // pairs whose count of turns in original_length is beta: n ln(length / (2 pi beta)) / ln(base)
     const double two_pi = 6.283185307179586;
+    // (a ramp may begin before the first pair, then it starts there; it may end behind the last
+    // one, or lie there whole: pairs that turn often enough keep what the ramp leaves them)
     double lo = 0.0, hi = 0.0;
     if (parts) {
       lo = floor(n * log(original_length / (two_pi * beta_fast)) / log(base));
       hi = ceil(n * log(original_length / (two_pi * beta_slow)) / log(base));
       if (lo < 0.0) lo = 0.0;
-      if (hi > n - 1.0) hi = n - 1.0;
     }
-    const double span = hi - lo > 1e-3 ? hi - lo : 1e-3;
     for (int j = 0; j < n; ++j) {
       double f = pow(b, -(double)j / n);
       if (scaling == ISPA_ROTARY_LINEAR) f /= factor;
       if (parts) {
-        double ramp = (j - lo) / span;
-        ramp = ramp < 0.0 ? 0.0 : ramp > 1.0 ? 1.0 : ramp;
+        const double ramp = j >= hi ? 1.0 : j <= lo ? 0.0 : (j - lo) / (hi - lo);
         f = f * (1.0 - ramp) + f / factor * ramp;
       }
       freqs[at++] = f;

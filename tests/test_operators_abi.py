@@ -240,3 +240,34 @@ def test_rotary_append_batch_refusals(want, kw):
         if name == "slots":
             args["n_real"] = 10 * MB
     assert call("ispa_rotary_append_batch", args, **kw) == want
+
+
+@pytest.mark.parametrize("pairs", [16, 64, 1])
+@pytest.mark.parametrize("length", [3.0, 40.0, 4096.0, 54000.0, 65536.0, 131072.0, 1e6, 1e8])
+@pytest.mark.parametrize("factor", [4.0, 16.0])
+def test_rotary_frequencies_in_parts(pairs, length, factor):
+    # trained lengths around 2 pi base: the ramp ends behind the last pair there, and lies
+    # behind it whole further on. The pair (not whole) that turns beta times in `length` is
+    # pairs ln(length / (2 pi beta)) / ln(base); the ramp runs between the whole ones around
+    # those of beta_fast and beta_slow, from the first pair on at the least
+    f, _ = frequencies(pairs, scaling="parts", factor=factor, original_length=length)
+    at = lambda beta: pairs * math.log(length / (2 * math.pi * beta)) / math.log(1e4)
+    lo, hi = max(0, math.floor(at(32.0))), math.ceil(at(1.0))
+    for j, x in enumerate(f):
+        y = 1e4 ** (-j / pairs)
+        turns = length * y / (2 * math.pi)
+        if turns > 32:
+            assert x == pytest.approx(y, rel=1e-13), j
+        elif turns < 1:
+            assert x == pytest.approx(y / factor, rel=1e-13), j
+        else:
+            ramp = min(1.0, max(0.0, (j - lo) / (hi - lo))) if hi > lo else 1.0
+            assert x == pytest.approx(y * (1 - ramp) + y / factor * ramp, rel=1e-12), j
+
+
+def test_rotary_frequencies_of_long_trained_lengths():
+    # 64 pairs, base 1e4, trained to 131072: the slowest pair turns 2.4 times there, more than
+    # beta_slow. Its place is 63 on a ramp from 45 to 70: 18 / 25 of the way to a quarter.
+    f, _ = frequencies(64, scaling="parts", factor=4.0, original_length=131072)
+    y = 1e4 ** (-63 / 64)
+    assert f[63] / y == pytest.approx(1 - 18 / 25 * 0.75, rel=1e-12)
