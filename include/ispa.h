@@ -657,7 +657,11 @@ int ispa_rotary_append_batch(const void* q, int64_t ld_q, const void* k, int64_t
  *               i / (n_heads / n_kv_heads); head_dim in {64, 128}
  *   scale       logit scale; <= 0 selects 1/sqrt(head_dim)
  *   out         [n_rows, n_heads * head_dim] of out_dtype, rows ld_out apart; a query
- *               without any key gets 0
+ *               without any key gets 0. An fp32 out has the weights in 16 bits (2^-16 of
+ *               sum w |v|). So has a bf16 one, except where more than 128 rows of the
+ *               tensors meet a key head (n_rows, for the own keys max_q, times n_heads /
+ *               n_kv_heads): there the weights enter the product with the values rounded
+ *               to bf16 (2^-8 of sum w |v| at most, about 2e-3 of the result)
  *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
  *   workspace   device, 256-byte aligned, at least ispa_attn_shared_workspace_bytes
  *               bytes for the same sizes on the same device. Used only during the call's

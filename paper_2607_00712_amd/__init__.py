@@ -967,7 +967,8 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
     [n_req, capacity, n_kv_heads * d] bf16, cache_lens[b] rows filled; q_start int32
     [n_req + 1] and cache_lens int32 [n_req] on the device. max_q: most rows of a request,
     a hint (None: the mean). Returns (out, lse); rows behind q_start[n_req] are left as
-    they were (uninitialised where out or lse is not given).
+    they were (uninitialised where out or lse is not given). An fp32 out keeps 16 bits of
+    the softmax weights whatever the rows; a bf16 one 8 where they are many.
     """
     L = lib()
     ld_q = _strided_rows(q, "q", None, torch.bfloat16)

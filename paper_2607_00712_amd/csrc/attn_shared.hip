@@ -164,9 +164,11 @@ __device__ __forceinline__ bf16x8 read_v1(const SWave<D, RB>& w, lds_char* blk, 
 // The weights of a block as product operands: rounded to bf16, and (F = 2) what the
 // rounding left, rounded again. Up to 128 rows the keys' bytes bound the work and the
 // second product is free: the weights then keep 16 bits, and an output's error is that of
-// its own rounding. Wider tiles are bound by the products and take the rounded weights
-// alone (2^-9 each, a relative error of about that of a bf16 output, as in chunk
-// attention), normalised by the sum of the rounded weights.
+// its own rounding. Tiles of 256 rows are bound by the products, three in place of two
+// (6240 rows of 12 heads against 37440 keys 1.49 ms with one part, 2.03 with two). There the
+// output's type decides: an fp32 output has the weights in 16 bits too, a bf16 one the
+// rounded weights alone, normalised by the sum of the rounded weights (2^-8 of a weight at
+// most, as in chunk attention: the output's error is 1.4 times that of its own rounding).
 template <int F>
 struct SWeights {
   bf16x8 p[F][2];
@@ -450,7 +452,7 @@ __device__ __forceinline__ void check_reference(const SharedArgs& a, SWave<D, RB
 // The keys of an item, met by KG = 1 or 2 groups of waves: steps of two blocks that the
 // workgroup loads together. The next block's scores and the last block's products run
 // beside a block's softmax, so that the matrix cores run through it.
-template <int D, int KG, int RB>
+template <int D, int KG, int RB, int F>
 __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w, lds_char* ring, const Keys& ks, int kg,
                                             int wave, int tid) {
   using C = SCfg<D>;
@@ -459,7 +461,6 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
   constexpr int kStepLoads = 2 * kStep * C::loads;
   constexpr int kStepBytes = kStep * C::blockBytes;
   constexpr int KB = kStep / KG;     // blocks of a step for this wave
-  constexpr int F = KG > 1 ? 2 : 1;  // (up to 128 rows: exact weights)
   const int hh = (tid & 63) >> 5;
   const int n_keys = (int)(ks.end - ks.begin);
   const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
@@ -710,8 +711,9 @@ __device__ __forceinline__ void write_part(const SharedArgs& a, const SWave<D, R
 }
 
 // A workgroup's item: rows [row0, row0 + 32 RB RG) of n_item_rows against `ks`, into the
-// partial rows from `part` on; RG = 4 / KG row groups.
-template <int D, int KG, int RB>
+// partial rows from `part` on; RG = 4 / KG row groups, FW the parts of a weight in the
+// widest tiles.
+template <int D, int KG, int RB, int FW>
 __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const Keys& ks, int kv_head, int first,
                                          int64_t row0, int64_t n_item_rows, int64_t part, int part_rows) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -729,7 +731,7 @@ __device__ __forceinline__ void run_item(const SharedArgs& a, char* smem, const 
     if (own.end > ks.end) own.end = ks.end;
     private_keys<D, RB>(a, w, ring + wave * (kRingBlocks * SCfg<D>::blockBytes / kShWaves), own, lane);
   } else {
-    shared_keys<D, KG, RB>(a, w, ring, ks, kg, wave, tid);
+    shared_keys<D, KG, RB, KG == 1 ? FW : 2>(a, w, ring, ks, kg, wave, tid);
   }
   arrived<0>();  // the ring is free
 #pragma unroll
@@ -764,7 +766,7 @@ __device__ __forceinline__ Prefix prefix_of(const SharedArgs& a, int total, int 
   return {tiles, a.prefix_len > 0 ? a.prefix_splits[i] : 0};
 }
 
-template <int D, int KGP, int RBP, int KGO, int RBO>
+template <int D, int KGP, int RBP, int KGO, int RBO, int FW>
 __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[kRingBlocks * SCfg<D>::blockBytes];
   const int total = clamp_int(a.q_start[a.n_req], 0, a.n_rows);  // rows of the batch, without padding
@@ -782,7 +784,7 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
     const int64_t b0 = blocks * split / pre.splits * kBlk, b1 = blocks * (split + 1) / pre.splits * kBlk;
     const Keys ks{a.k_prefix + head * D, a.v_prefix + head * D, a.ld_prefix, b0,
                   b1 < a.prefix_len ? b1 : a.prefix_len};
-    run_item<D, KGP, RBP>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, (int64_t)split * total, total);
+    run_item<D, KGP, RBP, FW>(a, smem, ks, head, 0, (int64_t)tile * kRows, rows, (int64_t)split * total, total);
     return;
   }
   // up to 32 rows: every wave an item of its own
@@ -819,7 +821,7 @@ __global__ __launch_bounds__(kShThreads) void attn_shared_kernel(SharedArgs a) {
       w.lr[0] = pair_sum32(w.lr[0]);
       write_part<D, 1>(a, w, r, part, a.n_rows, lane);
     } else {
-      run_item<D, KGO, RBO>(a, smem, ks, head, first, row0, rows, part, a.n_rows);
+      run_item<D, KGO, RBO, FW>(a, smem, ks, head, first, row0, rows, part, a.n_rows);
       __syncthreads();
     }
   }
@@ -909,18 +911,18 @@ int tile_shape(int64_t rows) {
   return s;
 }
 
-template <int D, int P, int O>
+template <int D, int P, int O, int FW>
 void* kernel_of(int prefix, int own) {
   // shape 0: 4 key groups x 32 rows; 1: 4 x 64; 2: 2 x 128; 3: 1 x 256
   if constexpr (P < 0) {
     return nullptr;
   } else if constexpr (O < 0) {
-    return kernel_of<D, P - 1, P - 1>(prefix, own);
+    return kernel_of<D, P - 1, P - 1, P == 3 ? 1 : FW>(prefix, own);
   } else {
     if (prefix == P && own == O)
       return (void*)attn_shared_kernel<D, P < 2 ? 4 : P == 2 ? 2 : 1, P == 0 ? 1 : 2, O < 2 ? 4 : O == 2 ? 2 : 1,
-                                       O == 0 ? 1 : 2>;
-    return kernel_of<D, P, O - 1>(prefix, own);
+                                       O == 0 ? 1 : 2, FW>;
+    return kernel_of<D, P, O - 1, FW>(prefix, own);
   }
 }
 
@@ -930,7 +932,8 @@ hipError_t launch_d(const SharedArgs& a, hipStream_t stream) {
   if (a.own_shape == 0) own = (own + kShWaves - 1) / kShWaves;  // an item to a wave
   const unsigned grid = (unsigned)(a.prefix_blocks + (own + kShXcds - 1) / kShXcds * kShXcds);
   // (a request has no more rows than the batch: its tiles are no wider)
-  void (*kernel)(SharedArgs) = (void (*)(SharedArgs))kernel_of<D, 3, 3>(a.prefix_shape, a.own_shape);
+  void (*kernel)(SharedArgs) = (void (*)(SharedArgs))(
+      a.out_bf16 ? kernel_of<D, 3, 3, 1>(a.prefix_shape, a.own_shape) : kernel_of<D, 3, 3, 2>(a.prefix_shape, a.own_shape));
   if (!kernel) return hipErrorInvalidConfiguration;
   if (grid > 0) {
     kernel<<<grid, kShThreads, 0, stream>>>(a);
