@@ -1,4 +1,5 @@
-"""attn_shared where a bound that fits every call says little.
+"""attn_shared where a bound that fits every call says little: the weights' 16 bits, every
+block of values, batches of more row tiles than the plan lists, tiles that take turns.
 
 Tolerances. The scores' error e, and B = sum w_i |v_i| + |O|, are those of
 test_gpu_attn_shared.py (`exact` there gives (2^-8 + 2 e + 2^-20) B as the tolerance of
@@ -95,3 +96,98 @@ def test_the_bound_tells_8_bits_from_16(case):
             w = (s - s.amax(1, keepdim=True)).exp().to(BF16).double()
             got[at, h * d:(h + 1) * d] = (w / w.sum(1, keepdim=True)) @ v[:, c:c + d]
     assert over(got, want, tol) > 1.5
+
+
+def stripe(t, kv_heads):
+    """Block i of 32 values is seen in every s-th channel from i % s on alone, s the blocks or the
+    channels of a head: a channel is the sum of few blocks, and a wrong one shows."""
+    for name in ("v_prefix", "v_cache"):
+        v = t[name]
+        keys = v.shape[-2]
+        d = v.shape[-1] // kv_heads
+        blocks = -(-keys // 32)
+        if blocks == 0:
+            continue
+        s = min(blocks, d)
+        seen = (torch.arange(keys)[:, None] // 32 % s) == (torch.arange(d)[None] % s)
+        t[name] = (v.view(*v.shape[:-1], kv_heads, d) * seen[:, None]).flatten(-2)
+    return t
+
+
+# counts, own lengths, prefix, capacity, heads, kv_heads, head_dim
+STRIPED = [
+    ([1] * 5, [3000, 0, 1, 2999, 512], 20011, 3000, 2, 2, 128), ([2], [7000], 9001, 7001, 1, 1, 64),
+    ([3, 30], [700, 1000], 2500, 1001, 2, 1, 128), ([50, 50], [90, 64], 1700, 100, 2, 2, 64),
+    ([130, 70, 200], [300, 0, 17], 1901, 300, 2, 2, 128), ([300, 9], [33, 1200], 2501, 1200, 2, 1, 64),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(STRIPED)))
+def test_every_block_of_values(case):
+    counts, lens, prefix, capacity, heads, kv_heads, d = STRIPED[case]
+    t = stripe(make(counts, lens, prefix, capacity, heads, kv_heads, d), kv_heads)
+    print(f"attn_shared striped {STRIPED[case]}", flush=True)
+    out, _ = ispa.attn_shared(**on_gpu(t), n_heads=heads, n_kv_heads=kv_heads, max_q=max(counts))
+    torch.cuda.synchronize()
+    want, _, tol, _ = exact(t, heads, kv_heads)
+    share = over(out, want, tol + 2.0 ** -8 * want.abs())
+    assert share <= 1, f"{share:.2f} of the tolerance"
+
+
+@pytest.mark.parametrize("case", [0, 1, 5])
+@pytest.mark.parametrize("wrong", ["zero", "reversed", "next", "channels"])
+def test_a_wrong_block_of_values_shows(case, wrong):
+    counts, lens, prefix, capacity, heads, kv_heads, d = STRIPED[case]
+    counts = [min(m, 4) for m in counts]
+    t = stripe(make(counts, lens, prefix, capacity, heads, kv_heads, d), kv_heads)
+    want, _, tol, _ = exact(t, heads, kv_heads)
+    blocks = -(-prefix // 32)
+    for i in (0, 1, blocks // 7, blocks // 2, blocks - 2):
+        v = t["v_prefix"].clone()
+        at = slice(32 * i, 32 * i + 32)
+        if wrong == "zero":
+            v[at] = 0
+        elif wrong == "reversed":
+            v[at] = v[at].flip(0)
+        elif wrong == "next":
+            v[at][:len(v[32 * i + 32:32 * i + 64])] = v[32 * i + 32:32 * i + 64]
+        else:
+            v[at] = v[at].roll(8, 1)
+        got, _, _, _ = exact({**t, "v_prefix": v}, heads, kv_heads)
+        assert over(got, want, tol + 2.0 ** -8 * want.abs()) > 1, (wrong, i)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("real", [1008, 1024, 1025, 1100, 9])
+def test_more_row_tiles_than_plans(real):
+    # 16 query heads to a key head: 69 tiles of 256 rows in the tensors, 63, 64, 65, 69 and 1 of real rows
+    heads, kv_heads, d = 16, 1, 64
+    counts = [real - 5, 5]
+    t = stripe(make(counts, [17, 40], 3000, 40, heads, kv_heads, d, pad=1100 - real), kv_heads)
+    out = torch.full((1100, heads * d), 4.0, dtype=BF16, device=DEV)
+    lse = torch.full((heads, 1100), 6.0, device=DEV)
+    print(f"attn_shared {real} of 1100 rows", flush=True)
+    ispa.attn_shared(**on_gpu(t), n_heads=heads, n_kv_heads=kv_heads, max_q=max(counts), out=out, lse=lse)
+    torch.cuda.synchronize()
+    want, want_lse, tol, lse_tol = exact(t, heads, kv_heads)
+    assert over(out[:real], want[:real], tol[:real] + 2.0 ** -8 * want[:real].abs()) <= 1
+    assert over(lse[:, :real], want_lse[:, :real], lse_tol[:, :real]) <= 1
+    assert (out[real:] == 4).all() and (lse[:, real:] == 6).all()
+
+
+@pytest.mark.gpu
+def test_row_tiles_take_turns():
+    # 2048 requests of 8 key heads leave room for 128 row tiles of a request in the grid:
+    # one request of 129 (33000 rows), the others of a row or none
+    heads, d, n_req = 8, 64, 2048
+    counts = [1 if b % 3 == 0 else 0 for b in range(n_req)]
+    counts[7] = 33000
+    lens = [b % 9 for b in range(n_req)]
+    lens[7] = 8
+    t = make(counts, lens, 33, 8, heads, heads, d)
+    out, lse = ispa.attn_shared(**on_gpu(t), n_heads=heads, max_q=33000)
+    torch.cuda.synchronize()
+    want, want_lse, tol, lse_tol = exact(t, heads, heads)
+    assert over(out, want, tol + 2.0 ** -8 * want.abs()) <= 1
+    assert over(lse, want_lse, lse_tol) <= 1
