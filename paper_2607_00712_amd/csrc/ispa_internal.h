@@ -193,8 +193,8 @@ struct NormArgs {
   float *d_gate, *d_post_weight, *d_weight, *d_bias, *d_scale, *d_shift;
   float* part;  // sums of each workgroup, or null where no vector takes part
   // set by the launch: lanes or waves to a row, rows of a workgroup at a time,
-  // workgroups to a group
-  int lanes, waves, block_rows, group_blocks;
+  // workgroups to a group and to the last one
+  int lanes, waves, block_rows, group_blocks, last_blocks;
   int64_t n_groups;
   int group_vectors, shared_vectors;  // gradients wanted of the groups' own and of shared vectors
 };

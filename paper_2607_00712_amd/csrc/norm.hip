@@ -287,7 +287,8 @@ __device__ __forceinline__ Place place_of(const NormArgs& a) {
   p.lane = threadIdx.x - p.slot * p.stride;
   return p;
 }
-// The rows [first, end) of workgroup blockIdx.x: an equal run of the rows of its group.
+// The rows [first, end) of workgroup blockIdx.x: an equal run of the rows of its group, of
+// which the last one may have fewer workgroups.
 struct Run {
   int64_t group;
   int first, end;
@@ -298,8 +299,9 @@ __device__ __forceinline__ Run run_of(const NormArgs& a) {
   const int part = (int)(blockIdx.x - r.group * a.group_blocks);
   const int64_t g0 = r.group * a.group_rows;
   const int64_t n = (g0 + a.group_rows < a.rows ? g0 + a.group_rows : a.rows) - g0;
-  r.first = (int)(g0 + n * part / a.group_blocks);
-  r.end = (int)(g0 + n * (part + 1) / a.group_blocks);
+  const int blocks = r.group == a.n_groups - 1 ? a.last_blocks : a.group_blocks;
+  r.first = (int)(g0 + n * part / blocks);
+  r.end = (int)(g0 + n * (part + 1) / blocks);
   return r;
 }
 
@@ -690,8 +692,11 @@ hipError_t launch_norm_residual(NormArgs a, hipStream_t stream) {
   a.block_rows = a.waves > 1 ? (a.waves >= 4 ? 1 : 4 / a.waves) : 256 / a.lanes;
   a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
   a.group_blocks = (int)((a.group_rows + a.block_rows - 1) / a.block_rows);
+  // (no workgroup without a row: a launch holds 2^32 - 1 threads, as many as 2^22 - 1 rows take)
+  const int64_t last_rows = a.rows - (a.n_groups - 1) * a.group_rows;
+  a.last_blocks = (int)((last_rows + a.block_rows - 1) / a.block_rows);
   const int threads = norm_threads(a);
-  const unsigned grid = (unsigned)(a.n_groups * a.group_blocks);
+  const unsigned grid = (unsigned)((a.n_groups - 1) * a.group_blocks + a.last_blocks);
   if (k == 1)
     forward_k<1>(a, grid, threads, stream);
   else if (k == 2)
@@ -705,7 +710,7 @@ hipError_t launch_norm_residual_backward(NormArgs a, hipStream_t stream) {
   const int k = norm_shape(&a, 1);
   if (a.norm == ISPA_NORM_NONE) a.h_f32 = 0;  // (the pass reads the stream in place of d_h)
   a.n_groups = (a.rows + a.group_rows - 1) / a.group_rows;
-  a.group_blocks = norm_group_blocks(a.rows, a.cols, a.group_rows, &a.block_rows);
+  a.group_blocks = a.last_blocks = norm_group_blocks(a.rows, a.cols, a.group_rows, &a.block_rows);
   const int threads = norm_threads(a);
   const size_t lds =
       (2 * kNMaxSums * kNMaxWaves + (a.block_rows > 1 ? (size_t)a.block_rows * a.cols : 0)) * sizeof(float);

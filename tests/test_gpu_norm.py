@@ -358,3 +358,27 @@ def test_repeats_streams_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, kept)), turn
+
+
+def test_a_short_last_group_of_very_many_rows():
+    # 2^22 - 1 rows in a group of all but one and a group of one: the grid counts the rows, not
+    # twice the long group's (whose 2^23 workgroups of nine waves no launch holds)
+    rows, cols = (1 << 22) - 1, 8200
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GB of free device memory")
+    x = torch.empty(rows, cols, dtype=BF16, device=DEV)
+    row = torch.randn(3, cols, generator=torch.Generator().manual_seed(5)).to(BF16)
+    at = [0, 1, rows // 2, rows - 2, rows - 1]
+    x.copy_(row[2].to(DEV).expand(rows, cols))
+    x[at[:4]] = row[[0, 1, 0, 1]].to(DEV)
+    scale = torch.randn(2, cols, generator=torch.Generator().manual_seed(6))
+    h = torch.empty_like(x)
+    _, h = ispa.norm_residual(x, scale=scale.to(DEV), group_rows=rows - 1, h=h)
+    torch.cuda.synchronize()
+    got, want_x = h[at].double().cpu(), row[[0, 1, 0, 1, 2]].double()
+    want = normed(want_x, "layer", 1e-6) * (1 + scale.double()[[0, 0, 0, 0, 1]])
+    size = size_of_norm(want_x, "layer", 1e-6) * (1 + scale.double().abs()[[0, 0, 0, 0, 1]])
+    check(got, want, want.abs() * half_step(BF16) + size * ROW, "h")
+    del x, h
+    torch.cuda.empty_cache()
