@@ -981,11 +981,12 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
     head_dim = hidden // n_heads
     kv = n_kv_heads * head_dim
     ld_p = _strided_rows(k_prefix, "k_prefix", dev, torch.bfloat16, kv)
-    if _strided_rows(v_prefix, "v_prefix", dev, torch.bfloat16, kv) != ld_p and k_prefix.shape[0] > 1:
-        raise ValueError("k_prefix and v_prefix must have the same row distance")
+    ld_v = _strided_rows(v_prefix, "v_prefix", dev, torch.bfloat16, kv)
     prefix_len = k_prefix.shape[0] if prefix_len is None else int(prefix_len)
     if prefix_len > k_prefix.shape[0] or prefix_len > v_prefix.shape[0]:
         raise ValueError("the prefix tensors hold fewer than prefix_len rows")
+    if ld_v != ld_p and prefix_len > 1:
+        raise ValueError("k_prefix and v_prefix must have the same row distance")
     _require(q_start, "q_start", torch.int32, dev, ndim=1)
     _require(cache_lens, "cache_lens", torch.int32, dev, ndim=1)
     n_req = cache_lens.shape[0]
@@ -998,12 +999,14 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
             raise ValueError(f"{name} must be [n_req, capacity, {kv}] on {dev}")
     capacity = k_cache.shape[1]
     ld_r, ld_c, one = k_cache.stride()
-    if v_cache.shape[1] != capacity or v_cache.stride() != (ld_r, ld_c, one) or one != 1:
-        raise ValueError("k_cache and v_cache must have the same shape and distances, and contiguous rows")
+    v_r, v_c, v_one = v_cache.stride()
+    # (distances to a request or a place that does not exist do not count)
+    if n_req <= 1 or capacity == 0:
+        ld_r = v_r = 0
     if capacity <= 1:
-        ld_c = kv
-    if n_req <= 1:
-        ld_r = 0
+        ld_c = v_c = kv
+    if v_cache.shape[1] != capacity or (v_r, v_c) != (ld_r, ld_c) or one != 1 or v_one != 1:
+        raise ValueError("k_cache and v_cache must have the same shape and distances, and contiguous rows")
     max_q = int(max_q) if max_q is not None else max(1, -(-rows // n_req))
     if out is None:
         out = q.new_empty((rows, hidden), dtype=out_dtype)

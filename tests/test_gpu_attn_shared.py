@@ -317,3 +317,29 @@ def test_repeats_streams_and_graph(counts):
         torch.cuda.synchronize()
         for got in kept:
             assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1]), turn
+
+
+def test_distances_that_no_row_uses():
+    # one request, one place, one prefix row: the distance to a next one does not exist and
+    # may differ between keys and values
+    t = make([3], [20], 40, 20, 2, 2, 64)
+    gpu = on_gpu(t)
+    want, want_lse = ispa.attn_shared(**gpu, n_heads=2)
+    room = torch.zeros(4, 33, 128, dtype=BF16, device=DEV)
+    room[2, :20] = gpu["k_cache"][0]
+    out, lse = ispa.attn_shared(**{**gpu, "k_cache": room[2:3, :20]}, n_heads=2)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    t = make([2, 1], [1, 1], 1, 1, 2, 2, 64)
+    gpu = on_gpu(t)
+    both = torch.zeros(2, 5, 128, dtype=BF16, device=DEV)
+    both[:, :1] = gpu["k_cache"]
+    other = torch.zeros(2, 5 * 128, dtype=BF16, device=DEV)
+    other[:, :128] = gpu["v_cache"][:, 0]
+    prefix = torch.zeros(3, 256, dtype=BF16, device=DEV)
+    prefix[0, :128] = gpu["k_prefix"][0]
+    args = {**gpu, "k_cache": both[:, :1], "v_cache": other[:, :128].unsqueeze(1), "k_prefix": prefix[:, :128]}
+    assert args["k_cache"].stride()[::2] == args["v_cache"].stride()[::2]
+    out, lse = ispa.attn_shared(**args, n_heads=2, prefix_len=1)
+    torch.cuda.synchronize()
+    check(out, lse, exact(t, 2, 2))
