@@ -664,8 +664,8 @@ int ispa_rotary_append_batch(const void* q, int64_t ld_q, const void* k, int64_t
  *               to bf16 (2^-8 of sum w |v| at most, about 2e-3 of the result)
  *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
  *   workspace   device, 256-byte aligned, at least ispa_attn_shared_workspace_bytes
- *               bytes for the same sizes on the same device. Used only during the call's
- *               device work.
+ *               bytes for the same sizes on the same device (may be NULL where that is 0:
+ *               no prefix and no capacity). Used only during the call's device work.
  * Row distances are multiples of 8 elements, pointers 16-byte aligned (lse 4). Keys and
  * values behind a set's end are never used, whatever they hold. Outputs must not overlap
  * the inputs or each other. The same call gives the same bits. Asynchronous on `stream`.
@@ -677,8 +677,8 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
                      void* out, int32_t out_dtype, int64_t ld_out, float* lse, void* workspace,
                      size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of ispa_attn_shared on the current device; 0 for invalid sizes or no
- * rows. */
+/* Workspace bytes of ispa_attn_shared on the current device; 0 for invalid sizes, no rows
+ * or no keys. */
 size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows,
                                         int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 

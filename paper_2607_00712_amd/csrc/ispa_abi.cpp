@@ -1038,7 +1038,7 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
     return ISPA_ERR_INVALID_ARG;
   if (n_rows == 0) return ISPA_OK;
   const size_t need = round_up(ispa::attn_shared_plan(&a, head_dim), kWsAlign);
-  if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return ISPA_ERR_INVALID_ARG;
+  if (need > 0 && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return ISPA_ERR_INVALID_ARG;
   const size_t pre = rows_bytes(prefix_len, ld_prefix, kv, 2),
                own = capacity > 0 ? ((size_t)(n_req - 1) * ld_request) * 2 + rows_bytes(capacity, ld_cache, kv, 2) : 0;
   const Span sq{q, rows_bytes(n_rows, ld_q, hidden, 2)};

@@ -343,3 +343,16 @@ def test_distances_that_no_row_uses():
     out, lse = ispa.attn_shared(**args, n_heads=2, prefix_len=1)
     torch.cuda.synchronize()
     check(out, lse, exact(t, 2, 2))
+
+
+def test_no_workspace_where_none_is_needed():
+    # nobody has a key: no partial results, and no buffer for them
+    L = ispa.lib()
+    assert L.ispa_attn_shared_workspace_bytes(0, 0, 2, 3, 2, 2, 2, 64) == 0
+    t = on_gpu(make([2, 1], [0, 0], 0, 0, 2, 2, 64))
+    out, lse = torch.ones(3, 128, dtype=BF16, device=DEV), torch.ones(2, 3, device=DEV)
+    st = L.ispa_attn_shared(t["q"].data_ptr(), 128, None, None, 0, 0, None, None, 0, 0, 0, t["q_start"].data_ptr(),
+                            t["cache_lens"].data_ptr(), 2, 3, 2, 2, 2, 64, 0.0, out.data_ptr(), ispa.DTYPE_BF16, 128,
+                            lse.data_ptr(), None, 0, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == ispa.ISPA_OK and not out.any() and (lse == -math.inf).all()
