@@ -732,7 +732,9 @@ def norm_residual(x, y=None, norm="layer", weight=None, bias=None, scale=None, s
     x, y [rows, cols] bf16 or fp32; weight, bias, post_weight fp32 [cols]; scale, shift,
     gate fp32 [groups, cols], one for every group_rows rows (None: one for all). norm and
     post: "layer", "rms" or "none". Returns (x_out, h): x_out is x itself where y is
-    None, h is None where norm is "none"; x_out=x updates the stream in place.
+    None, h is None where norm is "none"; x_out=x updates the stream in place. Like every
+    call here it records nothing for autograd: norm_residual_backward is its gradient, to
+    be called from the program's own backward pass (a torch.autograd.Function).
     """
     L = lib()
     _, group_rows = _norm_inputs(x, y, norm, weight, bias, scale, shift, post, post_weight, gate, group_rows)
@@ -858,7 +860,7 @@ def rotary(x, positions, freqs, n_heads, axes=None, interleaved=True, amplitude=
     x [rows, n_heads * head_dim] bf16 or fp32, rows may be apart (a slice of a wider
     product); positions int32 [rows, n_axes] (or [rows]); freqs fp64 on the device; axes:
     the pairs of each axis (None: one axis). inverse: the transpose, the gradient of the
-    forward call. out=x turns in place."""
+    forward call (nothing is recorded for autograd). out=x turns in place."""
     L = lib()
     ld = _strided_rows(x, "x")
     dev = x.device
