@@ -508,7 +508,7 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
     if (n_keys - kg * kBlk < kBlk) mask<RB>(first, n_keys - kg * kBlk, hh);
     maxima<RB>(first, w.m);
   }
-  const int n_steps = (n_keys + kStep * kBlk - 1) / (kStep * kBlk);
+  const int n_steps = n_keys / (kStep * kBlk) + (n_keys % (kStep * kBlk) != 0);  // (n_keys up to 2^31 - 1)
   int left = n_keys - kg * kBlk;       // keys from this wave's block on
   int cur = 0, prev = kSlots - 1;      // this step's slot and the one before
 #pragma unroll 1
