@@ -938,23 +938,24 @@ def rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, n
     n_real = None  # (a new q_out has nothing to keep: every row turns)
     if q_start is not None:
         _require(q_start, "q_start", torch.int32, dev, ndim=1)
-        if q_start.shape[0] < 2:
+        n_req = q_start.numel() - 1
+        if n_req < 1:
             raise ValueError("q_start must have an entry more than there are requests")
         if q_out is not None:
-            n_real = q_start.data_ptr() + 4 * (q_start.shape[0] - 1)
-    batch = q_out is None or n_real is not None
+            n_real = q_start.data_ptr() + 4 * n_req
+    padded = q_out is not None and n_real is None
     if q_out is None:
         q_out = q.new_empty((rows, hidden), dtype=torch.bfloat16)
     ld_out = _strided_rows(q_out, "q_out", dev, None, hidden)
     if q_out.shape[0] != rows:
         raise ValueError(f"q_out must have shape {(rows, hidden)}")
-    fn = L.ispa_rotary_append_batch if batch else L.ispa_rotary_append
-    st = _on(dev, lambda: fn(
-        q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[q.dtype], q_out.data_ptr(), _DT[q_out.dtype],
-        ld_out, k_cache.data_ptr(), v_cache.data_ptr(), k_cache.numel() // kv, slots.data_ptr(),
-        *((n_real,) if batch else ()), positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0],
-        int(bool(interleaved)), float(amplitude), rows, int(n_heads), n_kv_heads, head_dim,
-        _stream(dev)) if rows else ISPA_OK)
+    if rows == 0:
+        return q_out
+    to = (q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[q.dtype], q_out.data_ptr(), _DT[q_out.dtype],
+          ld_out, k_cache.data_ptr(), v_cache.data_ptr(), k_cache.numel() // kv, slots.data_ptr())
+    turn = (positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
+            float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _stream(dev))
+    st = _on(dev, lambda: L.ispa_rotary_append(*to, *turn) if padded else L.ispa_rotary_append_batch(*to, n_real, *turn))
     _check(st, "ispa_rotary_append")
     return q_out
 

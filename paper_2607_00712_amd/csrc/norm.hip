@@ -56,23 +56,18 @@ __device__ __forceinline__ F8 zero8() {
   for (int i = 0; i < 8; ++i) r.v[i] = 0.f;
   return r;
 }
-// eight values at element offset e of a bf16 or fp32 tensor
-__device__ __forceinline__ F8 load8(const void* p, bool f32, int64_t e) {
+// eight values of a vector from element e on
+__device__ __forceinline__ F8 load8(const float* p, int64_t e) {
   F8 r;
-  if (f32) {
-    const f32x4 a = *(const f32x4*)((const float*)p + e), b = *(const f32x4*)((const float*)p + e + 4);
+  const f32x4 a = *(const f32x4*)(p + e), b = *(const f32x4*)(p + e + 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r.v[i] = a[i];
-      r.v[4 + i] = b[i];
-    }
-  } else {
-    const bf16x8 a = *(const bf16x8*)((const uint16_t*)p + e);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = (float)a[i];
+  for (int i = 0; i < 4; ++i) {
+    r.v[i] = a[i];
+    r.v[4 + i] = b[i];
   }
   return r;
 }
+// eight values to element offset e of a bf16 or fp32 tensor
 __device__ __forceinline__ void store8(void* p, bool f32, int64_t e, const F8& x) {
   if (f32) {
     *(f32x4*)((float*)p + e) = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]};
@@ -313,7 +308,7 @@ __device__ __forceinline__ void with_vector(const float* v, int64_t base, Row<K>
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if (!in[k]) continue;
-    const F8 w = load8(v, true, base + col[k]);
+    const F8 w = load8(v, base + col[k]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x.c[k].v[i] = f(x.c[k].v[i], w.v[i]);
   }
