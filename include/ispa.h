@@ -584,7 +584,8 @@ int ispa_rotary(const void* x, int32_t x_dtype, int64_t ld_x, void* out, int32_t
  *               padding); 0 .. 2^31 - 1
  *   capacity    places of each request's cache, >= 1; with window > 0 exactly
  *               sink + window
- *   slots       device int64 [n_rows]: b * capacity + place, or -1 for padding and for a
+ *   slots       device int64 [n_rows]: b * capacity + place, or -1 for padding and (to be
+ *               told apart by the row's number, ispa_rotary_append_batch) for a
  *               token without a place (not kept, or behind the capacity)
  *   positions   device int32 [n_rows]: first_position + t, 0 for padding
  *   lens        device int32 [n_req]: before[b] + new tokens; must not overlap before

@@ -884,7 +884,8 @@ def rotary(x, positions, freqs, n_heads, axes=None, interleaved=True, amplitude=
 def slot_map(q_start, before, capacity, n_rows, sink=0, window=0, first_position=0):
     """Where the rows of a ragged batch go (ispa_slot_map): q_start int32 [n_req + 1] and
     before int32 [n_req] on the device. Returns (slots int64 [n_rows], positions int32
-    [n_rows], lens int32 [n_req]); window > 0: caches that are rings of sink + window."""
+    [n_rows], lens int32 [n_req]); window > 0: caches that are rings of sink + window. A
+    slot of -1 is padding or a token that its cache does not keep (rotary_append's q_start)."""
     L = lib()
     _require(q_start, "q_start", torch.int32, ndim=1)
     dev = q_start.device

@@ -43,11 +43,12 @@
 // weights are formed again, so that almost every block needs neither maxima nor
 // rescaling. The LSE takes the unrounded sum, in fp32.
 //
-// Measured, 128 values a head (a copy runs at 4.79 TB/s, a large bf16 product at 1210
+// Measured, 128 values a head (a copy runs at 4.79 TB/s, a large bf16 product at 1180-1210
 // TFLOP/s): 64 single tokens of 12 heads against 32760 shared keys and up to 1024 own ones
-// 101 us (4.2 TB/s of keys); 64 requests' own 1024 keys of 32 heads 190 us (5.65 TB/s); 6240
-// rows of 12 heads against 37440 keys 950 TFLOP/s; 32 heads on 8 against 16381 keys 39 us
-// for up to 64 tokens (one row tile), 71-75 for up to 128 (two).
+// 99-107 us (about 4 TB/s of keys, each fetched once); 64 requests' own 1024 keys of 32 heads
+// 190 us (5.65 TB/s); 6240 rows of 12 heads against 37440 keys 1.49 ms, 965 TFLOP/s, the
+// matrix cores busy 0.44 of the cycles of 1.96 GHz; 32 heads on 8 against 16381 keys 39 us for
+// up to 64 tokens (one row tile), 69-75 for up to 128 (two).
 #include "ispa_internal.h"
 
 #include <math.h>

@@ -33,11 +33,12 @@
 // each row waits for its own loads. A variance is the mean of the centred squares (no
 // cancellation). All arithmetic is fp32, rounded once at the store.
 //
-// Measured at 4680 rows, bf16 block output, gate, scale and shift (us, and TB/s of the
-// tensors read and written once; a copy of 48 MB runs at 5.0):
+// Measured at 4680 rows, bf16 block output, gate, scale and shift (us of a call's kernels
+// in turn, and TB/s of the tensors read and written once; torch's copy of three 48 MB tensors in
+// turn runs at 5.0):
 //   cols        1536 fp32   1536 bf16   5120 fp32   5120 bf16, RMS norm of y too
-//   forward      17 (5.0)    13 (4.5)    62 (4.7)    49 (3.9)
-//   backward     33 (3.9)    26 (3.3)   102 (4.2)    85 (3.4)
+//   forward      17 (5.0)    13 (4.4)    64 (4.5)    49 (3.9)
+//   backward     33 (3.9)    26 (3.3)   102 (4.2)    89 (3.2), 78 (3.7) without the three vectors
 #include "ispa_internal.h"
 
 namespace ispa {

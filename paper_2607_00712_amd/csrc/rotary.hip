@@ -15,9 +15,10 @@
 // (rotary_dim / 2 pairs of fp64 operations a token against n_heads x head_dim values of
 // traffic each way) while its first heads are on their way, and reads a unit of 16 values
 // of the next head while it turns this one.
-// Measured, bf16, heads of 128 (us, TB/s of the values read and written once; a copy of 48
-// MB runs at 5.0): 4680 rows of 40 heads 17 (5.6); with the append of k and v 4680 rows of
-// 12 + 12 + 12 heads 18 (4.8), 20000 rows 69 (5.3), 6240 rows of 32 + 8 + 8 heads 33 (4.7).
+// Measured, bf16, heads of 128 (us, TB/s of the values read and written once; torch's copy of
+// three 48 MB tensors in turn runs at 5.0): 4680 rows of 40 heads 16-18 (5.3-5.9); with the
+// append of k and v 4680 rows of 12 + 12 + 12 heads 18.5 (4.7), 20000 rows 69 (5.3), 6240 rows
+// of 32 + 8 + 8 heads 33 (4.7).
 //
 // slot_map: the place of each row of a ragged batch in its request's cache, by a
 // search of the request starts; one launch serves every layer of a step (2.2 us for
@@ -250,11 +251,10 @@ __global__ __launch_bounds__(256) void slot_map_kernel(SlotArgs a) {
 }  // namespace
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
-  // four tokens to a workgroup share its start; few tokens spread over the chip
-  // Tokens to a workgroup: about three rounds of its threads, and at least four workgroups
-  // to a compute unit. 4680 rows of 12 heads of 128 take 9.6 us with four tokens and 11.5
-  // with one, which has more starts; of 40 + 40 + 40 heads 81 with four and 64 with one
-  // (before the addresses came from registers: 59 now).
+  // Tokens to a workgroup: about three rounds of its threads, so that few heads share its
+  // start, and at least four workgroups to a compute unit. Heads of 128, us with 1, 2, 4 and 8
+  // tokens: 16384 rows of 2 heads 19.7, 12.2, 8.9, 8.7 (8 are taken, 8.9); 20000 of 12 + 12 +
+  // 12 74.5, 68.7, 71.3, 76.3 (2, 69.3); 4680 of 40 + 40 + 40 55.0, 59.0, 61.7, 70.1 (1, 54.7).
   const int units = (a.head_dim >> 4) * (a.n_heads + (a.k ? 2 * a.n_kv_heads : 0));
   const int64_t most = a.rows / 1024;
   a.tokens = 3 * kRThreads / units;
