@@ -191,3 +191,52 @@ def test_row_tiles_take_turns():
     want, want_lse, tol, lse_tol = exact(t, heads, heads)
     assert over(out, want, tol + 2.0 ** -8 * want.abs()) <= 1
     assert over(lse, want_lse, lse_tol) <= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_a_captured_batch_of_changing_rows(out_dtype):
+    # tensors of a fixed count of rows, captured once: the real rows are read on the device, from
+    # none to all, across every count of row tiles
+    heads, kv_heads, d, rows = 4, 2, 64, 400
+    t = make([rows - 50, 50], [60, 33], 900, 64, heads, kv_heads, d)
+    gpu = on_gpu(t)
+    out, lse = torch.empty(rows, heads * d, dtype=out_dtype, device=DEV), torch.empty(heads, rows, device=DEV)
+    call = lambda: ispa.attn_shared(**gpu, n_heads=heads, n_kv_heads=kv_heads, max_q=rows, out=out, lse=lse)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for counts in ([350, 50], [0, 0], [3, 1], [0, 64], [100, 30], [1, 256], [200, 200]):
+        starts = [0, counts[0], sum(counts)]
+        real = starts[2]
+        gpu["q_start"].copy_(torch.tensor(starts, dtype=torch.int32))
+        out.fill_(4.0), lse.fill_(6.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        assert (got[real:] == 4).all() and (got_lse[:, real:] == 6).all()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got) and torch.equal(lse, got_lse), counts
+        want, want_lse, tol, lse_tol = exact({**t, "q_start": torch.tensor(starts)}, heads, kv_heads)
+        if real:
+            assert over(got[:real], want[:real], tol[:real] + 2.0 ** -8 * want[:real].abs()) <= 1, counts
+            assert over(got_lse[:, :real], want_lse[:, :real], lse_tol[:, :real]) <= 1, counts
+
+
+@pytest.mark.gpu
+def test_requests_that_share_one_cache():
+    # a distance of 0 between requests: each reads its own length of the same rows
+    t = make([2, 3, 1], [40, 9, 33], 70, 40, 2, 2, 64)
+    t["k_cache"], t["v_cache"] = (t[x][:1].expand(3, 40, 128) for x in ("k_cache", "v_cache"))
+    gpu = on_gpu({k: v for k, v in t.items() if "cache" not in k or "lens" in k})
+    for x in ("k_cache", "v_cache"):
+        gpu[x] = t[x][0].to(DEV)[None].expand(3, 40, 128)
+        assert gpu[x].stride(0) == 0
+    out, _ = ispa.attn_shared(**gpu, n_heads=2)
+    torch.cuda.synchronize()
+    want, _, tol, _ = exact(t, 2, 2)
+    assert over(out, want, tol + 2.0 ** -8 * want.abs()) <= 1
