@@ -683,6 +683,159 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
 size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, int32_t n_req, int32_t n_rows,
                                         int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 
+/* --------------------------------- norms of heads with the position rotation */
+/*
+ * Norms of the queries' and keys' heads with the rotation of ispa_rotary in the same pass:
+ * for every head of q and of k
+ *   out = amplitude * R(position) (norm(x) * weight + bias)
+ * with mean and variance of the head's own head_dim values and R as in ispa_rotary (the
+ * values behind rotary_dim are normalised and not turned).
+ *   q           device [rows, n_heads * head_dim] of x_dtype, rows ld_q elements apart
+ *   k           device [rows, n_kv_heads * head_dim] of x_dtype, ld_k apart, or NULL: q alone
+ *   norm        ISPA_NORM_LAYER or ISPA_NORM_RMS
+ *   q_weight, k_weight, q_bias, k_bias   fp32 [head_dim] or NULL: one for all heads
+ *   eps         >= 0, finite
+ *   q_out, k_out  device, of out_dtype, rows ld_qo and ld_ko apart; q_out may be q and k_out
+ *               may be k (same dtype and row distance), else they must not overlap the inputs
+ *               (other columns of the same wider rows do not)
+ * Other arguments as for ispa_rotary; n_kv_heads * head_dim <= 2^20 too. Statistics and
+ * arithmetic are fp32 (angles fp64), each output is rounded once. Pointers 16-byte aligned,
+ * row distances multiples of 8. Asynchronous on `stream`.
+ */
+int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
+                     const float* q_weight, const float* k_weight, const float* q_bias, const float* k_bias, float eps,
+                     void* q_out, int64_t ld_qo, void* k_out, int64_t ld_ko, int32_t out_dtype,
+                     const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                     int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                     int32_t n_kv_heads, int32_t head_dim, hipStream_t stream);
+
+/*
+ * The backward pass of ispa_norm_rotary: from the gradients of its outputs those of
+ * everything that took part.
+ *   d_q_out, d_k_out  device [rows, heads * head_dim] of g_dtype, rows ld_gq and ld_gk apart;
+ *               d_k_out is NULL iff k is
+ *   q, k        as in the forward pass (not turned in place)
+ *   d_q, d_k    device, of x_dtype, rows ld_dq and ld_dk apart; may be d_q_out and d_k_out
+ *               (same dtype and row distance)
+ *   d_q_weight, d_k_weight, d_q_bias, d_k_bias   fp32 [head_dim] or NULL (not wanted); those
+ *               of k need k
+ *   workspace   device, 256-byte aligned, at least ispa_norm_rotary_backward_workspace_bytes
+ *               bytes; may be NULL where no gradient of a vector is wanted. Used only during
+ *               the call's device work.
+ * Sums over rows and heads are fp32, in an order that depends on the sizes alone: the same
+ * call gives the same bits. Asynchronous on `stream`.
+ */
+int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_k_out, int64_t ld_gk, int32_t g_dtype,
+                              const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
+                              const float* q_weight, const float* k_weight, float eps, void* d_q, int64_t ld_dq,
+                              void* d_k, int64_t ld_dk, float* d_q_weight, float* d_k_weight, float* d_q_bias,
+                              float* d_k_bias, const int32_t* positions, const double* freqs,
+                              const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                              float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ispa_norm_rotary_backward (n_kv_heads 0: without k); 0 for invalid sizes
+ * or no rows. */
+size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+
+/* ------------------------------------------------------ a cache in 4 bits */
+/*
+ * A 4-bit cache is a pool of pages of page_size tokens, and a table of the pages of each
+ * request: place p of request b is row p % page_size of page page_table[b][p / page_size].
+ * For every key head a page holds, one after the other,
+ *   keys     uint8 [page_size, head_dim / 2]: value 2i in the low and 2i + 1 in the high half
+ *            of byte i
+ *   values   the same
+ *   powers   uint8 [page_size, 2, head_dim / 32], of the keys' and of the values' blocks
+ * A block is 32 neighbouring values of a head: 4-bit numbers (bit 3 the sign, bits 0-2 one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(power - 127). The power is the smallest with no value
+ * above 7 times it, within 2^-120 .. 2^125, and each value is rounded to the nearest number,
+ * ties to the even code, so that it is off by at most half a step (one fifth of the block's
+ * largest value at most: a block whose largest is 5 times its power). A block with an infinity or a NaN has power 255 and reads as NaN.
+ *
+ * In all calls
+ *   cache       device uint8 [n_pages, n_kv_heads, ispa_kv4_page_bytes], 16-byte aligned
+ *   page_size   a power of two, 32 .. 65536; head_dim in {64, 128}
+ *   page_table  device int32 [n_req, max_pages]; max_pages * page_size <= 2^31 - 1. A page
+ *               number outside [0, n_pages) stands for no page: nothing is stored there and
+ *               its keys are not attended. Requests may share pages that are only read.
+ */
+/* Bytes of a page for one key head; 0 for sizes that are not supported. */
+size_t ispa_kv4_page_bytes(int64_t page_size, int32_t head_dim);
+
+/*
+ * New tokens into a 4-bit cache in one launch, as ispa_rotary_append_batch does for a bf16
+ * one: q and k are normalised (norm, weights and biases as for ispa_norm_rotary; or
+ * ISPA_NORM_NONE, without any of them) and turned, q into q_out, k and v into the place of
+ * their row.
+ *   q, k, v     device [rows, heads * head_dim] of x_dtype, rows ld_q, ld_k and ld_v apart
+ *   q_out       device, of out_dtype, rows ld_out apart; may be q (same dtype and row
+ *               distance); must not overlap anything else (other columns of the same wider
+ *               rows do not)
+ *   slots       device int64 [rows]: b * capacity + place with capacity = max_pages *
+ *               page_size, as ispa_slot_map gives them (rings too). A row whose slot is
+ *               negative or outside, or whose page there is not, is stored nowhere; its q is
+ *               turned all the same. No slot may come twice.
+ *   n_real      device int32, the count of real rows, those of padding are behind them: their
+ *               q_out is left as it is (q_start + n_req of ispa_slot_map); or NULL: all are
+ * Which number a key is rounded to is decided in fp64, q is computed in fp32. Pages that no
+ * row has a slot in are not touched. Asynchronous on `stream`.
+ */
+int ispa_kv4_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                    int32_t x_dtype, int32_t norm, const float* q_weight, const float* k_weight, const float* q_bias,
+                    const float* k_bias, float eps, void* q_out, int32_t out_dtype, int64_t ld_out, void* cache,
+                    int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req, int64_t max_pages,
+                    const int64_t* slots, const int32_t* n_real, const int32_t* positions, const double* freqs,
+                    const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                    float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    hipStream_t stream);
+
+/*
+ * Rows of a 4-bit cache as the values that they hold (exact in either type): k and v
+ * [rows, n_kv_heads * head_dim] of out_dtype, contiguous, of the places that slots (device
+ * int64 [rows], as for ispa_kv4_append; one may come more than once) stands for; zeros where
+ * there is no place. rows * n_kv_heads * head_dim < 2^34. Asynchronous on `stream`.
+ */
+int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req,
+                  int64_t max_pages, const int64_t* slots, int64_t rows, int32_t n_kv_heads, int32_t head_dim, void* k,
+                  void* v, int32_t out_dtype, hipStream_t stream);
+
+/*
+ * Attention of a batch of requests over a 4-bit cache: request b's queries see the keys at its
+ * places [0, cache_lens[b]), all of them (no mask inside a chunk, as in ispa_attn_chunk), less
+ * those of pages that there are not.
+ *   q           bf16 [n_rows, n_heads * head_dim], rows ld_q elements apart; request b has rows
+ *               q_start[b] .. q_start[b + 1] - 1
+ *   q_start     device int32 [n_req + 1], ascending, from 0; q_start[n_req] <= n_rows: rows
+ *               behind it are padding, and out and lse are left as they are there
+ *   cache_lens  device int32 [n_req]; values outside [0, max_pages * page_size] are taken as
+ *               the nearer end (a ring's count of tokens may stand for its filled places)
+ *   n_req >= 1; n_rows >= 0 (0: nothing is done); n_rows * n_heads <= 2^26 and
+ *               n_req * n_kv_heads <= 2^20
+ *   max_q       >= 1: most rows of a request, as far as the host knows; the layout of the work
+ *               follows it, the result does not depend on it beyond rounding
+ *   n_heads     a multiple of n_kv_heads: query head i reads key head i / (n_heads / n_kv_heads)
+ *   scale       logit scale; <= 0 selects 1/sqrt(head_dim)
+ *   out         [n_rows, n_heads * head_dim] of out_dtype, rows ld_out apart; a query without
+ *               any key gets 0
+ *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
+ *   workspace   device, 256-byte aligned, at least ispa_attn_kv4_workspace_bytes bytes for the
+ *               same sizes on the same device. Used only during the call's device work.
+ * The softmax weights enter the product with the values in 16 bits (2^-16 of sum w |v|). Row
+ * distances are multiples of 8 elements, pointers 16-byte aligned (lse and integers 4). Keys
+ * and values behind a request's end are never used, whatever their pages hold. Outputs must not
+ * overlap the inputs or each other. The same call gives the same bits. Asynchronous on `stream`.
+ */
+int ispa_attn_kv4(const void* q, int64_t ld_q, const void* cache, int64_t n_pages, int64_t page_size,
+                  const int32_t* page_table, int64_t max_pages, const int32_t* q_start, const int32_t* cache_lens,
+                  int32_t n_req, int32_t n_rows, int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                  float scale, void* out, int32_t out_dtype, int64_t ld_out, float* lse, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ispa_attn_kv4 on the current device; 0 for invalid sizes or no rows. */
+size_t ispa_attn_kv4_workspace_bytes(int64_t page_size, int64_t max_pages, int32_t n_req, int32_t n_rows, int32_t max_q,
+                                     int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,12 @@ works without the library, but every call raises if it is not built.
     slot_map(q_start, before, capacity, n_rows, ...) -> (slots, positions, lens)
     rotary_append(q, k, v, positions, slots, freqs, n_heads, k_cache, v_cache, q_start=..., ...) -> q_out
     attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_heads, ...) -> (out, lse)
+    norm_rotary(q, k, positions, freqs, n_heads, norm=..., ...) -> (q_out, k_out)
+    norm_rotary_backward(d_q_out, d_k_out, q, k, positions, freqs, n_heads, ...) -> gradients
+    kv4_cache(n_pages, page_size, n_kv_heads, head_dim) -> cache  (4-bit pages)
+    kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, norm=..., ...) -> q_out
+    kv4_read(cache, page_table, slots, head_dim) -> (k, v)
+    attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, ...) -> (out, lse)
 """
 
 import ctypes
@@ -30,7 +36,7 @@ __all__ = ["IspaError", "NotSPDError", "lib", "attn_chunk", "attn_chunk_noalloc"
            "status_string",
            "select_layers", "inject_modulation", "LocalKV", "project", "quantize_rows", "project_w8a8",
            "norm_residual", "norm_residual_backward", "rotary_frequencies", "rotary", "slot_map", "rotary_append",
-           "attn_shared",
+           "attn_shared", "norm_rotary", "norm_rotary_backward", "kv4_cache", "kv4_append", "kv4_read", "attn_kv4",
            "LIB_PATH", "ISPA_OK", "ISPA_ERR_INVALID_ARG", "ISPA_ERR_UNSUPPORTED",
            "ISPA_ERR_NOT_SPD", "ISPA_ERR_HIP", "ISPA_ERR_STATE", "ISPA_ERR_SCRATCH",
            "ISPA_STATIC_SCRATCH_BYTES"]
@@ -96,6 +102,25 @@ _SIGNATURES = {
                                         _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_f32, _c_p,
                                         _c_i32, _c_i64, _c_p, _c_p, _c_sz, _c_p]),
     "ispa_attn_shared_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "ispa_norm_rotary": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_f32, _c_p,
+                                        _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_p, ctypes.POINTER(_c_i32), _c_i32,
+                                        _c_i32, _c_i32, _c_f32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p]),
+    "ispa_norm_rotary_backward": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i32,
+                                                 _c_i32, _c_p, _c_p, _c_f32, _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_p,
+                                                 _c_p, _c_p, _c_p, _c_p, ctypes.POINTER(_c_i32), _c_i32, _c_i32, _c_i32,
+                                                 _c_f32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p, _c_sz, _c_p]),
+    "ispa_norm_rotary_backward_workspace_bytes": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32]),
+    "ispa_kv4_page_bytes": (_c_sz, [_c_i64, _c_i32]),
+    "ispa_kv4_append": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p,
+                                       _c_f32, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_i64, _c_p, _c_i32, _c_i64, _c_p,
+                                       _c_p, _c_p, _c_p, ctypes.POINTER(_c_i32), _c_i32, _c_i32, _c_i32, _c_f32, _c_i64,
+                                       _c_i32, _c_i32, _c_i32, _c_p]),
+    "ispa_kv4_read": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_i32, _c_i32, _c_p,
+                                     _c_p, _c_i32, _c_p]),
+    "ispa_attn_kv4": (ctypes.c_int, [_c_p, _c_i64, _c_p, _c_i64, _c_i64, _c_p, _c_i64, _c_p, _c_p, _c_i32, _c_i32,
+                                     _c_i32, _c_i32, _c_i32, _c_i32, _c_f32, _c_p, _c_i32, _c_i64, _c_p, _c_p, _c_sz,
+                                     _c_p]),
+    "ispa_attn_kv4_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
     "ispa_stats_workspace_bytes": (_c_sz, [_c_i32, _c_i32, _c_i64]),
     "ispa_stats_create": (ctypes.c_int, [ctypes.POINTER(_c_p), _c_p, _c_sz, _c_i32, _c_i32, _c_i64, _c_p]),
     "ispa_stats_reset": (ctypes.c_int, [_c_p]),
@@ -1033,4 +1058,267 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
             _ptr(lse), ws.data_ptr(), nbytes, _stream(dev))
 
     _check(_on(dev, call), "ispa_attn_shared")
+    return out, lse
+
+
+# ---- norms of heads with the position rotation, a cache in 4 bits ----
+def _head_vectors(dev, head_dim, **vectors):
+    for name, t in vectors.items():
+        if t is not None:
+            _vector(t, name, dev, (head_dim,))
+
+
+def _heads_of(q, k, n_heads, n_kv_heads):
+    """The row distances of q and k, the key heads and the head's values."""
+    ld_q = _strided_rows(q, "q")
+    rows, hidden = q.shape
+    n_kv_heads = n_heads if n_kv_heads is None else int(n_kv_heads)
+    if n_heads < 1 or hidden % n_heads or n_kv_heads < 1:
+        raise ValueError("hidden size is not a multiple of n_heads")
+    head_dim = hidden // n_heads
+    ld_k = 0
+    if k is not None:
+        ld_k = _strided_rows(k, "k", q.device, q.dtype, n_kv_heads * head_dim)
+        if k.shape[0] != rows:
+            raise ValueError("q and k must have the same number of rows")
+    return ld_q, ld_k, n_kv_heads, head_dim
+
+
+def _rows_output(t, name, like, dtype):
+    """The caller's output of like's shape, or a new one of dtype, and its row distance."""
+    if t is None:
+        t = like.new_empty(like.shape, dtype=dtype)
+    ld = _strided_rows(t, name, like.device, None, like.shape[1])
+    if t.shape[0] != like.shape[0]:
+        raise ValueError(f"{name} must have shape {tuple(like.shape)}")
+    return t, ld
+
+
+def norm_rotary(q, k, positions, freqs, n_heads, n_kv_heads=None, norm="rms", q_weight=None, k_weight=None, q_bias=None,
+                k_bias=None, eps=1e-6, axes=None, interleaved=True, amplitude=1.0, q_out=None, k_out=None,
+                out_dtype=None):
+    """Norms of the queries' and keys' heads with the position rotation in the same pass
+    (ispa_norm_rotary): every head of q and k is normalised ("rms" or "layer") over its own
+    values, times weight, plus bias, then turned as by rotary.
+
+    q [rows, n_heads * head_dim], k [rows, n_kv_heads * head_dim] or None, bf16 or fp32 of one
+    dtype, rows may be apart; weights and biases fp32 [head_dim]; positions, freqs, axes as for
+    rotary. Returns (q_out, k_out), of out_dtype (None: of q's dtype); q_out=q and k_out=k work
+    in place. Nothing is recorded for autograd: norm_rotary_backward is the gradient.
+    """
+    L = lib()
+    if norm not in ("rms", "layer"):
+        raise ValueError("norm must be 'rms' or 'layer'")
+    ld_q, ld_k, n_kv_heads, head_dim = _heads_of(q, k, int(n_heads), n_kv_heads)
+    dev, rows = q.device, q.shape[0]
+    if k is None and (k_weight is not None or k_bias is not None or k_out is not None):
+        raise ValueError("k_weight, k_bias and k_out need k")
+    _head_vectors(dev, head_dim, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias, k_bias=k_bias)
+    pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
+    dtype = out_dtype or (q_out.dtype if q_out is not None else q.dtype)
+    q_out, ld_qo = _rows_output(q_out, "q_out", q, dtype)
+    ld_ko = 0
+    if k is not None:
+        k_out, ld_ko = _rows_output(k_out, "k_out", k, q_out.dtype)
+        if k_out.dtype != q_out.dtype:
+            raise TypeError("q_out and k_out must share a dtype")
+    if rows == 0:
+        return q_out, k_out
+    st = _on(dev, lambda: L.ispa_norm_rotary(
+        q.data_ptr(), ld_q, _ptr(k), ld_k, _DT[q.dtype], _NORMS[norm], _ptr(q_weight), _ptr(k_weight), _ptr(q_bias),
+        _ptr(k_bias), float(eps), q_out.data_ptr(), ld_qo, _ptr(k_out), ld_ko, _DT[q_out.dtype], positions.data_ptr(),
+        freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)), float(amplitude), rows,
+        int(n_heads), n_kv_heads, head_dim, _stream(dev)))
+    _check(st, "ispa_norm_rotary")
+    return q_out, k_out
+
+
+def norm_rotary_backward(d_q_out, d_k_out, q, k, positions, freqs, n_heads, n_kv_heads=None, norm="rms", q_weight=None,
+                         k_weight=None, q_bias=None, k_bias=None, eps=1e-6, axes=None, interleaved=True,
+                         amplitude=1.0):
+    """The gradients of norm_rotary (ispa_norm_rotary_backward) from those of its outputs, as
+    a dict: "q", "k" (where k is given), and of "q_weight", "k_weight", "q_bias", "k_bias" those
+    that are given. q and k as the forward pass had them."""
+    L = lib()
+    if norm not in ("rms", "layer"):
+        raise ValueError("norm must be 'rms' or 'layer'")
+    ld_q, ld_k, n_kv_heads, head_dim = _heads_of(q, k, int(n_heads), n_kv_heads)
+    dev, rows = q.device, q.shape[0]
+    if (k is None) != (d_k_out is None) or (k is None and (k_weight is not None or k_bias is not None)):
+        raise ValueError("d_k_out goes with k, and k_weight and k_bias need it")
+    _head_vectors(dev, head_dim, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias, k_bias=k_bias)
+    ld_gq = _strided_rows(d_q_out, "d_q_out", dev, None, q.shape[1])
+    ld_gk = _strided_rows(d_k_out, "d_k_out", dev, d_q_out.dtype, k.shape[1]) if k is not None else 0
+    if d_q_out.shape[0] != rows or (k is not None and d_k_out.shape[0] != rows):
+        raise ValueError("the gradients must have the rows of q and k")
+    pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
+    out = {"q": q.new_empty(q.shape)}
+    if k is not None:
+        out["k"] = k.new_empty(k.shape)
+    new = torch.empty if rows else torch.zeros
+    for name, t in (("q_weight", q_weight), ("k_weight", k_weight), ("q_bias", q_bias), ("k_bias", k_bias)):
+        if t is not None:
+            out[name] = new((head_dim,), dtype=torch.float32, device=dev)
+    if rows == 0:
+        return out
+    nbytes, ws = 0, None
+    if len(out) > 1 + (k is not None):
+        nbytes = L.ispa_norm_rotary_backward_workspace_bytes(rows, int(n_heads), n_kv_heads if k is not None else 0,
+                                                             head_dim)
+        ws = q.new_empty(nbytes, dtype=torch.uint8)
+    grad = lambda name: _ptr(out.get(name))
+    st = _on(dev, lambda: L.ispa_norm_rotary_backward(
+        d_q_out.data_ptr(), ld_gq, _ptr(d_k_out), ld_gk, _DT[d_q_out.dtype], q.data_ptr(), ld_q, _ptr(k), ld_k,
+        _DT[q.dtype], _NORMS[norm], _ptr(q_weight), _ptr(k_weight), float(eps), grad("q"), q.shape[1], grad("k"),
+        k.shape[1] if k is not None else 0, grad("q_weight"), grad("k_weight"), grad("q_bias"), grad("k_bias"),
+        positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
+        float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _ptr(ws), nbytes, _stream(dev)))
+    _check(st, "ispa_norm_rotary_backward")
+    return out
+
+
+def kv4_cache(n_pages, page_size, n_kv_heads, head_dim, device=None):
+    """An empty 4-bit cache (zeros): uint8 [n_pages, n_kv_heads, bytes of a page of a head], for
+    page_size tokens a page, a power of two from 32 to 65536 (layout: include/ispa.h)."""
+    nbytes = lib().ispa_kv4_page_bytes(int(page_size), int(head_dim))
+    if nbytes == 0:
+        raise IspaError(ISPA_ERR_INVALID_ARG, "ispa_kv4_page_bytes")
+    return torch.zeros((int(n_pages), int(n_kv_heads), nbytes), dtype=torch.uint8,
+                       device="cuda" if device is None else device)
+
+
+def _kv4(cache, page_table, head_dim, dev=None):
+    """Checks a 4-bit cache and its table; returns (n_pages, page_size, n_req, max_pages, n_kv_heads)."""
+    _require(cache, "cache", torch.uint8, dev, ndim=3)
+    _require(page_table, "page_table", torch.int32, cache.device)
+    n_pages, n_kv_heads, nbytes = cache.shape
+    per = head_dim + head_dim // 16
+    if nbytes % per:
+        raise ValueError(f"cache must hold whole tokens of {per} bytes a head: it is one of another head_dim")
+    n_req, max_pages = page_table.shape
+    return n_pages, nbytes // per, n_req, max_pages, n_kv_heads
+
+
+def kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, n_kv_heads=None, norm="none", q_weight=None,
+               k_weight=None, q_bias=None, k_bias=None, eps=1e-6, axes=None, interleaved=True, amplitude=1.0, q_out=None,
+               q_start=None):
+    """New tokens into a 4-bit cache in one launch (ispa_kv4_append): q normalised and rotated
+    into q_out, k normalised and rotated into the place of its row, v beside it.
+
+    q [rows, n_heads * head_dim], k and v [rows, n_kv_heads * head_dim] of one dtype; norm
+    "none", "rms" or "layer" over each head of q and k, with fp32 [head_dim] weights and biases;
+    cache as from kv4_cache, page_table int32 [n_req, max_pages]; slots int64 [rows] as from
+    slot_map with the capacity max_pages * page_size. Returns q_out (bf16 by default; q_out=q
+    works in place). A row without a place (slot -1, a page outside the pool) reaches no cache,
+    its query is turned all the same; with q_start (slot_map's, int32 [n_req + 1]) a given q_out
+    keeps what it has in the padding behind q_start[n_req].
+    """
+    L = lib()
+    if norm not in _NORMS:
+        raise ValueError(f"norm must be one of {sorted(_NORMS)}")
+    ld_q, ld_k, n_kv_heads, head_dim = _heads_of(q, k, int(n_heads), n_kv_heads)
+    dev, rows = q.device, q.shape[0]
+    ld_v = _strided_rows(v, "v", dev, q.dtype, n_kv_heads * head_dim)
+    if k is None or v.shape[0] != rows:
+        raise ValueError("q, k and v must have the same number of rows")
+    _head_vectors(dev, head_dim, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias, k_bias=k_bias)
+    pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
+    n_pages, page_size, n_req, max_pages, heads = _kv4(cache, page_table, head_dim, dev)
+    if heads != n_kv_heads:
+        raise ValueError("cache must have n_kv_heads heads")
+    _require(slots, "slots", torch.int64, dev, ndim=1)
+    if slots.shape[0] != rows:
+        raise ValueError("slots must have an entry for every row")
+    n_real = None  # (a new q_out has nothing to keep: every row turns)
+    if q_start is not None:
+        _require(q_start, "q_start", torch.int32, dev, ndim=1)
+        if q_start.shape[0] != n_req + 1:
+            raise ValueError("q_start must have one entry more than page_table has requests")
+        if q_out is not None:
+            n_real = q_start.data_ptr() + 4 * n_req
+    q_out, ld_out = _rows_output(q_out, "q_out", q, torch.bfloat16)
+    if rows == 0:
+        return q_out
+    st = _on(dev, lambda: L.ispa_kv4_append(
+        q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _DT[q.dtype], _NORMS[norm], _ptr(q_weight),
+        _ptr(k_weight), _ptr(q_bias), _ptr(k_bias), float(eps), q_out.data_ptr(), _DT[q_out.dtype], ld_out,
+        cache.data_ptr(), n_pages, page_size, page_table.data_ptr(), n_req, max_pages, slots.data_ptr(), n_real,
+        positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
+        float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _stream(dev)))
+    _check(st, "ispa_kv4_append")
+    return q_out
+
+
+def kv4_read(cache, page_table, slots, head_dim, out_dtype=torch.bfloat16, k=None, v=None):
+    """Rows of a 4-bit cache as the values that they hold (ispa_kv4_read): (k, v), each [rows,
+    n_kv_heads * head_dim] of out_dtype, of the places that slots (int64 [rows], as for
+    kv4_append) stands for; zeros where there is no place. For example the rows of a history
+    that a LocalKV or a bf16 cache takes over."""
+    L = lib()
+    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, int(head_dim))
+    dev = cache.device
+    _require(slots, "slots", torch.int64, dev, ndim=1)
+    rows, kv = slots.shape[0], n_kv_heads * int(head_dim)
+    if k is None:
+        k = cache.new_empty((rows, kv), dtype=out_dtype)
+    if v is None:
+        v = torch.empty_like(k)
+    for name, t in (("k", k), ("v", v)):
+        _float_tensor(t, name, dev)
+        if t.shape != (rows, kv) or t.dtype != k.dtype:
+            raise ValueError(f"k and v must have shape {(rows, kv)} and one dtype")
+    if rows == 0:
+        return k, v
+    st = _on(dev, lambda: L.ispa_kv4_read(
+        cache.data_ptr(), n_pages, page_size, page_table.data_ptr(), n_req, max_pages, slots.data_ptr(), rows,
+        n_kv_heads, int(head_dim), k.data_ptr(), v.data_ptr(), _DT[k.dtype], _stream(dev)))
+    _check(st, "ispa_kv4_read")
+    return k, v
+
+
+def attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, max_q=None, scale=0.0, out=None, lse=None,
+             out_dtype=torch.bfloat16, need_lse=True):
+    """Attention of a batch of requests over a 4-bit cache (ispa_attn_kv4).
+
+    q [n_rows, n_heads * d] bf16, request b's rows from q_start[b] on; cache and page_table as
+    for kv4_append, the key heads are the cache's; q_start int32 [n_req + 1] and cache_lens
+    int32 [n_req] on the device: request b sees its places [0, cache_lens[b]). max_q: most rows
+    of a request, a hint (None: the mean). Returns (out, lse); rows behind q_start[n_req] are
+    left as they were (uninitialised where out or lse is not given).
+    """
+    L = lib()
+    ld_q = _strided_rows(q, "q", None, torch.bfloat16)
+    dev = q.device
+    rows, hidden = q.shape
+    n_heads = int(n_heads)
+    if n_heads < 1 or hidden % n_heads:
+        raise ValueError("hidden size must be a multiple of n_heads")
+    head_dim = hidden // n_heads
+    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, head_dim, dev)
+    if n_heads % n_kv_heads:
+        raise ValueError("n_heads must be a multiple of the cache's heads")
+    _require(q_start, "q_start", torch.int32, dev, ndim=1)
+    _require(cache_lens, "cache_lens", torch.int32, dev, ndim=1)
+    if cache_lens.shape[0] != n_req or q_start.shape[0] != n_req + 1:
+        raise ValueError("cache_lens must have an entry for every request of page_table, and q_start one more")
+    max_q = int(max_q) if max_q is not None else max(1, -(-rows // n_req))
+    if out is None:
+        out = q.new_empty((rows, hidden), dtype=out_dtype)
+    ld_out = _strided_rows(out, "out", dev, None, hidden)
+    if out.shape[0] != rows:
+        raise ValueError(f"out must have shape {(rows, hidden)}")
+    if lse is not None or need_lse:
+        lse = _output(lse, "lse", q, (n_heads, rows))
+    if rows == 0:
+        return out, lse
+
+    def call():
+        nbytes = L.ispa_attn_kv4_workspace_bytes(page_size, max_pages, n_req, rows, max_q, n_heads, n_kv_heads, head_dim)
+        ws = q.new_empty(max(nbytes, 1), dtype=torch.uint8)
+        return L.ispa_attn_kv4(
+            q.data_ptr(), ld_q, cache.data_ptr(), n_pages, page_size, page_table.data_ptr(), max_pages,
+            q_start.data_ptr(), cache_lens.data_ptr(), n_req, rows, max_q, n_heads, n_kv_heads, head_dim, float(scale),
+            out.data_ptr(), _DT[out.dtype], ld_out, _ptr(lse), ws.data_ptr(), nbytes, _stream(dev))
+
+    _check(_on(dev, call), "ispa_attn_kv4")
     return out, lse

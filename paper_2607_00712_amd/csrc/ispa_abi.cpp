@@ -1074,3 +1074,350 @@ int ispa_attn_shared(const void* q, int64_t ld_q, const void* k_prefix, const vo
 }
 
 }  // extern "C"
+
+// ---- norms of heads with the rotation, the 4-bit cache ----
+namespace {
+
+// What the calls over heads share: angles by rotary_common, norm and vectors.
+int heads_common(int32_t norm, const float* q_weight, const float* k_weight, const float* q_bias, const float* k_bias,
+                 float eps, const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                 int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                 int32_t n_kv_heads, int32_t head_dim, int32_t x_dtype, int32_t out_dtype, ispa::NormRotaryArgs* a) {
+  ispa::RotaryArgs r;
+  const int st = rotary_common(positions, freqs, axis_pairs, n_axes, rotary_dim, interleaved, amplitude, rows, n_heads,
+                               n_kv_heads, head_dim, x_dtype, out_dtype, &r);
+  if (st != ISPA_OK) return st;
+  if (norm < ISPA_NORM_NONE || norm > ISPA_NORM_RMS) return ISPA_ERR_UNSUPPORTED;
+  if (norm == ISPA_NORM_NONE && (q_weight || k_weight || q_bias || k_bias)) return ISPA_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || isinf(eps) || any_misaligned({q_weight, k_weight, q_bias, k_bias})) return ISPA_ERR_INVALID_ARG;
+  memset(a, 0, sizeof(*a));
+  a->x_f32 = r.x_f32;
+  a->out_f32 = r.out_f32;
+  a->norm = norm;
+  a->q_weight = q_weight;
+  a->k_weight = k_weight;
+  a->q_bias = q_bias;
+  a->k_bias = k_bias;
+  a->eps = eps;
+  a->positions = positions;
+  a->freqs = freqs;
+  a->n_axes = n_axes;
+  memcpy(a->axis_end, r.axis_end, sizeof(a->axis_end));
+  a->rotary_dim = rotary_dim;
+  a->head_dim = head_dim;
+  a->n_heads = n_heads;
+  a->n_kv_heads = n_kv_heads;
+  a->interleaved = r.interleaved;
+  a->amplitude = amplitude;
+  a->rows = rows;
+  return ISPA_OK;
+}
+
+bool kv4_sizes(int64_t page_size, int64_t max_pages, int32_t n_req, int32_t n_kv_heads, ispa::Kv4Cache* c) {
+  if (page_size < 32 || page_size > 65536 || (page_size & (page_size - 1)) != 0) return false;
+  if (max_pages < 1 || max_pages > 0x7fffffff / page_size || n_req < 1 || n_kv_heads < 1) return false;
+  memset(c, 0, sizeof(*c));
+  while (((int64_t)1 << c->log_page) < page_size) ++c->log_page;
+  c->max_pages = (int)max_pages;
+  c->n_req = n_req;
+  c->n_kv_heads = n_kv_heads;
+  return true;
+}
+int kv4_common(const void* cache, int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req,
+               int64_t max_pages, int32_t n_kv_heads, int32_t head_dim, ispa::Kv4Cache* c, Span* pages, Span* table) {
+  if (head_dim != 64 && head_dim != 128) return ISPA_ERR_UNSUPPORTED;
+  if (!kv4_sizes(page_size, max_pages, n_req, n_kv_heads, c)) return ISPA_ERR_INVALID_ARG;
+  if (n_pages < 1 || n_pages > 0x7fffffff || (int64_t)n_kv_heads * head_dim > (1 << 20)) return ISPA_ERR_INVALID_ARG;
+  if (!cache || !page_table || any_misaligned({cache}) || any_misaligned({page_table}, 3u)) return ISPA_ERR_INVALID_ARG;
+  const int64_t page = ispa::kv4_page_bytes(c->log_page, head_dim) * n_kv_heads;
+  if (n_pages > ((int64_t)1 << 44) / page) return ISPA_ERR_INVALID_ARG;
+  c->pages = (uint8_t*)cache;
+  c->table = page_table;
+  c->n_pages = (int)n_pages;
+  *pages = {cache, (size_t)(n_pages * page)};
+  *table = {page_table, (size_t)n_req * max_pages * 4};
+  return ISPA_OK;
+}
+
+bool kv4_attn_sizes(int32_t n_rows, int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    const ispa::Kv4Cache& c, ispa::Kv4AttnArgs* a) {
+  if (head_dim != 64 && head_dim != 128) return false;
+  if (n_rows < 0 || max_q < 1 || n_heads < 1 || n_heads % n_kv_heads != 0) return false;
+  if ((int64_t)n_heads * head_dim > (1 << 20)) return false;
+  if ((int64_t)n_rows * n_heads > (1 << 26) || (int64_t)c.n_req * n_kv_heads > (1 << 20)) return false;
+  memset(a, 0, sizeof(*a));
+  a->c = c;
+  a->n_rows = n_rows;
+  a->max_q = max_q;
+  a->group = n_heads / n_kv_heads;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
+                     const float* q_weight, const float* k_weight, const float* q_bias, const float* k_bias, float eps,
+                     void* q_out, int64_t ld_qo, void* k_out, int64_t ld_ko, int32_t out_dtype,
+                     const int32_t* positions, const double* freqs, const int32_t* axis_pairs, int32_t n_axes,
+                     int32_t rotary_dim, int32_t interleaved, float amplitude, int64_t rows, int32_t n_heads,
+                     int32_t n_kv_heads, int32_t head_dim, hipStream_t stream) {
+  ispa::NormRotaryArgs a;
+  const int st = heads_common(norm, q_weight, k_weight, q_bias, k_bias, eps, positions, freqs, axis_pairs, n_axes,
+                              rotary_dim, interleaved, amplitude, rows, n_heads, k ? n_kv_heads : 1, head_dim, x_dtype,
+                              out_dtype, &a);
+  if (st != ISPA_OK) return st;
+  if (norm == ISPA_NORM_NONE) return ISPA_ERR_UNSUPPORTED;
+  const int64_t hq = (int64_t)n_heads * head_dim, hk = k ? (int64_t)n_kv_heads * head_dim : 0;
+  if (!q || !q_out || ((k != nullptr) != (k_out != nullptr)) || (!k && (k_weight || k_bias))) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q, k, q_out, k_out}) || bad_ld(ld_q, hq) || bad_ld(ld_qo, hq) ||
+      (k && (bad_ld(ld_k, hk) || bad_ld(ld_ko, hk))))
+    return ISPA_ERR_INVALID_ARG;
+  const size_t es = dtype_size(x_dtype), eo = dtype_size(out_dtype), vec = (size_t)head_dim * 4;
+  const Rows in[] = {{q, rows, ld_q, hq, es}, {k, rows, ld_k, hk, es}},
+             out[] = {{q_out, rows, ld_qo, hq, eo}, {k_out, rows, ld_ko, hk, eo}};
+  for (int i = 0; i < (k ? 2 : 1); ++i) {
+    const Span so{out[i].p, rows_bytes(rows, out[i].ld, out[i].width, eo)};
+    if (meets(so, {{positions, (size_t)rows * n_axes * 4}, {freqs, (size_t)rotary_dim * 4}, {q_weight, vec},
+                   {k_weight, vec}, {q_bias, vec}, {k_bias, vec}}))
+      return ISPA_ERR_INVALID_ARG;
+    for (int j = 0; j < (k ? 2 : 1); ++j)
+      if (!(i == j && out[i].p == in[i].p && es == eo && out[i].ld == in[i].ld) && rows_meet(out[i], in[j]))
+        return ISPA_ERR_INVALID_ARG;
+  }
+  if (k && rows_meet(out[0], out[1])) return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_qo = ld_qo;
+  a.ld_ko = ld_ko;
+  return ispa::launch_norm_rotary(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (rows < 1 || rows >= (1 << 24) || n_heads < 1 || n_kv_heads < 0 || head_dim < 16 || head_dim > 256 ||
+      head_dim % 16 != 0 || (int64_t)n_heads * head_dim > (1 << 20) || (int64_t)n_kv_heads * head_dim > (1 << 20))
+    return 0;
+  const size_t blocks = ispa::norm_rotary_blocks(rows, n_heads, head_dim) +
+                        (n_kv_heads ? ispa::norm_rotary_blocks(rows, n_kv_heads, head_dim) : 0);
+  return round_up(blocks * 2 * head_dim * sizeof(float), kWsAlign);
+}
+
+int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_k_out, int64_t ld_gk, int32_t g_dtype,
+                              const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
+                              const float* q_weight, const float* k_weight, float eps, void* d_q, int64_t ld_dq,
+                              void* d_k, int64_t ld_dk, float* d_q_weight, float* d_k_weight, float* d_q_bias,
+                              float* d_k_bias, const int32_t* positions, const double* freqs,
+                              const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                              float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  ispa::NormRotaryArgs a;
+  const int st = heads_common(norm, q_weight, k_weight, nullptr, nullptr, eps, positions, freqs, axis_pairs, n_axes,
+                              rotary_dim, interleaved, amplitude, rows, n_heads, k ? n_kv_heads : 1, head_dim, x_dtype,
+                              g_dtype, &a);
+  if (st != ISPA_OK) return st;
+  if (norm == ISPA_NORM_NONE) return ISPA_ERR_UNSUPPORTED;
+  const int64_t hq = (int64_t)n_heads * head_dim, hk = k ? (int64_t)n_kv_heads * head_dim : 0;
+  if (!d_q_out || !q || !d_q || ((k != nullptr) != (d_k_out != nullptr)) || ((k != nullptr) != (d_k != nullptr)))
+    return ISPA_ERR_INVALID_ARG;
+  if (!k && (k_weight || d_k_weight || d_k_bias)) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({d_q_out, d_k_out, q, k, d_q, d_k, d_q_weight, d_k_weight, d_q_bias, d_k_bias}))
+    return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_gq, hq) || bad_ld(ld_q, hq) || bad_ld(ld_dq, hq) ||
+      (k && (bad_ld(ld_gk, hk) || bad_ld(ld_k, hk) || bad_ld(ld_dk, hk))))
+    return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  const bool sums = d_q_weight || d_k_weight || d_q_bias || d_k_bias;
+  const size_t need = sums ? ispa_norm_rotary_backward_workspace_bytes(rows, n_heads, k ? n_kv_heads : 0, head_dim) : 0;
+  if (sums && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return ISPA_ERR_INVALID_ARG;
+  if (!sums) workspace = nullptr;
+  const size_t es = dtype_size(x_dtype), eg = dtype_size(g_dtype), vec = (size_t)head_dim * 4;
+  const int tensors = k ? 2 : 1;
+  const Rows grad[] = {{d_q_out, rows, ld_gq, hq, eg}, {d_k_out, rows, ld_gk, hk, eg}},
+             in[] = {{q, rows, ld_q, hq, es}, {k, rows, ld_k, hk, es}},
+             out[] = {{d_q, rows, ld_dq, hq, es}, {d_k, rows, ld_dk, hk, es}};
+  const Span small[] = {{positions, (size_t)rows * n_axes * 4}, {freqs, (size_t)rotary_dim * 4}, {q_weight, vec},
+                        {k_weight, vec}};
+  const Span vectors[] = {{d_q_weight, vec}, {d_k_weight, vec}, {d_q_bias, vec}, {d_k_bias, vec}, {workspace, need}};
+  auto span = [](const Rows& r) { return Span{r.p, rows_bytes(r.rows, r.ld, r.width, r.esz)}; };
+  for (int i = 0; i < tensors; ++i) {
+    for (const Span& s : small)
+      if (meets(span(out[i]), {s})) return ISPA_ERR_INVALID_ARG;
+    for (int j = 0; j < tensors; ++j) {
+      if (rows_meet(out[i], in[j])) return ISPA_ERR_INVALID_ARG;
+      if (!(i == j && out[i].p == grad[i].p && es == eg && out[i].ld == grad[i].ld) && rows_meet(out[i], grad[j]))
+        return ISPA_ERR_INVALID_ARG;
+    }
+  }
+  if (k && rows_meet(out[0], out[1])) return ISPA_ERR_INVALID_ARG;
+  for (int i = 0; i < 5; ++i) {
+    for (int j = 0; j < tensors; ++j)
+      if (meets(vectors[i], {span(grad[j]), span(in[j]), span(out[j])})) return ISPA_ERR_INVALID_ARG;
+    for (const Span& s : small)
+      if (meets(vectors[i], {s})) return ISPA_ERR_INVALID_ARG;
+    for (int j = i + 1; j < 5; ++j)
+      if (meets(vectors[i], {vectors[j]})) return ISPA_ERR_INVALID_ARG;
+  }
+  a.d_q = d_q_out;
+  a.d_k = d_k_out;
+  a.q = q;
+  a.k = k;
+  a.q_out = d_q;
+  a.k_out = d_k;
+  a.ld_dq = ld_gq;
+  a.ld_dk = ld_gk;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_qo = ld_dq;
+  a.ld_ko = ld_dk;
+  a.d_q_weight = d_q_weight;
+  a.d_k_weight = d_k_weight;
+  a.d_q_bias = d_q_bias;
+  a.d_k_bias = d_k_bias;
+  a.part = (float*)workspace;
+  return ispa::launch_norm_rotary_backward(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+size_t ispa_kv4_page_bytes(int64_t page_size, int32_t head_dim) {
+  ispa::Kv4Cache c;
+  if ((head_dim != 64 && head_dim != 128) || !kv4_sizes(page_size, 1, 1, 1, &c)) return 0;
+  return (size_t)ispa::kv4_page_bytes(c.log_page, head_dim);
+}
+
+int ispa_kv4_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                    int32_t x_dtype, int32_t norm, const float* q_weight, const float* k_weight, const float* q_bias,
+                    const float* k_bias, float eps, void* q_out, int32_t out_dtype, int64_t ld_out, void* cache,
+                    int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req, int64_t max_pages,
+                    const int64_t* slots, const int32_t* n_real, const int32_t* positions, const double* freqs,
+                    const int32_t* axis_pairs, int32_t n_axes, int32_t rotary_dim, int32_t interleaved,
+                    float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    hipStream_t stream) {
+  ispa::Kv4AppendArgs a;
+  memset(&a, 0, sizeof(a));
+  int st = heads_common(norm, q_weight, k_weight, q_bias, k_bias, eps, positions, freqs, axis_pairs, n_axes, rotary_dim,
+                        interleaved, amplitude, rows, n_heads, n_kv_heads, head_dim, x_dtype, out_dtype, &a.t);
+  if (st != ISPA_OK) return st;
+  Span pages, table;
+  st = kv4_common(cache, n_pages, page_size, page_table, n_req, max_pages, n_kv_heads, head_dim, &a.c, &pages, &table);
+  if (st != ISPA_OK) return st;
+  const int64_t hidden = (int64_t)n_heads * head_dim, kv = (int64_t)n_kv_heads * head_dim;
+  if (!q || !k || !v || !q_out || !slots) return ISPA_ERR_INVALID_ARG;
+  if (any_misaligned({q, k, v, q_out}) || any_misaligned({slots}, 7u) || any_misaligned({n_real}, 3u))
+    return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_q, hidden) || bad_ld(ld_k, kv) || bad_ld(ld_v, kv) || bad_ld(ld_out, hidden))
+    return ISPA_ERR_INVALID_ARG;
+  const size_t es = dtype_size(x_dtype), eo = dtype_size(out_dtype), vec = (size_t)head_dim * 4;
+  const Span so{q_out, rows_bytes(rows, ld_out, hidden, eo)};
+  const Span small[] = {table, {slots, (size_t)rows * 8}, {n_real, 4}, {positions, (size_t)rows * n_axes * 4},
+                        {freqs, (size_t)rotary_dim * 4}, {q_weight, vec}, {k_weight, vec}, {q_bias, vec}, {k_bias, vec}};
+  for (const Span& s : small)
+    if (meets(pages, {s}) || meets(so, {s})) return ISPA_ERR_INVALID_ARG;
+  if (meets(pages, {{q, rows_bytes(rows, ld_q, hidden, es)}, {k, rows_bytes(rows, ld_k, kv, es)},
+                    {v, rows_bytes(rows, ld_v, kv, es)}, so}))
+    return ISPA_ERR_INVALID_ARG;
+  const Rows to{q_out, rows, ld_out, hidden, eo};
+  if (rows_meet(to, {k, rows, ld_k, kv, es}) || rows_meet(to, {v, rows, ld_v, kv, es})) return ISPA_ERR_INVALID_ARG;
+  if (!(q_out == q && x_dtype == out_dtype && ld_q == ld_out) && rows_meet(to, {q, rows, ld_q, hidden, es}))
+    return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.t.q = q;
+  a.t.k = k;
+  a.t.ld_q = ld_q;
+  a.t.ld_k = ld_k;
+  a.t.q_out = q_out;
+  a.t.ld_qo = ld_out;
+  a.v = v;
+  a.ld_v = ld_v;
+  a.slots = slots;
+  a.n_real = n_real;
+  return ispa::launch_kv4_append(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req,
+                  int64_t max_pages, const int64_t* slots, int64_t rows, int32_t n_kv_heads, int32_t head_dim, void* k,
+                  void* v, int32_t out_dtype, hipStream_t stream) {
+  if (bad_dtype(out_dtype)) return ISPA_ERR_UNSUPPORTED;
+  ispa::Kv4ReadArgs a;
+  memset(&a, 0, sizeof(a));
+  Span pages, table;
+  const int st = kv4_common(cache, n_pages, page_size, page_table, n_req, max_pages, n_kv_heads, head_dim, &a.c, &pages,
+                            &table);
+  if (st != ISPA_OK) return st;
+  const int64_t kv = (int64_t)n_kv_heads * head_dim;
+  if (!slots || !k || !v || any_misaligned({k, v}) || any_misaligned({slots}, 7u)) return ISPA_ERR_INVALID_ARG;
+  if (rows < 0 || rows >= ((int64_t)1 << 34) / kv) return ISPA_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)rows * kv * dtype_size(out_dtype);
+  const Span sk{k, bytes}, sv{v, bytes}, ss{slots, (size_t)rows * 8};
+  if (meets(sk, {sv, pages, table, ss}) || meets(sv, {pages, table, ss})) return ISPA_ERR_INVALID_ARG;
+  if (rows == 0) return ISPA_OK;
+  a.slots = slots;
+  a.rows = rows;
+  a.head_dim = head_dim;
+  a.out_f32 = out_dtype == ISPA_DTYPE_F32;
+  a.k = k;
+  a.v = v;
+  return ispa::launch_kv4_read(a, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+size_t ispa_attn_kv4_workspace_bytes(int64_t page_size, int64_t max_pages, int32_t n_req, int32_t n_rows, int32_t max_q,
+                                     int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  ispa::Kv4Cache c;
+  ispa::Kv4AttnArgs a;
+  if (!kv4_sizes(page_size, max_pages, n_req, n_kv_heads, &c) ||
+      !kv4_attn_sizes(n_rows, max_q, n_heads, n_kv_heads, head_dim, c, &a) || n_rows == 0)
+    return 0;
+  return round_up(ispa::attn_kv4_plan(&a, head_dim), kWsAlign);
+}
+
+int ispa_attn_kv4(const void* q, int64_t ld_q, const void* cache, int64_t n_pages, int64_t page_size,
+                  const int32_t* page_table, int64_t max_pages, const int32_t* q_start, const int32_t* cache_lens,
+                  int32_t n_req, int32_t n_rows, int32_t max_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                  float scale, void* out, int32_t out_dtype, int64_t ld_out, float* lse, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream) {
+  if (bad_dtype(out_dtype)) return ISPA_ERR_UNSUPPORTED;
+  ispa::Kv4Cache c;
+  Span pages, table;
+  const int st = kv4_common(cache, n_pages, page_size, page_table, n_req, max_pages, n_kv_heads, head_dim, &c, &pages,
+                            &table);
+  if (st != ISPA_OK) return st;
+  ispa::Kv4AttnArgs a;
+  if (!kv4_attn_sizes(n_rows, max_q, n_heads, n_kv_heads, head_dim, c, &a)) return ISPA_ERR_INVALID_ARG;
+  if (!(scale == scale) || isinf(scale)) return ISPA_ERR_INVALID_ARG;
+  const int64_t hidden = (int64_t)n_heads * head_dim;
+  if (!q || !out || !q_start || !cache_lens || any_misaligned({q, out}) || any_misaligned({q_start, cache_lens, lse}, 3u))
+    return ISPA_ERR_INVALID_ARG;
+  if (bad_ld(ld_q, hidden) || bad_ld(ld_out, hidden)) return ISPA_ERR_INVALID_ARG;
+  if (n_rows == 0) return ISPA_OK;
+  a.out_bf16 = out_dtype == ISPA_DTYPE_BF16;
+  const size_t need = round_up(ispa::attn_kv4_plan(&a, head_dim), kWsAlign);
+  if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return ISPA_ERR_INVALID_ARG;
+  const Span sq{q, rows_bytes(n_rows, ld_q, hidden, 2)}, so{out, rows_bytes(n_rows, ld_out, hidden, dtype_size(out_dtype))},
+      sl{lse, (size_t)n_heads * n_rows * 4}, sw{workspace, need};
+  const Span in[] = {pages, table, {q_start, ((size_t)n_req + 1) * 4}, {cache_lens, (size_t)n_req * 4}};
+  for (const Span& s : in)
+    if (meets(so, {s}) || meets(sl, {s}) || meets(sw, {s})) return ISPA_ERR_INVALID_ARG;
+  if (meets(so, {sl, sw}) || meets(sl, {sw, sq}) || meets(sw, {sq}) ||
+      rows_meet({out, n_rows, ld_out, hidden, dtype_size(out_dtype)}, {q, n_rows, ld_q, hidden, 2}))
+    return ISPA_ERR_INVALID_ARG;
+  a.q = (const uint16_t*)q;
+  a.ld_q = ld_q;
+  a.q_start = q_start;
+  a.lens = cache_lens;
+  a.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)head_dim);
+  a.scale_log2 = a.scale * 1.4426950408889634f;
+  a.out = out;
+  a.ld_out = ld_out;
+  a.lse = lse;
+  a.part_o = (float*)workspace;
+  a.part_stat = (float*)((char*)workspace + a.stat_offset);
+  a.run = (ispa::Kv4Run*)((char*)workspace + a.run_offset);
+  a.n_runs = (int*)(a.run + a.most_runs);
+  return ispa::launch_attn_kv4(a, head_dim, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -233,6 +233,91 @@ struct SlotArgs {
 };
 hipError_t launch_slot_map(const SlotArgs& a, hipStream_t stream);
 
+// ---- norms of heads with the rotation (norm_rotary.hip), 4-bit cache (kv4.hip) ----
+struct NormRotaryArgs {
+  const void *q, *k;  // k null: q alone
+  void *q_out, *k_out;
+  const void *d_q, *d_k;  // backward: gradients of q_out and k_out; q_out and k_out are those of q and k
+  int x_f32, out_f32;     // of q and k; of q_out and k_out (backward: of d_q and d_k)
+  int64_t ld_q, ld_k, ld_qo, ld_ko, ld_dq, ld_dk;
+  int norm;  // ISPA_NORM_*
+  const float *q_weight, *k_weight, *q_bias, *k_bias;  // [head_dim], each may be null
+  float eps;
+  const int32_t* positions;  // [rows, n_axes]
+  const double* freqs;       // [rotary_dim / 2]
+  int n_axes;
+  int axis_end[kRotaryAxes - 1];
+  int rotary_dim, head_dim, n_heads, n_kv_heads, interleaved;
+  float amplitude;
+  int64_t rows;
+  // backward
+  float *d_q_weight, *d_k_weight, *d_q_bias, *d_k_bias;  // [head_dim], each may be null
+  float* part;                                           // sums of each workgroup, or null
+  // set by the launch: rows of a workgroup at a time, lanes to a head; backward: workgroups
+  // of q and of k
+  int tokens, lanes, q_blocks, k_blocks;
+};
+hipError_t launch_norm_rotary(NormRotaryArgs a, hipStream_t stream);
+// workgroups of the backward pass over a tensor of `heads` heads
+int norm_rotary_blocks(int64_t rows, int heads, int head_dim);
+hipError_t launch_norm_rotary_backward(NormRotaryArgs a, hipStream_t stream);
+
+// A 4-bit cache: page (p, key head h) is kv4_page_bytes bytes at ((p n_kv_heads + h) page
+// bytes): the codes of its keys and of its values [page_size][head_dim / 2], then the
+// exponents [page_size][2][head_dim / 32].
+struct Kv4Cache {
+  uint8_t* pages;
+  const int32_t* table;  // [n_req, max_pages]
+  int n_pages, n_req, max_pages, log_page, n_kv_heads;
+};
+__host__ __device__ inline int64_t kv4_page_bytes(int log_page, int head_dim) {
+  return (int64_t)(head_dim + head_dim / 16) << log_page;
+}
+struct Kv4AppendArgs {
+  NormRotaryArgs t;  // q, k, q_out
+  const void* v;
+  int64_t ld_v;
+  Kv4Cache c;
+  const int64_t* slots;  // [rows]
+  const int32_t* n_real;  // count of real rows on the device; null: all
+};
+hipError_t launch_kv4_append(Kv4AppendArgs a, hipStream_t stream);
+struct Kv4ReadArgs {
+  Kv4Cache c;
+  const int64_t* slots;
+  int64_t rows;
+  int head_dim, out_f32;
+  void *k, *v;
+};
+hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t stream);
+
+// ---- attention over a 4-bit cache (attn_kv4.hip) ----
+// A run's first item: its units, where the run begins, and the rows that it stands for.
+struct Kv4Run {
+  int64_t item, end, begin;
+  int head, row0, first, rows;
+};
+struct Kv4AttnArgs {
+  const uint16_t* q;
+  int64_t ld_q, ld_out;
+  Kv4Cache c;
+  const int32_t *q_start, *lens;
+  int n_rows, max_q, group;  // group = n_heads / n_kv_heads
+  float scale, scale_log2;
+  void* out;
+  int out_bf16;
+  float* lse;
+  // set by the plan: rows of a tile, runs at most, units of a run at least, the parts
+  int tile_rows, most_runs, least_units;
+  size_t stat_offset, run_offset;
+  float *part_o, *part_stat;
+  Kv4Run* run;
+  int* n_runs;
+};
+// fills the plan and returns the workspace bytes
+size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim);
+hipError_t launch_attn_kv4(const Kv4AttnArgs& a, int head_dim, hipStream_t stream);
+
 // ---- attention over a shared prefix (attn_shared.hip) ----
 constexpr int kSharedPlans = 64;
 struct SharedArgs {

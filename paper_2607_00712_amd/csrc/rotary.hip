@@ -23,7 +23,7 @@
 // slot_map: the place of each row of a ragged batch in its request's cache, by a
 // search of the request starts; one launch serves every layer of a step (2.2 us for
 // 64 requests of a token, 3 for four of 1560).
-#include "ispa_internal.h"
+#include "head_units.h"
 
 namespace ispa {
 namespace {
@@ -31,55 +31,6 @@ namespace {
 constexpr int kRThreads = 256;
 constexpr int kRMaxTokens = 8;   // tokens of a workgroup
 constexpr int kRMaxPairs = 128;  // rotary_dim / 2
-
-template <class T>
-using Global = __attribute__((address_space(1))) T;
-
-// Eight values as they lie in memory, so that several loads are in flight at once; p the
-// tensor's address, e an element
-template <bool F32>
-struct Chunk {
-  f32x4 lo, hi;
-  __device__ __forceinline__ void load(uintptr_t p, int64_t e) {
-    const auto* at = (const Global<f32x4>*)(p + e * 4);
-    lo = at[0];
-    hi = at[1];
-  }
-  __device__ __forceinline__ void values(float (&r)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r[i] = lo[i];
-      r[4 + i] = hi[i];
-    }
-  }
-};
-template <>
-struct Chunk<false> {
-  bf16x8 b;
-  __device__ __forceinline__ void load(uintptr_t p, int64_t e) { b = *(const Global<bf16x8>*)(p + e * 2); }
-  __device__ __forceinline__ void values(float (&r)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (float)b[i];
-  }
-};
-__device__ __forceinline__ void rstore8(uintptr_t p, bool f32, int64_t e, const float (&x)[8]) {
-  if (f32) {
-    auto* at = (Global<f32x4>*)(p + e * 4);
-    at[0] = f32x4{x[0], x[1], x[2], x[3]};
-    at[1] = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-    bf16x8 a;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = (__bf16)x[i];
-    *(Global<bf16x8>*)(p + e * 2) = a;
-  }
-}
-
-// One unit: 16 values of a head as they lie in memory
-template <bool F32>
-struct Unit {
-  Chunk<F32> c0, c1;
-};
 
 // What stands in place of a row's slot where it has none: its query turns all the same (a
 // token that its cache does not keep attends like the others), or the row is left alone.
@@ -100,12 +51,9 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   const int u = threadIdx.x % per_head;  // place in the head
   const int heads = a.n_heads + (a.k ? 2 * a.n_kv_heads : 0);  // of a row
   const int end = (int)threadIdx.x < step * per_head ? n * heads : 0;
-  // a unit's two chunks of 8 and the first pairs of their angles: the same place in both
-  // halves of the rotated part (lanes side by side then read side by side, in either order
-  // of the pairs), or side by side behind it
-  const bool turned = u < (a.rotary_dim >> 4);
-  const int e0 = turned ? 8 * u : 16 * u, e1 = turned ? pairs + 8 * u : 16 * u + 8;
-  const int p0 = a.interleaved ? 4 * u : 8 * u, p1 = a.interleaved ? (pairs >> 1) + 4 * u : 8 * u + 4;
+  const UnitPlace at_unit = unit_place(u, a.rotary_dim, a.interleaved);
+  const bool turned = at_unit.turned;
+  const int e0 = at_unit.e0, e1 = at_unit.e1;
   // in registers for certain: a choice between arguments is otherwise made by a load from
   // the chosen one's place, which every unit's load then waits for
   uintptr_t q = (uintptr_t)a.q, k = (uintptr_t)a.k, v = (uintptr_t)a.v;
@@ -153,32 +101,7 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
     float x[8], y[8];
     p.c0.values(x);
     p.c1.values(y);
-    if (turn) {
-      const float2* at = cs + t * pairs;
-      float2 c[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = at[p0 + i];
-        c[4 + i] = at[p1 + i];
-      }
-      if (a.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float xa = x[2 * i], xb = x[2 * i + 1], ya = y[2 * i], yb = y[2 * i + 1];
-          x[2 * i] = xa * c[i].x - xb * c[i].y;
-          x[2 * i + 1] = xa * c[i].y + xb * c[i].x;
-          y[2 * i] = ya * c[4 + i].x - yb * c[4 + i].y;
-          y[2 * i + 1] = ya * c[4 + i].y + yb * c[4 + i].x;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float xa = x[i], xb = y[i];
-          x[i] = xa * c[i].x - xb * c[i].y;
-          y[i] = xa * c[i].y + xb * c[i].x;
-        }
-      }
-    }
+    if (turn) turn_unit(x, y, cs + t * pairs, at_unit, a.interleaved);
     rstore8(dst, f32, d + e0, x);
     rstore8(dst, f32, d + e1, y);
   };
@@ -188,9 +111,7 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   fetch(w, now);  // on its way while the angles are formed
   for (int i = threadIdx.x; i < n * pairs; i += kRThreads) {
     const int t = i / pairs, j = i - t * pairs;
-    int axis = 0;
-#pragma unroll
-    for (int k = 0; k < kRotaryAxes - 1; ++k) axis += j >= a.axis_end[k] ? 1 : 0;
+    const int axis = pair_axis(a.axis_end, j);
     const double turns = (double)a.positions[(row0 + t) * a.n_axes + axis] * a.freqs[j] * 0.15915494309189535;
     const float f = 2.0f * (float)(turns - rint(turns));  // in half turns, within [-1, 1]
     float s, c;
