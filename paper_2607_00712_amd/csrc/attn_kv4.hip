@@ -15,46 +15,24 @@
 // its part (weighted values, sum and reference of each row) in the workspace, two at most, and a
 // second launch joins them by Eq. 11-12, in order: the result does not depend on the order of
 // execution.
+#include "attn_rows.h"
 #include "kv4_units.h"
 
-#include <math.h>
-
+#ifndef ISPA_NB
+#define ISPA_NB 2
+#endif
+#ifndef ISPA_NW
+#define ISPA_NW 2
+#endif
 namespace ispa {
 namespace {
 
-constexpr int kABlk = 32;  // keys of a unit
-constexpr int kAWaves = 4;
-constexpr int kAThreads = kAWaves * 64;
-constexpr float kAFar = 1024.f;  // a lane's sum of weights of a unit that moves the softmax reference
+constexpr int kAXcds = 8;
+constexpr int kJoinThreads = 512;
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef ISPA_LDS char lds_char;
+typedef ISPA_LDS char lds_byte;
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
-
-// 64 x 16 (or 4) bytes from HBM to LDS at `lds` + 16 (4) lane: lane i's from byte voff of the
-// descriptor, zero past its end. In assembly, so that the compiler's LDS reads wait for LDS
-// reads alone; the statement has no register outputs, and arrival is waited for by count.
-// (m0 is written here alone: nothing that the compiler makes of these kernels uses it.)
-__device__ __forceinline__ void load16_to_lds(i32x4 desc, int voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(desc), "s"(lds)
-               : "memory");
-}
-__device__ __forceinline__ void load4_to_lds(i32x4 desc, int voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(desc), "s"(lds)
-               : "memory");
-}
-template <int N>
-__device__ __forceinline__ void loads_left() {
-  static_assert(N >= 0 && N <= 63, "vmcnt range");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
-}
-__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ i32x4 descriptor(const uint8_t* p, int bytes) {
-  const uint64_t u = (uint64_t)(uintptr_t)p;
-  return i32x4{(int)(uint32_t)u, (int)(uint32_t)(u >> 32) & 0xffff, bytes, 0x00020000};
-}
 
 // Values that are the same in all lanes of a wave, in scalar registers; `fixed` reads memory
 // that no kernel writes meanwhile (a scalar load where the address is the wave's).
@@ -82,42 +60,68 @@ __device__ __forceinline__ Request request_of(const Kv4AttnArgs& a, int total, i
   const int64_t len = held < 0 ? 0 : held < capacity ? held : capacity;
   r.len = (int)len;
   // (a request without keys has a unit without keys, which writes its zeros)
-  r.blocks = len == 0 ? 1 : (int)((len + kABlk - 1) / kABlk);
+  r.blocks = len == 0 ? 1 : (int)((len + kBlk - 1) / kBlk);
   return r;
 }
 __device__ __forceinline__ int64_t units_of(const Kv4AttnArgs& a, const Request& r) {
   return (int64_t)a.c.n_kv_heads * r.tiles * r.blocks;
 }
 
-// Runs that T units are cut into, and where run g begins.
-__host__ __device__ __forceinline__ int64_t runs_of(int64_t units, int most, int least_units) {
-  const int64_t n = (units + least_units - 1) / least_units;
-  return n < most ? n : most;
+// a / b for the same a and b in all lanes, mostly small: a 64-bit division takes 0.4 us of a
+// run's start.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+  return a / b;
 }
+// Runs that the line is cut into: the first `longer` of them of each + 1 units, the others of each.
+struct Cut {
+  int64_t runs, each, longer;
+  __device__ __forceinline__ Cut(int64_t units, int most, int least_units) {
+    runs = divide(units + least_units - 1, least_units);
+    runs = runs < most ? runs : most;
+    each = runs ? divide(units, runs) : 0;
+    longer = units - each * runs;
+  }
+  __device__ __forceinline__ int64_t begin(int64_t run) const { return run * each + (run < longer ? run : longer); }
+  // the run that unit u lies in
+  __device__ __forceinline__ int64_t run_of(int64_t u) const {
+    const int64_t in_longer = longer * (each + 1);
+    return u < in_longer ? divide(u, each + 1) : longer + divide(u - in_longer, each);
+  }
+};
 
+// A request, and its first unit and item.
+struct Start {
+  int64_t unit;
+  int b, item;
+};
 // A place in the line: a block of an item.
 template <int TR>
 struct Walk {
   int b, head, tile, block;
   Request r;
   int64_t item;  // first unit of the item
+  int number;    // of the item
 
-  // from unit u, in request b whose first unit is `base`
-  __device__ __forceinline__ void start(const Kv4AttnArgs& a, int total, int b0, int64_t base, int64_t u) {
-    b = b0;
+  // from unit u, in the request of `s`
+  __device__ __forceinline__ void start(const Kv4AttnArgs& a, int total, const Start& s, int64_t u) {
+    b = uniform(s.b);
+    const int64_t base = uniform(s.unit);
     r = request_of<TR>(a, total, b);
     int64_t i = u - base;
     const int64_t per = (int64_t)r.tiles * r.blocks;
-    head = (int)(i / per);
+    head = (int)divide(i, per);
     i -= head * per;
-    tile = (int)(i / r.blocks);
+    tile = (int)divide(i, r.blocks);
     block = (int)(i - (int64_t)tile * r.blocks);
     item = u - block;
+    number = uniform(s.item) + head * r.tiles + tile;
   }
   // to the next block, of the next item behind the last one
   __device__ __forceinline__ void next(const Kv4AttnArgs& a, int total) {
     if (++block < r.blocks) return;
     item += r.blocks;
+    ++number;
     block = 0;
     if (++tile < r.tiles) return;
     tile = 0;
@@ -130,62 +134,122 @@ struct Walk {
   }
 };
 
-// What a workgroup finds out first: the units in all, the runs, and where its own begin.
+// What a workgroup finds out first: the units in all, the runs, and the requests that its own
+// runs begin in. (With XCDS the runs that share keys, one after the other, are on one XCD, which
+// takes every eighth workgroup.)
 struct Line {
-  int64_t units, runs;
+  Cut cut;
+  int64_t first;  // the workgroup's first run
 };
-template <int TR>
-__device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, int first_run, int n_runs, int (&start_b)[kAWaves],
-                                          int64_t (&start_base)[kAWaves]) {
-  __shared__ int64_t waves[kAWaves];
+template <int TR, int N, bool XCDS>
+__device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start (&starts)[N]) {
+  __shared__ int64_t wave_units[kShWaves];
+  __shared__ int wave_items[kShWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int b0 = (int)((int64_t)a.c.n_req * threadIdx.x / kAThreads), b1 = (int)((int64_t)a.c.n_req * (threadIdx.x + 1) / kAThreads);
+  const int b0 = (int)((int64_t)a.c.n_req * threadIdx.x / kShThreads), b1 = (int)((int64_t)a.c.n_req * (threadIdx.x + 1) / kShThreads);
   int64_t own = 0;
-  for (int b = b0; b < b1; ++b) own += units_of(a, request_of<TR>(a, total, b));
+  int own_items = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Request r = request_of<TR>(a, total, b);
+    own += units_of(a, r);
+    own_items += a.c.n_kv_heads * r.tiles;
+  }
   int64_t upto = own;  // inclusive, over the wave
+  int items = own_items;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const int64_t x = __shfl_up(upto, d);
-    if (lane >= d) upto += x;
+    const int y = __shfl_up(items, d);
+    if (lane >= d) {
+      upto += x;
+      items += y;
+    }
   }
-  if (lane == 63) waves[wave] = upto;
+  if (lane == 63) {
+    wave_units[wave] = upto;
+    wave_items[wave] = items;
+  }
   __syncthreads();
   int64_t before = upto - own;
-  Line l{0, 0};
-  for (int w = 0; w < kAWaves; ++w) {
-    if (w < wave) before += waves[w];
-    l.units += waves[w];
+  items -= own_items;
+  int64_t units = 0;
+  for (int w = 0; w < kShWaves; ++w) {
+    if (w < wave) {
+      before += wave_units[w];
+      items += wave_items[w];
+    }
+    units += wave_units[w];
   }
-  l.units = uniform(l.units);
-  l.runs = runs_of(l.units, a.most_runs, a.least_units);
-  for (int i = 0; i < n_runs; ++i) {
-    if (first_run + i >= l.runs) break;
-    const int64_t u = l.units * (first_run + i) / l.runs;
+  units = uniform(units);
+  Line l{Cut(units, a.most_runs, a.least_units), (int64_t)blockIdx.x * N};
+  if (XCDS) {
+    const int64_t per = (l.cut.runs + kAXcds - 1) / kAXcds;
+    l.first = blockIdx.x / kAXcds < per ? blockIdx.x % kAXcds * per + blockIdx.x / kAXcds : l.cut.runs;
+  }
+  for (int i = 0; i < N; ++i) {
+    if (l.first + i >= l.cut.runs) break;
+    const int64_t u = l.cut.begin(l.first + i);
     if (u < before || u >= before + own) continue;
     int64_t at = before;
+    int item = items;
     for (int b = b0; b < b1; ++b) {
-      const int64_t n = units_of(a, request_of<TR>(a, total, b));
+      const Request r = request_of<TR>(a, total, b);
+      const int64_t n = units_of(a, r);
       if (u < at + n) {
-        start_b[i] = b;
-        start_base[i] = at;
+        starts[i] = Start{at, b, item};
         break;
       }
       at += n;
+      item += a.c.n_kv_heads * r.tiles;
     }
+  }
+  if (blockIdx.x == 0) {  // for the join
+    if (threadIdx.x == 0) {
+      a.line[0] = units;
+    }
+    if (threadIdx.x == kShThreads - 1) a.line[1] = items + own_items;
   }
   __syncthreads();
   return l;
 }
 
+// An item's first part is told by the run that it begins in.
+template <int TR>
+__device__ __forceinline__ void tell_item(const Kv4AttnArgs& a, int64_t run, const Walk<TR>& w) {
+  Kv4Item r;
+  r.begin = w.item;
+  r.end = w.item + w.r.blocks;
+  r.run = run;
+  r.head = w.head;
+  r.row0 = w.tile * TR;
+  r.first = w.r.first;
+  r.rows = w.r.rows;
+  a.items[w.number] = r;
+}
+
+// Which keys of a block there are, and where: the bytes of its page and its row there. A block
+// without keys reads as keys of page 0, none of them valid.
+struct Block {
+  const uint8_t* base;
+  int row, keys;
+};
+__device__ __forceinline__ Block block_at(const Kv4AttnArgs& a, int b, int head, int len, int block, int64_t page_bytes) {
+  Block r{a.c.pages, 0, 0};
+  const int64_t key = (int64_t)block * kBlk;
+  if (key >= len) return r;
+  const int page = fixed(a.c.table, (int64_t)b * a.c.max_pages + (key >> a.c.log_page));
+  if ((unsigned)page >= (unsigned)a.c.n_pages) return r;  // keys of a page that there is not are not attended
+  r.base += ((int64_t)page * a.c.n_kv_heads + head) * page_bytes;
+  r.row = (int)(key & (((int64_t)1 << a.c.log_page) - 1));
+  r.keys = len - key < kBlk ? (int)(len - key) : kBlk;
+  return r;
+}
+
 // ---- narrow tiles: a run to a wave ----
 template <int D>
 struct NCfg {
-  static constexpr int codeBytes = kABlk * D / 2;  // keys' or values' codes of a block
-  static constexpr int scaleAt = 2 * codeBytes;
-  static constexpr int slotBytes = 2 * codeBytes + 256;
-  static constexpr int loads = 2 * codeBytes / 1024 + 1;
-  static constexpr int steps = D / 32;    // k steps of K Q^T
-  static constexpr int dBlocks = D / 16;  // output blocks
+  static constexpr int steps = D / 32;           // k steps of K Q^T
+  static constexpr int dBlocks = D / 16;         // output blocks
   static constexpr int stageBytes = 16 * D * 2;  // values of 16 keys in bf16
 };
 
@@ -202,51 +266,65 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// The blocks of a run, loaded ahead of their use into a ring of NB slots of the wave's own.
-template <int D, int TR, int NB>
-struct Feeder {
-  using C = NCfg<D>;
-  Walk<TR> w;
-  int64_t left;        // units to load
-  uint64_t valid = 0;  // keys of the blocks in the ring, 8 bits each, the oldest lowest
-  uint32_t ring;       // LDS address
-  int lane;
+// A block's codes and powers on their way from HBM, a lane's as the products take them: of keys
+// 16 i + lane % 16 the quarter lane / 16, and 16 bytes (a block of 32 values) of a key's values.
+template <int D>
+struct Raw {
+  uint32_t k[2][D / 32], v[D / 64][4];
+  uint8_t ke[2], ve[D / 64];
+  int keys;
+};
+template <class T>
+using Global = __attribute__((address_space(1))) const T;
 
-  __device__ __forceinline__ void load(const Kv4AttnArgs& a, int total, int slot) {
-    int nv = 0, row = 0;
-    const uint8_t* base = a.c.pages;
+// The blocks of a run in order.
+template <int D, int TR>
+struct Feeder {
+  Walk<TR> w;
+  int64_t left;  // units to fetch
+  uint32_t k_at, v_at, ke_at, ve_at;  // the lane's bytes in a block
+
+  __device__ __forceinline__ void start(const Walk<TR>& walk, int64_t n, int lane) {
+    constexpr int kPer = D / 32;
+    w = walk;
+    left = n;
+    k_at = (lane & 15) * (D / 2) + (lane >> 4) * (D / 8);
+    v_at = lane * 16;
+    ke_at = (lane & 15) * (D / 16) + (lane >> 4) * D / 128;
+    ve_at = lane / kPer * (D / 16) + D / 32 + lane % kPer;
+  }
+  __device__ __forceinline__ void fetch(const Kv4AttnArgs& a, int total, Raw<D>& to) {
     const int64_t size = (int64_t)1 << a.c.log_page;
+    Block b{a.c.pages, 0, 0};
     if (left > 0) {
-      const int64_t key = (int64_t)w.block * kABlk;
-      nv = w.r.len - key < kABlk ? (int)(w.r.len - key) : kABlk;
-      if (nv > 0) {
-        const int page = fixed(a.c.table, (int64_t)w.b * a.c.max_pages + (key >> a.c.log_page));
-        row = (int)(key & (size - 1));
-        if ((unsigned)page < (unsigned)a.c.n_pages)
-          base += ((int64_t)page * a.c.n_kv_heads + w.head) * kv4_page_bytes(a.c.log_page, D);
-        else
-          nv = 0;  // keys of a page that there is not are not attended
-      }
+      b = block_at(a, w.b, w.head, w.r.len, w.block, kv4_page_bytes(a.c.log_page, D));
       w.next(a, total);
       --left;
     }
-    // behind the last valid key: zeros, whatever the page holds there
-    const i32x4 dk = descriptor(base + (int64_t)row * (D / 2), nv * (D / 2)),
-                dv = descriptor(base + (size + row) * (D / 2), nv * (D / 2)),
-                ds = descriptor(base + size * D + row * (D / 16), nv * (D / 16));
-    const uint32_t to = ring + slot * C::slotBytes;
+    to.keys = b.keys;
+    const auto *k = (Global<uint8_t>*)(b.base + (int64_t)b.row * (D / 2)),
+               *v = (Global<uint8_t>*)(b.base + (size + b.row) * (D / 2)),
+               *e = (Global<uint8_t>*)(b.base + size * D + (int64_t)b.row * (D / 16));
 #pragma unroll
-    for (int i = 0; i < C::codeBytes / 1024; ++i) {
-      load16_to_lds(dk, lane * 16 + i * 1024, to + i * 1024);
-      load16_to_lds(dv, lane * 16 + i * 1024, to + C::codeBytes + i * 1024);
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (D == 128) {
+        const u32x4 x = *(Global<u32x4>*)(k + (k_at + 8u * D * i));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to.k[i][j] = x[j];
+      } else {
+        const u32x2 x = *(Global<u32x2>*)(k + (k_at + 8u * D * i));
+        to.k[i][0] = x[0];
+        to.k[i][1] = x[1];
+      }
+      to.ke[i] = e[ke_at + (uint32_t)D * i];
     }
-    load4_to_lds(ds, lane * 4, to + C::scaleAt);
-    valid |= (uint64_t)nv << (8 * (NB - 1));
-  }
-  __device__ __forceinline__ int take() {
-    const int nv = (int)(valid & 255);
-    valid >>= 8;
-    return nv;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const u32x4 x = *(Global<u32x4>*)(v + (v_at + 1024u * i));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) to.v[i][j] = x[j];
+      to.ve[i] = e[ve_at + (uint32_t)D * i];
+    }
   }
 };
 
@@ -256,7 +334,7 @@ struct NWave {
   using C = NCfg<D>;
   f32x4 acc[RB][C::dBlocks];  // O^T: values 16 d + 4 (lane / 16) .. + 3
   bf16x8 q[RB][C::steps];     // Q^T operand: step s holds values D / 4 (lane / 16) + 8 s .. + 7
-  float m[RB], l[RB];         // reference (raw scores), sum of the weights of the lane's keys
+  float m[RB], l[RB], lr[RB];  // reference (raw scores), sums of the weights of the lane's keys and of the rounded ones
 };
 
 template <int D, int RB>
@@ -274,7 +352,7 @@ __device__ __forceinline__ void start_item(const Kv4AttnArgs& a, NWave<D, RB>& s
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) s.acc[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     s.m[b] = -INFINITY;
-    s.l[b] = 0.f;
+    s.l[b] = s.lr[b] = 0.f;
   }
 }
 
@@ -298,14 +376,11 @@ __device__ __forceinline__ void finish_item(const Kv4AttnArgs& a, NWave<D, RB>& 
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const int in_tile = b * 16 + (lane & 15), row = w.tile * 16 * RB + in_tile;
-    const float l = quad_sum(s.l[b]);
+    const float l = quad_sum(s.l[b]), lr = quad_sum(s.lr[b]);
     if (row >= w.r.rows) continue;
     if (slot >= 0) {
       const int64_t at = slot * 16 * RB + in_tile;
-      if (g == 0) {
-        a.part_stat[2 * at] = s.m[b];
-        a.part_stat[2 * at + 1] = l;
-      }
+      if (g == 0) *(f32x4*)(a.part_stat + 4 * at) = f32x4{s.m[b], l, lr, 0.f};
 #pragma unroll
       for (int d = 0; d < C::dBlocks; ++d) *(f32x4*)(a.part_o + at * D + 16 * d + 4 * g) = s.acc[b][d];
       continue;
@@ -313,7 +388,7 @@ __device__ __forceinline__ void finish_item(const Kv4AttnArgs& a, NWave<D, RB>& 
     const int64_t token = w.r.first + row / a.group;
     const int head = w.head * a.group + row % a.group;
     if (a.lse && g == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(s.m[b], l, a.scale);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = lr == 0.f ? 0.f : 1.0f / lr;
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) put4(a, token, head * D + 16 * d + 4 * g, s.acc[b][d] * inv);
   }
@@ -331,216 +406,469 @@ __device__ __forceinline__ void follow(const Kv4AttnArgs& a, NWave<D, RB>& s, co
     // (a row whose scores are all -inf so far keeps its zeros)
     const float alpha = s.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s.m[b] - m) * a.scale_log2);
     s.l[b] *= alpha;
+    s.lr[b] *= alpha;
 #pragma unroll
     for (int d = 0; d < NCfg<D>::dBlocks; ++d) s.acc[b][d] *= alpha;
     s.m[b] = m;
   }
 }
 
-// The weights as product operands: rounded to bf16, and what the rounding left, rounded
-// again: 16 bits of a weight.
-struct Weights {
-  bf16x8 hi, lo;
-};
-__device__ __forceinline__ float weights(const f32x4 (&sc)[2], float m, float scale_log2, Weights& p) {
+// The weights as product operands: rounded to bf16, and (F = 2) what the rounding left,
+// rounded again; and their sums, of the weights and (F = 1) of the rounded ones.
+template <int F>
+__device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float scale_log2, bf16x8 (&p)[F], float& sum,
+                                          float& rounded) {
   const float mc = m == -INFINITY ? 0.f : m * scale_log2;
-  float sum[2] = {0.f, 0.f};
+  float s[2] = {0.f, 0.f};
+  rounded = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float e = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], scale_log2, -mc));
-    sum[i & 1] += e;
-    const __bf16 hi = (__bf16)e;
-    p.hi[i] = hi;
-    p.lo[i] = (__bf16)(e - (float)hi);
+  for (int i = 0; i < 8; i += 2) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], scale_log2, -mc));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][(i & 3) + 1], scale_log2, -mc));
+    s[0] += e0;
+    s[1] += e1;
+    const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
+    p[0][i] = hi[0];
+    p[0][i + 1] = hi[1];
+    if constexpr (F == 2) {
+      p[1][i] = (__bf16)(e0 - (float)hi[0]);
+      p[1][i + 1] = (__bf16)(e1 - (float)hi[1]);
+    } else {
+      rounded = __builtin_amdgcn_fdot2_f32_bf16(hi, bf16x2{(__bf16)1.f, (__bf16)1.f}, rounded, false);
+    }
   }
-  return sum[0] + sum[1];
+  sum = s[0] + s[1];
 }
 
-// Workgroups to a compute unit: two, or one where a wave needs more than half of a SIMD's registers.
-constexpr int narrow_groups(int head_dim, int rb) { return head_dim == 128 && rb == 4 ? 1 : 2; }
-constexpr int narrow_ring(int head_dim, int rb) { return narrow_groups(head_dim, rb) == 1 ? 6 : 3; }
-
-template <int D, int RB, int NB>
-__global__ __launch_bounds__(kAThreads, narrow_groups(D, RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
+// One block: scores, weights, values.
+template <int D, int RB, int F>
+__device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s, const Raw<D>& raw, lds_byte* stage, int lane) {
   using C = NCfg<D>;
-  constexpr int TR = 16 * RB;
-  __shared__ __attribute__((aligned(1024))) char smem[kAWaves * (NB * C::slotBytes + C::stageBytes)];
-  __shared__ int start_b[kAWaves];
-  __shared__ int64_t start_base[kAWaves];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kPer = D / 32;  // blocks of 32 values of a key
   const int g = lane >> 4, m16 = lane & 15;
-  const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
-  const int run = blockIdx.x * kAWaves + wave;
-  const Line line = find_line<TR>(a, total, blockIdx.x * kAWaves, kAWaves, start_b, start_base);
-  if (run == 0 && lane == 0) *a.n_runs = (int)line.runs;
-  if (run >= line.runs) return;
-  const int64_t u0 = line.units * run / line.runs, u1 = line.units * (run + 1) / line.runs;
-  Walk<TR> w;
-  w.start(a, total, uniform(start_b[wave]), uniform(start_base[wave]), u0);
-  if (lane == 0) {
-    Kv4Run r;
-    r.item = w.item;
-    r.end = w.item + w.r.blocks;
-    r.begin = u0;
-    r.head = w.head;
-    r.row0 = w.tile * TR;
-    r.first = w.r.first;
-    r.rows = w.r.rows;
-    a.run[run] = r;
+  // S^T = K Q^T: lane (g, m16) holds row m16's scores of keys 16 i + 4 g .. + 3
+  f32x4 sc[RB][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float scale = kv4_scale(raw.ke[i]);
+#pragma unroll
+    for (int j = 0; j < C::steps; ++j) {
+      const bf16x8 k = kv4_values(raw.k[i][j], scale);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) sc[b][i] = mfma16(k, s.q[b][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[b][i]);
+    }
   }
-  lds_char* ring = (lds_char*)smem + wave * (NB * C::slotBytes + C::stageBytes);
-  lds_char* stage = ring + NB * C::slotBytes;
-  Feeder<D, TR, NB> f;
-  f.w = w;
-  f.left = u1 - u0;
-  f.ring = (uint32_t)(uintptr_t)ring;
-  f.lane = lane;
-  loads_left<0>();
+  uint32_t vc[D / 64][4], ve[D / 64];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    f.valid >>= 8;
-    f.load(a, total, i);
+  for (int i = 0; i < D / 64; ++i) {
+    ve[i] = raw.ve[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vc[i][j] = raw.v[i][j];
   }
-  NWave<D, RB> s;
-  start_item<D, RB>(a, s, w, lane);
-  int slot = 0;
-  for (int64_t u = u0; u < u1; ++u) {
-    loads_left<(NB - 1) * C::loads>();
-    lds_char* at = ring + slot * C::slotBytes;
-    // the block's codes and powers into registers, then its slot is free
-    uint32_t kc[2][D / 32], vc[D / 64][4];
-    uint32_t ke[2], ve[D / 64];
+  if (raw.keys < kBlk) {  // behind the last valid key: no scores, and zeros whatever the page holds there
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if constexpr (D == 128) {
-        const u32x4 x = *(ISPA_LDS const u32x4*)(at + (16 * i + m16) * 64 + g * 16);
+    for (int i = 0; i < 8; ++i)
+      if (16 * (i >> 2) + 4 * g + (i & 3) >= raw.keys) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kc[i][j] = x[j];
-      } else {
-        const u32x2 x = *(ISPA_LDS const u32x2*)(at + (16 * i + m16) * 32 + g * 8);
-        kc[i][0] = x[0];
-        kc[i][1] = x[1];
+        for (int b = 0; b < RB; ++b) sc[b][i >> 2][i & 3] = -INFINITY;
       }
-      ke[i] = *(ISPA_LDS const uint8_t*)(at + C::scaleAt + (16 * i + m16) * (D / 16) + g * D / 128);
-    }
-    // values: 16 bytes of a key's codes are a block of 32 values
-    constexpr int kPer = D / 32;  // blocks of a key
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const u32x4 x = *(ISPA_LDS const u32x4*)(at + C::codeBytes + i * 1024 + lane * 16);
+    for (int i = 0; i < D / 64; ++i)
+      if ((i * 64 + lane) / kPer >= raw.keys) {
+        ve[i] = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) vc[i][j] = x[j];
-      const int key = (i * 64 + lane) / kPer;
-      ve[i] = *(ISPA_LDS const uint8_t*)(at + C::scaleAt + key * (D / 16) + D / 32 + lane % kPer);
-    }
-    lds_done();
-    const int nv = f.take();
-    f.load(a, total, slot);
-    slot = slot + 1 == NB ? 0 : slot + 1;
+        for (int j = 0; j < 4; ++j) vc[i][j] = 0;
+      }
+  }
+  bf16x8 p[RB][F];
+  float sum[RB], rounded[RB];
+  bool far = false;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b], rounded[b]);
+    far = far || sum[b] > kShFar || s.m[b] == -INFINITY;
+  }
+  if (__any(far)) {
+    follow<D, RB>(a, s, sc);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b], rounded[b]);
+  }
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    s.l[b] += sum[b];
+    s.lr[b] += F == 2 ? sum[b] : rounded[b];
+  }
 
-    // S^T = K Q^T: lane (g, m16) holds row m16's scores of keys 16 i + 4 g .. + 3
-    f32x4 sc[RB][2];
+  // O^T += V^T P^T: the contraction runs over keys 4 g .. + 3 and 16 + 4 g .. + 3 of lane
+  // group g, as the scores lie; V's values of 16 keys at a time go through LDS, where transpose
+  // reads put keys side by side. Chunks of 8 values are swizzled: the reads take 32 bytes of 8
+  // rows at a time, the writes 16 bytes of two (or four) rows.
+  union Operand {
+    s16x4 half[2];
+    bf16x8 v;
+  } v[C::dBlocks];
+  auto swizzle = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float scale = kv4_scale(ke[i]);
+  for (int h = 0; h < 2; ++h) {
+    const int i = D == 128 ? h : 0;
+    const int key = D == 128 ? lane >> 2 : (lane >> 1) - 16 * h, c = 4 * (lane % kPer);
+    if (D == 128 || (lane >> 5) == h) {
+      const float scale = kv4_scale(ve[i]);
 #pragma unroll
-      for (int j = 0; j < C::steps; ++j) {
-        const bf16x8 k = kv4_values(kc[i][j], scale);
-#pragma unroll
-        for (int b = 0; b < RB; ++b) sc[b][i] = mfma16(k, s.q[b][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[b][i]);
-      }
+      for (int j = 0; j < 4; ++j)
+        *(ISPA_LDS bf16x8*)(stage + key * (D * 2) + (((c + j) ^ swizzle(key)) << 4)) = kv4_values(vc[i][j], scale);
     }
-    if (nv < kABlk) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (16 * (i >> 2) + 4 * g + (i & 3) >= nv) {
-#pragma unroll
-          for (int b = 0; b < RB; ++b) sc[b][i >> 2][i & 3] = -INFINITY;
-        }
-    }
-    Weights p[RB];
-    float sum[RB];
-    bool far = false;
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      sum[b] = weights(sc[b], s.m[b], a.scale_log2, p[b]);
-      far = far || sum[b] > kAFar || s.m[b] == -INFINITY;
-    }
-    if (__any(far)) {
-      follow<D, RB>(a, s, sc);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) sum[b] = weights(sc[b], s.m[b], a.scale_log2, p[b]);
-    }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) s.l[b] += sum[b];
-
-    // O^T += V^T P^T: the contraction runs over keys 4 g .. + 3 and 16 + 4 g .. + 3 of lane
-    // group g, as the scores lie; V's values of 16 keys at a time go through LDS, where
-    // transpose reads put keys side by side. Chunks of 8 values are swizzled: the reads take 32
-    // bytes of 8 rows at a time, the writes 16 bytes of two (or four) rows.
-    union Operand {
-      s16x4 half[2];
-      bf16x8 v;
-    } v[C::dBlocks];
-    auto swizzle = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = D == 128 ? h : 0;
-      const int key = D == 128 ? lane >> 2 : (lane >> 1) - 16 * h, c = 4 * (lane % kPer);
-      if (D == 128 || (lane >> 5) == h) {
-        const float scale = kv4_scale(ve[i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *(ISPA_LDS bf16x8*)(stage + key * (D * 2) + (((c + j) ^ swizzle(key)) << 4)) = kv4_values(vc[i][j], scale);
-      }
-      asm volatile("" ::: "memory");  // (the wave's LDS operations are done in order)
-      const int row = 4 * g + (m16 >> 2);
-#pragma unroll
-      for (int d = 0; d < C::dBlocks; ++d)
-        v[d].half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (ISPA_LDS s16x4*)(stage + row * (D * 2) + (((2 * d + ((m16 & 3) >> 1)) ^ swizzle(row)) << 4) + ((m16 & 1) << 3)));
-      asm volatile("" ::: "memory");
-    }
+    asm volatile("" ::: "memory");  // (the wave's LDS operations are done in order)
+    const int row = 4 * g + (m16 >> 2);
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d)
-#pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        s.acc[b][d] = mfma16(v[d].v, p[b].hi, s.acc[b][d]);
-        s.acc[b][d] = mfma16(v[d].v, p[b].lo, s.acc[b][d]);
-      }
-
-    const bool last = w.block + 1 == w.r.blocks;
-    if (last || u + 1 == u1) {
-      const bool whole = last && w.item >= u0;
-      finish_item<D, RB>(a, s, w, whole ? -1 : 2 * (int64_t)run + (w.item >= u0 ? 1 : 0), lane);
-      loads_left<0>();  // (the stores count as loads do)
-      w.next(a, total);
-      if (u + 1 < u1) start_item<D, RB>(a, s, w, lane);
-    } else {
-      ++w.block;
-    }
+      v[d].half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (ISPA_LDS s16x4*)(stage + row * (D * 2) + (((2 * d + ((m16 & 3) >> 1)) ^ swizzle(row)) << 4) + ((m16 & 1) << 3)));
+    asm volatile("" ::: "memory");
   }
-  loads_left<0>();  // the loads behind the end are done with the ring
+#pragma unroll
+  for (int d = 0; d < C::dBlocks; ++d)
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int f = 0; f < F; ++f) s.acc[b][d] = mfma16(v[d].v, p[b][f], s.acc[b][d]);
 }
 
-// Joins the parts of an item that lies in several runs: workgroup x is run x + 1's, and joins
-// if that run begins inside an item whose first part is the run's before it. 16 rows to a
-// workgroup in y.
+// Waves to a SIMD, as the registers allow.
+constexpr int narrow_waves(int head_dim, int rb) { return rb == 4 ? (head_dim == 128 ? 1 : 2) : rb == 2 ? 2 : ISPA_NW; }
+
+template <int D, int RB, int NB, int F>
+__global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
+  using C = NCfg<D>;
+  constexpr int TR = 16 * RB;
+  __shared__ __attribute__((aligned(1024))) char smem[kShWaves * C::stageBytes];
+  __shared__ Start starts[kShWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
+  const int run = blockIdx.x * kShWaves + wave;
+  const Line line = find_line<TR, kShWaves, false>(a, total, starts);
+  if (run >= line.cut.runs) return;
+  const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
+  Walk<TR> w;
+  w.start(a, total, starts[wave], u0);
+  if (lane == 0 && w.block == 0) tell_item(a, run, w);
+  lds_byte* stage = (lds_byte*)smem + wave * C::stageBytes;
+  Feeder<D, TR> f;
+  f.start(w, u1 - u0, lane);
+  Raw<D> raw[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) f.fetch(a, total, raw[i]);
+  NWave<D, RB> s;
+  start_item<D, RB>(a, s, w, lane);
+  for (int64_t u = u0; u < u1;) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (u < u1) {
+        meet_block<D, RB, F>(a, s, raw[i], stage, lane);
+        f.fetch(a, total, raw[i]);
+        ++u;
+        const bool last = w.block + 1 == w.r.blocks;
+        if (last || u == u1) {
+          const bool whole = last && w.item >= u0;
+          finish_item<D, RB>(a, s, w, whole ? -1 : 2 * (int64_t)run + (w.item >= u0 ? 1 : 0), lane);
+          w.next(a, total);
+          if (u < u1) {
+            if (lane == 0) tell_item(a, run, w);
+            start_item<D, RB>(a, s, w, lane);
+          }
+        } else {
+          ++w.block;
+        }
+      }
+    }
+  }
+}
+
+// ---- wide tiles: a run to a workgroup ----
+// Four waves of 64 rows (two row blocks), RG groups of rows times KG groups of keys, as in
+// attention over a bf16 prefix (attn_rows.h): steps of 64 keys in LDS in bf16, four of them in
+// turn. What fills them differs: a thread fetches its share of a step's codes (a quarter of a
+// key, and of its values) two steps ahead into registers and converts it one step ahead, between
+// the matrix instructions of the step before.
 template <int D>
-__global__ __launch_bounds__(256) void attn_kv4_join_kernel(Kv4AttnArgs a, int tile_rows) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
-  __shared__ f32x4 part_o[256];
-  __shared__ float part_m[kGroups], part_l[kGroups];
-  const int run = blockIdx.x + 1, runs = *a.n_runs;
-  if (run >= runs) return;
-  const Kv4Run r = a.run[run];
-  if (r.item >= r.begin || a.run[run - 1].begin > r.item) return;
-  int n = 2;  // parts
-  while (run + n - 1 < runs && a.run[run + n - 1].begin < r.end) ++n;
-  const int rows = r.rows - r.row0 < tile_rows ? r.rows - r.row0 : tile_rows;
-  const int y0 = blockIdx.y * 16, y1 = rows < y0 + 16 ? rows : y0 + 16;
+struct WCfg {
+  static constexpr int step = 2;  // blocks
+  static constexpr int slots = 4;
+  static constexpr int stepBytes = step * SCfg<D>::blockBytes;
+  static constexpr int words = D / 32;  // of 8 codes, a thread's share of a key
+  static constexpr int smem = slots * stepBytes;
+};
+
+// A thread's codes of a step, as they lie in memory, and their powers.
+template <int D>
+struct Share {
+  uint32_t c[2][WCfg<D>::words];  // of the key and of the values
+  uint32_t e[2];
+};
+
+// Where a thread's share of a step goes and comes from.
+template <int D>
+struct Lay {
+  int row[2];     // of its block, for the key and the values
+  int quarter, block;
+  int at[2][WCfg<D>::words];  // bytes in a step
+  __device__ __forceinline__ explicit Lay(int tid) {
+    using C = SCfg<D>;
+    constexpr int W = WCfg<D>::words;
+    const int lane = tid & 63, wave = tid >> 6;
+    block = wave >> 1;
+    quarter = lane & 3;
+    const int r = lane >> 2;
+    row[0] = 16 * (wave & 1) + r;
+    // (rows beside each other 4 apart: their chunks lie in other banks)
+    row[1] = 16 * (wave & 1) + (r & 10) + ((r & 1) << 2) + ((r >> 2) & 1);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      at[0][i] = block * C::blockBytes + row[0] * C::rowBytes + (((W * quarter + i) ^ swizzle_k<D>(row[0])) << 4);
+      at[1][i] = block * C::blockBytes + C::tileBytes + row[1] * C::rowBytes + (((W * quarter + i) ^ swizzle_v<D>(row[1])) << 4);
+    }
+  }
+};
+
+// The blocks of a piece of an item.
+struct Source {
+  int b, head, len, block, end;  // next block to fetch and the piece's end
+};
+
+// The next step's codes on their way; returns the keys of its two blocks (8 bits each). Rows
+// that are no keys come from inside a page all the same and become zeros, whatever it holds.
+template <int D>
+__device__ __forceinline__ int fetch_step(const Kv4AttnArgs& a, Source& src, const Lay<D>& lay, int wave_block, Share<D>& to) {
+  const int64_t size = (int64_t)1 << a.c.log_page, page_bytes = kv4_page_bytes(a.c.log_page, D);
+  Block at[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    at[i] = Block{a.c.pages, 0, 0};
+    if (src.block + i < src.end) at[i] = block_at(a, src.b, src.head, src.len, src.block + i, page_bytes);
+  }
+  const uint8_t* base = wave_block ? at[1].base : at[0].base;
+  const int row = wave_block ? at[1].row : at[0].row;
+  src.block += 2;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint8_t* p = base + (i * size + row + lay.row[i]) * (D / 2) + lay.quarter * (D / 8);
+    if constexpr (D == 128) {
+      const u32x4 x = *(const u32x4*)p;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) to.c[i][j] = x[j];
+    } else {
+      const u32x2 x = *(const u32x2*)p;
+      to.c[i][0] = x[0];
+      to.c[i][1] = x[1];
+    }
+    to.e[i] = base[size * D + (int64_t)(row + lay.row[i]) * (D / 16) + i * (D / 32) + lay.quarter * D / 128];
+  }
+  return at[0].keys | at[1].keys << 8;
+}
+// Word i (keys first) of a share into the step at `to`; nv: keys of the thread's block.
+template <int D>
+__device__ __forceinline__ void convert(const Share<D>& s, const Lay<D>& lay, int nv, lds_byte* to, int i) {
+  constexpr int W = WCfg<D>::words;
+  const int t = i / W, j = i % W;
+  const bool key = lay.row[t] < nv;
+  *(ISPA_LDS bf16x8*)(to + lay.at[t][j]) = kv4_values(key ? s.c[t][j] : 0u, kv4_scale(key ? s.e[t] : 0u));
+}
+
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The blocks of a piece, met by KG = 1 or 2 groups of waves.
+template <int D, int KG, int F>
+__device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w, lds_byte* smem, Source src, int kg, int wave,
+                                           int tid, const Lay<D>& lay) {
+  using C = SCfg<D>;
+  using WC = WCfg<D>;
+  constexpr int RB = 2, KB = WC::step / KG, kWords = 2 * WC::words;
+  const int hh = (tid & 63) >> 5;
+  const int n_steps = (src.end - src.block + WC::step - 1) / WC::step;
+  const int own = wave >> 1;  // the block of a step that this wave converts
+  auto slot = [&](int s) __attribute__((always_inline)) { return smem + (s & (WC::slots - 1)) * WC::stepBytes; };
+  auto mine = [&](int nv) __attribute__((always_inline)) { return nv >> (8 * own) & 255; };
+  Share<D> now, next_share;
+  // steps 0 and 1, and a step of zero values before the first one, whose (zero) weights the
+  // first turn applies
+#pragma unroll
+  for (int i = 0; i < WC::words; ++i) *(ISPA_LDS u32x4*)(slot(-1) + lay.at[1][i]) = u32x4{0, 0, 0, 0};
+  const int nv0 = fetch_step<D>(a, src, lay, own, now);
+  const int nv1 = fetch_step<D>(a, src, lay, own, next_share);
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) convert<D>(now, lay, mine(nv0), slot(0), i);
+  int nv2 = fetch_step<D>(a, src, lay, own, now);
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) convert<D>(next_share, lay, mine(nv1), slot(1), i);
+  int nv_now = nv0, nv_next = nv1;
+  rows_here<D, RB>(w);
+  f32x16 sc[RB];
+  float sum[RB], rounded[RB];
+  bf16x8 v[2 * C::dBlocks];
+  SWeights<F> p[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) p[b].p[f][h] = bf16x8{};
+  lds_barrier();
+  {
+    bf16x8 k[C::slices];
+    read_k<D, RB>(w, slot(0) + kg * C::blockBytes, k);
+    scores<D, RB>(w, k, sc);
+    // the first block's maxima are the first reference
+    f32x16 first[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) first[b] = sc[b];
+    const int nv = nv_now >> (8 * kg) & 255;
+    if (nv < kBlk) mask<RB>(first, nv, hh);
+    maxima<RB>(first, w.m);
+  }
+#pragma unroll 1
+  for (int s = 0; s < n_steps; ++s) {
+    lds_byte* vblk = slot(s - 1) + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+#pragma unroll
+    for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+    // the next step has been converted, and every wave is done with the step before the last,
+    // whose slot is filled again
+    lds_barrier();
+    const int nv3 = fetch_step<D>(a, src, lay, own, next_share);
+    lds_byte* to = slot(s + 2);
+    const int nv_own = mine(nv2);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      if (kb > 0) {
+        vblk = slot(s);
+#pragma unroll
+        for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+      }
+      lds_byte* kblk = kb + 1 < KB ? slot(s) + C::blockBytes : slot(s + 1) + (KB == 2 ? 0 : kg * C::blockBytes);
+      const int nv = nv_now >> (8 * (KB == 2 ? kb : kg)) & 255;
+      if (nv < kBlk) mask<RB>(sc, nv, hh);
+      f32x16 next[RB];
+      pipelined<D, RB, F>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [&](int t, int n) __attribute__((always_inline)) {
+        constexpr int kPer = kWords / KB;  // words beside a block
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (t == (i + 1) * n / (kPer + 1)) convert<D>(now, lay, nv_own, to, kb * kPer + i);
+      });
+      check_reference<D, RB, F>(a, w, sc, p, sum, rounded);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) sc[b] = next[b];
+    }
+    now = next_share;
+    nv_now = nv_next;
+    nv_next = nv2;
+    nv2 = nv3;
+  }
+  lds_byte* vblk = slot(n_steps - 1) + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+#pragma unroll
+  for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
+#pragma unroll
+  for (int b = 0; b < RB; ++b) products<D, RB, F>(w, b, v, p[b]);
+  lds_barrier();  // the steps' room is free
+}
+
+// KG: groups of waves that meet other keys of a step; F: the parts of a weight.
+template <int D, int KG, int F>
+__global__ __launch_bounds__(kShThreads) void attn_kv4_wide_kernel(Kv4AttnArgs a) {
+  using C = SCfg<D>;
+  constexpr int RB = 2, TR = kShWaves / KG * RB * kBlk;
+  __shared__ __attribute__((aligned(1024))) char smem[WCfg<D>::smem];
+  __shared__ Start starts[1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = wave % KG, rg = wave / KG;
+  const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
+  const Line line = find_line<TR, 1, true>(a, total, starts);
+  const int64_t run = line.first;
+  if (run >= line.cut.runs) return;
+  const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
+  Walk<TR> at;
+  at.start(a, total, starts[0], u0);
+  const Lay<D> lay(tid);
+  for (int64_t u = u0; u < u1;) {
+    if (tid == 0 && at.block == 0) tell_item(a, run, at);
+    const int n = u1 - u < at.r.blocks - at.block ? (int)(u1 - u) : at.r.blocks - at.block;
+    SWave<D, RB> w;
+    SRows<RB> rows;
+    start_rows<D, RB>(a, w, rows, at.head, at.r.first, (int64_t)at.tile * TR + rg * RB * kBlk, at.r.rows, lane);
+    piece_keys<D, KG, F>(a, w, (lds_byte*)smem, Source{at.b, at.head, at.r.len, at.block, at.block + n}, kg, wave, tid, lay);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      w.l[b] = pair_sum32(w.l[b]);
+      w.lr[b] = pair_sum32(w.lr[b]);
+    }
+    if constexpr (KG > 1) {
+      join_groups<D, KG, RB>(a, w, smem, kg, rg, lane);
+      __syncthreads();
+    }
+    const bool last = at.block + n == at.r.blocks, whole = last && at.item >= u0;
+    if (kg == 0) {
+      const int hh = lane >> 5;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        if (!rows.live[b]) continue;
+        if (whole) {
+          if (a.lse && hh == 0) a.lse[(int64_t)rows.head[b] * a.n_rows + rows.token[b]] = lse_of(w.m[b], w.l[b], a.scale);
+          const float inv = w.lr[b] == 0.f ? 0.f : 1.0f / w.lr[b];
+#pragma unroll
+          for (int d = 0; d < C::dBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              put4(a, rows.token[b], rows.head[b] * D + 32 * d + 8 * i + 4 * hh,
+                   f32x4{w.acc[b][d][4 * i] * inv, w.acc[b][d][4 * i + 1] * inv, w.acc[b][d][4 * i + 2] * inv,
+                         w.acc[b][d][4 * i + 3] * inv});
+          continue;
+        }
+        const int64_t part = (2 * run + (at.item >= u0 ? 1 : 0)) * TR + rg * RB * kBlk + b * kBlk + (lane & 31);
+        if (hh == 0) *(f32x4*)(a.part_stat + 4 * part) = f32x4{w.m[b], w.l[b], w.lr[b], 0.f};
+#pragma unroll
+        for (int d = 0; d < C::dBlocks; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *(f32x4*)(a.part_o + part * D + 32 * d + 8 * i + 4 * hh) =
+                f32x4{w.acc[b][d][4 * i], w.acc[b][d][4 * i + 1], w.acc[b][d][4 * i + 2], w.acc[b][d][4 * i + 3]};
+      }
+    }
+    u += n;
+    at.block += n - 1;
+    at.next(a, total);
+  }
+}
+
+// One part of a row into its running join.
+struct Joined {
+  float m = -INFINITY, l = 0.f, lr = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+};
+__device__ __forceinline__ void join_part(Joined& r, float scale_log2, float m, float l, float lr, const f32x4& o) {
+  const float top = fmaxf(r.m, m);
+  const float ea = r.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.m - top) * scale_log2);
+  const float eb = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * scale_log2);
+  r.l = r.l * ea + l * eb;
+  r.lr = r.lr * ea + lr * eb;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) r.o[k] = r.o[k] * ea + o[k] * eb;
+  r.m = top;
+}
+
+// Joins the parts of an item that lies in several runs, a.join_rows of its rows to a workgroup:
+// side by side, and where there are few of them slices of the parts too.
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs a) {
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes, kBatch = 4;
+  __shared__ f32x4 part_o[kJoinThreads];
+  __shared__ f32x4 part_stat[kGroups];
+  const int64_t units = a.line[0], items = a.line[1];
+  const Kv4Item r = a.items[blockIdx.x];  // (on its way with the count)
+  if (blockIdx.x >= items) return;
+  const int n = (int)(Cut(units, a.most_runs, a.least_units).run_of(r.end - 1) - r.run) + 1;  // parts
+  if (n < 2) return;
+  const int64_t run = r.run + 1;
+  const int rows = r.rows - r.row0 < a.tile_rows ? r.rows - r.row0 : a.tile_rows;
+  const int y0 = blockIdx.y * a.join_rows, y1 = rows < y0 + a.join_rows ? rows : y0 + a.join_rows;
   if (y0 >= y1) return;
-  // rows side by side, and where there are few of them slices of the parts too
   int side = 1;
   while (side < kGroups && side < y1 - y0) side *= 2;
   const int slices = kGroups / side;
@@ -548,88 +876,104 @@ __global__ __launch_bounds__(256) void attn_kv4_join_kernel(Kv4AttnArgs a, int t
   for (int y = y0; y < y1; y += side) {
     const int row = y + group % side;
     const bool live = row < y1;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    Joined j;
     if (live) {
-      for (int i = n * slice / slices; i < n * (slice + 1) / slices; ++i) {
-        const int64_t at = (2 * (int64_t)(run - 1 + i) + (i == 0 ? 1 : 0)) * tile_rows + row;
-        const float mi = a.part_stat[2 * at], li = a.part_stat[2 * at + 1];
-        const f32x4 oi = *(const f32x4*)(a.part_o + at * D + 4 * c);
-        const float top = fmaxf(m, mi);
-        const float ea = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
-        const float eb = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - top) * a.scale_log2);
-        l = l * ea + li * eb;
+      const int end = n * (slice + 1) / slices;
+      for (int i0 = n * slice / slices; i0 < end; i0 += kBatch) {
+        f32x4 st[kBatch], o[kBatch];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = o[k] * ea + oi[k] * eb;
-        m = top;
+        for (int i = 0; i < kBatch; ++i) {  // (loads in flight together)
+          const int p = i0 + i < end ? i0 + i : end - 1;
+          const int64_t at = (2 * (run - 1 + p) + (p == 0 ? 1 : 0)) * a.tile_rows + row;
+          st[i] = *(const f32x4*)(a.part_stat + 4 * at);
+          o[i] = *(const f32x4*)(a.part_o + at * D + 4 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (i0 + i < end) join_part(j, a.scale_log2, st[i][0], st[i][1], st[i][2], o[i]);
       }
     }
     if (slices > 1) {
-      part_o[threadIdx.x] = o;
-      if (c == 0) {
-        part_m[group] = m;
-        part_l[group] = l;
-      }
+      part_o[threadIdx.x] = j.o;
+      if (c == 0) part_stat[group] = f32x4{j.m, j.l, j.lr, 0.f};
       __syncthreads();
-      if (slice == 0) {
+      if (slice == 0)
         for (int i = 1; i < slices; ++i) {
           const int other = i * side + group;
-          const float mi = part_m[other], li = part_l[other];
-          const f32x4 oi = part_o[other * kLanes + c];
-          const float top = fmaxf(m, mi);
-          const float ea = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
-          const float eb = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - top) * a.scale_log2);
-          l = l * ea + li * eb;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] = o[k] * ea + oi[k] * eb;
-          m = top;
+          const f32x4 st = part_stat[other];
+          join_part(j, a.scale_log2, st[0], st[1], st[2], part_o[other * kLanes + c]);
         }
-      }
       __syncthreads();
     }
     if (!live || slice != 0) continue;
     const int at = r.row0 + row;
     const int64_t token = r.first + at / a.group;
     const int head = r.head * a.group + at % a.group;
-    if (a.lse && c == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(m, l, a.scale);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    put4(a, token, head * D + 4 * c, o * inv);
+    if (a.lse && c == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(j.m, j.l, a.scale);
+    const float inv = j.lr == 0.f ? 0.f : 1.0f / j.lr;
+    put4(a, token, head * D + 4 * c, j.o * inv);
   }
 }
 
+template <int D>
+hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.most_runs < 2) return e;
+  attn_kv4_join_kernel<D><<<dim3(a.most_items, a.tile_rows / a.join_rows), kJoinThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
 template <int D, int RB>
 hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
-  attn_kv4_kernel<D, RB, narrow_ring(D, RB)><<<(unsigned)((a.most_runs + kAWaves - 1) / kAWaves), kAThreads, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.most_runs < 2) return e;
-  attn_kv4_join_kernel<D><<<dim3(a.most_runs - 1, RB), 256, 0, stream>>>(a, 16 * RB);
-  return hipGetLastError();
+  const unsigned grid = (unsigned)((a.most_runs + kShWaves - 1) / kShWaves);
+  if (a.out_bf16 && RB > 1)
+    attn_kv4_kernel<D, RB, ISPA_NB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
+  else
+    attn_kv4_kernel<D, RB, ISPA_NB, 2><<<grid, kShThreads, 0, stream>>>(a);
+  return launch_join<D>(a, stream);
+}
+template <int D, int KG>
+hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)((a.most_runs + kAXcds - 1) / kAXcds * kAXcds);
+  if (a.out_bf16)
+    attn_kv4_wide_kernel<D, KG, 1><<<grid, kShThreads, 0, stream>>>(a);
+  else
+    attn_kv4_wide_kernel<D, KG, 2><<<grid, kShThreads, 0, stream>>>(a);
+  return launch_join<D>(a, stream);
 }
 template <int D>
 hipError_t launch_d(const Kv4AttnArgs& a, hipStream_t stream) {
-  return a.tile_rows == 16 ? launch_narrow<D, 1>(a, stream)
-         : a.tile_rows == 32 ? launch_narrow<D, 2>(a, stream)
-                             : launch_narrow<D, 4>(a, stream);
+  switch (a.tile_rows) {
+    case 16: return launch_narrow<D, 1>(a, stream);
+    case 32: return launch_narrow<D, 2>(a, stream);
+    case 64: return launch_narrow<D, 4>(a, stream);
+    case 128: return launch_wide<D, 2>(a, stream);
+    default: return launch_wide<D, 1>(a, stream);
+  }
 }
 
 }  // namespace
 
 size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   const int64_t rows = (int64_t)(a->max_q < a->n_rows ? a->max_q : a->n_rows) * a->group;
-  a->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  a->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
-  a->most_runs = n_cu * narrow_groups(head_dim, a->tile_rows / 16) * kAWaves;
-  a->least_units = 4;
+  const bool wide = a->tile_rows >= 128;
+  a->most_runs = wide ? n_cu * (head_dim == 64 ? 2 : 1) : n_cu * narrow_waves(head_dim, a->tile_rows / 16) * kShWaves;
+  a->least_units = wide ? 8 : 4;
   // no more runs than there can be units
   const int64_t capacity = (int64_t)a->c.max_pages << a->c.log_page;
   const int64_t tiles = (int64_t)a->n_rows * a->group / a->tile_rows + a->c.n_req;
-  const int64_t blocks = capacity / kABlk > 0 ? capacity / kABlk : 1;
-  const int64_t runs = runs_of(tiles * a->c.n_kv_heads * blocks, a->most_runs, a->least_units);
-  a->most_runs = (int)(runs < 1 ? 1 : runs);
-  const size_t o = (size_t)a->most_runs * 2 * a->tile_rows * head_dim * sizeof(float);
-  a->stat_offset = o;
-  a->run_offset = o + (size_t)a->most_runs * 2 * a->tile_rows * 2 * sizeof(float);
-  return a->run_offset + (size_t)a->most_runs * sizeof(Kv4Run) + 16;
+  const int64_t blocks = capacity / kBlk > 0 ? capacity / kBlk : 1;
+  const int64_t runs = (tiles * a->c.n_kv_heads * blocks + a->least_units - 1) / a->least_units;
+  if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
+  a->most_items = (int)(tiles * a->c.n_kv_heads);
+  // few items: their rows to more workgroups of the join
+  a->join_rows = a->tile_rows < 16 ? a->tile_rows : 16;
+  while (a->join_rows > 1 && (int64_t)a->most_items * a->tile_rows / a->join_rows < 1024) a->join_rows /= 2;
+  const size_t parts = (size_t)a->most_runs * 2 * a->tile_rows;
+  a->stat_offset = parts * head_dim * sizeof(float);
+  a->item_offset = a->stat_offset + parts * 4 * sizeof(float);
+  return a->item_offset + (size_t)a->most_items * sizeof(Kv4Item) + 2 * sizeof(int64_t);
 }
 
 hipError_t launch_attn_kv4(const Kv4AttnArgs& a, int head_dim, hipStream_t stream) {

@@ -1415,8 +1415,8 @@ int ispa_attn_kv4(const void* q, int64_t ld_q, const void* cache, int64_t n_page
   a.lse = lse;
   a.part_o = (float*)workspace;
   a.part_stat = (float*)((char*)workspace + a.stat_offset);
-  a.run = (ispa::Kv4Run*)((char*)workspace + a.run_offset);
-  a.n_runs = (int*)(a.run + a.most_runs);
+  a.items = (ispa::Kv4Item*)((char*)workspace + a.item_offset);
+  a.line = (int64_t*)(a.items + a.most_items);
   return ispa::launch_attn_kv4(a, head_dim, stream) == hipSuccess ? ISPA_OK : ISPA_ERR_HIP;
 }
 

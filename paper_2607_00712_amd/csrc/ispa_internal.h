@@ -292,9 +292,9 @@ struct Kv4ReadArgs {
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t stream);
 
 // ---- attention over a 4-bit cache (attn_kv4.hip) ----
-// A run's first item: its units, where the run begins, and the rows that it stands for.
-struct Kv4Run {
-  int64_t item, end, begin;
+// An item: its units, the run that its first one lies in, and the rows that it stands for.
+struct Kv4Item {
+  int64_t begin, end, run;
   int head, row0, first, rows;
 };
 struct Kv4AttnArgs {
@@ -307,12 +307,13 @@ struct Kv4AttnArgs {
   void* out;
   int out_bf16;
   float* lse;
-  // set by the plan: rows of a tile, runs at most, units of a run at least, the parts
-  int tile_rows, most_runs, least_units;
-  size_t stat_offset, run_offset;
+  // set by the plan: rows of a tile, runs and items at most, units of a run at least, rows to a
+  // workgroup of the join, the parts
+  int tile_rows, most_runs, most_items, least_units, join_rows;
+  size_t stat_offset, item_offset;
   float *part_o, *part_stat;
-  Kv4Run* run;
-  int* n_runs;
+  Kv4Item* items;
+  int64_t* line;  // units in all, runs, items
 };
 // fills the plan and returns the workspace bytes
 size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim);
