@@ -18,17 +18,12 @@
 #include "attn_rows.h"
 #include "kv4_units.h"
 
-#ifndef ISPA_NB
-#define ISPA_NB 2
-#endif
-#ifndef ISPA_NW
-#define ISPA_NW 2
-#endif
 namespace ispa {
 namespace {
 
 constexpr int kAXcds = 8;
 constexpr int kJoinThreads = 512;
+constexpr int kInFlight = 2;  // blocks that a wave of narrow tiles has on their way
 
 typedef ISPA_LDS char lds_byte;
 
@@ -64,7 +59,7 @@ __device__ __forceinline__ Request request_of(const Kv4AttnArgs& a, int total, i
   return r;
 }
 __device__ __forceinline__ int64_t units_of(const Kv4AttnArgs& a, const Request& r) {
-  return (int64_t)a.c.n_kv_heads * r.tiles * r.blocks;
+  return (int64_t)a.c.n_kv_heads * r.tiles * (a.ahead + r.blocks);
 }
 
 // a / b for the same a and b in all lanes, mostly small: a 64-bit division takes 0.4 us of a
@@ -95,12 +90,13 @@ struct Start {
   int64_t unit;
   int b, item;
 };
-// A place in the line: a block of an item.
+// A place in the line: a block of an item. An item's start and end take time as some of its
+// blocks do: a.ahead units without keys stand for it, before its blocks.
 template <int TR>
 struct Walk {
   int b, head, tile, block;
   Request r;
-  int64_t item;  // first unit of the item
+  int64_t item;  // unit of the item's first block
   int number;    // of the item
 
   // from unit u, in the request of `s`
@@ -109,18 +105,19 @@ struct Walk {
     const int64_t base = uniform(s.unit);
     r = request_of<TR>(a, total, b);
     int64_t i = u - base;
-    const int64_t per = (int64_t)r.tiles * r.blocks;
+    const int64_t each = a.ahead + r.blocks, per = r.tiles * each;
     head = (int)divide(i, per);
     i -= head * per;
-    tile = (int)divide(i, r.blocks);
-    block = (int)(i - (int64_t)tile * r.blocks);
-    item = u - block;
+    tile = (int)divide(i, each);
+    i -= tile * each;
+    item = u - i + a.ahead;
+    block = i < a.ahead ? 0 : (int)i - a.ahead;
     number = uniform(s.item) + head * r.tiles + tile;
   }
   // to the next block, of the next item behind the last one
   __device__ __forceinline__ void next(const Kv4AttnArgs& a, int total) {
     if (++block < r.blocks) return;
-    item += r.blocks;
+    item += r.blocks + a.ahead;  // (as many units ahead of every item)
     ++number;
     block = 0;
     if (++tile < r.tiles) return;
@@ -281,13 +278,14 @@ using Global = __attribute__((address_space(1))) const T;
 template <int D, int TR>
 struct Feeder {
   Walk<TR> w;
-  int64_t left;  // units to fetch
+  int64_t u, end;  // the next block's unit, and the run's end
   uint32_t k_at, v_at, ke_at, ve_at;  // the lane's bytes in a block
 
-  __device__ __forceinline__ void start(const Walk<TR>& walk, int64_t n, int lane) {
+  __device__ __forceinline__ void start(const Walk<TR>& walk, int64_t first, int64_t last, int lane) {
     constexpr int kPer = D / 32;
     w = walk;
-    left = n;
+    u = first;
+    end = last;
     k_at = (lane & 15) * (D / 2) + (lane >> 4) * (D / 8);
     v_at = lane * 16;
     ke_at = (lane & 15) * (D / 16) + (lane >> 4) * D / 128;
@@ -296,10 +294,10 @@ struct Feeder {
   __device__ __forceinline__ void fetch(const Kv4AttnArgs& a, int total, Raw<D>& to) {
     const int64_t size = (int64_t)1 << a.c.log_page;
     Block b{a.c.pages, 0, 0};
-    if (left > 0) {
+    if (u < end) {
       b = block_at(a, w.b, w.head, w.r.len, w.block, kv4_page_bytes(a.c.log_page, D));
       w.next(a, total);
-      --left;
+      u = w.item + w.block;
     }
     to.keys = b.keys;
     const auto *k = (Global<uint8_t>*)(b.base + (int64_t)b.row * (D / 2)),
@@ -535,9 +533,9 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
 }
 
 // Waves to a SIMD, as the registers allow.
-constexpr int narrow_waves(int head_dim, int rb) { return rb == 4 ? (head_dim == 128 ? 1 : 2) : rb == 2 ? 2 : ISPA_NW; }
+constexpr int narrow_waves(int head_dim, int rb) { return head_dim == 128 && rb == 4 ? 1 : 2; }
 
-template <int D, int RB, int NB, int F>
+template <int D, int RB, int F>
 __global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
   using C = NCfg<D>;
   constexpr int TR = 16 * RB;
@@ -551,18 +549,20 @@ __global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kern
   const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
   Walk<TR> w;
   w.start(a, total, starts[wave], u0);
+  int64_t u = u0 > w.item ? u0 : w.item;  // the unit of a block
+  if (u >= u1) return;
   if (lane == 0 && w.block == 0) tell_item(a, run, w);
   lds_byte* stage = (lds_byte*)smem + wave * C::stageBytes;
   Feeder<D, TR> f;
-  f.start(w, u1 - u0, lane);
-  Raw<D> raw[NB];
+  f.start(w, u, u1, lane);
+  Raw<D> raw[kInFlight];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) f.fetch(a, total, raw[i]);
+  for (int i = 0; i < kInFlight; ++i) f.fetch(a, total, raw[i]);
   NWave<D, RB> s;
   start_item<D, RB>(a, s, w, lane);
-  for (int64_t u = u0; u < u1;) {
+  while (u < u1) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
+    for (int i = 0; i < kInFlight; ++i) {
       if (u < u1) {
         meet_block<D, RB, F>(a, s, raw[i], stage, lane);
         f.fetch(a, total, raw[i]);
@@ -572,6 +572,7 @@ __global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kern
           const bool whole = last && w.item >= u0;
           finish_item<D, RB>(a, s, w, whole ? -1 : 2 * (int64_t)run + (w.item >= u0 ? 1 : 0), lane);
           w.next(a, total);
+          if (last) u = w.item;
           if (u < u1) {
             if (lane == 0) tell_item(a, run, w);
             start_item<D, RB>(a, s, w, lane);
@@ -787,7 +788,7 @@ __global__ __launch_bounds__(kShThreads) void attn_kv4_wide_kernel(Kv4AttnArgs a
   Walk<TR> at;
   at.start(a, total, starts[0], u0);
   const Lay<D> lay(tid);
-  for (int64_t u = u0; u < u1;) {
+  for (int64_t u = u0 > at.item ? u0 : at.item; u < u1;) {
     if (tid == 0 && at.block == 0) tell_item(a, run, at);
     const int n = u1 - u < at.r.blocks - at.block ? (int)(u1 - u) : at.r.blocks - at.block;
     SWave<D, RB> w;
@@ -834,6 +835,7 @@ __global__ __launch_bounds__(kShThreads) void attn_kv4_wide_kernel(Kv4AttnArgs a
     u += n;
     at.block += n - 1;
     at.next(a, total);
+    if (last) u = at.item;
   }
 }
 
@@ -926,9 +928,9 @@ template <int D, int RB>
 hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((a.most_runs + kShWaves - 1) / kShWaves);
   if (a.out_bf16 && RB > 1)
-    attn_kv4_kernel<D, RB, ISPA_NB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_kernel<D, RB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
   else
-    attn_kv4_kernel<D, RB, ISPA_NB, 2><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_kernel<D, RB, 2><<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
 template <int D, int KG>
@@ -958,13 +960,15 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   a->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
   const bool wide = a->tile_rows >= 128;
-  a->most_runs = wide ? n_cu * (head_dim == 64 ? 2 : 1) : n_cu * narrow_waves(head_dim, a->tile_rows / 16) * kShWaves;
-  a->least_units = wide ? 8 : 4;
+  a->most_runs = n_cu * (wide ? 1 : narrow_waves(head_dim, a->tile_rows / 16) * kShWaves);
+  // (a workgroup's run has a start, and a part to be joined, as long as some 16 blocks)
+  a->least_units = wide ? 16 : 4;
+  a->ahead = wide ? 8 : 2;
   // no more runs than there can be units
   const int64_t capacity = (int64_t)a->c.max_pages << a->c.log_page;
   const int64_t tiles = (int64_t)a->n_rows * a->group / a->tile_rows + a->c.n_req;
   const int64_t blocks = capacity / kBlk > 0 ? capacity / kBlk : 1;
-  const int64_t runs = (tiles * a->c.n_kv_heads * blocks + a->least_units - 1) / a->least_units;
+  const int64_t runs = (tiles * a->c.n_kv_heads * (blocks + a->ahead) + a->least_units - 1) / a->least_units;
   if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
   a->most_items = (int)(tiles * a->c.n_kv_heads);
   // few items: their rows to more workgroups of the join
