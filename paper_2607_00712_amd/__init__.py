@@ -28,6 +28,7 @@ works without the library, but every call raises if it is not built.
 """
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -846,10 +847,14 @@ def norm_residual_backward(d_h, x_out, y=None, d_x_out=None, norm="layer", weigh
 _axis_types = [_c_i32 * n for n in range(1, 5)]
 
 
-def _pairs(axes, freqs):
-    axes = (freqs.shape[0],) if axes is None else tuple(int(n) for n in axes)
+@functools.lru_cache(maxsize=64)
+def _axis_array(axes):
     n = len(axes)
-    return (_axis_types[n - 1] if 0 < n <= 4 else _c_i32 * n)(*axes), n
+    return (_axis_types[n - 1] if 0 < n <= 4 else _c_i32 * n)(*axes), n, sum(axes)
+
+
+def _pairs(axes, freqs):
+    return _axis_array((freqs.shape[0],) if axes is None else tuple(map(int, axes)))
 
 
 def rotary_frequencies(axis_pairs, base=10000.0, scaling="none", factor=1.0, original_length=0.0, beta_fast=32.0,
@@ -870,10 +875,17 @@ def rotary_frequencies(axis_pairs, base=10000.0, scaling="none", factor=1.0, ori
 
 
 def _angles(positions, freqs, axes, dev, rows):
+    pairs, n_axes, total = _pairs(axes, freqs) if isinstance(freqs, torch.Tensor) and freqs.dim() == 1 else (None, 0, -1)
+    # one expression for the usual case; the reasons only when it fails
+    if (isinstance(positions, torch.Tensor) and positions.dtype == torch.int32 and positions.numel() == rows * n_axes
+            and 0 < positions.dim() <= 2 and positions.shape[0] == rows and positions.device == dev
+            and positions.is_contiguous() and freqs.dtype == torch.float64 and freqs.device == dev
+            and freqs.is_contiguous() and total == freqs.shape[0]):
+        return pairs, n_axes
     _require(positions, "positions", torch.int32, dev, ndim=positions.dim() if isinstance(positions, torch.Tensor) else 2)
     _require(freqs, "freqs", torch.float64, dev, ndim=1)
-    pairs, n_axes = _pairs(axes, freqs)
-    if axes is not None and sum(pairs) != freqs.shape[0]:
+    pairs, n_axes, total = _pairs(axes, freqs)
+    if total != freqs.shape[0]:
         raise ValueError("axes must add up to the pairs of freqs")
     if positions.shape != (rows, n_axes) and not (n_axes == 1 and positions.shape == (rows,)):
         raise ValueError(f"positions must have shape {(rows, n_axes)}")
@@ -1064,8 +1076,10 @@ def attn_shared(q, k_prefix, v_prefix, k_cache, v_cache, q_start, cache_lens, n_
 # ---- norms of heads with the position rotation, a cache in 4 bits ----
 def _head_vectors(dev, head_dim, **vectors):
     for name, t in vectors.items():
-        if t is not None:
-            _vector(t, name, dev, (head_dim,))
+        if t is None or (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.dim() == 1
+                         and t.shape[0] == head_dim and t.device == dev and t.is_contiguous()):
+            continue
+        _vector(t, name, dev, (head_dim,))
 
 
 def _heads_of(q, k, n_heads, n_kv_heads):
@@ -1087,7 +1101,9 @@ def _heads_of(q, k, n_heads, n_kv_heads):
 def _rows_output(t, name, like, dtype):
     """The caller's output of like's shape, or a new one of dtype, and its row distance."""
     if t is None:
-        t = like.new_empty(like.shape, dtype=dtype)
+        if dtype not in _DT:
+            raise TypeError(f"{name} must be a bf16 or fp32 torch.Tensor")
+        return like.new_empty(like.shape, dtype=dtype), like.shape[1]
     ld = _strided_rows(t, name, like.device, None, like.shape[1])
     if t.shape[0] != like.shape[0]:
         raise ValueError(f"{name} must have shape {tuple(like.shape)}")
@@ -1155,10 +1171,9 @@ def norm_rotary_backward(d_q_out, d_k_out, q, k, positions, freqs, n_heads, n_kv
     out = {"q": q.new_empty(q.shape)}
     if k is not None:
         out["k"] = k.new_empty(k.shape)
-    new = torch.empty if rows else torch.zeros
     for name, t in (("q_weight", q_weight), ("k_weight", k_weight), ("q_bias", q_bias), ("k_bias", k_bias)):
         if t is not None:
-            out[name] = new((head_dim,), dtype=torch.float32, device=dev)
+            out[name] = torch.empty_like(t) if rows else torch.zeros_like(t)
     if rows == 0:
         return out
     nbytes, ws = 0, None
@@ -1189,8 +1204,12 @@ def kv4_cache(n_pages, page_size, n_kv_heads, head_dim, device=None):
 
 def _kv4(cache, page_table, head_dim, dev=None):
     """Checks a 4-bit cache and its table; returns (n_pages, page_size, n_req, max_pages, n_kv_heads)."""
-    _require(cache, "cache", torch.uint8, dev, ndim=3)
-    _require(page_table, "page_table", torch.int32, cache.device)
+    if not (isinstance(cache, torch.Tensor) and isinstance(page_table, torch.Tensor) and cache.dtype == torch.uint8
+            and page_table.dtype == torch.int32 and cache.is_cuda and cache.dim() == 3 and page_table.dim() == 2
+            and (dev is None or cache.device == dev) and page_table.device == cache.device and cache.is_contiguous()
+            and page_table.is_contiguous()):
+        _require(cache, "cache", torch.uint8, dev, ndim=3)
+        _require(page_table, "page_table", torch.int32, cache.device)
     n_pages, n_kv_heads, nbytes = cache.shape
     per = head_dim + head_dim // 16
     if nbytes % per:
@@ -1259,14 +1278,16 @@ def kv4_read(cache, page_table, slots, head_dim, out_dtype=torch.bfloat16, k=Non
     dev = cache.device
     _require(slots, "slots", torch.int64, dev, ndim=1)
     rows, kv = slots.shape[0], n_kv_heads * int(head_dim)
-    if k is None:
+    if k is None and v is None and out_dtype in _DT:
         k = cache.new_empty((rows, kv), dtype=out_dtype)
-    if v is None:
         v = torch.empty_like(k)
-    for name, t in (("k", k), ("v", v)):
-        _float_tensor(t, name, dev)
-        if t.shape != (rows, kv) or t.dtype != k.dtype:
-            raise ValueError(f"k and v must have shape {(rows, kv)} and one dtype")
+    else:
+        k = cache.new_empty((rows, kv), dtype=out_dtype) if k is None else k
+        v = torch.empty_like(k) if v is None else v
+        for name, t in (("k", k), ("v", v)):
+            _float_tensor(t, name, dev)
+            if t.shape != (rows, kv) or t.dtype != k.dtype:
+                raise ValueError(f"k and v must have shape {(rows, kv)} and one dtype")
     if rows == 0:
         return k, v
     st = _on(dev, lambda: L.ispa_kv4_read(

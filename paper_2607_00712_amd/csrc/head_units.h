@@ -145,7 +145,10 @@ __device__ __forceinline__ T head_norm(T (&x)[8], T (&y)[8], T eps, int head_dim
 #pragma unroll
   for (int i = 0; i < 8; ++i) s += x[i] * x[i] + y[i] * y[i];
   const T var = head_sum<T>(mine ? s : (T)0, lanes) * inv + eps;
-  return (T)1 / (sizeof(T) == 8 ? (T)sqrt((double)var) : (T)sqrtf((float)var));
+  if constexpr (sizeof(T) == 8)
+    return 1.0 / sqrt(var);
+  else
+    return __builtin_amdgcn_rsqf(var);  // (within a unit in the last place)
 }
 
 // A unit's values of a vector of a head

@@ -1203,8 +1203,8 @@ size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, 
   if (rows < 1 || rows >= (1 << 24) || n_heads < 1 || n_kv_heads < 0 || head_dim < 16 || head_dim > 256 ||
       head_dim % 16 != 0 || (int64_t)n_heads * head_dim > (1 << 20) || (int64_t)n_kv_heads * head_dim > (1 << 20))
     return 0;
-  const size_t blocks = ispa::norm_rotary_blocks(rows, n_heads, head_dim) +
-                        (n_kv_heads ? ispa::norm_rotary_blocks(rows, n_kv_heads, head_dim) : 0);
+  const size_t blocks = ispa::norm_rotary_blocks(rows, n_heads, n_kv_heads, head_dim) +
+                        (n_kv_heads ? ispa::norm_rotary_blocks(rows, n_kv_heads, n_heads, head_dim) : 0);
   return round_up(blocks * 2 * head_dim * sizeof(float), kWsAlign);
 }
 

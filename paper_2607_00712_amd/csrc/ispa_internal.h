@@ -258,8 +258,8 @@ struct NormRotaryArgs {
   int tokens, lanes, q_blocks, k_blocks;
 };
 hipError_t launch_norm_rotary(NormRotaryArgs a, hipStream_t stream);
-// workgroups of the backward pass over a tensor of `heads` heads
-int norm_rotary_blocks(int64_t rows, int heads, int head_dim);
+// workgroups of the backward pass over a tensor of `heads` heads, beside one of other_heads
+int norm_rotary_blocks(int64_t rows, int heads, int other_heads, int head_dim);
 hipError_t launch_norm_rotary_backward(NormRotaryArgs a, hipStream_t stream);
 
 // A 4-bit cache: page (p, key head h) is kv4_page_bytes bytes at ((p n_kv_heads + h) page

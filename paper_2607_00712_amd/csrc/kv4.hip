@@ -229,10 +229,11 @@ auto append_kernel(bool x_f32, int head_dim) {
 }  // namespace
 
 hipError_t launch_kv4_append(Kv4AppendArgs a, hipStream_t stream) {
-  // about two runs of heads to a wave, at least four workgroups to a compute unit
+  // about four runs of heads to a wave, so that few of them are filled in part, and at least four
+  // workgroups to a compute unit (6240 rows of 12 + 12 + 12 heads: 31 us with two, 24 with four)
   const int values = (a.t.n_heads + 2 * a.c.n_kv_heads) * a.t.head_dim;
   const int64_t most = a.t.rows / 1024;
-  a.t.tokens = 2 * kQWaves * kQValues / values;
+  a.t.tokens = 4 * kQWaves * kQValues / values;
   if (a.t.tokens > most) a.t.tokens = (int)most;
   a.t.tokens = a.t.tokens < 1 ? 1 : a.t.tokens > kQMaxTokens ? kQMaxTokens : a.t.tokens;
   const unsigned grid = (unsigned)((a.t.rows + a.t.tokens - 1) / a.t.tokens);
