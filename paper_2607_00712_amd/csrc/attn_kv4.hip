@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kAXcds = 8;
 constexpr int kJoinThreads = 512;
+constexpr int kNarrowGroups = 2;  // workgroups of narrow tiles to a compute unit
 constexpr int kInFlight = 2;  // blocks that a wave of narrow tiles has on their way
 
 typedef ISPA_LDS char lds_byte;
@@ -89,6 +90,7 @@ struct Cut {
 struct Start {
   int64_t unit;
   int b, item;
+  Request r;
 };
 // A place in the line: a block of an item. An item's start and end take time as some of its
 // blocks do: a.ahead units without keys stand for it, before its blocks.
@@ -100,10 +102,10 @@ struct Walk {
   int number;    // of the item
 
   // from unit u, in the request of `s`
-  __device__ __forceinline__ void start(const Kv4AttnArgs& a, int total, const Start& s, int64_t u) {
+  __device__ __forceinline__ void start(const Kv4AttnArgs& a, const Start& s, int64_t u) {
     b = uniform(s.b);
     const int64_t base = uniform(s.unit);
-    r = request_of<TR>(a, total, b);
+    r = Request{uniform(s.r.first), uniform(s.r.rows), uniform(s.r.tiles), uniform(s.r.blocks), uniform(s.r.len)};
     int64_t i = u - base;
     const int64_t each = a.ahead + r.blocks, per = r.tiles * each;
     head = (int)divide(i, per);
@@ -146,8 +148,9 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
   const int b0 = (int)((int64_t)a.c.n_req * threadIdx.x / kShThreads), b1 = (int)((int64_t)a.c.n_req * (threadIdx.x + 1) / kShThreads);
   int64_t own = 0;
   int own_items = 0;
+  Request r{};
   for (int b = b0; b < b1; ++b) {
-    const Request r = request_of<TR>(a, total, b);
+    r = request_of<TR>(a, total, b);
     own += units_of(a, r);
     own_items += a.c.n_kv_heads * r.tiles;
   }
@@ -190,10 +193,10 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
     int64_t at = before;
     int item = items;
     for (int b = b0; b < b1; ++b) {
-      const Request r = request_of<TR>(a, total, b);
+      if (b1 - b0 > 1) r = request_of<TR>(a, total, b);  // (else the one at hand)
       const int64_t n = units_of(a, r);
       if (u < at + n) {
-        starts[i] = Start{at, b, item};
+        starts[i] = Start{at, b, item, r};
         break;
       }
       at += n;
@@ -532,23 +535,20 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
       for (int f = 0; f < F; ++f) s.acc[b][d] = mfma16(v[d].v, p[b][f], s.acc[b][d]);
 }
 
-// Waves to a SIMD, as the registers allow.
-constexpr int narrow_waves(int head_dim, int rb) { return head_dim == 128 && rb == 4 ? 1 : 2; }
-
 template <int D, int RB, int F>
-__global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(kShThreads, kNarrowGroups) void attn_kv4_kernel(Kv4AttnArgs a) {
   using C = NCfg<D>;
   constexpr int TR = 16 * RB;
   __shared__ __attribute__((aligned(1024))) char smem[kShWaves * C::stageBytes];
   __shared__ Start starts[kShWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
-  const int run = blockIdx.x * kShWaves + wave;
   const Line line = find_line<TR, kShWaves, false>(a, total, starts);
+  const int64_t run = line.first + wave;
   if (run >= line.cut.runs) return;
   const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
   Walk<TR> w;
-  w.start(a, total, starts[wave], u0);
+  w.start(a, starts[wave], u0);
   int64_t u = u0 > w.item ? u0 : w.item;  // the unit of a block
   if (u >= u1) return;
   if (lane == 0 && w.block == 0) tell_item(a, run, w);
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kern
         const bool last = w.block + 1 == w.r.blocks;
         if (last || u == u1) {
           const bool whole = last && w.item >= u0;
-          finish_item<D, RB>(a, s, w, whole ? -1 : 2 * (int64_t)run + (w.item >= u0 ? 1 : 0), lane);
+          finish_item<D, RB>(a, s, w, whole ? -1 : 2 * run + (w.item >= u0 ? 1 : 0), lane);
           w.next(a, total);
           if (last) u = w.item;
           if (u < u1) {
@@ -586,9 +586,8 @@ __global__ __launch_bounds__(kShThreads, narrow_waves(D, RB)) void attn_kv4_kern
 }
 
 // ---- wide tiles: a run to a workgroup ----
-// Four waves of 64 rows (two row blocks), RG groups of rows times KG groups of keys, as in
-// attention over a bf16 prefix (attn_rows.h): steps of 64 keys in LDS in bf16, four of them in
-// turn. What fills them differs: a thread fetches its share of a step's codes (a quarter of a
+// Four waves of 64 rows (two row blocks), as in attention over a bf16 prefix (attn_rows.h): steps
+// of 64 keys in LDS in bf16, four of them in turn. What fills them differs: a thread fetches its share of a step's codes (a quarter of a
 // key, and of its values) two steps ahead into registers and converts it one step ahead, between
 // the matrix instructions of the step before.
 template <int D>
@@ -677,13 +676,13 @@ __device__ __forceinline__ void convert(const Share<D>& s, const Lay<D>& lay, in
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The blocks of a piece, met by KG = 1 or 2 groups of waves.
-template <int D, int KG, int F>
-__device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w, lds_byte* smem, Source src, int kg, int wave,
-                                           int tid, const Lay<D>& lay) {
+// The blocks of a piece, met by all four waves.
+template <int D, int F>
+__device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w, lds_byte* smem, Source src, int wave, int tid,
+                                           const Lay<D>& lay) {
   using C = SCfg<D>;
   using WC = WCfg<D>;
-  constexpr int RB = 2, KB = WC::step / KG, kWords = 2 * WC::words;
+  constexpr int RB = 2, kWords = 2 * WC::words;
   const int hh = (tid & 63) >> 5;
   const int n_steps = (src.end - src.block + WC::step - 1) / WC::step;
   const int own = wave >> 1;  // the block of a step that this wave converts
@@ -716,19 +715,19 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w,
   lds_barrier();
   {
     bf16x8 k[C::slices];
-    read_k<D, RB>(w, slot(0) + kg * C::blockBytes, k);
+    read_k<D, RB>(w, slot(0), k);
     scores<D, RB>(w, k, sc);
     // the first block's maxima are the first reference
     f32x16 first[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) first[b] = sc[b];
-    const int nv = nv_now >> (8 * kg) & 255;
+    const int nv = nv_now & 255;
     if (nv < kBlk) mask<RB>(first, nv, hh);
     maxima<RB>(first, w.m);
   }
 #pragma unroll 1
   for (int s = 0; s < n_steps; ++s) {
-    lds_byte* vblk = slot(s - 1) + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+    lds_byte* vblk = slot(s - 1) + C::blockBytes;
 #pragma unroll
     for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
     // the next step has been converted, and every wave is done with the step before the last,
@@ -738,18 +737,18 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w,
     lds_byte* to = slot(s + 2);
     const int nv_own = mine(nv2);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int kb = 0; kb < WC::step; ++kb) {
       if (kb > 0) {
         vblk = slot(s);
 #pragma unroll
         for (int o = 0; o < kVAhead; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
       }
-      lds_byte* kblk = kb + 1 < KB ? slot(s) + C::blockBytes : slot(s + 1) + (KB == 2 ? 0 : kg * C::blockBytes);
-      const int nv = nv_now >> (8 * (KB == 2 ? kb : kg)) & 255;
+      lds_byte* kblk = kb == 0 ? slot(s) + C::blockBytes : slot(s + 1);
+      const int nv = nv_now >> (8 * kb) & 255;
       if (nv < kBlk) mask<RB>(sc, nv, hh);
       f32x16 next[RB];
       pipelined<D, RB, F>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [&](int t, int n) __attribute__((always_inline)) {
-        constexpr int kPer = kWords / KB;  // words beside a block
+        constexpr int kPer = kWords / WC::step;  // words beside a block
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
           if (t == (i + 1) * n / (kPer + 1)) convert<D>(now, lay, nv_own, to, kb * kPer + i);
@@ -763,7 +762,7 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w,
     nv_next = nv2;
     nv2 = nv3;
   }
-  lds_byte* vblk = slot(n_steps - 1) + (KB == 2 ? C::blockBytes : kg * C::blockBytes);
+  lds_byte* vblk = slot(n_steps - 1) + C::blockBytes;
 #pragma unroll
   for (int o = 0; o < 2 * C::dBlocks; ++o) v[o] = read_v1<D, RB>(w, vblk, o);
 #pragma unroll
@@ -771,66 +770,59 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w,
   lds_barrier();  // the steps' room is free
 }
 
-// KG: groups of waves that meet other keys of a step; F: the parts of a weight.
-template <int D, int KG, int F>
+// F: the parts of a weight.
+template <int D, int F>
 __global__ __launch_bounds__(kShThreads) void attn_kv4_wide_kernel(Kv4AttnArgs a) {
   using C = SCfg<D>;
-  constexpr int RB = 2, TR = kShWaves / KG * RB * kBlk;
+  constexpr int RB = 2, TR = kShWaves * RB * kBlk;
   __shared__ __attribute__((aligned(1024))) char smem[WCfg<D>::smem];
   __shared__ Start starts[1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = wave % KG, rg = wave / KG;
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
   const Line line = find_line<TR, 1, true>(a, total, starts);
   const int64_t run = line.first;
   if (run >= line.cut.runs) return;
   const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
   Walk<TR> at;
-  at.start(a, total, starts[0], u0);
+  at.start(a, starts[0], u0);
   const Lay<D> lay(tid);
   for (int64_t u = u0 > at.item ? u0 : at.item; u < u1;) {
     if (tid == 0 && at.block == 0) tell_item(a, run, at);
     const int n = u1 - u < at.r.blocks - at.block ? (int)(u1 - u) : at.r.blocks - at.block;
     SWave<D, RB> w;
     SRows<RB> rows;
-    start_rows<D, RB>(a, w, rows, at.head, at.r.first, (int64_t)at.tile * TR + rg * RB * kBlk, at.r.rows, lane);
-    piece_keys<D, KG, F>(a, w, (lds_byte*)smem, Source{at.b, at.head, at.r.len, at.block, at.block + n}, kg, wave, tid, lay);
+    start_rows<D, RB>(a, w, rows, at.head, at.r.first, (int64_t)at.tile * TR + wave * RB * kBlk, at.r.rows, lane);
+    piece_keys<D, F>(a, w, (lds_byte*)smem, Source{at.b, at.head, at.r.len, at.block, at.block + n}, wave, tid, lay);
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       w.l[b] = pair_sum32(w.l[b]);
       w.lr[b] = pair_sum32(w.lr[b]);
     }
-    if constexpr (KG > 1) {
-      join_groups<D, KG, RB>(a, w, smem, kg, rg, lane);
-      __syncthreads();
-    }
     const bool last = at.block + n == at.r.blocks, whole = last && at.item >= u0;
-    if (kg == 0) {
-      const int hh = lane >> 5;
+    const int hh = lane >> 5;
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        if (!rows.live[b]) continue;
-        if (whole) {
-          if (a.lse && hh == 0) a.lse[(int64_t)rows.head[b] * a.n_rows + rows.token[b]] = lse_of(w.m[b], w.l[b], a.scale);
-          const float inv = w.lr[b] == 0.f ? 0.f : 1.0f / w.lr[b];
-#pragma unroll
-          for (int d = 0; d < C::dBlocks; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              put4(a, rows.token[b], rows.head[b] * D + 32 * d + 8 * i + 4 * hh,
-                   f32x4{w.acc[b][d][4 * i] * inv, w.acc[b][d][4 * i + 1] * inv, w.acc[b][d][4 * i + 2] * inv,
-                         w.acc[b][d][4 * i + 3] * inv});
-          continue;
-        }
-        const int64_t part = (2 * run + (at.item >= u0 ? 1 : 0)) * TR + rg * RB * kBlk + b * kBlk + (lane & 31);
-        if (hh == 0) *(f32x4*)(a.part_stat + 4 * part) = f32x4{w.m[b], w.l[b], w.lr[b], 0.f};
+    for (int b = 0; b < RB; ++b) {
+      if (!rows.live[b]) continue;
+      if (whole) {
+        if (a.lse && hh == 0) a.lse[(int64_t)rows.head[b] * a.n_rows + rows.token[b]] = lse_of(w.m[b], w.l[b], a.scale);
+        const float inv = w.lr[b] == 0.f ? 0.f : 1.0f / w.lr[b];
 #pragma unroll
         for (int d = 0; d < C::dBlocks; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *(f32x4*)(a.part_o + part * D + 32 * d + 8 * i + 4 * hh) =
-                f32x4{w.acc[b][d][4 * i], w.acc[b][d][4 * i + 1], w.acc[b][d][4 * i + 2], w.acc[b][d][4 * i + 3]};
+            put4(a, rows.token[b], rows.head[b] * D + 32 * d + 8 * i + 4 * hh,
+                 f32x4{w.acc[b][d][4 * i] * inv, w.acc[b][d][4 * i + 1] * inv, w.acc[b][d][4 * i + 2] * inv,
+                       w.acc[b][d][4 * i + 3] * inv});
+        continue;
       }
+      const int64_t part = (2 * run + (at.item >= u0 ? 1 : 0)) * TR + wave * RB * kBlk + b * kBlk + (lane & 31);
+      if (hh == 0) *(f32x4*)(a.part_stat + 4 * part) = f32x4{w.m[b], w.l[b], w.lr[b], 0.f};
+#pragma unroll
+      for (int d = 0; d < C::dBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(f32x4*)(a.part_o + part * D + 32 * d + 8 * i + 4 * hh) =
+              f32x4{w.acc[b][d][4 * i], w.acc[b][d][4 * i + 1], w.acc[b][d][4 * i + 2], w.acc[b][d][4 * i + 3]};
     }
     u += n;
     at.block += n - 1;
@@ -933,35 +925,40 @@ hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
     attn_kv4_kernel<D, RB, 2><<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
-template <int D, int KG>
+template <int D>
 hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((a.most_runs + kAXcds - 1) / kAXcds * kAXcds);
   if (a.out_bf16)
-    attn_kv4_wide_kernel<D, KG, 1><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 1><<<grid, kShThreads, 0, stream>>>(a);
   else
-    attn_kv4_wide_kernel<D, KG, 2><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 2><<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
 template <int D>
 hipError_t launch_d(const Kv4AttnArgs& a, hipStream_t stream) {
-  switch (a.tile_rows) {
-    case 16: return launch_narrow<D, 1>(a, stream);
-    case 32: return launch_narrow<D, 2>(a, stream);
-    case 64: return launch_narrow<D, 4>(a, stream);
-    case 128: return launch_wide<D, 2>(a, stream);
-    default: return launch_wide<D, 1>(a, stream);
-  }
+  return a.tile_rows == 16 ? launch_narrow<D, 1>(a, stream)
+         : a.tile_rows == 32 ? launch_narrow<D, 2>(a, stream)
+                             : launch_wide<D>(a, stream);
 }
 
 }  // namespace
 
 size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
+  // Rows of a tile. Up to 16 rows one block of 16 to a wave, up to 128 two: each tile meets the
+  // keys again, but few rows give the chip more runs that way, and tiles of 32 fit what a request
+  // has (64 rows of 32 requests against up to 16384 keys 118 us, and 168 in tiles of 64; 16
+  // requests of up to 128 rows 109 us, and 135 in tiles of 128). Beyond, a workgroup takes 256
+  // rows and meets its keys once (one request's 256 rows of 8 heads against 32768 keys 66 us, 73
+  // in tiles of 32; 512 rows 103 and 121). Requests of one batch mostly differ: several keep the
+  // narrow tiles up to 320 rows (24 requests of up to 154 rows 50 us, 70 in tiles of 256; four of
+  // up to 300 53 and 63).
   const int64_t rows = (int64_t)(a->max_q < a->n_rows ? a->max_q : a->n_rows) * a->group;
-  a->tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  a->tile_rows = rows <= 16 ? 16 : rows <= (a->c.n_req > 1 ? 320 : 128) ? 32 : 256;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
-  const bool wide = a->tile_rows >= 128;
-  a->most_runs = n_cu * (wide ? 1 : narrow_waves(head_dim, a->tile_rows / 16) * kShWaves);
-  // (a workgroup's run has a start, and a part to be joined, as long as some 16 blocks)
+  const bool wide = a->tile_rows == 256;
+  a->most_runs = n_cu * (wide ? 1 : kNarrowGroups * kShWaves);
+  // (a workgroup's run has a start, and a part to be joined, as long as some 16 blocks; a wave's
+  // short runs are worth it: one row of 12 heads against 32760 keys 25 us with 4, 28 with 12)
   a->least_units = wide ? 16 : 4;
   a->ahead = wide ? 8 : 2;
   // no more runs than there can be units
@@ -972,7 +969,7 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
   a->most_items = (int)(tiles * a->c.n_kv_heads);
   // few items: their rows to more workgroups of the join
-  a->join_rows = a->tile_rows < 16 ? a->tile_rows : 16;
+  a->join_rows = 16;
   while (a->join_rows > 1 && (int64_t)a->most_items * a->tile_rows / a->join_rows < 1024) a->join_rows /= 2;
   const size_t parts = (size_t)a->most_runs * 2 * a->tile_rows;
   a->stat_offset = parts * head_dim * sizeof(float);

@@ -339,58 +339,5 @@ __device__ __forceinline__ void check_reference(const A& a, SWave<D, RB>& w, con
   }
 }
 
-// The key groups of a row group join in LDS, one row block after the other, each lane
-// its own values; the result is kg 0's.
-template <int D, int KG, int RB, class A>
-__device__ __forceinline__ void join_groups(const A& a, SWave<D, RB>& w, char* smem, int kg, int rg, int lane) {
-  using C = SCfg<D>;
-  constexpr int kVec = C::dBlocks * 4;                                      // f32x4 of a lane's accumulators
-  f32x4* dump = (f32x4*)smem;                                               // [(KG - 1) RG][kVec][64]
-  float* stat = (float*)(smem + (kShWaves - kShWaves / KG) * kVec * 1024);  // [(KG - 1) RG][3][64]
-#pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    if (b > 0) __syncthreads();
-    if (kg > 0) {
-      const int p = rg * (KG - 1) + kg - 1;
-#pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        const f32x16& o = w.acc[b][v >> 2];
-        const int i = 4 * (v & 3);
-        dump[(p * kVec + v) * 64 + lane] = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-      }
-      stat[(p * 3 + 0) * 64 + lane] = w.m[b];
-      stat[(p * 3 + 1) * 64 + lane] = w.l[b];
-      stat[(p * 3 + 2) * 64 + lane] = w.lr[b];
-    }
-    __syncthreads();
-    if (kg == 0) {
-      float m = w.m[b];
-#pragma unroll
-      for (int j = 0; j < KG - 1; ++j) m = fmaxf(m, stat[((rg * (KG - 1) + j) * 3) * 64 + lane]);
-      float e = w.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w.m[b] - m) * a.scale_log2);
-      w.l[b] *= e;
-      w.lr[b] *= e;
-#pragma unroll
-      for (int d = 0; d < C::dBlocks; ++d) w.acc[b][d] *= e;
-#pragma unroll
-      for (int j = 0; j < KG - 1; ++j) {
-        const int p = rg * (KG - 1) + j;
-        const float mj = stat[(p * 3) * 64 + lane];
-        e = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mj - m) * a.scale_log2);
-        w.l[b] = fmaf(e, stat[(p * 3 + 1) * 64 + lane], w.l[b]);
-        w.lr[b] = fmaf(e, stat[(p * 3 + 2) * 64 + lane], w.lr[b]);
-#pragma unroll
-        for (int v = 0; v < kVec; ++v) {
-          const f32x4 o = dump[(p * kVec + v) * 64 + lane];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w.acc[b][v >> 2][4 * (v & 3) + i] = fmaf(e, o[i], w.acc[b][v >> 2][4 * (v & 3) + i]);
-        }
-      }
-      w.m[b] = m;
-    }
-  }
-}
-
 }  // namespace
 }  // namespace ispa

@@ -297,7 +297,7 @@ ATTN = [
     # items that lie in many runs, and runs that hold many items
     ([1] * 5, [3000, 0, 1, 2999, 512], 64, 47, 2, 2, 128), ([2], [7000], 1024, 7, 1, 1, 64), ([1], [9000], 32, 282, 1, 1, 128),
     ([1] * 300, [(37 * i) % 70 for i in range(300)], 32, 3, 4, 2, 64), ([2] * 40, [(31 * i) % 97 for i in range(40)], 32, 4, 8, 8, 128),
-    # tiles of 16, 32, 64 and 256 rows, and past them
+    # tiles of 16, 32 and 256 rows, and past them
     ([16], [40], 32, 2, 1, 1, 128), ([17], [40], 32, 2, 1, 1, 128), ([20, 20], [40, 64], 32, 2, 2, 2, 128),
     ([33], [300], 32, 10, 1, 1, 64), ([64], [90], 32, 3, 2, 1, 64), ([65], [300], 32, 10, 1, 1, 128),
     ([50, 50], [40, 700], 64, 11, 3, 1, 128), ([130, 70, 200], [300, 0, 701], 64, 11, 2, 2, 128),
