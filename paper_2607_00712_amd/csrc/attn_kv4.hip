@@ -250,7 +250,7 @@ template <int D>
 struct NCfg {
   static constexpr int steps = D / 32;           // k steps of K Q^T
   static constexpr int dBlocks = D / 16;         // output blocks
-  static constexpr int stageBytes = 16 * D * 2;  // values of 16 keys in bf16
+  static constexpr int stageBytes = kBlk * D * 2;  // a block's values in bf16
 };
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -441,12 +441,45 @@ __device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float s
   sum = s[0] + s[1];
 }
 
-// One block: scores, weights, values.
+// One block: scores, weights, values; the next block to come takes its registers as soon as the
+// scores are formed.
 template <int D, int RB, int F>
-__device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s, const Raw<D>& raw, lds_byte* stage, int lane) {
+__device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s, Raw<D>& raw, Feeder<D, 16 * RB>& feed, int total,
+                                           lds_byte* stage, int lane) {
   using C = NCfg<D>;
   constexpr int kPer = D / 32;  // blocks of 32 values of a key
   const int g = lane >> 4, m16 = lane & 15;
+  // V's values go through LDS, where transpose reads put keys side by side; written first, they
+  // are there when the weights are. Chunks of 8 values are swizzled: the reads take 32 bytes of
+  // 8 rows at a time, the writes 16 bytes of two (or four) rows.
+  auto swizzle = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
+  {
+    uint32_t vc[D / 64][4], ve[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      ve[i] = raw.ve[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vc[i][j] = raw.v[i][j];
+    }
+    if (raw.keys < kBlk) {  // behind the last valid key: zeros, whatever the page holds there
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        if ((i * 64 + lane) / kPer >= raw.keys) {
+          ve[i] = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) vc[i][j] = 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const float scale = kv4_scale(ve[i]);
+      const int key = (i * 64 + lane) / kPer, c = 4 * (lane % kPer);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(ISPA_LDS bf16x8*)(stage + key * (D * 2) + (((c + j) ^ swizzle(key)) << 4)) = kv4_values(vc[i][j], scale);
+    }
+  }
+  asm volatile("" ::: "memory");  // (the wave's LDS operations are done in order)
   // S^T = K Q^T: lane (g, m16) holds row m16's scores of keys 16 i + 4 g .. + 3
   f32x4 sc[RB][2];
 #pragma unroll
@@ -459,26 +492,29 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
       for (int b = 0; b < RB; ++b) sc[b][i] = mfma16(k, s.q[b][j], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[b][i]);
     }
   }
-  uint32_t vc[D / 64][4], ve[D / 64];
+  const int keys = raw.keys;
+  feed.fetch(a, total, raw);
+  // V^T operands: the contraction runs over keys 4 g .. + 3 and 16 + 4 g .. + 3 of lane group g,
+  // as the scores lie
+  union Operand {
+    s16x4 half[2];
+    bf16x8 v;
+  } v[C::dBlocks];
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    ve[i] = raw.ve[i];
+  for (int d = 0; d < C::dBlocks; ++d)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) vc[i][j] = raw.v[i][j];
-  }
-  if (raw.keys < kBlk) {  // behind the last valid key: no scores, and zeros whatever the page holds there
+    for (int h = 0; h < 2; ++h) {
+      const int row = 16 * h + 4 * g + (m16 >> 2);
+      v[d].half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (ISPA_LDS s16x4*)(stage + row * (D * 2) + (((2 * d + ((m16 & 3) >> 1)) ^ swizzle(row)) << 4) + ((m16 & 1) << 3)));
+    }
+  asm volatile("" ::: "memory");
+  if (keys < kBlk) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (16 * (i >> 2) + 4 * g + (i & 3) >= raw.keys) {
+      if (16 * (i >> 2) + 4 * g + (i & 3) >= keys) {
 #pragma unroll
         for (int b = 0; b < RB; ++b) sc[b][i >> 2][i & 3] = -INFINITY;
-      }
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i)
-      if ((i * 64 + lane) / kPer >= raw.keys) {
-        ve[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) vc[i][j] = 0;
       }
   }
   bf16x8 p[RB][F];
@@ -500,33 +536,7 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
     s.lr[b] += F == 2 ? sum[b] : rounded[b];
   }
 
-  // O^T += V^T P^T: the contraction runs over keys 4 g .. + 3 and 16 + 4 g .. + 3 of lane
-  // group g, as the scores lie; V's values of 16 keys at a time go through LDS, where transpose
-  // reads put keys side by side. Chunks of 8 values are swizzled: the reads take 32 bytes of 8
-  // rows at a time, the writes 16 bytes of two (or four) rows.
-  union Operand {
-    s16x4 half[2];
-    bf16x8 v;
-  } v[C::dBlocks];
-  auto swizzle = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int i = D == 128 ? h : 0;
-    const int key = D == 128 ? lane >> 2 : (lane >> 1) - 16 * h, c = 4 * (lane % kPer);
-    if (D == 128 || (lane >> 5) == h) {
-      const float scale = kv4_scale(ve[i]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *(ISPA_LDS bf16x8*)(stage + key * (D * 2) + (((c + j) ^ swizzle(key)) << 4)) = kv4_values(vc[i][j], scale);
-    }
-    asm volatile("" ::: "memory");  // (the wave's LDS operations are done in order)
-    const int row = 4 * g + (m16 >> 2);
-#pragma unroll
-    for (int d = 0; d < C::dBlocks; ++d)
-      v[d].half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (ISPA_LDS s16x4*)(stage + row * (D * 2) + (((2 * d + ((m16 & 3) >> 1)) ^ swizzle(row)) << 4) + ((m16 & 1) << 3)));
-    asm volatile("" ::: "memory");
-  }
+  // O^T += V^T P^T
 #pragma unroll
   for (int d = 0; d < C::dBlocks; ++d)
 #pragma unroll
@@ -564,8 +574,7 @@ __global__ __launch_bounds__(kShThreads, kNarrowGroups) void attn_kv4_kernel(Kv4
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
       if (u < u1) {
-        meet_block<D, RB, F>(a, s, raw[i], stage, lane);
-        f.fetch(a, total, raw[i]);
+        meet_block<D, RB, F>(a, s, raw[i], f, total, stage, lane);
         ++u;
         const bool last = w.block + 1 == w.r.blocks;
         if (last || u == u1) {
