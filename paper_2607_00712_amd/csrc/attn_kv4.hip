@@ -11,10 +11,21 @@
 // request against its keys, and a unit is 32 of them. The units of all items stand in one line,
 // and every run (a wave's, or a workgroup's where the tiles are wide) takes an equal part of it,
 // wherever that begins and ends: the lengths, which only the device knows, may be as different
-// as they like. An item that lies in one run is written out whole; of the others each run leaves
-// its part (weighted values, sum and reference of each row) in the workspace, two at most, and a
-// second launch joins them by Eq. 11-12, in order: the result does not depend on the order of
-// execution.
+// as they like (every workgroup sums them up for itself, which takes less than a launch). An item
+// that lies in one run is written out whole; of the others each run leaves its part (weighted
+// values, sums and reference of each row) in the workspace, two at most, and a second launch joins
+// them by Eq. 11-12, in order: the result does not depend on the order of execution.
+//
+// Narrow tiles (16 or 32 rows): a block's codes come from HBM into a lane's registers as the
+// matrix instructions take them, 2 KB of keys and of values that lie together in a page; a key's
+// 16 bytes of codes are 32 values with one power, converted two to an instruction. Values take a
+// trip through LDS for their transposition.
+//
+// Measured, 128 values a head, two kernels and the launches (a large copy runs at 4.9 TB/s, a
+// reader of the same pages without any arithmetic at 5.4, a large bf16 product at 1223 TFLOP/s):
+// 64 tokens of 32 heads on 8 against up to 16384 keys each 121 us (5.1 TB/s of pages), three
+// requests of up to 5 tokens against up to 131072 78 us (4.6), one token of 12 heads against 32760
+// 25 us (19 the runs, 7 the join); wide tiles below.
 #include "attn_rows.h"
 #include "kv4_units.h"
 
@@ -22,6 +33,7 @@ namespace ispa {
 namespace {
 
 constexpr int kAXcds = 8;
+constexpr int kWideWaves = 8;
 constexpr int kJoinThreads = 512;
 constexpr int kNarrowGroups = 2;  // workgroups of narrow tiles to a compute unit
 constexpr int kInFlight = 2;  // blocks that a wave of narrow tiles has on their way
@@ -140,12 +152,12 @@ struct Line {
   Cut cut;
   int64_t first;  // the workgroup's first run
 };
-template <int TR, int N, bool XCDS>
+template <int TR, int W, int N, bool XCDS>
 __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start (&starts)[N]) {
-  __shared__ int64_t wave_units[kShWaves];
-  __shared__ int wave_items[kShWaves];
+  __shared__ int64_t wave_units[W];
+  __shared__ int wave_items[W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int b0 = (int)((int64_t)a.c.n_req * threadIdx.x / kShThreads), b1 = (int)((int64_t)a.c.n_req * (threadIdx.x + 1) / kShThreads);
+  const int b0 = (int)((int64_t)a.c.n_req * threadIdx.x / (W * 64)), b1 = (int)((int64_t)a.c.n_req * (threadIdx.x + 1) / (W * 64));
   int64_t own = 0;
   int own_items = 0;
   Request r{};
@@ -173,7 +185,7 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
   int64_t before = upto - own;
   items -= own_items;
   int64_t units = 0;
-  for (int w = 0; w < kShWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     if (w < wave) {
       before += wave_units[w];
       items += wave_items[w];
@@ -207,7 +219,7 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
     if (threadIdx.x == 0) {
       a.line[0] = units;
     }
-    if (threadIdx.x == kShThreads - 1) a.line[1] = items + own_items;
+    if (threadIdx.x == (W * 64) - 1) a.line[1] = items + own_items;
   }
   __syncthreads();
   return l;
@@ -553,7 +565,7 @@ __global__ __launch_bounds__(kShThreads, kNarrowGroups) void attn_kv4_kernel(Kv4
   __shared__ Start starts[kShWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
-  const Line line = find_line<TR, kShWaves, false>(a, total, starts);
+  const Line line = find_line<TR, kShWaves, kShWaves, false>(a, total, starts);
   const int64_t run = line.first + wave;
   if (run >= line.cut.runs) return;
   const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
@@ -595,16 +607,20 @@ __global__ __launch_bounds__(kShThreads, kNarrowGroups) void attn_kv4_kernel(Kv4
 }
 
 // ---- wide tiles: a run to a workgroup ----
-// Four waves of 64 rows (two row blocks), as in attention over a bf16 prefix (attn_rows.h): steps
-// of 64 keys in LDS in bf16, four of them in turn. What fills them differs: a thread fetches its share of a step's codes (a quarter of a
-// key, and of its values) two steps ahead into registers and converts it one step ahead, between
-// the matrix instructions of the step before.
+// Eight waves of 32 rows, two to a SIMD, with the loop of attention over a bf16 prefix
+// (attn_rows.h): the next block's scores and the last block's products beside a block's softmax.
+// Steps of 64 keys lie in LDS in bf16, four of them in turn; a thread fetches its share of a
+// step's codes (an eighth of a key, and of its values) two steps ahead into registers and converts
+// it one step ahead, between the matrix instructions of the step before. 4680 rows of 12 heads
+// against 32760 keys: 997 us = 945 TFLOP/s; four waves of 64 rows, which read half as much of LDS,
+// 1056. The vector instructions bound it (140 to a wave's block beside 16 matrix instructions,
+// which are busy 0.42 of the cycles, vector issue 0.56, LDS 0.31).
 template <int D>
 struct WCfg {
   static constexpr int step = 2;  // blocks
   static constexpr int slots = 4;
   static constexpr int stepBytes = step * SCfg<D>::blockBytes;
-  static constexpr int words = D / 32;  // of 8 codes, a thread's share of a key
+  static constexpr int words = D / 8 / kWideWaves;  // of 8 codes, a thread's share of a key
   static constexpr int smem = slots * stepBytes;
 };
 
@@ -618,23 +634,19 @@ struct Share {
 // Where a thread's share of a step goes and comes from.
 template <int D>
 struct Lay {
-  int row[2];     // of its block, for the key and the values
-  int quarter, block;
+  int row, part, block;  // a key of a block, an eighth of it
   int at[2][WCfg<D>::words];  // bytes in a step
   __device__ __forceinline__ explicit Lay(int tid) {
     using C = SCfg<D>;
-    constexpr int W = WCfg<D>::words;
+    constexpr int N = WCfg<D>::words;
     const int lane = tid & 63, wave = tid >> 6;
-    block = wave >> 1;
-    quarter = lane & 3;
-    const int r = lane >> 2;
-    row[0] = 16 * (wave & 1) + r;
-    // (rows beside each other 4 apart: their chunks lie in other banks)
-    row[1] = 16 * (wave & 1) + (r & 10) + ((r & 1) << 2) + ((r >> 2) & 1);
+    block = wave / 4;
+    part = lane % 8;
+    row = 8 * (wave % 4) + lane / 8;
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      at[0][i] = block * C::blockBytes + row[0] * C::rowBytes + (((W * quarter + i) ^ swizzle_k<D>(row[0])) << 4);
-      at[1][i] = block * C::blockBytes + C::tileBytes + row[1] * C::rowBytes + (((W * quarter + i) ^ swizzle_v<D>(row[1])) << 4);
+    for (int i = 0; i < N; ++i) {
+      at[0][i] = block * C::blockBytes + row * C::rowBytes + (((N * part + i) ^ swizzle_k<D>(row)) << 4);
+      at[1][i] = block * C::blockBytes + C::tileBytes + row * C::rowBytes + (((N * part + i) ^ swizzle_v<D>(row)) << 4);
     }
   }
 };
@@ -648,6 +660,7 @@ struct Source {
 // that are no keys come from inside a page all the same and become zeros, whatever it holds.
 template <int D>
 __device__ __forceinline__ int fetch_step(const Kv4AttnArgs& a, Source& src, const Lay<D>& lay, int wave_block, Share<D>& to) {
+  constexpr int N = WCfg<D>::words;
   const int64_t size = (int64_t)1 << a.c.log_page, page_bytes = kv4_page_bytes(a.c.log_page, D);
   Block at[2];
 #pragma unroll
@@ -660,26 +673,24 @@ __device__ __forceinline__ int fetch_step(const Kv4AttnArgs& a, Source& src, con
   src.block += 2;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint8_t* p = base + (i * size + row + lay.row[i]) * (D / 2) + lay.quarter * (D / 8);
-    if constexpr (D == 128) {
-      const u32x4 x = *(const u32x4*)p;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) to.c[i][j] = x[j];
-    } else {
+    const uint8_t* p = base + (i * size + row + lay.row) * (D / 2) + lay.part * (4 * N);
+    if constexpr (N == 2) {
       const u32x2 x = *(const u32x2*)p;
       to.c[i][0] = x[0];
       to.c[i][1] = x[1];
+    } else {
+      to.c[i][0] = *(const uint32_t*)p;
     }
-    to.e[i] = base[size * D + (int64_t)(row + lay.row[i]) * (D / 16) + i * (D / 32) + lay.quarter * D / 128];
+    to.e[i] = base[size * D + (int64_t)(row + lay.row) * (D / 16) + i * (D / 32) + lay.part * N / 4];
   }
   return at[0].keys | at[1].keys << 8;
 }
 // Word i (keys first) of a share into the step at `to`; nv: keys of the thread's block.
 template <int D>
 __device__ __forceinline__ void convert(const Share<D>& s, const Lay<D>& lay, int nv, lds_byte* to, int i) {
-  constexpr int W = WCfg<D>::words;
-  const int t = i / W, j = i % W;
-  const bool key = lay.row[t] < nv;
+  constexpr int N = WCfg<D>::words;
+  const int t = i / N, j = i % N;
+  const bool key = lay.row < nv;
   *(ISPA_LDS bf16x8*)(to + lay.at[t][j]) = kv4_values(key ? s.c[t][j] : 0u, kv4_scale(key ? s.e[t] : 0u));
 }
 
@@ -687,14 +698,14 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 
 // The blocks of a piece, met by all four waves.
 template <int D, int F>
-__device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w, lds_byte* smem, Source src, int wave, int tid,
+__device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 1>& w, lds_byte* smem, Source src, int wave, int tid,
                                            const Lay<D>& lay) {
   using C = SCfg<D>;
   using WC = WCfg<D>;
-  constexpr int RB = 2, kWords = 2 * WC::words;
+  constexpr int RB = 1, kWords = 2 * WC::words;
   const int hh = (tid & 63) >> 5;
   const int n_steps = (src.end - src.block + WC::step - 1) / WC::step;
-  const int own = wave >> 1;  // the block of a step that this wave converts
+  const int own = wave / 4;  // the block of a step that this wave converts
   auto slot = [&](int s) __attribute__((always_inline)) { return smem + (s & (WC::slots - 1)) * WC::stepBytes; };
   auto mine = [&](int nv) __attribute__((always_inline)) { return nv >> (8 * own) & 255; };
   Share<D> now, next_share;
@@ -781,14 +792,14 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 2>& w,
 
 // F: the parts of a weight.
 template <int D, int F>
-__global__ __launch_bounds__(kShThreads) void attn_kv4_wide_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnArgs a) {
   using C = SCfg<D>;
-  constexpr int RB = 2, TR = kShWaves * RB * kBlk;
+  constexpr int RB = 1, TR = kWideWaves * RB * kBlk;
   __shared__ __attribute__((aligned(1024))) char smem[WCfg<D>::smem];
   __shared__ Start starts[1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
-  const Line line = find_line<TR, 1, true>(a, total, starts);
+  const Line line = find_line<TR, kWideWaves, 1, true>(a, total, starts);
   const int64_t run = line.first;
   if (run >= line.cut.runs) return;
   const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
@@ -938,9 +949,9 @@ template <int D>
 hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((a.most_runs + kAXcds - 1) / kAXcds * kAXcds);
   if (a.out_bf16)
-    attn_kv4_wide_kernel<D, 1><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 1><<<grid, kWideWaves * 64, 0, stream>>>(a);
   else
-    attn_kv4_wide_kernel<D, 2><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 2><<<grid, kWideWaves * 64, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
 template <int D>
@@ -957,8 +968,8 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   // keys again, but few rows give the chip more runs that way, and tiles of 32 fit what a request
   // has (64 rows of 32 requests against up to 16384 keys 118 us, and 168 in tiles of 64; 16
   // requests of up to 128 rows 109 us, and 135 in tiles of 128). Beyond, a workgroup takes 256
-  // rows and meets its keys once (one request's 256 rows of 8 heads against 32768 keys 66 us, 73
-  // in tiles of 32; 512 rows 103 and 121). Requests of one batch mostly differ: several keep the
+  // rows and meets its keys once (one request's 256 rows of 8 heads against 32768 keys 64 us, 73
+  // in tiles of 32; 512 rows 99 and 121). Requests of one batch mostly differ: several keep the
   // narrow tiles up to 320 rows (24 requests of up to 154 rows 50 us, 70 in tiles of 256; four of
   // up to 300 53 and 63).
   const int64_t rows = (int64_t)(a->max_q < a->n_rows ? a->max_q : a->n_rows) * a->group;
