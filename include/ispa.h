@@ -720,10 +720,10 @@ int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, i
  *   d_q_weight, d_k_weight, d_q_bias, d_k_bias   fp32 [head_dim] or NULL (not wanted); those
  *               of k need k
  *   workspace   device, 256-byte aligned, at least ispa_norm_rotary_backward_workspace_bytes
- *               bytes; may be NULL where no gradient of a vector is wanted. Used only during
+ *               bytes for the same sizes on the same device; may be NULL where no gradient of a vector is wanted. Used only during
  *               the call's device work.
- * Sums over rows and heads are fp32, in an order that depends on the sizes alone: the same
- * call gives the same bits. Asynchronous on `stream`.
+ * Sums over rows and heads are fp32, in an order that depends on the sizes and the device alone:
+ * the same call gives the same bits. Asynchronous on `stream`.
  */
 int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_k_out, int64_t ld_gk, int32_t g_dtype,
                               const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
@@ -734,8 +734,8 @@ int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_
                               float amplitude, int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                               void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes of ispa_norm_rotary_backward (n_kv_heads 0: without k); 0 for invalid sizes
- * or no rows. */
+/* Workspace bytes of ispa_norm_rotary_backward on the current device (n_kv_heads 0: without k);
+ * 0 for invalid sizes or no rows. */
 size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 
 /* ------------------------------------------------------ a cache in 4 bits */
@@ -821,9 +821,9 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
  *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
  *   workspace   device, 256-byte aligned, at least ispa_attn_kv4_workspace_bytes bytes for the
  *               same sizes on the same device. Used only during the call's device work.
- * An fp32 out has the softmax weights in 16 bits (2^-16 of sum w |v|). So has a bf16 one, except
- * where max_q (or n_rows, if that is less) times n_heads / n_kv_heads is more than 16: there the
- * weights enter the product with the values rounded to bf16 (2^-8 of sum w |v| at most). Row
+ * An fp32 out has the softmax weights as fp32 numbers. A bf16 one has them in 16 bits (2^-16 of
+ * sum w |v|), except where max_q (or n_rows, if that is less) times n_heads / n_kv_heads is more
+ * than 16: there the weights enter the product with the values rounded to bf16 (2^-8 of sum w |v| at most). Row
  * distances are multiples of 8 elements, pointers 16-byte aligned (lse and integers 4). Keys
  * and values behind a request's end are never used, whatever their pages hold. Outputs must not
  * overlap the inputs or each other. The same call gives the same bits. Asynchronous on `stream`.

@@ -1176,19 +1176,22 @@ def norm_rotary_backward(d_q_out, d_k_out, q, k, positions, freqs, n_heads, n_kv
             out[name] = torch.empty_like(t) if rows else torch.zeros_like(t)
     if rows == 0:
         return out
-    nbytes, ws = 0, None
-    if len(out) > 1 + (k is not None):
-        nbytes = L.ispa_norm_rotary_backward_workspace_bytes(rows, int(n_heads), n_kv_heads if k is not None else 0,
-                                                             head_dim)
-        ws = q.new_empty(nbytes, dtype=torch.uint8)
     grad = lambda name: _ptr(out.get(name))
-    st = _on(dev, lambda: L.ispa_norm_rotary_backward(
-        d_q_out.data_ptr(), ld_gq, _ptr(d_k_out), ld_gk, _DT[d_q_out.dtype], q.data_ptr(), ld_q, _ptr(k), ld_k,
-        _DT[q.dtype], _NORMS[norm], _ptr(q_weight), _ptr(k_weight), float(eps), grad("q"), q.shape[1], grad("k"),
-        k.shape[1] if k is not None else 0, grad("q_weight"), grad("k_weight"), grad("q_bias"), grad("k_bias"),
-        positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
-        float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _ptr(ws), nbytes, _stream(dev)))
-    _check(st, "ispa_norm_rotary_backward")
+
+    def call():
+        nbytes, ws = 0, None
+        if len(out) > 1 + (k is not None):
+            nbytes = L.ispa_norm_rotary_backward_workspace_bytes(rows, int(n_heads), n_kv_heads if k is not None else 0,
+                                                                 head_dim)
+            ws = q.new_empty(nbytes, dtype=torch.uint8)
+        return L.ispa_norm_rotary_backward(
+            d_q_out.data_ptr(), ld_gq, _ptr(d_k_out), ld_gk, _DT[d_q_out.dtype], q.data_ptr(), ld_q, _ptr(k), ld_k,
+            _DT[q.dtype], _NORMS[norm], _ptr(q_weight), _ptr(k_weight), float(eps), grad("q"), q.shape[1], grad("k"),
+            k.shape[1] if k is not None else 0, grad("q_weight"), grad("k_weight"), grad("q_bias"), grad("k_bias"),
+            positions.data_ptr(), freqs.data_ptr(), pairs, n_axes, 2 * freqs.shape[0], int(bool(interleaved)),
+            float(amplitude), rows, int(n_heads), n_kv_heads, head_dim, _ptr(ws), nbytes, _stream(dev))
+
+    _check(_on(dev, call), "ispa_norm_rotary_backward")
     return out
 
 
@@ -1320,7 +1323,7 @@ def attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, max_q=None, sca
         raise ValueError("n_heads must be a multiple of the cache's heads")
     _require(q_start, "q_start", torch.int32, dev, ndim=1)
     _require(cache_lens, "cache_lens", torch.int32, dev, ndim=1)
-    if cache_lens.shape[0] != n_req or q_start.shape[0] != n_req + 1:
+    if n_req < 1 or cache_lens.shape[0] != n_req or q_start.shape[0] != n_req + 1:
         raise ValueError("cache_lens must have an entry for every request of page_table, and q_start one more")
     max_q = int(max_q) if max_q is not None else max(1, -(-rows // n_req))
     if out is None:

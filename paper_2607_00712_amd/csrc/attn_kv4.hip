@@ -219,7 +219,7 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
     if (threadIdx.x == 0) {
       a.line[0] = units;
     }
-    if (threadIdx.x == (W * 64) - 1) a.line[1] = items + own_items;
+    if (threadIdx.x == W * 64 - 1) a.line[1] = items + own_items;
   }
   __syncthreads();
   return l;
@@ -228,6 +228,7 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
 // An item's first part is told by the run that it begins in.
 template <int TR>
 __device__ __forceinline__ void tell_item(const Kv4AttnArgs& a, int64_t run, const Walk<TR>& w) {
+  if ((unsigned)w.number >= (unsigned)a.most_items) return;  // (request starts that do not ascend)
   Kv4Item r;
   r.begin = w.item;
   r.end = w.item + w.r.blocks;
@@ -426,8 +427,12 @@ __device__ __forceinline__ void follow(const Kv4AttnArgs& a, NWave<D, RB>& s, co
   }
 }
 
-// The weights as product operands: rounded to bf16, and (F = 2) what the rounding left,
-// rounded again; and their sums, of the weights and (F = 1) of the rounded ones.
+// The weights as product operands: rounded to bf16, and (F = 2 and 3) what the rounding left,
+// rounded again; and their sums, of the weights and (F = 1) of the rounded ones. An fp32 output
+// takes all 24 bits of a weight (F = 3), a bf16 one 16 where the pages' bytes bound the call (16
+// rows; 2^-17 of a weight is nothing beside its own rounding) and 8 where the products do,
+// normalised by the sum of the rounded weights (2^-9 of a weight, as in chunk attention: the
+// output's error is 1.35 times that of its own rounding).
 template <int F>
 __device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float scale_log2, bf16x8 (&p)[F], float& sum,
                                           float& rounded) {
@@ -443,9 +448,16 @@ __device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float s
     const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
     p[0][i] = hi[0];
     p[0][i + 1] = hi[1];
-    if constexpr (F == 2) {
-      p[1][i] = (__bf16)(e0 - (float)hi[0]);
-      p[1][i + 1] = (__bf16)(e1 - (float)hi[1]);
+    if constexpr (F > 1) {
+      float r0 = e0 - (float)hi[0], r1 = e1 - (float)hi[1];  // (exact)
+#pragma unroll
+      for (int f = 1; f < F; ++f) {
+        const bf16x2 lo = {(__bf16)r0, (__bf16)r1};
+        p[f][i] = lo[0];
+        p[f][i + 1] = lo[1];
+        r0 -= (float)lo[0];
+        r1 -= (float)lo[1];
+      }
     } else {
       rounded = __builtin_amdgcn_fdot2_f32_bf16(hi, bf16x2{(__bf16)1.f, (__bf16)1.f}, rounded, false);
     }
@@ -545,7 +557,7 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     s.l[b] += sum[b];
-    s.lr[b] += F == 2 ? sum[b] : rounded[b];
+    s.lr[b] += F > 1 ? sum[b] : rounded[b];
   }
 
   // O^T += V^T P^T
@@ -876,7 +888,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
   __shared__ f32x4 part_stat[kGroups];
   const int64_t units = a.line[0], items = a.line[1];
   const Kv4Item r = a.items[blockIdx.x];  // (on its way with the count)
-  if (blockIdx.x >= items) return;
+  if (blockIdx.x >= items) return;  // (the grid is the items that there can be)
   const int n = (int)(Cut(units, a.most_runs, a.least_units).run_of(r.end - 1) - r.run) + 1;  // parts
   if (n < 2) return;
   const int64_t run = r.run + 1;
@@ -939,10 +951,10 @@ hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
 template <int D, int RB>
 hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((a.most_runs + kShWaves - 1) / kShWaves);
-  if (a.out_bf16 && RB > 1)
+  if (a.out_bf16)
     attn_kv4_kernel<D, RB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
   else
-    attn_kv4_kernel<D, RB, 2><<<grid, kShThreads, 0, stream>>>(a);
+    attn_kv4_kernel<D, RB, 3><<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
 template <int D>
@@ -951,7 +963,7 @@ hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
   if (a.out_bf16)
     attn_kv4_wide_kernel<D, 1><<<grid, kWideWaves * 64, 0, stream>>>(a);
   else
-    attn_kv4_wide_kernel<D, 2><<<grid, kWideWaves * 64, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 3><<<grid, kWideWaves * 64, 0, stream>>>(a);
   return launch_join<D>(a, stream);
 }
 template <int D>

@@ -108,9 +108,16 @@ __device__ __forceinline__ void put_pair(SWeights<F>& p, int i, float e0, float 
   const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
   p.p[0][i / 8][i % 8] = hi[0];
   p.p[0][i / 8][i % 8 + 1] = hi[1];
-  if constexpr (F == 2) {
-    p.p[1][i / 8][i % 8] = (__bf16)(e0 - (float)hi[0]);
-    p.p[1][i / 8][i % 8 + 1] = (__bf16)(e1 - (float)hi[1]);
+  if constexpr (F > 1) {
+    float r0 = e0 - (float)hi[0], r1 = e1 - (float)hi[1];  // (exact)
+#pragma unroll
+    for (int f = 1; f < F; ++f) {
+      const bf16x2 lo = {(__bf16)r0, (__bf16)r1};
+      p.p[f][i / 8][i % 8] = lo[0];
+      p.p[f][i / 8][i % 8 + 1] = lo[1];
+      r0 -= (float)lo[0];
+      r1 -= (float)lo[1];
+    }
   } else {
     const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
     rounded = __builtin_amdgcn_fdot2_f32_bf16(hi, one, rounded, false);
@@ -335,7 +342,7 @@ __device__ __forceinline__ void check_reference(const A& a, SWave<D, RB>& w, con
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     w.l[b] += sum[b];
-    w.lr[b] += F == 2 ? sum[b] : rounded[b];
+    w.lr[b] += F > 1 ? sum[b] : rounded[b];
   }
 }
 

@@ -148,7 +148,7 @@ __device__ __forceinline__ T head_norm(T (&x)[8], T (&y)[8], T eps, int head_dim
   if constexpr (sizeof(T) == 8)
     return 1.0 / sqrt(var);
   else
-    return __builtin_amdgcn_rsqf(var);  // (within a unit in the last place)
+    return rsqrtf(var);
 }
 
 // A unit's values of a vector of a head

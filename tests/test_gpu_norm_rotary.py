@@ -168,6 +168,33 @@ def test_backward(case):
                 check(got[n], want, size, 2.0 ** -14, n)
 
 
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("types", [(BF16, F32), (F32, BF16), (BF16, BF16), (F32, F32)])
+def test_every_kind_of_gradient(types, bias, norm):
+    """Types of the values and of the gradients, with and without a bias's."""
+    rows, heads, kv, d, axes = 53, 7, 2, 128, (40, 24)
+    g = torch.Generator().manual_seed(11)
+    r = lambda *s: torch.randn(*s, generator=g)
+    x = {"q": (r(rows, heads * d) + 0.3).to(types[0]), "k": r(rows, kv * d).to(types[0])}
+    dz = {"q": r(rows, heads * d).to(types[1]), "k": r(rows, kv * d).to(types[1])}
+    w = {n: 1 + 0.3 * r(d) for n in "qk"}
+    p = torch.randint(0, 5000, (rows, 2), generator=g, dtype=torch.int32)
+    f, _ = ispa.rotary_frequencies(axes, device="cpu")
+    b = torch.zeros(d, device=DEV) if bias else None
+    put = lambda t: t.to(DEV)
+    got = ispa.norm_rotary_backward(put(dz["q"]), put(dz["k"]), put(x["q"]), put(x["k"]), put(p), put(f), heads, kv, norm,
+                                    put(w["q"]), put(w["k"]), b, b, axes=axes, interleaved=bias, amplitude=0.8)
+    torch.cuda.synchronize()
+    for n in "qk":
+        (dx, dx_size), (dw, dw_size), (db, db_size) = backward(dz[n], x[n], w[n], p, f, axes, d, norm, bias, 0.8)
+        assert got[n].dtype == types[0]
+        check(got[n], dx, dx_size, 2.0 ** -17, n)
+        check(got[n + "_weight"], dw, dw_size, 2.0 ** -14, n + "_weight")
+        if bias:
+            check(got[n + "_bias"], db, db_size, 2.0 ** -14, n + "_bias")
+
+
 def test_gradient_against_differences():
     """<gradient, direction> against differences of the definition: steps h and 2 h, whose
     disagreement is three times the error of the smaller one."""
