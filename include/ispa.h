@@ -720,8 +720,8 @@ int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, i
  *   d_q_weight, d_k_weight, d_q_bias, d_k_bias   fp32 [head_dim] or NULL (not wanted); those
  *               of k need k
  *   workspace   device, 256-byte aligned, at least ispa_norm_rotary_backward_workspace_bytes
- *               bytes for the same sizes on the same device; may be NULL where no gradient of a vector is wanted. Used only during
- *               the call's device work.
+ *               bytes for the same sizes on the same device; may be NULL where no gradient of
+ *               a vector is wanted. Used only during the call's device work.
  * Sums over rows and heads are fp32, in an order that depends on the sizes and the device alone:
  * the same call gives the same bits. Asynchronous on `stream`.
  */
@@ -751,7 +751,8 @@ size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, 
  * 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(power - 127). The power is the smallest with no value
  * above 7 times it, within 2^-120 .. 2^125, and each value is rounded to the nearest number,
  * ties to the even code, so that it is off by at most half a step (one fifth of the block's
- * largest value at most: a block whose largest is 5 times its power). A block with an infinity or a NaN has power 255 and reads as NaN.
+ * largest value at most: a block whose largest is 5 times its power). A block with an infinity
+ * or a NaN has power 255 and reads as NaN.
  *
  * In all calls
  *   cache       device uint8 [n_pages, n_kv_heads, ispa_kv4_page_bytes], 16-byte aligned
@@ -823,10 +824,11 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
  *               same sizes on the same device. Used only during the call's device work.
  * An fp32 out has the softmax weights as fp32 numbers. A bf16 one has them in 16 bits (2^-16 of
  * sum w |v|), except where max_q (or n_rows, if that is less) times n_heads / n_kv_heads is more
- * than 16: there the weights enter the product with the values rounded to bf16 (2^-8 of sum w |v| at most). Row
- * distances are multiples of 8 elements, pointers 16-byte aligned (lse and integers 4). Keys
- * and values behind a request's end are never used, whatever their pages hold. Outputs must not
- * overlap the inputs or each other. The same call gives the same bits. Asynchronous on `stream`.
+ * than 16: there the weights enter the product with the values rounded to bf16 (2^-8 of
+ * sum w |v| at most). Row distances are multiples of 8 elements, pointers 16-byte aligned (lse
+ * and integers 4). Keys and values behind a request's end are never used, whatever their pages
+ * hold. Outputs must not overlap the inputs or each other. The same call gives the same bits.
+ * Asynchronous on `stream`.
  */
 int ispa_attn_kv4(const void* q, int64_t ld_q, const void* cache, int64_t n_pages, int64_t page_size,
                   const int32_t* page_table, int64_t max_pages, const int32_t* q_start, const int32_t* cache_lens,

@@ -1215,7 +1215,7 @@ def _kv4(cache, page_table, head_dim, dev=None):
         _require(page_table, "page_table", torch.int32, cache.device)
     n_pages, n_kv_heads, nbytes = cache.shape
     per = head_dim + head_dim // 16
-    if nbytes % per:
+    if per < 1 or nbytes % per:
         raise ValueError(f"cache must hold whole tokens of {per} bytes a head: it is one of another head_dim")
     n_req, max_pages = page_table.shape
     return n_pages, nbytes // per, n_req, max_pages, n_kv_heads

@@ -163,10 +163,6 @@ __device__ __forceinline__ void unit_vector(const float* p, const UnitPlace& u, 
     }
   }
 }
-__device__ __forceinline__ void unit_constant(float c, float (&x)[8], float (&y)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = y[i] = c;
-}
 
 // lanes to a head: its units, a power of two of them
 __host__ __device__ __forceinline__ int head_lanes(int head_dim) {

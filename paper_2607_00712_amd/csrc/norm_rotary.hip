@@ -225,13 +225,23 @@ __global__ __launch_bounds__(kHThreads) void norm_rotary_back_kernel(NormRotaryA
   if (!a.part) return;
   // the sums of the lanes with the same place in a head, then of the waves, in order
   auto join = [&](float (&v)[8], float* to, int e) __attribute__((always_inline)) {
+    if (mine && (threadIdx.x & 63) < (unsigned)a.lanes) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float s = v[j];
-      for (int d = a.lanes; d < 64; d *= 2) s += __shfl_xor(s, d);
-      if (mine && (threadIdx.x & 63) < (unsigned)a.lanes) to[e + j] = s;
+      for (int j = 0; j < 8; ++j) to[e + j] = v[j];
     }
   };
+  // (the steps outside: the values' exchanges of one step are in flight together)
+  for (int d = a.lanes; d < 64; d *= 2) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      dw0[j] += __shfl_xor(dw0[j], d);
+      dw1[j] += __shfl_xor(dw1[j], d);
+      if (BIAS) {
+        db0[j] += __shfl_xor(db0[j], d);
+        db1[j] += __shfl_xor(db1[j], d);
+      }
+    }
+  }
   float(&own)[2][2 * kHMaxPairs] = sums[threadIdx.x >> 6];
   join(dw0, own[0], u.e0);
   join(dw1, own[0], u.e1);
