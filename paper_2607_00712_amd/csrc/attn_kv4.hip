@@ -35,7 +35,10 @@ namespace {
 constexpr int kAXcds = 8;
 constexpr int kWideWaves = 8;
 constexpr int kJoinThreads = 512;
-constexpr int kNarrowGroups = 2;  // workgroups of narrow tiles to a compute unit
+// Workgroups of narrow tiles to a compute unit, as many as the registers allow (64 tokens of 32
+// heads of 64 values on 8 against up to 16384 keys: 74 us with three, 89 with two; tiles of 32
+// rows spill with three and gain nothing).
+constexpr int narrow_groups(int head_dim, int tile_rows) { return head_dim == 64 && tile_rows == 16 ? 3 : 2; }
 constexpr int kInFlight = 2;  // blocks that a wave of narrow tiles has on their way
 
 typedef ISPA_LDS char lds_byte;
@@ -570,7 +573,7 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
 }
 
 template <int D, int RB, int F>
-__global__ __launch_bounds__(kShThreads, kNarrowGroups) void attn_kv4_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
   using C = NCfg<D>;
   constexpr int TR = 16 * RB;
   __shared__ __attribute__((aligned(1024))) char smem[kShWaves * C::stageBytes];
@@ -708,7 +711,7 @@ __device__ __forceinline__ void convert(const Share<D>& s, const Lay<D>& lay, in
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The blocks of a piece, met by all four waves.
+// The blocks of a piece, met by all waves.
 template <int D, int F>
 __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 1>& w, lds_byte* smem, Source src, int wave, int tid,
                                            const Lay<D>& lay) {
@@ -988,7 +991,7 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   a->tile_rows = rows <= 16 ? 16 : rows <= (a->c.n_req > 1 ? 320 : 128) ? 32 : 256;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
   const bool wide = a->tile_rows == 256;
-  a->most_runs = n_cu * (wide ? 1 : kNarrowGroups * kShWaves);
+  a->most_runs = n_cu * (wide ? 1 : narrow_groups(head_dim, a->tile_rows) * kShWaves);
   // (a workgroup's run has a start, and a part to be joined, as long as some 16 blocks; a wave's
   // short runs are worth it: one row of 12 heads against 32760 keys 25 us with 4, 28 with 12)
   a->least_units = wide ? 16 : 4;
@@ -1000,8 +1003,9 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   const int64_t runs = (tiles * a->c.n_kv_heads * (blocks + a->ahead) + a->least_units - 1) / a->least_units;
   if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
   a->most_items = (int)(tiles * a->c.n_kv_heads);
-  // few items: their rows to more workgroups of the join
-  a->join_rows = 16;
+  // a pass of the join's threads over the rows of its workgroup; few items: fewer rows each
+  a->join_rows = kJoinThreads / (head_dim / 4);
+  if (a->join_rows > a->tile_rows) a->join_rows = a->tile_rows;
   while (a->join_rows > 1 && (int64_t)a->most_items * a->tile_rows / a->join_rows < 1024) a->join_rows /= 2;
   const size_t parts = (size_t)a->most_runs * 2 * a->tile_rows;
   a->stat_offset = parts * head_dim * sizeof(float);
