@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kAXcds = 8;
 constexpr int kWideWaves = 8;
+constexpr int kWideRows = kWideWaves * 32;
 constexpr int kJoinThreads = 512;
 // Workgroups of narrow tiles to a compute unit, as many as the registers allow (64 tokens of 32
 // heads of 64 values on 8 against up to 16384 keys: 74 us with three, 89 with two; tiles of 32
@@ -572,12 +573,58 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
       for (int f = 0; f < F; ++f) s.acc[b][d] = mfma16(v[d].v, p[b][f], s.acc[b][d]);
 }
 
+// The parts of a workgroup's four runs as one, where all of them lie inside one item: a quarter of
+// the output blocks to a wave.
+template <int D, int RB>
+__device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D, RB>& s, int rows, int64_t slot, lds_byte* smem,
+                                             ISPA_LDS f32x4 (&stats)[kShWaves][16], int wave, int lane) {
+  using C = NCfg<D>;
+  constexpr int kOwn = C::dBlocks / kShWaves;
+  const int g = lane >> 4, m16 = lane & 15;
+  auto block = [&](int w, int d) __attribute__((always_inline)) {
+    return (ISPA_LDS f32x4*)(smem + w * C::stageBytes) + d * 64 + lane;
+  };
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const float l = quad_sum(s.l[b]), lr = quad_sum(s.lr[b]);
+    __syncthreads();  // the stages, or the rows before, have been read
+#pragma unroll
+    for (int d = 0; d < C::dBlocks; ++d) *block(wave, d) = s.acc[b][d];
+    if (g == 0) stats[wave][m16] = f32x4{s.m[b], l, lr, 0.f};
+    __syncthreads();
+    f32x4 st[kShWaves];
+#pragma unroll
+    for (int w = 0; w < kShWaves; ++w) st[w] = stats[w][m16];
+    float m = st[0][0];
+#pragma unroll
+    for (int w = 1; w < kShWaves; ++w) m = fmaxf(m, st[w][0]);
+    f32x4 all = {m, 0.f, 0.f, 0.f}, o[kOwn];
+#pragma unroll
+    for (int d = 0; d < kOwn; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kShWaves; ++w) {
+      const float e = st[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st[w][0] - m) * a.scale_log2);
+      all[1] += st[w][1] * e;
+      all[2] += st[w][2] * e;
+#pragma unroll
+      for (int d = 0; d < kOwn; ++d) o[d] += *block(w, wave * kOwn + d) * e;
+    }
+    const int in_tile = b * 16 + m16;
+    if (in_tile >= rows) continue;
+    const int64_t at = slot * 16 * RB + in_tile;
+    if (wave == 0 && g == 0) *(f32x4*)(a.part_stat + 4 * at) = all;
+#pragma unroll
+    for (int d = 0; d < kOwn; ++d) *(f32x4*)(a.part_o + at * D + 16 * (wave * kOwn + d) + 4 * g) = o[d];
+  }
+}
+
 template <int D, int RB, int F>
 __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
   using C = NCfg<D>;
   constexpr int TR = 16 * RB;
   __shared__ __attribute__((aligned(1024))) char smem[kShWaves * C::stageBytes];
   __shared__ Start starts[kShWaves];
+  __shared__ f32x4 stats[kShWaves][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
   const Line line = find_line<TR, kShWaves, kShWaves, false>(a, total, starts);
@@ -589,6 +636,9 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
   int64_t u = u0 > w.item ? u0 : w.item;  // the unit of a block
   if (u >= u1) return;
   if (lane == 0 && w.block == 0) tell_item(a, run, w);
+  // (the same for all waves: the item begins before the first one's run and ends behind the last one's)
+  const bool grouped = w.item < line.cut.begin(line.first) && w.item + w.r.blocks > line.cut.begin(line.first + kShWaves);
+  const int rows = w.r.rows - w.tile * TR;
   lds_byte* stage = (lds_byte*)smem + wave * C::stageBytes;
   Feeder<D, TR> f;
   f.start(w, u, u1, lane);
@@ -605,6 +655,7 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
         ++u;
         const bool last = w.block + 1 == w.r.blocks;
         if (last || u == u1) {
+          if (grouped) break;
           const bool whole = last && w.item >= u0;
           finish_item<D, RB>(a, s, w, whole ? -1 : 2 * run + (w.item >= u0 ? 1 : 0), lane);
           w.next(a, total);
@@ -619,6 +670,7 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
       }
     }
   }
+  if (grouped) finish_group<D, RB>(a, s, rows, 2 * line.first, (lds_byte*)smem, (ISPA_LDS f32x4(&)[kShWaves][16])stats, wave, lane);
 }
 
 // ---- wide tiles: a run to a workgroup ----
@@ -809,7 +861,7 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 1>& w,
 template <int D, int F>
 __global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnArgs a) {
   using C = SCfg<D>;
-  constexpr int RB = 1, TR = kWideWaves * RB * kBlk;
+  constexpr int RB = 1, TR = kWideRows;
   __shared__ __attribute__((aligned(1024))) char smem[WCfg<D>::smem];
   __shared__ Start starts[1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -883,8 +935,8 @@ __device__ __forceinline__ void join_part(Joined& r, float scale_log2, float m, 
 }
 
 // Joins the parts of an item that lies in several runs, a.join_rows of its rows to a workgroup:
-// side by side, and where there are few of them slices of the parts too.
-template <int D>
+// side by side, and where there are few of them slices of the parts too. W: runs of a workgroup.
+template <int D, int W>
 __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs a) {
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes, kBatch = 4;
   __shared__ f32x4 part_o[kJoinThreads];
@@ -892,9 +944,21 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
   const int64_t units = a.line[0], items = a.line[1];
   const Kv4Item r = a.items[blockIdx.x];  // (on its way with the count)
   if (blockIdx.x >= items) return;  // (the grid is the items that there can be)
-  const int n = (int)(Cut(units, a.most_runs, a.least_units).run_of(r.end - 1) - r.run) + 1;  // parts
-  if (n < 2) return;
-  const int64_t run = r.run + 1;
+  const uint32_t first = (uint32_t)r.run, last = (uint32_t)Cut(units, a.most_runs, a.least_units).run_of(r.end - 1);
+  if (first == last) return;
+  // The parts: those of the first runs, of workgroups of W whole runs, of the last runs.
+  const uint32_t g0 = (first / W + 1) * W, g1 = last / W * W;
+  const int groups = W > 1 && g1 > g0 ? (int)((g1 - g0) / W) : 0;
+  const int lead = (int)(groups ? g0 - first : last - first + 1);
+  const int n = lead + (groups ? groups + (int)(last - g1) + 1 : 0);
+  auto slot = [&](int p) __attribute__((always_inline)) {
+    int run = (int)first + p;
+    if (W > 1 && p >= lead) {
+      p -= lead;
+      run = p < groups ? (int)g0 + W * p : (int)g1 + p - groups;
+    }
+    return 2 * run + (run == (int)first ? 1 : 0);
+  };
   const int rows = r.rows - r.row0 < a.tile_rows ? r.rows - r.row0 : a.tile_rows;
   const int y0 = blockIdx.y * a.join_rows, y1 = rows < y0 + a.join_rows ? rows : y0 + a.join_rows;
   if (y0 >= y1) return;
@@ -913,7 +977,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {  // (loads in flight together)
           const int p = i0 + i < end ? i0 + i : end - 1;
-          const int64_t at = (2 * (run - 1 + p) + (p == 0 ? 1 : 0)) * a.tile_rows + row;
+          const int64_t at = (int64_t)slot(p) * a.tile_rows + row;
           st[i] = *(const f32x4*)(a.part_stat + 4 * at);
           o[i] = *(const f32x4*)(a.part_o + at * D + 4 * c);
         }
@@ -944,11 +1008,11 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
   }
 }
 
-template <int D>
+template <int D, int W>
 hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.most_runs < 2) return e;
-  attn_kv4_join_kernel<D><<<dim3(a.most_items, a.tile_rows / a.join_rows), kJoinThreads, 0, stream>>>(a);
+  attn_kv4_join_kernel<D, W><<<dim3(a.most_items, a.tile_rows / a.join_rows), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <int D, int RB>
@@ -958,7 +1022,7 @@ hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
     attn_kv4_kernel<D, RB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
   else
     attn_kv4_kernel<D, RB, 3><<<grid, kShThreads, 0, stream>>>(a);
-  return launch_join<D>(a, stream);
+  return launch_join<D, kShWaves>(a, stream);
 }
 template <int D>
 hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
@@ -967,7 +1031,7 @@ hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
     attn_kv4_wide_kernel<D, 1><<<grid, kWideWaves * 64, 0, stream>>>(a);
   else
     attn_kv4_wide_kernel<D, 3><<<grid, kWideWaves * 64, 0, stream>>>(a);
-  return launch_join<D>(a, stream);
+  return launch_join<D, 1>(a, stream);
 }
 template <int D>
 hipError_t launch_d(const Kv4AttnArgs& a, hipStream_t stream) {
@@ -988,9 +1052,9 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   // narrow tiles up to 320 rows (24 requests of up to 154 rows 50 us, 70 in tiles of 256; four of
   // up to 300 53 and 63).
   const int64_t rows = (int64_t)(a->max_q < a->n_rows ? a->max_q : a->n_rows) * a->group;
-  a->tile_rows = rows <= 16 ? 16 : rows <= (a->c.n_req > 1 ? 320 : 128) ? 32 : 256;
+  a->tile_rows = rows <= 16 ? 16 : rows <= (a->c.n_req > 1 ? 320 : 128) ? 32 : kWideRows;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
-  const bool wide = a->tile_rows == 256;
+  const bool wide = a->tile_rows == kWideRows;
   a->most_runs = n_cu * (wide ? 1 : narrow_groups(head_dim, a->tile_rows) * kShWaves);
   // (a workgroup's run has a start, and a part to be joined, as long as some 16 blocks; a wave's
   // short runs are worth it: one row of 12 heads against 32760 keys 25 us with 4, 28 with 12)
