@@ -505,6 +505,20 @@ def test_many_requests():
             check(*attend(on_gpu(one), 2, out_dtype=F32), exact(one, 2), b)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_items_of_many_runs(rows, d):
+    """Items cut into some ten to thirty runs, which begin and end at every place of a workgroup's
+    four: parts of runs, of whole workgroups, and of runs without any key (missing pages)."""
+    for i, keys in enumerate([900, 1025, 1151, 1280, 1409, 1537, 1666, 1793, 2200, 2944, 3333, 4096]):
+        t = make([rows, 1], [keys, 700], 32, 128, 4, 4, d, seed=i)
+        if i % 3 == 1:
+            t["table"][0, 5:22] = -1
+        got = attend(on_gpu(t), 4, max_q=rows, out_dtype=F32)
+        check(*got, exact(t, 4), keys)
+        assert all(torch.equal(x, y) for x, y in zip(got, attend(on_gpu(t), 4, max_q=rows, out_dtype=F32)))
+
+
 def test_far_pages():
     """A pool of more than 2^32 bytes: pages at its end are read, written and attended."""
     d, kv, page = 128, 8, 512
