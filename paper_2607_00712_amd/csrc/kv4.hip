@@ -101,6 +101,9 @@ __global__ __launch_bounds__(kQThreads) void kv4_append_kernel(Kv4AppendArgs a) 
   const int64_t row0 = (int64_t)blockIdx.x * r.tokens;
   const int n = (int)(r.rows - row0 < r.tokens ? r.rows - row0 : r.tokens);
   const int pairs = r.rotary_dim >> 1;
+  const int64_t n_real = a.n_real ? *a.n_real : r.rows;
+  // padding without a place: nothing to do
+  if (row0 >= n_real && !__syncthreads_or(threadIdx.x < (unsigned)n && a.slots[row0 + threadIdx.x] >= 0)) return;
   for (int i = threadIdx.x; i < n * pairs; i += kQThreads) {
     const int t = i / pairs, j = i - t * pairs;
     // the angle less whole turns, in two parts of 2 pi
@@ -114,7 +117,7 @@ __global__ __launch_bounds__(kQThreads) void kv4_append_kernel(Kv4AppendArgs a) 
   if (threadIdx.x < (unsigned)n) {
     const int64_t row = row0 + threadIdx.x;
     place[threadIdx.x] = kv4_place(a.c, a.slots[row]);
-    real[threadIdx.x] = !a.n_real || row < *a.n_real;
+    real[threadIdx.x] = row < n_real;
   }
   __syncthreads();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
