@@ -23,9 +23,12 @@
 //
 // Measured, 128 values a head, two kernels and the launches (a large copy runs at 4.9 TB/s, a
 // reader of the same pages without any arithmetic at 5.4, a large bf16 product at 1223 TFLOP/s):
-// 64 tokens of 32 heads on 8 against up to 16384 keys each 121 us (5.1 TB/s of pages), three
-// requests of up to 5 tokens against up to 131072 78 us (4.6), one token of 12 heads against 32760
-// 25 us (19 the runs, 7 the join); wide tiles below.
+// 64 tokens of 32 heads on 8 against up to 16384 keys each 115-119 us (5.3 TB/s of pages), three
+// requests of up to 5 tokens against up to 131072 71-75 us (4.7), one token of 12 heads against
+// 32760 23-24 us (18.5 the runs, of which some 6 are the start of a run and its first block's
+// way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 36-39 us
+// (vector issue 0.56 of the cycles, matrix cores 0.12): 17 blocks a wave, its start and end as
+// long as half of them; join 8. Wide tiles below.
 #include "attn_rows.h"
 #include "kv4_units.h"
 
