@@ -27,7 +27,7 @@
 // requests of up to 5 tokens against up to 131072 71-75 us (4.7), one token of 12 heads against
 // 32760 23-24 us (18.5 the runs, of which some 6 are the start of a run and its first block's
 // way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 36-39 us
-// (vector issue 0.56 of the cycles, matrix cores 0.12): 17 blocks a wave, its start and end as
+// (vector issue 0.51 of the busy cycles, matrix cores 0.16): 17 blocks a wave, its start and end as
 // long as half of them; join 8. Wide tiles below.
 #include "attn_rows.h"
 #include "kv4_units.h"

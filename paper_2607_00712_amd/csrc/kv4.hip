@@ -17,7 +17,7 @@
 //
 // Measured, bf16, 128 values a head: four requests' 5800 rows (of 6240 with the padding) of 12 +
 // 12 + 12 heads 24 us (3.4 TB/s), 64 rows of 32 + 8 + 8 heads 6.7. The first is bound by the fp64
-// steps (vector issue 0.46 of the cycles) as much as by its bytes: with the next run's loads ahead
+// steps (vector issue 0.72 of the cycles that a compute unit has waves) as much as by its bytes: with the next run's loads ahead
 // it took 30 (160 registers instead of 121, three waves to a SIMD instead of four), and for more
 // waves than four the fp64 values spill (call 53 us instead of 38). Rows read back: 6240 of 12 + 12
 // heads 12 us (4.1 TB/s), bound by the bytes.
