@@ -29,9 +29,38 @@ namespace {
 
 constexpr int kQThreads = 256;
 constexpr int kQWaves = kQThreads / 64;
+constexpr int kQGroups = 4;  // workgroups to a compute unit
 constexpr int kQMaxTokens = 8;
 constexpr int kQPairs = 64;     // rotary_dim / 2 at most
 constexpr int kQValues = 1024;  // values of a wave's run of heads
+
+// Cosine and sine in fp64: the angle less quarter turns, in two parts of pi / 2, and the series
+// up to x^17 / 17!, of which the next terms are below 2^-58 at pi / 4. (The library's function,
+// for all arguments, takes 124 registers, and with them a wave of the kernel's from each SIMD.)
+__device__ __forceinline__ double2 angle_of(double angle) {
+  const double q = rint(angle * 0.6366197723675814);
+  const double x = fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, angle)), z = x * x;
+  double s = 1 / 355687428096000., c = 1 / 20922789888000.;  // 17!, 16!
+  s = fma(s, z, -1 / 1307674368000.);
+  c = fma(c, z, -1 / 87178291200.);
+  s = fma(s, z, 1 / 6227020800.);
+  c = fma(c, z, 1 / 479001600.);
+  s = fma(s, z, -1 / 39916800.);
+  c = fma(c, z, -1 / 3628800.);
+  s = fma(s, z, 1 / 362880.);
+  c = fma(c, z, 1 / 40320.);
+  s = fma(s, z, -1 / 5040.);
+  c = fma(c, z, -1 / 720.);
+  s = fma(s, z, 1 / 120.);
+  c = fma(c, z, 1 / 24.);
+  s = fma(s, z, -1 / 6.);
+  c = fma(c, z, -0.5);
+  s = fma(x * z, s, x);
+  c = fma(c, z, 1.);
+  const int quarter = (int)fma(-4., rint(q * 0.25), q);
+  const double cosine = quarter & 1 ? s : c, sine = quarter & 1 ? c : s;
+  return make_double2((quarter + 1) & 2 ? -cosine : cosine, quarter & 2 ? -sine : sine);
+}
 
 // To fp32 by rounding to odd.
 __device__ __forceinline__ float to_odd(double x) {
@@ -42,10 +71,37 @@ __device__ __forceinline__ float to_odd(double x) {
   return __builtin_bit_cast(float, b);
 }
 
+// Where a row goes, of key head 0: bytes of the pool, or -1 for no place.
+struct Row {
+  int64_t codes, powers;  // of the keys
+};
+template <int D>
+__device__ __forceinline__ Row row_of(const Kv4Cache& c, int64_t slot) {
+  const Kv4Place at = kv4_place(c, slot);
+  if (at.page < 0) return {-1, -1};
+  const int64_t page = (int64_t)at.page * c.n_kv_heads * kv4_page_bytes(c.log_page, D);
+  return {page + at.row * (D / 2), page + ((int64_t)D << c.log_page) + at.row * (D / 16)};
+}
+
+// Head w of a list of `heads` a row: its row and head there. (For the less than 2^17 heads of a
+// workgroup w + 0.5 is 2^-15 of a row or more away from the next one, its product off by 2^-19 at most.)
+struct HeadOf {
+  int heads;
+  float inverse;
+  __device__ __forceinline__ explicit HeadOf(int n) : heads(n), inverse(1.f / n) {}
+  __device__ __forceinline__ int row(int w) const { return (int)(((float)w + 0.5f) * inverse); }
+  __device__ __forceinline__ int head(int w, int t) const { return w - __mul24(t, heads); }
+};
+// Element e of a head of row t. Only the lower half of the row distance is multiplied: where it
+// has an upper one a workgroup has one row.
+__device__ __forceinline__ int64_t element(int64_t row0, int t, int64_t ld, int e) {
+  return row0 * ld + (int64_t)((uint64_t)(uint32_t)t * (uint32_t)ld + (uint32_t)e);
+}
+
 // Eight neighbouring values of a head (a quarter of a block; its other quarters are in the
 // lanes beside) into their place.
 template <int D>
-__device__ __forceinline__ void store_codes(const Kv4Cache& c, const Kv4Place& at, int head, int e, bool is_v,
+__device__ __forceinline__ void store_codes(const Kv4Cache& c, const Row& at, int head, int e, bool is_v,
                                             const float (&x)[8]) {
   uint32_t top = 0;
 #pragma unroll
@@ -58,11 +114,10 @@ __device__ __forceinline__ void store_codes(const Kv4Cache& c, const Kv4Place& a
   top = other(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));
   const uint32_t exponent = kv4_exponent(top);
   const uint32_t codes = kv4_codes(x, kv4_scale(exponent));
-  if (at.page < 0) return;
-  const int64_t size = (int64_t)1 << c.log_page;
-  uint8_t* base = c.pages + ((int64_t)at.page * c.n_kv_heads + head) * kv4_page_bytes(c.log_page, D);
-  *(uint32_t*)(base + ((is_v ? size : 0) + at.row) * (D / 2) + e / 2) = codes;
-  if ((e & 31) == 0) base[size * D + (at.row * 2 + (is_v ? 1 : 0)) * (D / 32) + e / 32] = (uint8_t)exponent;
+  if (at.codes < 0) return;
+  uint8_t* base = c.pages + (uint64_t)(uint32_t)head * (uint32_t)kv4_page_bytes(c.log_page, D);
+  *(uint32_t*)(base + ((is_v ? (int64_t)(D / 2) << c.log_page : 0) + at.codes) + e / 2) = codes;
+  if ((e & 31) == 0) base[at.powers + (is_v ? D / 32 : 0) + e / 32] = (uint8_t)exponent;
 }
 
 // norm(x) weight + bias of a unit
@@ -96,13 +151,46 @@ __device__ __forceinline__ void normed(T (&x)[8], T (&y)[8], T eps, const float*
   }
 }
 
+// The pairs of a unit turned as turn_unit does it, rounded to odd into `to`: half of them at a
+// time, since 32 fp64 values with their angles and results take a wave of the kernel's from each SIMD.
+__device__ __forceinline__ void turn_to_odd(const double (&x)[8], const double (&y)[8], const double2* at, const UnitPlace& u,
+                                            bool interleaved, float* to) {
+#pragma unroll
+  for (int i0 = 0; i0 < 8; i0 += 4) {
+    asm volatile("" ::: "memory");
+    float xs[4], ys[4];
+    if (interleaved) {
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const double2 c = at[u.p0 + (i0 + i) / 2], d = at[u.p1 + (i0 + i) / 2];
+        xs[i] = to_odd(x[i0 + i] * c.x - x[i0 + i + 1] * c.y);
+        xs[i + 1] = to_odd(x[i0 + i] * c.y + x[i0 + i + 1] * c.x);
+        ys[i] = to_odd(y[i0 + i] * d.x - y[i0 + i + 1] * d.y);
+        ys[i + 1] = to_odd(y[i0 + i] * d.y + y[i0 + i + 1] * d.x);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double2 c = at[(i0 == 0 ? u.p0 : u.p1) + i];
+        xs[i] = to_odd(x[i0 + i] * c.x - y[i0 + i] * c.y);
+        ys[i] = to_odd(x[i0 + i] * c.y + y[i0 + i] * c.x);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      to[u.e0 + i0 + i] = xs[i];
+      to[u.e1 + i0 + i] = ys[i];
+    }
+  }
+}
+
 template <bool F32, int D, int NORM>
-__global__ __launch_bounds__(kQThreads) void kv4_append_kernel(Kv4AppendArgs a) {
+__global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4AppendArgs a) {
   constexpr int kLanes = D / 16, kHeads = 64 / kLanes;  // lanes to a head, heads of a run
   static_assert(kHeads * D == kQValues, "a run of heads");
   __shared__ double2 cs[kQMaxTokens * kQPairs];
   __shared__ float exchange[kQWaves][kQValues];
-  __shared__ Kv4Place place[kQMaxTokens];
+  __shared__ Row place[kQMaxTokens];
   __shared__ int real[kQMaxTokens];
   const NormRotaryArgs& r = a.t;
   const int64_t row0 = (int64_t)blockIdx.x * r.tokens;
@@ -113,17 +201,12 @@ __global__ __launch_bounds__(kQThreads) void kv4_append_kernel(Kv4AppendArgs a) 
   if (row0 >= n_real && !__syncthreads_or(threadIdx.x < (unsigned)n && a.slots[row0 + threadIdx.x] >= 0)) return;
   for (int i = threadIdx.x; i < n * pairs; i += kQThreads) {
     const int t = i / pairs, j = i - t * pairs;
-    // the angle less whole turns, in two parts of 2 pi
-    const double angle = (double)r.positions[(row0 + t) * r.n_axes + pair_axis(r.axis_end, j)] * r.freqs[j];
-    const double turns = rint(angle * 0.15915494309189535);
-    const double rest = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, angle));
-    double s, c;
-    sincos(rest, &s, &c);
-    cs[i] = make_double2(c * r.amplitude, s * r.amplitude);
+    const double2 at = angle_of((double)r.positions[(row0 + t) * r.n_axes + pair_axis(r.axis_end, j)] * r.freqs[j]);
+    cs[i] = make_double2(at.x * r.amplitude, at.y * r.amplitude);
   }
   if (threadIdx.x < (unsigned)n) {
     const int64_t row = row0 + threadIdx.x;
-    place[threadIdx.x] = kv4_place(a.c, a.slots[row]);
+    place[threadIdx.x] = row_of<D>(a.c, a.slots[row]);
     real[threadIdx.x] = row < n_real;
   }
   __syncthreads();
@@ -131,72 +214,87 @@ __global__ __launch_bounds__(kQThreads) void kv4_append_kernel(Kv4AppendArgs a) 
   const int n_q = n * r.n_heads, n_kv = n * a.c.n_kv_heads;
   const int q_runs = (n_q + kHeads - 1) / kHeads, kv_runs = (n_kv + kHeads - 1) / kHeads;
   const UnitPlace u = unit_place(lane % kLanes, r.rotary_dim, r.interleaved);
+  const HeadOf q_head(r.n_heads), kv_head(a.c.n_kv_heads);
+  // eight values of a run's half, a lane's in the order of the run, into their place
+  auto put = [&](int first, int half, bool is_v, const float (&x)[8]) __attribute__((always_inline)) {
+    const int w = first + lane * 8 / D + half * (kHeads / 2), head = w < n_kv ? w : n_kv - 1;
+    const int t = kv_head.row(head);
+    Row to = place[t];
+    if (w >= n_kv) to.codes = -1;
+    store_codes<D>(a.c, to, kv_head.head(head, t), lane * 8 % D, is_v, x);
+  };
   for (int run = wave; run < q_runs + 2 * kv_runs; run += kQWaves) {
     const int kind = run < q_runs ? 0 : run < q_runs + kv_runs ? 1 : 2;
     const int first = (run - (kind == 0 ? 0 : kind == 1 ? q_runs : q_runs + kv_runs)) * kHeads;
-    if (kind < 2) {
-      const int heads = kind ? a.c.n_kv_heads : r.n_heads, end = kind ? n_kv : n_q;
-      const int w = first + lane / kLanes, at = w < end ? w : end - 1;
-      const int t = at / heads, h = at - t * heads;
-      Unit<F32> p;
-      const int64_t e = (row0 + t) * (kind ? r.ld_k : r.ld_q) + h * D;
-      p.c0.load((uintptr_t)(kind ? r.k : r.q), e + u.e0);
-      p.c1.load((uintptr_t)(kind ? r.k : r.q), e + u.e1);
-      const float* weight = kind ? r.k_weight : r.q_weight;
-      const float* bias = kind ? r.k_bias : r.q_bias;
-      float xf[8], yf[8];
-      p.c0.values(xf);
-      p.c1.values(yf);
-      if (kind == 0) {
-        normed<NORM>(xf, yf, r.eps, weight, bias, u, D, kLanes);
-        if (u.turned) turn_unit(xf, yf, cs + t * pairs, u, r.interleaved);
-        if (w < end && real[t]) {
-          const int64_t d = (row0 + t) * r.ld_qo + h * D;
-          rstore8((uintptr_t)r.q_out, r.out_f32, d + u.e0, xf);
-          rstore8((uintptr_t)r.q_out, r.out_f32, d + u.e1, yf);
-        }
-        continue;
-      }
-      double x[8], y[8];
+    if (kind == 2) {
+      Chunk<F32> c[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = xf[i];
-        y[i] = yf[i];
+      for (int half = 0; half < 2; ++half) {  // (both on their way together)
+        const int w = first + lane * 8 / D + half * (kHeads / 2), head = w < n_kv ? w : n_kv - 1;
+        const int t = kv_head.row(head);
+        c[half].load((uintptr_t)a.v, element(row0, t, a.ld_v, kv_head.head(head, t) * D + lane * 8 % D));
       }
-      normed<NORM>(x, y, (double)r.eps, weight, bias, u, D, kLanes);
-      if (u.turned) turn_unit(x, y, cs + t * pairs, u, r.interleaved);
-      // into the order of the head, for the blocks (the wave's own room: no barrier)
-      float* to = exchange[wave] + lane / kLanes * D;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float x[8];
+        c[half].values(x);
+        put(first, half, true, x);
+      }
+      continue;
+    }
+    const int end = kind ? n_kv : n_q;
+    const int w = first + lane / kLanes, at = w < end ? w : end - 1;
+    const HeadOf of = kind ? kv_head : q_head;
+    const int t = of.row(at), h = of.head(at, t);
+    Unit<F32> p;
+    const int64_t e = element(row0, t, kind ? r.ld_k : r.ld_q, h * D);
+    p.c0.load((uintptr_t)(kind ? r.k : r.q), e + u.e0);
+    p.c1.load((uintptr_t)(kind ? r.k : r.q), e + u.e1);
+    const float* weight = kind ? r.k_weight : r.q_weight;
+    const float* bias = kind ? r.k_bias : r.q_bias;
+    float xf[8], yf[8];
+    p.c0.values(xf);
+    p.c1.values(yf);
+    if (kind == 0) {
+      normed<NORM>(xf, yf, r.eps, weight, bias, u, D, kLanes);
+      if (u.turned) turn_unit(xf, yf, cs + t * pairs, u, r.interleaved);
+      if (w < end && real[t]) {
+        const int64_t d = element(row0, t, r.ld_qo, h * D);
+        rstore8((uintptr_t)r.q_out, r.out_f32, d + u.e0, xf);
+        rstore8((uintptr_t)r.q_out, r.out_f32, d + u.e1, yf);
+      }
+      continue;
+    }
+    double x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = xf[i];
+      y[i] = yf[i];
+    }
+    normed<NORM>(x, y, (double)r.eps, weight, bias, u, D, kLanes);
+    // into the order of the head, for the blocks (the wave's own room: no barrier)
+    float* to = exchange[wave] + lane / kLanes * D;
+    if (u.turned) {
+      turn_to_odd(x, y, cs + t * pairs, u, r.interleaved, to);
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         to[u.e0 + i] = to_odd(x[i]);
         to[u.e1 + i] = to_odd(y[i]);
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    // 8 values a lane, of both halves of the run
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int at = lane * 8 + half * (kQValues / 2);
-      const int w = first + at / D, e = at % D, head = w < n_kv ? w : n_kv - 1;
-      const int t = head / a.c.n_kv_heads, h = head - t * a.c.n_kv_heads;
       float x[8];
-      if (kind == 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = exchange[wave][at + i];
-      } else {
-        Chunk<F32> c;
-        c.load((uintptr_t)a.v, (row0 + t) * a.ld_v + h * D + e);
-        c.values(x);
-      }
-      Kv4Place to = place[t];
-      if (w >= n_kv) to.page = -1;
-      store_codes<D>(a.c, to, h, e, kind == 2, x);
+      for (int i = 0; i < 8; ++i) x[i] = exchange[wave][lane * 8 + half * (kQValues / 2) + i];
+      put(first, half, false, x);
     }
-    if (kind == 1) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -245,6 +343,7 @@ hipError_t launch_kv4_append(Kv4AppendArgs a, hipStream_t stream) {
   const int64_t most = a.t.rows / 1024;
   a.t.tokens = 4 * kQWaves * kQValues / values;
   if (a.t.tokens > most) a.t.tokens = (int)most;
+  if ((a.t.ld_q | a.t.ld_k | a.t.ld_qo | a.ld_v) >> 32) a.t.tokens = 1;
   a.t.tokens = a.t.tokens < 1 ? 1 : a.t.tokens > kQMaxTokens ? kQMaxTokens : a.t.tokens;
   const unsigned grid = (unsigned)((a.t.rows + a.t.tokens - 1) / a.t.tokens);
   auto kernel = a.t.norm == ISPA_NORM_LAYER ? append_kernel<ISPA_NORM_LAYER>(a.t.x_f32, a.t.head_dim)
