@@ -74,15 +74,9 @@ __device__ __forceinline__ UnitPlace unit_place(int u, int rotary_dim, bool inte
   return r;
 }
 
-// The pairs of a unit turned by `at` (cos and sin of a token's pairs, with the amplitude).
+// The pairs of a unit turned by c (cos and sin of its pairs, with the amplitude).
 template <class T, class T2>
-__device__ __forceinline__ void turn_unit(T (&x)[8], T (&y)[8], const T2* at, const UnitPlace& u, bool interleaved) {
-  T2 c[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c[i] = at[u.p0 + i];
-    c[4 + i] = at[u.p1 + i];
-  }
+__device__ __forceinline__ void turn_pairs(T (&x)[8], T (&y)[8], const T2 (&c)[8], bool interleaved) {
   if (interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -102,6 +96,18 @@ __device__ __forceinline__ void turn_unit(T (&x)[8], T (&y)[8], const T2* at, co
       y[i] = xa * ss + xb * cc;
     }
   }
+}
+
+// The same by `at`, those of all pairs of a token.
+template <class T, class T2>
+__device__ __forceinline__ void turn_unit(T (&x)[8], T (&y)[8], const T2* at, const UnitPlace& u, bool interleaved) {
+  T2 c[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c[i] = at[u.p0 + i];
+    c[4 + i] = at[u.p1 + i];
+  }
+  turn_pairs(x, y, c, interleaved);
 }
 
 // A sum over the `lanes` (1, 2, 4, 8 or 16) neighbouring lanes of a head: every lane gets it.

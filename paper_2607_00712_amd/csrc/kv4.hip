@@ -151,10 +151,25 @@ __device__ __forceinline__ void normed(T (&x)[8], T (&y)[8], T eps, const float*
   }
 }
 
-// The pairs of a unit turned as turn_unit does it, rounded to odd into `to`: half of them at a
-// time, since 32 fp64 values with their angles and results take a wave of the kernel's from each SIMD.
-__device__ __forceinline__ void turn_to_odd(const double (&x)[8], const double (&y)[8], const double2* at, const UnitPlace& u,
-                                            bool interleaved, float* to) {
+// A token's angles in LDS: the k-th pairs of all units side by side (lanes' reads meet no bank
+// twice), units = pairs / 8. pair_slot: where pair j goes, the other way round.
+__device__ __forceinline__ int pair_slot(int j, int pairs, bool interleaved) {
+  const int units = pairs >> 3, half = pairs >> 1;
+  if (!interleaved) return (j & 7) * units + (j >> 3);
+  return (j < half ? 0 : half) + (j & 3) * units + ((j < half ? j : j - half) >> 2);
+}
+
+// A run's values in LDS: the first four of every eight, and the others behind them all.
+template <class T>
+__device__ __forceinline__ T* upper_four(T* p) {
+  return p + kQValues / 2;
+}
+
+// The pairs of a unit turned as turn_pairs does it, rounded to odd into `tx` and `ty`: half of them
+// at a time, since 32 fp64 values with their angles and results take a wave of the kernel's from
+// each SIMD.
+__device__ __forceinline__ void turn_to_odd(const double (&x)[8], const double (&y)[8], const double2* at, int units,
+                                            bool interleaved, float* tx, float* ty) {
 #pragma unroll
   for (int i0 = 0; i0 < 8; i0 += 4) {
     asm volatile("" ::: "memory");
@@ -162,7 +177,7 @@ __device__ __forceinline__ void turn_to_odd(const double (&x)[8], const double (
     if (interleaved) {
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        const double2 c = at[u.p0 + (i0 + i) / 2], d = at[u.p1 + (i0 + i) / 2];
+        const double2 c = at[(i0 + i) / 2 * units], d = at[(4 + (i0 + i) / 2) * units];
         xs[i] = to_odd(x[i0 + i] * c.x - x[i0 + i + 1] * c.y);
         xs[i + 1] = to_odd(x[i0 + i] * c.y + x[i0 + i + 1] * c.x);
         ys[i] = to_odd(y[i0 + i] * d.x - y[i0 + i + 1] * d.y);
@@ -171,15 +186,15 @@ __device__ __forceinline__ void turn_to_odd(const double (&x)[8], const double (
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const double2 c = at[(i0 == 0 ? u.p0 : u.p1) + i];
+        const double2 c = at[(i0 + i) * units];
         xs[i] = to_odd(x[i0 + i] * c.x - y[i0 + i] * c.y);
         ys[i] = to_odd(x[i0 + i] * c.y + y[i0 + i] * c.x);
       }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      to[u.e0 + i0 + i] = xs[i];
-      to[u.e1 + i0 + i] = ys[i];
+      (i0 ? upper_four(tx) : tx)[i] = xs[i];
+      (i0 ? upper_four(ty) : ty)[i] = ys[i];
     }
   }
 }
@@ -202,7 +217,7 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
   for (int i = threadIdx.x; i < n * pairs; i += kQThreads) {
     const int t = i / pairs, j = i - t * pairs;
     const double2 at = angle_of((double)r.positions[(row0 + t) * r.n_axes + pair_axis(r.axis_end, j)] * r.freqs[j]);
-    cs[i] = make_double2(at.x * r.amplitude, at.y * r.amplitude);
+    cs[t * pairs + pair_slot(j, pairs, r.interleaved)] = make_double2(at.x * r.amplitude, at.y * r.amplitude);
   }
   if (threadIdx.x < (unsigned)n) {
     const int64_t row = row0 + threadIdx.x;
@@ -213,6 +228,7 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n_q = n * r.n_heads, n_kv = n * a.c.n_kv_heads;
   const int q_runs = (n_q + kHeads - 1) / kHeads, kv_runs = (n_kv + kHeads - 1) / kHeads;
+  const int units = pairs >> 3;
   const UnitPlace u = unit_place(lane % kLanes, r.rotary_dim, r.interleaved);
   const HeadOf q_head(r.n_heads), kv_head(a.c.n_kv_heads);
   // eight values of a run's half, a lane's in the order of the run, into their place
@@ -257,7 +273,12 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
     p.c1.values(yf);
     if (kind == 0) {
       normed<NORM>(xf, yf, r.eps, weight, bias, u, D, kLanes);
-      if (u.turned) turn_unit(xf, yf, cs + t * pairs, u, r.interleaved);
+      if (u.turned) {
+        double2 c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = cs[t * pairs + i * units + lane % kLanes];
+        turn_pairs(xf, yf, c, r.interleaved);
+      }
       if (w < end && real[t]) {
         const int64_t d = element(row0, t, r.ld_qo, h * D);
         rstore8((uintptr_t)r.q_out, r.out_f32, d + u.e0, xf);
@@ -273,14 +294,16 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
     }
     normed<NORM>(x, y, (double)r.eps, weight, bias, u, D, kLanes);
     // into the order of the head, for the blocks (the wave's own room: no barrier)
-    float* to = exchange[wave] + lane / kLanes * D;
+    float *tx = exchange[wave] + (lane / kLanes * D + u.e0) / 2, *ty = exchange[wave] + (lane / kLanes * D + u.e1) / 2;
     if (u.turned) {
-      turn_to_odd(x, y, cs + t * pairs, u, r.interleaved, to);
+      turn_to_odd(x, y, cs + t * pairs + lane % kLanes, units, r.interleaved, tx, ty);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        to[u.e0 + i] = to_odd(x[i]);
-        to[u.e1 + i] = to_odd(y[i]);
+      for (int i = 0; i < 4; ++i) {
+        tx[i] = to_odd(x[i]);
+        upper_four(tx)[i] = to_odd(x[4 + i]);
+        ty[i] = to_odd(y[i]);
+        upper_four(ty)[i] = to_odd(y[4 + i]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -288,9 +311,9 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
     // 8 values a lane, of both halves of the run
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = exchange[wave][lane * 8 + half * (kQValues / 2) + i];
+      const float* from = exchange[wave] + lane * 4 + half * (kQValues / 4);
+      const float x[8] = {from[0], from[1], from[2], from[3], upper_four(from)[0], upper_four(from)[1], upper_four(from)[2],
+                          upper_four(from)[3]};
       put(first, half, false, x);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
