@@ -16,11 +16,11 @@
 // diverges; the angles are formed once for a workgroup's tokens.
 //
 // Measured, bf16, 128 values a head: four requests' 5800 rows (of 6240 with the padding) of 12 +
-// 12 + 12 heads 24 us (3.4 TB/s), 64 rows of 32 + 8 + 8 heads 6.7. The first is bound by the fp64
-// steps (vector issue 0.72 of the cycles that a compute unit has waves) as much as by its bytes: with the next run's loads ahead
-// it took 30 (160 registers instead of 121, three waves to a SIMD instead of four), and for more
-// waves than four the fp64 values spill (call 53 us instead of 38). Rows read back: 6240 of 12 + 12
-// heads 12 us (4.1 TB/s), bound by the bytes.
+// 12 + 12 heads 21.6 us (3.8 TB/s), with rms norms 26; 64 rows of 32 + 8 + 8 heads 6.4. The first is
+// bound by its fp64 steps (vector issue 0.69 of the cycles that a compute unit has waves) as
+// much as by its bytes, and by the registers that these take: a value's loads wait for the run
+// before, and loads ahead of it gained nothing at four waves to a SIMD and lost 6 us at three.
+// Rows read back: 6240 of 12 + 12 heads 11.7 us (4.2 TB/s), bound by the bytes.
 #include "head_units.h"
 #include "kv4_units.h"
 
