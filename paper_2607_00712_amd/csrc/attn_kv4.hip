@@ -837,7 +837,8 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 1>& w,
       const int nv = nv_now >> (8 * kb) & 255;
       if (nv < kBlk) mask<RB>(sc, nv, hh);
       f32x16 next[RB];
-      pipelined<D, RB, F>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [&](int t, int n) __attribute__((always_inline)) {
+      // (not pinned: the compiler's own order is 2 to 4% faster where codes are converted beside)
+      pipelined<D, RB, F, false>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [&](int t, int n) __attribute__((always_inline)) {
         constexpr int kPer = kWords / WC::step;  // words beside a block
 #pragma unroll
         for (int i = 0; i < kPer; ++i)

@@ -210,12 +210,12 @@ __device__ __forceinline__ void weights(const A& a, const SWave<D, RB>& w, int b
 }
 
 // One block of the pipelined loop, of three blocks in a row, as one straight run of
-// matrix instructions with the vector work between them (the order is pinned): the
+// matrix instructions with the vector work between them (PINNED: in this very order): the
 // products of block j - 1 (weights p, operands at `vblk`), then the scores of block
 // j + 1 (operands at `kblk`) into `next`, and beside them the softmax of block j (sc)
 // into p. The first V operands come in `v`, read before. `beside(t, n)` is called at each of
 // the n matrix instructions, for other work of the wave.
-template <int D, int RB, int F, class A, class B>
+template <int D, int RB, int F, bool PINNED, class A, class B>
 __device__ __forceinline__ void pipelined(const A& a, SWave<D, RB>& w, lds_char* vblk, lds_char* kblk,
                                           const f32x16 (&sc)[RB], f32x16 (&next)[RB], SWeights<F> (&p)[RB],
                                           bf16x8 (&v)[2 * SCfg<D>::dBlocks], float (&sum)[RB], float (&rounded)[RB], B&& beside) {
@@ -257,7 +257,7 @@ __device__ __forceinline__ void pipelined(const A& a, SWave<D, RB>& w, lds_char*
       put_pair<F>(pn[b], r, e0, e1, i % 2 == 0 ? rounded[b] : r1[b]);
     }
     beside(t, kSteps);
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PINNED) __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
   for (int b = 0; b < RB; ++b) {

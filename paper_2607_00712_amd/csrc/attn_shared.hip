@@ -206,7 +206,7 @@ __device__ __forceinline__ void shared_keys(const SharedArgs& a, SWave<D, RB>& w
       if (left < kBlk) mask<RB>(sc, left, hh);
       left -= KG * kBlk;
       f32x16 next[RB];
-      pipelined<D, RB, F>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [](int, int) {});
+      pipelined<D, RB, F, true>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [](int, int) {});
       check_reference<D, RB, F>(a, w, sc, p, sum, rounded);
 #pragma unroll
       for (int b = 0; b < RB; ++b) sc[b] = next[b];
