@@ -24,9 +24,9 @@
 // Measured, 128 values a head, two kernels and the launches (a large copy runs at 4.9 TB/s, a
 // reader of the same pages without any arithmetic at 5.4, a large bf16 product at 1223 TFLOP/s):
 // 64 tokens of 32 heads on 8 against up to 16384 keys each 115-119 us (5.3 TB/s of pages), three
-// requests of up to 5 tokens against up to 131072 71-75 us (4.7), one token of 12 heads against
+// requests of up to 5 tokens against up to 131072 60-75 us (4.7), one token of 12 heads against
 // 32760 23-24 us (18.5 the runs, of which some 6 are the start of a run and its first block's
-// way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 36-39 us
+// way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 35-39 us
 // (vector issue 0.51 of the busy cycles, matrix cores 0.16): 17 blocks a wave, its start and end as
 // long as half of them; join 8. Wide tiles below.
 #include "attn_rows.h"
@@ -682,9 +682,9 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
 // Steps of 64 keys lie in LDS in bf16, four of them in turn; a thread fetches its share of a
 // step's codes (an eighth of a key, and of its values) two steps ahead into registers and converts
 // it one step ahead, between the matrix instructions of the step before. 4680 rows of 12 heads
-// against 32760 keys: 997 us = 945 TFLOP/s; four waves of 64 rows, which read half as much of LDS,
-// 1056. The vector instructions bound it (140 to a wave's block beside 16 matrix instructions,
-// which are busy 0.42 of the cycles, vector issue 0.56, LDS 0.31).
+// against 32760 keys: 990 us = 951 TFLOP/s; four waves of 64 rows, which read half as much of LDS,
+// were 6% slower. The vector instructions bound it (140 to a wave's block beside 16 matrix
+// instructions, which are busy 0.43 of the cycles, vector issue 0.58, LDS 0.31).
 template <int D>
 struct WCfg {
   static constexpr int step = 2;  // blocks
