@@ -700,7 +700,7 @@ size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, in
  *               (other columns of the same wider rows do not)
  * Other arguments as for ispa_rotary; n_kv_heads * head_dim <= 2^20 too. Statistics and
  * arithmetic are fp32 (angles fp64), each output is rounded once. Pointers 16-byte aligned,
- * row distances multiples of 8. Asynchronous on `stream`.
+ * row distances multiples of 8 and at most 2^24. Asynchronous on `stream`.
  */
 int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
                      const float* q_weight, const float* k_weight, const float* q_bias, const float* k_bias, float eps,
@@ -722,7 +722,7 @@ int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, i
  *   workspace   device, 256-byte aligned, at least ispa_norm_rotary_backward_workspace_bytes
  *               bytes for the same sizes on the same device; may be NULL where no gradient of
  *               a vector is wanted. Used only during the call's device work.
- * Sums over rows and heads are fp32, in an order that depends on the sizes and the device alone:
+ * Row distances as for ispa_norm_rotary. Sums over rows and heads are fp32, in an order that depends on the sizes and the device alone:
  * the same call gives the same bits. Asynchronous on `stream`.
  */
 int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_k_out, int64_t ld_gk, int32_t g_dtype,
@@ -779,6 +779,7 @@ size_t ispa_kv4_page_bytes(int64_t page_size, int32_t head_dim);
  *               turned all the same. No slot may come twice.
  *   n_real      device int32, the count of real rows, those of padding are behind them: their
  *               q_out is left as it is (q_start + n_req of ispa_slot_map); or NULL: all are
+ * Pointers 16-byte aligned (slots 8, integers 4), row distances multiples of 8 and at most 2^24.
  * Which number a key is rounded to is decided in fp64, q is computed in fp32. Pages that no
  * row has a slot in are not touched. Asynchronous on `stream`.
  */
@@ -825,8 +826,8 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
  * An fp32 out has the softmax weights as fp32 numbers. A bf16 one has them in 16 bits (2^-16 of
  * sum w |v|), except where max_q (or n_rows, if that is less) times n_heads / n_kv_heads is more
  * than 16: there the weights enter the product with the values rounded to bf16 (2^-8 of
- * sum w |v| at most). Row distances are multiples of 8 elements, pointers 16-byte aligned (lse
- * and integers 4). Keys and values behind a request's end are never used, whatever their pages
+ * sum w |v| at most). Row distances are multiples of 8 elements and at most 2^24, pointers
+ * 16-byte aligned (lse and integers 4). Keys and values behind a request's end are never used, whatever their pages
  * hold. Outputs must not overlap the inputs or each other. The same call gives the same bits.
  * Asynchronous on `stream`.
  */

@@ -92,10 +92,9 @@ struct HeadOf {
   __device__ __forceinline__ int row(int w) const { return (int)(((float)w + 0.5f) * inverse); }
   __device__ __forceinline__ int head(int w, int t) const { return w - __mul24(t, heads); }
 };
-// Element e of a head of row t. Only the lower half of the row distance is multiplied: where it
-// has an upper one a workgroup has one row.
+// Element e of a workgroup's row t (row distances are 2^24 at most: the second part has 32 bits).
 __device__ __forceinline__ int64_t element(int64_t row0, int t, int64_t ld, int e) {
-  return row0 * ld + (int64_t)((uint64_t)(uint32_t)t * (uint32_t)ld + (uint32_t)e);
+  return row0 * ld + ((uint32_t)t * (uint32_t)ld + (uint32_t)e);
 }
 
 // Eight neighbouring values of a head (a quarter of a block; its other quarters are in the
@@ -366,7 +365,6 @@ hipError_t launch_kv4_append(Kv4AppendArgs a, hipStream_t stream) {
   const int64_t most = a.t.rows / 1024;
   a.t.tokens = 4 * kQWaves * kQValues / values;
   if (a.t.tokens > most) a.t.tokens = (int)most;
-  if ((a.t.ld_q | a.t.ld_k | a.t.ld_qo | a.ld_v) >> 32) a.t.tokens = 1;
   a.t.tokens = a.t.tokens < 1 ? 1 : a.t.tokens > kQMaxTokens ? kQMaxTokens : a.t.tokens;
   const unsigned grid = (unsigned)((a.t.rows + a.t.tokens - 1) / a.t.tokens);
   auto kernel = a.t.norm == ISPA_NORM_LAYER ? append_kernel<ISPA_NORM_LAYER>(a.t.x_f32, a.t.head_dim)

@@ -505,6 +505,42 @@ def test_many_requests():
             check(*attend(on_gpu(one), 2, out_dtype=F32), exact(one, 2), b)
 
 
+def test_rows_far_apart():
+    """Rows of one wide tensor as far apart as they may be, over more than 2^32 elements: the same as
+    rows side by side."""
+    rows, heads, kv, d, ld = 260, 2, 1, 128, 1 << 24
+    width = (heads + 2 * kv) * d
+    wide = torch.empty((rows - 1) * ld + width, dtype=BF16, device=DEV)
+    x = wide.as_strided((rows, width), (ld, 1))
+    x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(3)).to(BF16))
+    close = x.contiguous()
+    f = ispa.rotary_frequencies(d // 2, device=DEV)[0]
+    at, slots = torch.arange(rows, dtype=torch.int32, device=DEV), torch.arange(rows, device=DEV)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device=DEV)
+    start, lens = (torch.tensor(v, dtype=torch.int32, device=DEV) for v in ([0, rows], [rows]))
+    w = torch.linspace(0.5, 1.5, d, device=DEV)
+    results = []
+    for t in (x, close):
+        q, k, v = t[:, :heads * d], t[:, heads * d:(heads + kv) * d], t[:, (heads + kv) * d:]
+        cache = ispa.kv4_cache(2, 256, kv, d, device=DEV)
+        turned = ispa.norm_rotary(q, k, at, f, heads, kv, q_weight=w)
+        grads = ispa.norm_rotary_backward(q, k, q, k, at, f, heads, kv, q_weight=w)
+        out = ispa.kv4_append(q, k, v, at, slots, f, heads, cache, table, kv, norm="rms", k_weight=w)
+        seen = [y for n in (1, 20, rows) for y in ispa.attn_kv4(q, cache, table, start, lens, heads, max_q=n)]
+        results.append([*turned, *grads.values(), out, cache, *seen])
+    for i, (p, r) in enumerate(zip(*results)):
+        assert torch.equal(p, r), i
+    # outputs as far apart: in place, and attention's beside its queries
+    q, k, v = x[:, :heads * d], x[:, heads * d:(heads + kv) * d], x[:, (heads + kv) * d:]
+    ispa.norm_rotary(q, k, at, f, heads, kv, q_weight=w, q_out=q, k_out=k)
+    assert torch.equal(q, results[1][0]) and torch.equal(k, results[1][1])
+    ispa.attn_kv4(close[:, :d], cache, table, start, lens, 1, out=v)
+    assert torch.equal(v, ispa.attn_kv4(close[:, :d], cache, table, start, lens, 1)[0])
+    args = close[:, :heads * d], close[:, :d], close[:, :d], at, slots, f, heads, cache, table, kv
+    ispa.kv4_append(*args, q_out=q)
+    assert torch.equal(q, ispa.kv4_append(*args))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("rows", [1, 20])
 def test_items_of_many_runs(rows, d):
