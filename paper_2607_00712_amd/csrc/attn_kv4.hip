@@ -14,7 +14,8 @@
 // as they like (every workgroup sums them up for itself, which takes less than a launch). An item
 // that lies in one run is written out whole; of the others each run leaves its part (weighted
 // values, sums and reference of each row) in the workspace, two at most, and a second launch joins
-// them by Eq. 11-12, in order: the result does not depend on the order of execution.
+// them by Eq. 11-12, in order: the result does not depend on the order of execution. Where the
+// caches are short and the items few, every item is a run and there is one launch.
 //
 // Narrow tiles (16 or 32 rows): a block's codes come from HBM into a lane's registers as the
 // matrix instructions take them, 2 KB of keys and of values that lie together in a page; a key's
@@ -78,8 +79,12 @@ __device__ __forceinline__ Request request_of(const Kv4AttnArgs& a, int total, i
   r.blocks = len == 0 ? 1 : (int)((len + kBlk - 1) / kBlk);
   return r;
 }
+// The units of an item: its blocks and those ahead, or as many for every item.
+__device__ __forceinline__ int item_units(const Kv4AttnArgs& a, int blocks) {
+  return a.item_units ? a.item_units : a.ahead + blocks;
+}
 __device__ __forceinline__ int64_t units_of(const Kv4AttnArgs& a, const Request& r) {
-  return (int64_t)a.c.n_kv_heads * r.tiles * (a.ahead + r.blocks);
+  return (int64_t)a.c.n_kv_heads * r.tiles * item_units(a, r.blocks);
 }
 
 // a / b for the same a and b in all lanes, mostly small: a 64-bit division takes 0.4 us of a
@@ -126,7 +131,7 @@ struct Walk {
     const int64_t base = uniform(s.unit);
     r = Request{uniform(s.r.first), uniform(s.r.rows), uniform(s.r.tiles), uniform(s.r.blocks), uniform(s.r.len)};
     int64_t i = u - base;
-    const int64_t each = a.ahead + r.blocks, per = r.tiles * each;
+    const int64_t each = item_units(a, r.blocks), per = r.tiles * each;
     head = (int)divide(i, per);
     i -= head * per;
     tile = (int)divide(i, each);
@@ -138,7 +143,7 @@ struct Walk {
   // to the next block, of the next item behind the last one
   __device__ __forceinline__ void next(const Kv4AttnArgs& a, int total) {
     if (++block < r.blocks) return;
-    item += r.blocks + a.ahead;  // (as many units ahead of every item)
+    item += item_units(a, r.blocks);  // (as many of them ahead in every item)
     ++number;
     block = 0;
     if (++tile < r.tiles) return;
@@ -200,6 +205,10 @@ __device__ __forceinline__ Line find_line(const Kv4AttnArgs& a, int total, Start
     units += wave_units[w];
   }
   units = uniform(units);
+  if (a.item_units) {  // (request starts that do not ascend may name more items than there are runs)
+    const int64_t most = (int64_t)a.most_runs * a.item_units;
+    units = units < most ? units : most;
+  }
   Line l{Cut(units, a.most_runs, a.least_units), (int64_t)blockIdx.x * N};
   if (XCDS) {
     const int64_t per = (l.cut.runs + kAXcds - 1) / kAXcds;
@@ -1015,7 +1024,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
 template <int D, int W>
 hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.most_runs < 2) return e;
+  if (e != hipSuccess || a.most_runs < 2 || a.item_units) return e;
   attn_kv4_join_kernel<D, W><<<dim3(a.most_items, a.tile_rows / a.join_rows), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
@@ -1071,11 +1080,21 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   const int64_t runs = (tiles * a->c.n_kv_heads * (blocks + a->ahead) + a->least_units - 1) / a->least_units;
   if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
   a->most_items = (int)(tiles * a->c.n_kv_heads);
+  // Short caches and few items: a run to an item, all of the same units, and no second launch (64
+  // tokens of 32 heads on 8 against up to 256 keys 14.4 us, and 16.5 with a join; against up to 384
+  // 18.1 and 17.2; one request's 1000 rows of 8 heads, in wide tiles, against 768 keys 35.1 and 37.4,
+  // against 1024 43.2 and 38.9).
+  a->item_units = 0;
+  if (blocks <= (wide ? 24 : 8) && a->most_items <= n_cu * (wide ? 1 : narrow_groups(head_dim, a->tile_rows) * kShWaves)) {
+    a->item_units = (int)blocks + a->ahead;
+    a->least_units = a->item_units;
+    a->most_runs = a->most_items;
+  }
   // a pass of the join's threads over the rows of its workgroup; few items: fewer rows each
   a->join_rows = kJoinThreads / (head_dim / 4);
   if (a->join_rows > a->tile_rows) a->join_rows = a->tile_rows;
   while (a->join_rows > 1 && (int64_t)a->most_items * a->tile_rows / a->join_rows < 1024) a->join_rows /= 2;
-  const size_t parts = (size_t)a->most_runs * 2 * a->tile_rows;
+  const size_t parts = a->item_units ? 0 : (size_t)a->most_runs * 2 * a->tile_rows;
   a->stat_offset = parts * head_dim * sizeof(float);
   a->item_offset = a->stat_offset + parts * 4 * sizeof(float);
   return a->item_offset + (size_t)a->most_items * sizeof(Kv4Item) + 2 * sizeof(int64_t);

@@ -308,8 +308,9 @@ struct Kv4AttnArgs {
   int out_bf16;
   float* lse;
   // set by the plan: rows of a tile, runs and items at most, units of a run at least, units that
-  // stand for an item's start and end, rows to a workgroup of the join, the parts
-  int tile_rows, most_runs, most_items, least_units, ahead, join_rows;
+  // stand for an item's start and end, units of every item (0: as it has blocks), rows to a
+  // workgroup of the join, the parts
+  int tile_rows, most_runs, most_items, least_units, ahead, item_units, join_rows;
   size_t stat_offset, item_offset;
   float *part_o, *part_stat;
   Kv4Item* items;

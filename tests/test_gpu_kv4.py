@@ -467,18 +467,19 @@ def test_layouts_streams_and_lengths_beyond():
     check(*attend(on_gpu(t), 4), exact(t, 4), "lengths")
 
 
-def test_starts_that_do_not_ascend():
+@pytest.mark.parametrize("pages", [3, 40])
+def test_starts_that_do_not_ascend(pages):
     """Request starts that go back name more rows than there are: nothing behind the workspace or
     the outputs is written."""
     n, rows, heads, d = 40, 50, 2, 64
-    t = on_gpu(make([rows] + [0] * (n - 1), [70] * n, 32, 3, heads, 1, d))
+    t = on_gpu(make([rows] + [0] * (n - 1), [70] * n, 32, pages, heads, 1, d))
     t["q_start"][1:n:2], t["q_start"][2:n:2] = rows, 0
     t["q_start"][n] = rows
     L = ispa.lib()
-    need = L.ispa_attn_kv4_workspace_bytes(32, 3, n, rows, 1, heads, 1, d)
+    need = L.ispa_attn_kv4_workspace_bytes(32, pages, n, rows, 1, heads, 1, d)
     ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV)
     out = torch.full((rows + 8, heads * d), 3.0, dtype=BF16, device=DEV)
-    st = L.ispa_attn_kv4(t["q"].data_ptr(), heads * d, t["cache"].data_ptr(), len(t["cache"]), 32, t["table"].data_ptr(), 3,
+    st = L.ispa_attn_kv4(t["q"].data_ptr(), heads * d, t["cache"].data_ptr(), len(t["cache"]), 32, t["table"].data_ptr(), pages,
                          t["q_start"].data_ptr(), t["lens"].data_ptr(), n, rows, 1, heads, 1, d, 0.0, out.data_ptr(),
                          ispa.DTYPE_BF16, heads * d, None, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
     assert st == ispa.ISPA_OK
@@ -539,6 +540,19 @@ def test_rows_far_apart():
     args = close[:, :heads * d], close[:, :d], close[:, :d], at, slots, f, heads, cache, table, kv
     ispa.kv4_append(*args, q_out=q)
     assert torch.equal(q, ispa.kv4_append(*args))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,pages", [(1, 1), (1, 8), (1, 9), (30, 7), (30, 8), (30, 9), (300, 2), (300, 23), (300, 25)])
+def test_short_caches(rows, pages, d):
+    """Capacities on both sides of where a run takes an item whole, lengths from none to all, one
+    request and several, and more items than the device has runs."""
+    lens = [32 * pages, 0, 1, 16 * pages + 5, 32 * pages - 1, 31]
+    several = [([rows], 2), ([rows, 2, rows, 1, 0, rows], 2), ([rows] * 6, 4 if rows < 300 else 1)]
+    for counts, kv in several + [([3] * 700, 4)] * (pages == 1):
+        t = make(counts, [lens[i % 6] for i in range(len(counts))], 32, pages, 4, kv, d)
+        got = attend(on_gpu(t), 4, max_q=max(counts), out_dtype=F32)
+        check(*got, exact(t, 4), f"{len(counts)} requests")
 
 
 @pytest.mark.parametrize("d", [64, 128])
