@@ -15,7 +15,7 @@
 // that lies in one run is written out whole; of the others each run leaves its part (weighted
 // values, sums and reference of each row) in the workspace, two at most, and a second launch joins
 // them by Eq. 11-12, in order: the result does not depend on the order of execution. Where the
-// caches are short and the items few, every item is a run and there is one launch.
+// caches are short and the items few, an item is a workgroup's and there is one launch.
 //
 // Narrow tiles (16 or 32 rows): a block's codes come from HBM into a lane's registers as the
 // matrix instructions take them, 2 KB of keys and of values that lie together in a page; a key's
@@ -585,11 +585,11 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
       for (int f = 0; f < F; ++f) s.acc[b][d] = mfma16(v[d].v, p[b][f], s.acc[b][d]);
 }
 
-// The parts of a workgroup's four runs as one, where all of them lie inside one item: a quarter of
-// the output blocks to a wave.
+// The parts of a workgroup's waves as one, where all of them lie inside one item (slot: in the
+// workspace) or are all of it (slot < 0): a quarter of the output blocks to a wave.
 template <int D, int RB>
-__device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D, RB>& s, int rows, int64_t slot, lds_byte* smem,
-                                             ISPA_LDS f32x4 (&stats)[kShWaves][16], int wave, int lane) {
+__device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D, RB>& s, const Walk<16 * RB>& item, int64_t slot,
+                                             lds_byte* smem, ISPA_LDS f32x4 (&stats)[kShWaves][16], int wave, int lane) {
   using C = NCfg<D>;
   constexpr int kOwn = C::dBlocks / kShWaves;
   const int g = lane >> 4, m16 = lane & 15;
@@ -621,8 +621,17 @@ __device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D
 #pragma unroll
       for (int d = 0; d < kOwn; ++d) o[d] += *block(w, wave * kOwn + d) * e;
     }
-    const int in_tile = b * 16 + m16;
-    if (in_tile >= rows) continue;
+    const int in_tile = b * 16 + m16, row = item.tile * 16 * RB + in_tile;
+    if (row >= item.r.rows) continue;
+    if (slot < 0) {
+      const int64_t token = item.r.first + row / a.group;
+      const int head = item.head * a.group + row % a.group;
+      if (a.lse && wave == 0 && g == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(m, all[1], a.scale);
+      const float inv = all[2] == 0.f ? 0.f : 1.0f / all[2];
+#pragma unroll
+      for (int d = 0; d < kOwn; ++d) put4(a, token, head * D + 16 * (wave * kOwn + d) + 4 * g, o[d] * inv);
+      continue;
+    }
     const int64_t at = slot * 16 * RB + in_tile;
     if (wave == 0 && g == 0) *(f32x4*)(a.part_stat + 4 * at) = all;
 #pragma unroll
@@ -630,27 +639,36 @@ __device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D
   }
 }
 
-template <int D, int RB, int F>
+// WHOLE: a run is an item, and a workgroup's, a quarter of its blocks to a wave.
+template <int D, int RB, int F, bool WHOLE>
 __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv4_kernel(Kv4AttnArgs a) {
   using C = NCfg<D>;
   constexpr int TR = 16 * RB;
   __shared__ __attribute__((aligned(1024))) char smem[kShWaves * C::stageBytes];
-  __shared__ Start starts[kShWaves];
+  __shared__ Start starts[WHOLE ? 1 : kShWaves];
   __shared__ f32x4 stats[kShWaves][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int total = clamp_int(fixed(a.q_start, a.c.n_req), 0, a.n_rows);
-  const Line line = find_line<TR, kShWaves, kShWaves, false>(a, total, starts);
-  const int64_t run = line.first + wave;
+  const Line line = find_line<TR, kShWaves, WHOLE ? 1 : kShWaves, false>(a, total, starts);
+  const int64_t run = line.first + (WHOLE ? 0 : wave);
   if (run >= line.cut.runs) return;
-  const int64_t u0 = line.cut.begin(run), u1 = line.cut.begin(run + 1);
+  const int64_t u0 = line.cut.begin(run);
   Walk<TR> w;
-  w.start(a, starts[wave], u0);
-  int64_t u = u0 > w.item ? u0 : w.item;  // the unit of a block
-  if (u >= u1) return;
-  if (lane == 0 && w.block == 0) tell_item(a, run, w);
-  // (the same for all waves: the item begins before the first one's run and ends behind the last one's)
-  const bool grouped = w.item < line.cut.begin(line.first) && w.item + w.r.blocks > line.cut.begin(line.first + kShWaves);
-  const int rows = w.r.rows - w.tile * TR;
+  w.start(a, starts[WHOLE ? 0 : wave], u0);
+  int64_t u = u0 > w.item ? u0 : w.item, u1;  // the unit of a block, and of the end
+  bool grouped = true;
+  if constexpr (WHOLE) {
+    const int each = (w.r.blocks + kShWaves - 1) / kShWaves;
+    w.block = wave * each < w.r.blocks ? wave * each : w.r.blocks;
+    u = w.item + w.block;
+    u1 = w.item + (w.block + each < w.r.blocks ? w.block + each : w.r.blocks);
+  } else {
+    u1 = line.cut.begin(run + 1);
+    if (u >= u1) return;
+    if (lane == 0 && w.block == 0) tell_item(a, run, w);
+    // (the same for all waves: the item begins before the first one's run and ends behind the last one's)
+    grouped = w.item < line.cut.begin(line.first) && w.item + w.r.blocks > line.cut.begin(line.first + kShWaves);
+  }
   lds_byte* stage = (lds_byte*)smem + wave * C::stageBytes;
   Feeder<D, TR> f;
   f.start(w, u, u1, lane);
@@ -682,7 +700,7 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
       }
     }
   }
-  if (grouped) finish_group<D, RB>(a, s, rows, 2 * line.first, (lds_byte*)smem, (ISPA_LDS f32x4(&)[kShWaves][16])stats, wave, lane);
+  if (grouped) finish_group<D, RB>(a, s, w, WHOLE ? -1 : 2 * line.first, (lds_byte*)smem, (ISPA_LDS f32x4(&)[kShWaves][16])stats, wave, lane);
 }
 
 // ---- wide tiles: a run to a workgroup ----
@@ -1030,11 +1048,11 @@ hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
 }
 template <int D, int RB>
 hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)((a.most_runs + kShWaves - 1) / kShWaves);
-  if (a.out_bf16)
-    attn_kv4_kernel<D, RB, RB == 1 ? 2 : 1><<<grid, kShThreads, 0, stream>>>(a);
-  else
-    attn_kv4_kernel<D, RB, 3><<<grid, kShThreads, 0, stream>>>(a);
+  constexpr int F = RB == 1 ? 2 : 1;  // (of a bf16 output)
+  const unsigned grid = (unsigned)(a.item_units ? a.most_runs : (a.most_runs + kShWaves - 1) / kShWaves);
+  auto kernel = a.item_units ? (a.out_bf16 ? attn_kv4_kernel<D, RB, F, true> : attn_kv4_kernel<D, RB, 3, true>)
+                             : (a.out_bf16 ? attn_kv4_kernel<D, RB, F, false> : attn_kv4_kernel<D, RB, 3, false>);
+  kernel<<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D, kShWaves>(a, stream);
 }
 template <int D>
@@ -1080,12 +1098,15 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   const int64_t runs = (tiles * a->c.n_kv_heads * (blocks + a->ahead) + a->least_units - 1) / a->least_units;
   if (runs < a->most_runs) a->most_runs = (int)(runs < 1 ? 1 : runs);
   a->most_items = (int)(tiles * a->c.n_kv_heads);
-  // Short caches and few items: a run to an item, all of the same units, and no second launch (64
-  // tokens of 32 heads on 8 against up to 256 keys 14.4 us, and 16.5 with a join; against up to 384
-  // 18.1 and 17.2; one request's 1000 rows of 8 heads, in wide tiles, against 768 keys 35.1 and 37.4,
-  // against 1024 43.2 and 38.9).
+  // Short caches and few items: an item to a workgroup, and no second launch. Narrow tiles (against
+  // the same in equal runs with a join): 64 tokens of 32 heads on 8 against up to 512 keys 12.6 us and
+  // 19, 1024 16.9 and 21, 1536 20.5 and 23; one row of 12 heads against up to 1536 16.0 and 16.6, 2048
+  // 19 and 16.5; 60 tokens of 16 heads against up to 1024 26.6 and 27.7, 1536 35.5 and 34.5; 120
+  // against up to 512 33.8 and 32. Wide ones: 1000 rows of 8 heads against up to 768 keys 35.1 and 37.4,
+  // 1024 43.2 and 38.9.
+  const int64_t items = a->most_items;
   a->item_units = 0;
-  if (blocks <= (wide ? 24 : 8) && a->most_items <= n_cu * (wide ? 1 : narrow_groups(head_dim, a->tile_rows) * kShWaves)) {
+  if (wide ? blocks <= 24 && items <= n_cu : blocks <= 48 && items <= 6 * n_cu && items * blocks <= 128 * n_cu) {
     a->item_units = (int)blocks + a->ahead;
     a->least_units = a->item_units;
     a->most_runs = a->most_items;

@@ -543,9 +543,9 @@ def test_rows_far_apart():
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("rows,pages", [(1, 1), (1, 8), (1, 9), (30, 7), (30, 8), (30, 9), (300, 2), (300, 23), (300, 25)])
+@pytest.mark.parametrize("rows,pages", [(1, 1), (1, 8), (1, 48), (1, 49), (30, 7), (30, 47), (30, 49), (300, 2), (300, 24), (300, 25)])
 def test_short_caches(rows, pages, d):
-    """Capacities on both sides of where a run takes an item whole, lengths from none to all, one
+    """Capacities on both sides of where a workgroup takes an item whole, lengths from none to all, one
     request and several, and more items than the device has runs."""
     lens = [32 * pages, 0, 1, 16 * pages + 5, 32 * pages - 1, 31]
     several = [([rows], 2), ([rows, 2, rows, 1, 0, rows], 2), ([rows] * 6, 4 if rows < 300 else 1)]
