@@ -318,8 +318,15 @@ def check(got, got_lse, want, what="", rows=1):
         f"{what}: lse {(got_lse - lse)[full].abs().max():.3e}")
 
 
-def attend(t, heads, **kw):
-    return ispa.attn_kv4(t["q"], t["cache"], t["table"], t["q_start"], t["lens"], heads, **kw)
+@pytest.fixture(params=[0, 100])
+def more(request):
+    """Pages that there are not, behind the others: few pages and many take different ways."""
+    return request.param
+
+
+def attend(t, heads, more=0, **kw):
+    table = torch.nn.functional.pad(t["table"], (0, more), value=-1)
+    return ispa.attn_kv4(t["q"], t["cache"], table, t["q_start"], t["lens"], heads, **kw)
 
 
 ATTN = [
@@ -347,13 +354,13 @@ ATTN = [
 
 @pytest.mark.parametrize("out_dtype", [BF16, F32])
 @pytest.mark.parametrize("case", range(len(ATTN)))
-def test_attention(case, out_dtype):
+def test_attention(case, out_dtype, more):
     counts, lens, page, pages, heads, kv_heads, d = ATTN[case]
     print(f"attn_kv4 {ATTN[case]} {out_dtype}", flush=True)
     t = make(counts, lens, page, pages, heads, kv_heads, d)
     g = on_gpu(t)
-    out, lse = attend(g, heads, max_q=max(counts + [1]), out_dtype=out_dtype)
-    again, lse2 = attend(g, heads, max_q=max(counts + [1]), out_dtype=out_dtype)
+    out, lse = attend(g, heads, more, max_q=max(counts + [1]), out_dtype=out_dtype)
+    again, lse2 = attend(g, heads, more, max_q=max(counts + [1]), out_dtype=out_dtype)
     torch.cuda.synchronize()
     check(out, lse, exact(t, heads), ATTN[case], max(counts) * heads // kv_heads)
     assert torch.equal(out, again) and torch.equal(lse, lse2)  # the same bits
@@ -361,13 +368,13 @@ def test_attention(case, out_dtype):
 
 @pytest.mark.parametrize("max_q", [1, 9, 20, 70, 5000])
 @pytest.mark.parametrize("d", [64, 128])
-def test_any_hint(max_q, d):
+def test_any_hint(max_q, d, more):
     """What the host knows of the rows changes the layout of the work alone."""
     t = make([1, 70, 0, 300, 9], [100, 33, 64, 257, 0], 64, 5, 2, 1, d, pad=4)
     g = on_gpu(t)
     out = torch.full_like(g["q"], 7.0)
     lse = torch.full((2, len(t["q"])), 7.0, device=DEV)
-    attend(g, 2, max_q=max_q, out=out, lse=lse)
+    attend(g, 2, more, max_q=max_q, out=out, lse=lse)
     torch.cuda.synchronize()
     assert (out[-4:] == 7).all() and (lse[:, -4:] == 7).all()  # padding is left as it was
     want = exact({**t, "q": t["q"][:-4]}, 2)
@@ -375,11 +382,11 @@ def test_any_hint(max_q, d):
 
 
 @pytest.mark.parametrize("rows", [1, 20, 60, 300])
-def test_keys_that_are_not_attended(rows):
+def test_keys_that_are_not_attended(rows, more):
     """What lies behind a request's end, in pages of no request, and pages that there are not:
     infinities and NaN there (power 255) change nothing."""
     t = make([rows, 2], [100, 37], 32, 5, 4, 2, 128)
-    clean = attend(on_gpu(t), 4, max_q=rows)
+    clean = attend(on_gpu(t), 4, more, max_q=rows)
     used = torch.zeros(len(t["cache"]), 32, dtype=torch.bool)
     for b, n in enumerate((100, 37)):
         for i in range(n):
@@ -388,27 +395,27 @@ def test_keys_that_are_not_attended(rows):
     spoil = lambda c, e: (torch.where(used[:, None, :, None], c, 15), torch.where(used[:, None, :, None], e, 255))
     spoilt = {**t, "cache": pack(spoil(kc, ke), spoil(vc, ve)), "table": t["table"].clone()}
     spoilt["table"][0, 4], spoilt["table"][1, 2:] = -7, 1 << 30
-    got = attend(on_gpu(spoilt), 4, max_q=rows)
+    got = attend(on_gpu(spoilt), 4, more, max_q=rows)
     assert all(torch.equal(a, b) for a, b in zip(got, clean))
     # pages out of the pool among the attended ones: as if their keys were not there
     holes = {**t, "table": t["table"].clone()}
     holes["table"][0, 1], holes["table"][1, 0] = -1, len(t["cache"])
-    check(*attend(on_gpu(holes), 4, max_q=rows), exact(holes, 4), "holes", 2 * rows)
+    check(*attend(on_gpu(holes), 4, more, max_q=rows), exact(holes, 4), "holes", 2 * rows)
     holes["table"][:] = -1
-    out, lse = attend(on_gpu(holes), 4, max_q=rows)
+    out, lse = attend(on_gpu(holes), 4, more, max_q=rows)
     assert (out == 0).all() and (lse == -math.inf).all()
     # a NaN that is attended shows in its rows alone
     bad = {**t, "cache": t["cache"].clone()}
     (_, e), _ = unpack(bad["cache"], 128)
     e[t["table"][1, 0], 1, 5, 2] = 255
-    out, lse = attend(on_gpu(bad), 4, max_q=rows)
+    out, lse = attend(on_gpu(bad), 4, more, max_q=rows)
     assert torch.equal(out[:rows], clean[0][:rows]) and torch.isnan(lse[2:, rows:]).all()
     assert torch.equal(out[rows:, :256], clean[0][rows:, :256]) and torch.isnan(out[rows:, 256:]).all()
 
 
 @pytest.mark.parametrize("q_scale", [8.0, 60.0])
 @pytest.mark.parametrize("rows", [1, 30, 64, 290])
-def test_large_scores(rows, q_scale):
+def test_large_scores(rows, q_scale, more):
     """Scores that grow along the keys, so that the softmax reference moves."""
     t = make([rows, 3], [700, 450], 64, 11, 2, 2, 128, q_scale=q_scale)
     (kc, ke), v = unpack(t["cache"], 128)
@@ -416,11 +423,11 @@ def test_large_scores(rows, q_scale):
         for i in range(11):  # later pages larger
             ke[t["table"][b, i]] += i // 3
     t["cache"] = pack((kc, ke), v)
-    check(*attend(on_gpu(t), 2, max_q=rows, out_dtype=F32), exact(t, 2), q_scale)
-    check(*attend(on_gpu(t), 2, max_q=rows, scale=0.01), exact(t, 2, 0.01), "scale", rows)
+    check(*attend(on_gpu(t), 2, more, max_q=rows, out_dtype=F32), exact(t, 2), q_scale)
+    check(*attend(on_gpu(t), 2, more, max_q=rows, scale=0.01), exact(t, 2, 0.01), "scale", rows)
 
 
-def test_every_value_shows():
+def test_every_value_shows(more):
     """One key of large weight in every place of a unit, and values of its own in every place:
     each output is that key's. The scores are whole numbers below 2^13, exact in fp32, and the
     largest is ahead by more than 1000, so that the other weights are zero: O = (hi + lo) v / w
@@ -439,7 +446,7 @@ def test_every_value_shows():
         q = k.view(n, d)[:: n // rows].to(BF16)
         t = on_gpu(dict(q=q, cache=cache, table=torch.tensor([[0, 1, 2]], dtype=torch.int32),
                         q_start=torch.tensor([0, rows], dtype=torch.int32), lens=torch.tensor([n], dtype=torch.int32)))
-        out, _ = attend(t, 1, scale=1.0, out_dtype=F32)
+        out, _ = attend(t, 1, more, scale=1.0, out_dtype=F32)
         want = held.view(n, d)[:: n // rows]
         assert torch.all((out.double().cpu() - want).abs() <= want.abs() * 2.0 ** -15)
 
