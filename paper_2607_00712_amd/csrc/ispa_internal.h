@@ -314,7 +314,7 @@ struct Kv4AttnArgs {
   size_t stat_offset, item_offset;
   float *part_o, *part_stat;
   Kv4Item* items;
-  int64_t* line;  // units in all, runs, items
+  int64_t* line;  // units in all, items
 };
 // fills the plan and returns the workspace bytes
 size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim);
