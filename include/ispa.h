@@ -823,10 +823,8 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
  *   lse         fp32 [n_heads, n_rows] (natural log; -inf without any key) or NULL
  *   workspace   device, 256-byte aligned, at least ispa_attn_kv4_workspace_bytes bytes for the
  *               same sizes on the same device. Used only during the call's device work.
- * An fp32 out has the softmax weights as fp32 numbers. A bf16 one has them in 16 bits (2^-16 of
- * sum w |v|), except where max_q (or n_rows, if that is less) times n_heads / n_kv_heads is more
- * than 16: there the weights enter the product with the values rounded to bf16 (2^-8 of
- * sum w |v| at most). Row distances are multiples of 8 elements and at most 2^24, pointers
+ * An fp32 out has the softmax weights as fp32 numbers, a bf16 one in 16 bits (2^-16 of
+ * sum w |v|). Row distances are multiples of 8 elements and at most 2^24, pointers
  * 16-byte aligned (lse and integers 4). Keys and values behind a request's end are never used, whatever their pages
  * hold. Outputs must not overlap the inputs or each other. The same call gives the same bits.
  * Asynchronous on `stream`.

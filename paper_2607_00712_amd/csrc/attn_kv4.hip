@@ -364,7 +364,7 @@ struct NWave {
   using C = NCfg<D>;
   f32x4 acc[RB][C::dBlocks];  // O^T: values 16 d + 4 (lane / 16) .. + 3
   bf16x8 q[RB][C::steps];     // Q^T operand: step s holds values D / 4 (lane / 16) + 8 s .. + 7
-  float m[RB], l[RB], lr[RB];  // reference (raw scores), sums of the weights of the lane's keys and of the rounded ones
+  float m[RB], l[RB];  // reference (raw scores), sum of the weights of the lane's keys
 };
 
 template <int D, int RB>
@@ -382,7 +382,7 @@ __device__ __forceinline__ void start_item(const Kv4AttnArgs& a, NWave<D, RB>& s
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) s.acc[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     s.m[b] = -INFINITY;
-    s.l[b] = s.lr[b] = 0.f;
+    s.l[b] = 0.f;
   }
 }
 
@@ -406,11 +406,11 @@ __device__ __forceinline__ void finish_item(const Kv4AttnArgs& a, NWave<D, RB>& 
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const int in_tile = b * 16 + (lane & 15), row = w.tile * 16 * RB + in_tile;
-    const float l = quad_sum(s.l[b]), lr = quad_sum(s.lr[b]);
+    const float l = quad_sum(s.l[b]);
     if (row >= w.r.rows) continue;
     if (slot >= 0) {
       const int64_t at = slot * 16 * RB + in_tile;
-      if (g == 0) *(f32x4*)(a.part_stat + 4 * at) = f32x4{s.m[b], l, lr, 0.f};
+      if (g == 0) *(f32x4*)(a.part_stat + 4 * at) = f32x4{s.m[b], l, 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < C::dBlocks; ++d) *(f32x4*)(a.part_o + at * D + 16 * d + 4 * g) = s.acc[b][d];
       continue;
@@ -418,7 +418,7 @@ __device__ __forceinline__ void finish_item(const Kv4AttnArgs& a, NWave<D, RB>& 
     const int64_t token = w.r.first + row / a.group;
     const int head = w.head * a.group + row % a.group;
     if (a.lse && g == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(s.m[b], l, a.scale);
-    const float inv = lr == 0.f ? 0.f : 1.0f / lr;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) put4(a, token, head * D + 16 * d + 4 * g, s.acc[b][d] * inv);
   }
@@ -436,46 +436,37 @@ __device__ __forceinline__ void follow(const Kv4AttnArgs& a, NWave<D, RB>& s, co
     // (a row whose scores are all -inf so far keeps its zeros)
     const float alpha = s.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s.m[b] - m) * a.scale_log2);
     s.l[b] *= alpha;
-    s.lr[b] *= alpha;
 #pragma unroll
     for (int d = 0; d < NCfg<D>::dBlocks; ++d) s.acc[b][d] *= alpha;
     s.m[b] = m;
   }
 }
 
-// The weights as product operands: rounded to bf16, and (F = 2 and 3) what the rounding left,
-// rounded again; and their sums, of the weights and (F = 1) of the rounded ones. An fp32 output
-// takes all 24 bits of a weight (F = 3), a bf16 one 16 where the pages' bytes bound the call (16
-// rows; 2^-17 of a weight is nothing beside its own rounding) and 8 where the products do,
-// normalised by the sum of the rounded weights (2^-9 of a weight, as in chunk attention: the
-// output's error is 1.35 times that of its own rounding).
+// The weights as product operands, rounded to bf16, what the rounding left, rounded again, and (F =
+// 3) once more; and their sum. An fp32 output takes all 24 bits of a weight (F = 3), a bf16 one 16
+// (F = 2: 2^-16 of a weight is nothing beside its own rounding) in every tile, so that neither the
+// batch that a row is in nor max_q decides how exact it is.
 template <int F>
-__device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float scale_log2, bf16x8 (&p)[F], float& sum,
-                                          float& rounded) {
+__device__ __forceinline__ void weights16(const f32x4 (&sc)[2], float m, float scale_log2, bf16x8 (&p)[F], float& sum) {
   const float mc = m == -INFINITY ? 0.f : m * scale_log2;
   float s[2] = {0.f, 0.f};
-  rounded = 0.f;
+  const Less less;
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], scale_log2, -mc));
-    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][(i & 3) + 1], scale_log2, -mc));
+    float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], scale_log2, -mc));
+    float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][(i & 3) + 1], scale_log2, -mc));
     s[0] += e0;
     s[1] += e1;
     const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
     p[0][i] = hi[0];
     p[0][i + 1] = hi[1];
-    if constexpr (F > 1) {
-      float r0 = e0 - (float)hi[0], r1 = e1 - (float)hi[1];  // (exact)
+    less(e0, e1, hi);
 #pragma unroll
-      for (int f = 1; f < F; ++f) {
-        const bf16x2 lo = {(__bf16)r0, (__bf16)r1};
-        p[f][i] = lo[0];
-        p[f][i + 1] = lo[1];
-        r0 -= (float)lo[0];
-        r1 -= (float)lo[1];
-      }
-    } else {
-      rounded = __builtin_amdgcn_fdot2_f32_bf16(hi, bf16x2{(__bf16)1.f, (__bf16)1.f}, rounded, false);
+    for (int f = 1; f < F; ++f) {
+      const bf16x2 lo = {(__bf16)e0, (__bf16)e1};
+      p[f][i] = lo[0];
+      p[f][i + 1] = lo[1];
+      if (f + 1 < F) less(e0, e1, lo);
     }
   }
   sum = s[0] + s[1];
@@ -558,23 +549,20 @@ __device__ __forceinline__ void meet_block(const Kv4AttnArgs& a, NWave<D, RB>& s
       }
   }
   bf16x8 p[RB][F];
-  float sum[RB], rounded[RB];
+  float sum[RB];
   bool far = false;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b], rounded[b]);
+    weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b]);
     far = far || sum[b] > kShFar || s.m[b] == -INFINITY;
   }
   if (__any(far)) {
     follow<D, RB>(a, s, sc);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b], rounded[b]);
+    for (int b = 0; b < RB; ++b) weights16<F>(sc[b], s.m[b], a.scale_log2, p[b], sum[b]);
   }
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    s.l[b] += sum[b];
-    s.lr[b] += F > 1 ? sum[b] : rounded[b];
-  }
+  for (int b = 0; b < RB; ++b) s.l[b] += sum[b];
 
   // O^T += V^T P^T
 #pragma unroll
@@ -598,11 +586,11 @@ __device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D
   };
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    const float l = quad_sum(s.l[b]), lr = quad_sum(s.lr[b]);
+    const float l = quad_sum(s.l[b]);
     __syncthreads();  // the stages, or the rows before, have been read
 #pragma unroll
     for (int d = 0; d < C::dBlocks; ++d) *block(wave, d) = s.acc[b][d];
-    if (g == 0) stats[wave][m16] = f32x4{s.m[b], l, lr, 0.f};
+    if (g == 0) stats[wave][m16] = f32x4{s.m[b], l, 0.f, 0.f};
     __syncthreads();
     f32x4 st[kShWaves];
 #pragma unroll
@@ -617,7 +605,6 @@ __device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D
     for (int w = 0; w < kShWaves; ++w) {
       const float e = st[w][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st[w][0] - m) * a.scale_log2);
       all[1] += st[w][1] * e;
-      all[2] += st[w][2] * e;
 #pragma unroll
       for (int d = 0; d < kOwn; ++d) o[d] += *block(w, wave * kOwn + d) * e;
     }
@@ -627,7 +614,7 @@ __device__ __forceinline__ void finish_group(const Kv4AttnArgs& a, const NWave<D
       const int64_t token = item.r.first + row / a.group;
       const int head = item.head * a.group + row % a.group;
       if (a.lse && wave == 0 && g == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(m, all[1], a.scale);
-      const float inv = all[2] == 0.f ? 0.f : 1.0f / all[2];
+      const float inv = all[1] == 0.f ? 0.f : 1.0f / all[1];
 #pragma unroll
       for (int d = 0; d < kOwn; ++d) put4(a, token, head * D + 16 * (wave * kOwn + d) + 4 * g, o[d] * inv);
       continue;
@@ -912,10 +899,7 @@ __global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnA
     start_rows<D, RB>(a, w, rows, at.head, at.r.first, (int64_t)at.tile * TR + wave * RB * kBlk, at.r.rows, lane);
     piece_keys<D, F>(a, w, (lds_byte*)smem, Source{at.b, at.head, at.r.len, at.block, at.block + n}, wave, tid, lay);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      w.l[b] = pair_sum32(w.l[b]);
-      w.lr[b] = pair_sum32(w.lr[b]);
-    }
+    for (int b = 0; b < RB; ++b) w.l[b] = pair_sum32(w.l[b]);
     const bool last = at.block + n == at.r.blocks, whole = last && at.item >= u0;
     const int hh = lane >> 5;
 #pragma unroll
@@ -923,7 +907,7 @@ __global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnA
       if (!rows.live[b]) continue;
       if (whole) {
         if (a.lse && hh == 0) a.lse[(int64_t)rows.head[b] * a.n_rows + rows.token[b]] = lse_of(w.m[b], w.l[b], a.scale);
-        const float inv = w.lr[b] == 0.f ? 0.f : 1.0f / w.lr[b];
+        const float inv = w.l[b] == 0.f ? 0.f : 1.0f / w.l[b];
 #pragma unroll
         for (int d = 0; d < C::dBlocks; ++d)
 #pragma unroll
@@ -934,7 +918,7 @@ __global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnA
         continue;
       }
       const int64_t part = (2 * run + (at.item >= u0 ? 1 : 0)) * TR + wave * RB * kBlk + b * kBlk + (lane & 31);
-      if (hh == 0) *(f32x4*)(a.part_stat + 4 * part) = f32x4{w.m[b], w.l[b], w.lr[b], 0.f};
+      if (hh == 0) *(f32x4*)(a.part_stat + 4 * part) = f32x4{w.m[b], w.l[b], 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < C::dBlocks; ++d)
 #pragma unroll
@@ -951,15 +935,14 @@ __global__ __launch_bounds__(kWideWaves * 64) void attn_kv4_wide_kernel(Kv4AttnA
 
 // One part of a row into its running join.
 struct Joined {
-  float m = -INFINITY, l = 0.f, lr = 0.f;
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
 };
-__device__ __forceinline__ void join_part(Joined& r, float scale_log2, float m, float l, float lr, const f32x4& o) {
+__device__ __forceinline__ void join_part(Joined& r, float scale_log2, float m, float l, const f32x4& o) {
   const float top = fmaxf(r.m, m);
   const float ea = r.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((r.m - top) * scale_log2);
   const float eb = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * scale_log2);
   r.l = r.l * ea + l * eb;
-  r.lr = r.lr * ea + lr * eb;
 #pragma unroll
   for (int k = 0; k < 4; ++k) r.o[k] = r.o[k] * ea + o[k] * eb;
   r.m = top;
@@ -1014,18 +997,18 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
-          if (i0 + i < end) join_part(j, a.scale_log2, st[i][0], st[i][1], st[i][2], o[i]);
+          if (i0 + i < end) join_part(j, a.scale_log2, st[i][0], st[i][1], o[i]);
       }
     }
     if (slices > 1) {
       part_o[threadIdx.x] = j.o;
-      if (c == 0) part_stat[group] = f32x4{j.m, j.l, j.lr, 0.f};
+      if (c == 0) part_stat[group] = f32x4{j.m, j.l, 0.f, 0.f};
       __syncthreads();
       if (slice == 0)
         for (int i = 1; i < slices; ++i) {
           const int other = i * side + group;
           const f32x4 st = part_stat[other];
-          join_part(j, a.scale_log2, st[0], st[1], st[2], part_o[other * kLanes + c]);
+          join_part(j, a.scale_log2, st[0], st[1], part_o[other * kLanes + c]);
         }
       __syncthreads();
     }
@@ -1034,7 +1017,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_kv4_join_kernel(Kv4AttnArgs
     const int64_t token = r.first + at / a.group;
     const int head = r.head * a.group + at % a.group;
     if (a.lse && c == 0) a.lse[(int64_t)head * a.n_rows + token] = lse_of(j.m, j.l, a.scale);
-    const float inv = j.lr == 0.f ? 0.f : 1.0f / j.lr;
+    const float inv = j.l == 0.f ? 0.f : 1.0f / j.l;
     put4(a, token, head * D + 4 * c, j.o * inv);
   }
 }
@@ -1048,10 +1031,9 @@ hipError_t launch_join(const Kv4AttnArgs& a, hipStream_t stream) {
 }
 template <int D, int RB>
 hipError_t launch_narrow(const Kv4AttnArgs& a, hipStream_t stream) {
-  constexpr int F = RB == 1 ? 2 : 1;  // (of a bf16 output)
   const unsigned grid = (unsigned)(a.item_units ? a.most_runs : (a.most_runs + kShWaves - 1) / kShWaves);
-  auto kernel = a.item_units ? (a.out_bf16 ? attn_kv4_kernel<D, RB, F, true> : attn_kv4_kernel<D, RB, 3, true>)
-                             : (a.out_bf16 ? attn_kv4_kernel<D, RB, F, false> : attn_kv4_kernel<D, RB, 3, false>);
+  auto kernel = a.item_units ? (a.out_bf16 ? attn_kv4_kernel<D, RB, 2, true> : attn_kv4_kernel<D, RB, 3, true>)
+                             : (a.out_bf16 ? attn_kv4_kernel<D, RB, 2, false> : attn_kv4_kernel<D, RB, 3, false>);
   kernel<<<grid, kShThreads, 0, stream>>>(a);
   return launch_join<D, kShWaves>(a, stream);
 }
@@ -1059,7 +1041,7 @@ template <int D>
 hipError_t launch_wide(const Kv4AttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((a.most_runs + kAXcds - 1) / kAXcds * kAXcds);
   if (a.out_bf16)
-    attn_kv4_wide_kernel<D, 1><<<grid, kWideWaves * 64, 0, stream>>>(a);
+    attn_kv4_wide_kernel<D, 2><<<grid, kWideWaves * 64, 0, stream>>>(a);
   else
     attn_kv4_wide_kernel<D, 3><<<grid, kWideWaves * 64, 0, stream>>>(a);
   return launch_join<D, 1>(a, stream);

@@ -91,6 +91,25 @@ __device__ __forceinline__ bf16x8 read_v1(const SWave<D, RB>& w, lds_char* blk, 
         (ISPA_LDS s16x4*)(blk + w.vad[i][o % C::dBlocks] + C::tileBytes + 16 * (o / C::dBlocks) * C::rowBytes));
   return u.v;
 }
+
+// x and y less the pair of numbers that they were rounded to, exactly: dot products with (-1, 0) and
+// (0, -1), half the instructions of taking the pair apart. (The factors in registers: the compiler
+// writes (-1, 0) as the instruction's own constant -1.0, which the dot product reads as (0, -1).)
+struct Less {
+  bf16x2 low, high;
+  __device__ __forceinline__ Less() {
+    uint32_t l, h;
+    asm("s_mov_b32 %0, 0xbf80" : "=s"(l));
+    asm("s_mov_b32 %0, 0xbf800000" : "=s"(h));
+    low = __builtin_bit_cast(bf16x2, l);
+    high = __builtin_bit_cast(bf16x2, h);
+  }
+  __device__ __forceinline__ void operator()(float& x, float& y, bf16x2 pair) const {
+    x = __builtin_amdgcn_fdot2_f32_bf16(pair, low, x, false);
+    y = __builtin_amdgcn_fdot2_f32_bf16(pair, high, y, false);
+  }
+};
+
 // The weights of a block as product operands: rounded to bf16, and (F = 2) what the
 // rounding left, rounded again. Up to 128 rows the keys' bytes bound the work and the
 // second product is free: the weights then keep 16 bits, and an output's error is that of
@@ -104,19 +123,18 @@ struct SWeights {
   bf16x8 p[F][2];
 };
 template <int F>
-__device__ __forceinline__ void put_pair(SWeights<F>& p, int i, float e0, float e1, float& rounded) {
+__device__ __forceinline__ void put_pair(SWeights<F>& p, int i, float e0, float e1, float& rounded, const Less& less) {
   const bf16x2 hi = {(__bf16)e0, (__bf16)e1};
   p.p[0][i / 8][i % 8] = hi[0];
   p.p[0][i / 8][i % 8 + 1] = hi[1];
   if constexpr (F > 1) {
-    float r0 = e0 - (float)hi[0], r1 = e1 - (float)hi[1];  // (exact)
+    less(e0, e1, hi);
 #pragma unroll
     for (int f = 1; f < F; ++f) {
-      const bf16x2 lo = {(__bf16)r0, (__bf16)r1};
+      const bf16x2 lo = {(__bf16)e0, (__bf16)e1};
       p.p[f][i / 8][i % 8] = lo[0];
       p.p[f][i / 8][i % 8 + 1] = lo[1];
-      r0 -= (float)lo[0];
-      r1 -= (float)lo[1];
+      if (f + 1 < F) less(e0, e1, lo);
     }
   } else {
     const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
@@ -197,13 +215,14 @@ __device__ __forceinline__ void weights(const A& a, const SWave<D, RB>& w, int b
                                         SWeights<F>& p, float& sum, float& rounded) {
   const float mc = w.m[b] == -INFINITY ? 0.f : w.m[b] * a.scale_log2;
   float s[2] = {0.f, 0.f}, r[2] = {0.f, 0.f};
+  const Less less;
 #pragma unroll
   for (int i = 0; i < 16; i += 2) {
     const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -mc));
     const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -mc));
     s[0] += e0;
     s[1] += e1;
-    put_pair<F>(p, i, e0, e1, r[i / 2 % 2]);
+    put_pair<F>(p, i, e0, e1, r[i / 2 % 2], less);
   }
   sum = s[0] + s[1];
   rounded = r[0] + r[1];
@@ -224,6 +243,7 @@ __device__ __forceinline__ void pipelined(const A& a, SWave<D, RB>& w, lds_char*
   constexpr int kEach = RB * F;                       // products of a V operand
   constexpr int kSteps = kEach * kV + RB * kK;        // matrix instructions
   constexpr int kPairs = 8 * RB;
+  const Less less;
   bf16x8 k[kK];
   SWeights<F> pn[RB];
   float mc[RB], s1[RB], r1[RB];
@@ -254,7 +274,7 @@ __device__ __forceinline__ void pipelined(const A& a, SWave<D, RB>& w, lds_char*
       const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[b][r + 1], a.scale_log2, -mc[b]));
       sum[b] += e0;
       s1[b] += e1;
-      put_pair<F>(pn[b], r, e0, e1, i % 2 == 0 ? rounded[b] : r1[b]);
+      put_pair<F>(pn[b], r, e0, e1, i % 2 == 0 ? rounded[b] : r1[b], less);
     }
     beside(t, kSteps);
     if constexpr (PINNED) __builtin_amdgcn_sched_barrier(0);
