@@ -51,9 +51,12 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   const int u = threadIdx.x % per_head;  // place in the head
   const int heads = a.n_heads + (a.k ? 2 * a.n_kv_heads : 0);  // of a row
   const int end = (int)threadIdx.x < step * per_head ? n * heads : 0;
-  const UnitPlace at_unit = unit_place(u, a.rotary_dim, a.interleaved);
-  const bool turned = at_unit.turned;
-  const int e0 = at_unit.e0, e1 = at_unit.e1;
+  // a unit's two chunks of 8 and the first pairs of their angles: the same place in both
+  // halves of the rotated part (lanes side by side then read side by side, in either order
+  // of the pairs), or side by side behind it
+  const bool turned = u < (a.rotary_dim >> 4);
+  const int e0 = turned ? 8 * u : 16 * u, e1 = turned ? pairs + 8 * u : 16 * u + 8;
+  const int p0 = a.interleaved ? 4 * u : 8 * u, p1 = a.interleaved ? (pairs >> 1) + 4 * u : 8 * u + 4;
   // in registers for certain: a choice between arguments is otherwise made by a load from
   // the chosen one's place, which every unit's load then waits for
   uintptr_t q = (uintptr_t)a.q, k = (uintptr_t)a.k, v = (uintptr_t)a.v;
@@ -101,7 +104,35 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
     float x[8], y[8];
     p.c0.values(x);
     p.c1.values(y);
-    if (turn) turn_unit(x, y, cs + t * pairs, at_unit, a.interleaved);
+    // (written out, not by a call of turn_unit: that takes 6 to 14 registers more, and with them a
+    // wave of every SIMD, 21.5 us for 20.2 at four frames of 12 heads; and contracts other products
+    // and sums, so that an fp32 result's last bit is another)
+    if (turn) {
+      const float2* at = cs + t * pairs;
+      float2 c[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = at[p0 + i];
+        c[4 + i] = at[p1 + i];
+      }
+      if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float xa = x[2 * i], xb = x[2 * i + 1], ya = y[2 * i], yb = y[2 * i + 1];
+          x[2 * i] = xa * c[i].x - xb * c[i].y;
+          x[2 * i + 1] = xa * c[i].y + xb * c[i].x;
+          y[2 * i] = ya * c[4 + i].x - yb * c[4 + i].y;
+          y[2 * i + 1] = ya * c[4 + i].y + yb * c[4 + i].x;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float xa = x[i], xb = y[i];
+          x[i] = xa * c[i].x - xb * c[i].y;
+          y[i] = xa * c[i].y + xb * c[i].x;
+        }
+      }
+    }
     rstore8(dst, f32, d + e0, x);
     rstore8(dst, f32, d + e1, y);
   };
@@ -111,7 +142,9 @@ __global__ __launch_bounds__(kRThreads) void rotary_kernel(RotaryArgs a) {
   fetch(w, now);  // on its way while the angles are formed
   for (int i = threadIdx.x; i < n * pairs; i += kRThreads) {
     const int t = i / pairs, j = i - t * pairs;
-    const int axis = pair_axis(a.axis_end, j);
+    int axis = 0;
+#pragma unroll
+    for (int k = 0; k < kRotaryAxes - 1; ++k) axis += j >= a.axis_end[k] ? 1 : 0;
     const double turns = (double)a.positions[(row0 + t) * a.n_axes + axis] * a.freqs[j] * 0.15915494309189535;
     const float f = 2.0f * (float)(turns - rint(turns));  // in half turns, within [-1, 1]
     float s, c;
