@@ -1197,15 +1197,33 @@ def norm_rotary_backward(d_q_out, d_k_out, q, k, positions, freqs, n_heads, n_kv
 
 def kv4_cache(n_pages, page_size, n_kv_heads, head_dim, device=None):
     """An empty 4-bit cache (zeros): uint8 [n_pages, n_kv_heads, bytes of a page of a head], for
-    page_size tokens a page, a power of two from 32 to 65536 (layout: include/ispa.h)."""
+    page_size tokens a page, a power of two from 32 to 65536 (layout: include/ispa.h).
+
+    The tensor has the attribute page_size, by which the calls below refuse it for another
+    head_dim: the bytes alone do not tell 2 n tokens of 64 values from n of 128. torch.save and
+    deepcopy keep it; clones, views and moves to a device do not: give page_size to the calls, or
+    set the attribute."""
     nbytes = lib().ispa_kv4_page_bytes(int(page_size), int(head_dim))
     if nbytes == 0:
         raise IspaError(ISPA_ERR_INVALID_ARG, "ispa_kv4_page_bytes")
-    return torch.zeros((int(n_pages), int(n_kv_heads), nbytes), dtype=torch.uint8,
-                       device="cuda" if device is None else device)
+    cache = torch.zeros((int(n_pages), int(n_kv_heads), nbytes), dtype=torch.uint8,
+                        device="cuda" if device is None else device)
+    cache.page_size = int(page_size)
+    return cache
 
 
-def _kv4(cache, page_table, head_dim, dev=None):
+def _kv4_page_size(cache, head_dim, page_size):
+    """Tokens of a page of head_dim values, if the cache's bytes, its attribute and the caller agree."""
+    nbytes, per = cache.shape[2], head_dim + head_dim // 16
+    if per < 1 or nbytes % per:
+        raise ValueError(f"cache must hold whole tokens of {per} bytes a head: it is one of another head_dim")
+    for known in (page_size, getattr(cache, "page_size", None)):
+        if known is not None and known * per != nbytes:
+            raise ValueError(f"cache must have pages of {known} tokens: for head_dim {head_dim} it has {nbytes // per}")
+    return nbytes // per
+
+
+def _kv4(cache, page_table, head_dim, page_size, dev=None):
     """Checks a 4-bit cache and its table; returns (n_pages, page_size, n_req, max_pages, n_kv_heads)."""
     if not (isinstance(cache, torch.Tensor) and isinstance(page_table, torch.Tensor) and cache.dtype == torch.uint8
             and page_table.dtype == torch.int32 and cache.is_cuda and cache.dim() == 3 and page_table.dim() == 2
@@ -1213,27 +1231,25 @@ def _kv4(cache, page_table, head_dim, dev=None):
             and page_table.is_contiguous()):
         _require(cache, "cache", torch.uint8, dev, ndim=3)
         _require(page_table, "page_table", torch.int32, cache.device)
-    n_pages, n_kv_heads, nbytes = cache.shape
-    per = head_dim + head_dim // 16
-    if per < 1 or nbytes % per:
-        raise ValueError(f"cache must hold whole tokens of {per} bytes a head: it is one of another head_dim")
+    n_pages, n_kv_heads, _ = cache.shape
     n_req, max_pages = page_table.shape
-    return n_pages, nbytes // per, n_req, max_pages, n_kv_heads
+    return n_pages, _kv4_page_size(cache, head_dim, page_size), n_req, max_pages, n_kv_heads
 
 
 def kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, n_kv_heads=None, norm="none", q_weight=None,
                k_weight=None, q_bias=None, k_bias=None, eps=1e-6, axes=None, interleaved=True, amplitude=1.0, q_out=None,
-               q_start=None):
+               q_start=None, page_size=None):
     """New tokens into a 4-bit cache in one launch (ispa_kv4_append): q normalised and rotated
     into q_out, k normalised and rotated into the place of its row, v beside it.
 
     q [rows, n_heads * head_dim], k and v [rows, n_kv_heads * head_dim] of one dtype; norm
     "none", "rms" or "layer" over each head of q and k, with fp32 [head_dim] weights and biases;
-    cache as from kv4_cache, page_table int32 [n_req, max_pages]; slots int64 [rows] as from
-    slot_map with the capacity max_pages * page_size. Returns q_out (bf16 by default; q_out=q
-    works in place). A row without a place (slot -1, a page outside the pool) reaches no cache,
-    its query is turned all the same; with q_start (slot_map's, int32 [n_req + 1]) a given q_out
-    keeps what it has in the padding behind q_start[n_req].
+    cache as from kv4_cache (page_size: its tokens a page, checked; None: as the cache says),
+    page_table int32 [n_req, max_pages]; slots int64 [rows] as from slot_map with the capacity
+    max_pages * page_size. Returns q_out (bf16 by default; q_out=q works in place). A row without
+    a place (slot -1, a page outside the pool) reaches no cache, its query is turned all the same;
+    with q_start (slot_map's, int32 [n_req + 1]) a given q_out keeps what it has in the padding
+    behind q_start[n_req].
     """
     L = lib()
     if norm not in _NORMS:
@@ -1245,7 +1261,7 @@ def kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, n_k
         raise ValueError("q, k and v must have the same number of rows")
     _head_vectors(dev, head_dim, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias, k_bias=k_bias)
     pairs, n_axes = _angles(positions, freqs, axes, dev, rows)
-    n_pages, page_size, n_req, max_pages, heads = _kv4(cache, page_table, head_dim, dev)
+    n_pages, page_size, n_req, max_pages, heads = _kv4(cache, page_table, head_dim, page_size, dev)
     if heads != n_kv_heads:
         raise ValueError("cache must have n_kv_heads heads")
     _require(slots, "slots", torch.int64, dev, ndim=1)
@@ -1271,13 +1287,13 @@ def kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, n_k
     return q_out
 
 
-def kv4_read(cache, page_table, slots, head_dim, out_dtype=torch.bfloat16, k=None, v=None):
+def kv4_read(cache, page_table, slots, head_dim, out_dtype=torch.bfloat16, k=None, v=None, page_size=None):
     """Rows of a 4-bit cache as the values that they hold (ispa_kv4_read): (k, v), each [rows,
     n_kv_heads * head_dim] of out_dtype, of the places that slots (int64 [rows], as for
-    kv4_append) stands for; zeros where there is no place. For example the rows of a history
-    that a LocalKV or a bf16 cache takes over."""
+    kv4_append) stands for; zeros where there is no place; page_size as for kv4_append. For
+    example the rows of a history that a LocalKV or a bf16 cache takes over."""
     L = lib()
-    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, int(head_dim))
+    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, int(head_dim), page_size)
     dev = cache.device
     _require(slots, "slots", torch.int64, dev, ndim=1)
     rows, kv = slots.shape[0], n_kv_heads * int(head_dim)
@@ -1301,11 +1317,11 @@ def kv4_read(cache, page_table, slots, head_dim, out_dtype=torch.bfloat16, k=Non
 
 
 def attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, max_q=None, scale=0.0, out=None, lse=None,
-             out_dtype=torch.bfloat16, need_lse=True):
+             out_dtype=torch.bfloat16, need_lse=True, page_size=None):
     """Attention of a batch of requests over a 4-bit cache (ispa_attn_kv4).
 
-    q [n_rows, n_heads * d] bf16, request b's rows from q_start[b] on; cache and page_table as
-    for kv4_append, the key heads are the cache's; q_start int32 [n_req + 1] and cache_lens
+    q [n_rows, n_heads * d] bf16, request b's rows from q_start[b] on; cache, page_table and
+    page_size as for kv4_append, the key heads are the cache's; q_start int32 [n_req + 1] and cache_lens
     int32 [n_req] on the device: request b sees its places [0, cache_lens[b]). max_q: most rows
     of a request, a hint (None: the mean). Returns (out, lse); rows behind q_start[n_req] are
     left as they were (uninitialised where out or lse is not given).
@@ -1318,7 +1334,7 @@ def attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, max_q=None, sca
     if n_heads < 1 or hidden % n_heads:
         raise ValueError("hidden size must be a multiple of n_heads")
     head_dim = hidden // n_heads
-    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, head_dim, dev)
+    n_pages, page_size, n_req, max_pages, n_kv_heads = _kv4(cache, page_table, head_dim, page_size, dev)
     if n_heads % n_kv_heads:
         raise ValueError("n_heads must be a multiple of the cache's heads")
     _require(q_start, "q_start", torch.int32, dev, ndim=1)
