@@ -796,7 +796,7 @@ int ispa_kv4_append(const void* q, int64_t ld_q, const void* k, int64_t ld_k, co
  * Rows of a 4-bit cache as the values that they hold (exact in either type): k and v
  * [rows, n_kv_heads * head_dim] of out_dtype, contiguous, of the places that slots (device
  * int64 [rows], as for ispa_kv4_append; one may come more than once) stands for; zeros where
- * there is no place. rows * n_kv_heads * head_dim < 2^34. Asynchronous on `stream`.
+ * there is no place. rows * n_kv_heads * head_dim <= 2^34 - 1024. Asynchronous on `stream`.
  */
 int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const int32_t* page_table, int32_t n_req,
                   int64_t max_pages, const int64_t* slots, int64_t rows, int32_t n_kv_heads, int32_t head_dim, void* k,

@@ -1350,7 +1350,8 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
   if (st != ISPA_OK) return st;
   const int64_t kv = (int64_t)n_kv_heads * head_dim;
   if (!slots || !k || !v || any_misaligned({k, v}) || any_misaligned({slots}, 7u)) return ISPA_ERR_INVALID_ARG;
-  if (rows < 0 || rows >= ((int64_t)1 << 34) / kv) return ISPA_ERR_INVALID_ARG;
+  // (a workgroup of the launch is 1024 values of k and of v: fewer than 2^24 of them)
+  if (rows < 0 || rows > (((int64_t)1 << 34) - 1024) / kv) return ISPA_ERR_INVALID_ARG;
   const size_t bytes = (size_t)rows * kv * dtype_size(out_dtype);
   const Span sk{k, bytes}, sv{v, bytes}, ss{slots, (size_t)rows * 8};
   if (meets(sk, {sv, pages, table, ss}) || meets(sv, {pages, table, ss})) return ISPA_ERR_INVALID_ARG;
