@@ -877,8 +877,8 @@ def rotary_frequencies(axis_pairs, base=10000.0, scaling="none", factor=1.0, ori
 def _angles(positions, freqs, axes, dev, rows):
     pairs, n_axes, total = _pairs(axes, freqs) if isinstance(freqs, torch.Tensor) and freqs.dim() == 1 else (None, 0, -1)
     # one expression for the usual case; the reasons only when it fails
-    if (isinstance(positions, torch.Tensor) and positions.dtype == torch.int32 and positions.numel() == rows * n_axes
-            and 0 < positions.dim() <= 2 and positions.shape[0] == rows and positions.device == dev
+    if (rows and pairs is not None and isinstance(positions, torch.Tensor) and positions.dtype == torch.int32
+            and positions.numel() == rows * n_axes and 0 < positions.dim() <= 2 and positions.shape[0] == rows and positions.device == dev
             and positions.is_contiguous() and freqs.dtype == torch.float64 and freqs.device == dev
             and freqs.is_contiguous() and total == freqs.shape[0]):
         return pairs, n_axes
