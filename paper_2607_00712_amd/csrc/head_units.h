@@ -110,6 +110,39 @@ __device__ __forceinline__ void turn_unit(T (&x)[8], T (&y)[8], const T2* at, co
   turn_pairs(x, y, c, interleaved);
 }
 
+// Cosine and sine in fp64: the angle less quarter turns, in two parts of pi / 2, and the series
+// up to x^17 / 17!, of which the next terms are below 2^-58 at pi / 4. (The library's function,
+// for all arguments, takes 124 registers, and with them a wave of the append's from each SIMD.)
+// LOADED: the series' factors come from memory at every call. As numbers in the code they leave a
+// loop around the call, and the 32 registers that hold them cost the backward pass of the head
+// norms a third of its waves (fp32 with biases, 4680 rows of 12 + 12 heads 35.5 -> 41.5 us); where
+// the call is outside of such loops they are 0.1 us faster.
+#define ISPA_SINE {1 / 355687428096000., -1 / 1307674368000., 1 / 6227020800., -1 / 39916800., 1 / 362880., -1 / 5040., 1 / 120., -1 / 6.}
+#define ISPA_COSINE {1 / 20922789888000., -1 / 87178291200., 1 / 479001600., -1 / 3628800., 1 / 40320., -1 / 720., 1 / 24., -1 / 2.}
+__constant__ const double kSine[8] = ISPA_SINE, kCosine[8] = ISPA_COSINE;
+template <bool LOADED>
+__device__ __forceinline__ double2 angle_of(double angle) {
+  typedef const __attribute__((address_space(4))) double* Factors;
+  constexpr double sine_of[8] = ISPA_SINE, cosine_of[8] = ISPA_COSINE;
+  Factors sines = (Factors)kSine, cosines = (Factors)kCosine;
+  if constexpr (LOADED) asm volatile("" : "+s"(sines), "+s"(cosines));
+  const double q = rint(angle * 0.6366197723675814);
+  const double x = fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, angle)), z = x * x;
+  double s = LOADED ? sines[0] : sine_of[0], c = LOADED ? cosines[0] : cosine_of[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    s = fma(s, z, LOADED ? sines[i] : sine_of[i]);
+    c = fma(c, z, LOADED ? cosines[i] : cosine_of[i]);
+  }
+  s = fma(x * z, s, x);
+  c = fma(c, z, 1.);
+  const int quarter = (int)fma(-4., rint(q * 0.25), q);
+  const double cosine = quarter & 1 ? s : c, sine = quarter & 1 ? c : s;
+  return make_double2((quarter + 1) & 2 ? -cosine : cosine, quarter & 2 ? -sine : sine);
+}
+#undef ISPA_SINE
+#undef ISPA_COSINE
+
 // A sum over the `lanes` (1, 2, 4, 8 or 16) neighbouring lanes of a head: every lane gets it.
 template <int CTRL>
 __device__ __forceinline__ float head_dpp(float x) {

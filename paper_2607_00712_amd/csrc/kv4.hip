@@ -34,34 +34,6 @@ constexpr int kQMaxTokens = 8;
 constexpr int kQPairs = 64;     // rotary_dim / 2 at most
 constexpr int kQValues = 1024;  // values of a wave's run of heads
 
-// Cosine and sine in fp64: the angle less quarter turns, in two parts of pi / 2, and the series
-// up to x^17 / 17!, of which the next terms are below 2^-58 at pi / 4. (The library's function,
-// for all arguments, takes 124 registers, and with them a wave of the kernel's from each SIMD.)
-__device__ __forceinline__ double2 angle_of(double angle) {
-  const double q = rint(angle * 0.6366197723675814);
-  const double x = fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, angle)), z = x * x;
-  double s = 1 / 355687428096000., c = 1 / 20922789888000.;  // 17!, 16!
-  s = fma(s, z, -1 / 1307674368000.);
-  c = fma(c, z, -1 / 87178291200.);
-  s = fma(s, z, 1 / 6227020800.);
-  c = fma(c, z, 1 / 479001600.);
-  s = fma(s, z, -1 / 39916800.);
-  c = fma(c, z, -1 / 3628800.);
-  s = fma(s, z, 1 / 362880.);
-  c = fma(c, z, 1 / 40320.);
-  s = fma(s, z, -1 / 5040.);
-  c = fma(c, z, -1 / 720.);
-  s = fma(s, z, 1 / 120.);
-  c = fma(c, z, 1 / 24.);
-  s = fma(s, z, -1 / 6.);
-  c = fma(c, z, -0.5);
-  s = fma(x * z, s, x);
-  c = fma(c, z, 1.);
-  const int quarter = (int)fma(-4., rint(q * 0.25), q);
-  const double cosine = quarter & 1 ? s : c, sine = quarter & 1 ? c : s;
-  return make_double2((quarter + 1) & 2 ? -cosine : cosine, quarter & 2 ? -sine : sine);
-}
-
 // To fp32 by rounding to odd.
 __device__ __forceinline__ float to_odd(double x) {
   const float t = (float)x;
@@ -215,7 +187,7 @@ __global__ __launch_bounds__(kQThreads, kQGroups) void kv4_append_kernel(Kv4Appe
   if (row0 >= n_real && !__syncthreads_or(threadIdx.x < (unsigned)n && a.slots[row0 + threadIdx.x] >= 0)) return;
   for (int i = threadIdx.x; i < n * pairs; i += kQThreads) {
     const int t = i / pairs, j = i - t * pairs;
-    const double2 at = angle_of((double)r.positions[(row0 + t) * r.n_axes + pair_axis(r.axis_end, j)] * r.freqs[j]);
+    const double2 at = angle_of<false>((double)r.positions[(row0 + t) * r.n_axes + pair_axis(r.axis_end, j)] * r.freqs[j]);
     cs[t * pairs + pair_slot(j, pairs, r.interleaved)] = make_double2(at.x * r.amplitude, at.y * r.amplitude);
   }
   if (threadIdx.x < (unsigned)n) {

@@ -30,17 +30,15 @@ constexpr int kHMaxPairs = 128;  // rotary_dim / 2
 // workgroups of the backward pass to a compute unit, as many as its registers allow
 constexpr int kBackGroups = 3;
 
-// cos and sin of the pairs of n tokens from row0 on, with the amplitude; sign < 0: of the
-// opposite angles.
-__device__ __forceinline__ void form_angles(const NormRotaryArgs& a, float2* cs, int64_t row0, int n, float sign) {
+// cos and sin of the pairs of n tokens from row0 on, with the amplitude, each rounded once;
+// BACK: of the opposite angles.
+template <bool BACK>
+__device__ __forceinline__ void form_angles(const NormRotaryArgs& a, float2* cs, int64_t row0, int n) {
   const int pairs = a.rotary_dim >> 1;
   for (int i = threadIdx.x; i < n * pairs; i += kHThreads) {
     const int t = i / pairs, j = i - t * pairs;
-    const double turns = (double)a.positions[(row0 + t) * a.n_axes + pair_axis(a.axis_end, j)] * a.freqs[j] *
-                         0.15915494309189535;
-    float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-    cs[i] = make_float2(c * a.amplitude, s * a.amplitude * sign);
+    const double2 at = angle_of<BACK>((double)a.positions[(row0 + t) * a.n_axes + pair_axis(a.axis_end, j)] * a.freqs[j]);
+    cs[i] = make_float2((float)(at.x * a.amplitude), (float)(at.y * (BACK ? -a.amplitude : a.amplitude)));
   }
 }
 
@@ -95,7 +93,7 @@ __global__ __launch_bounds__(kHThreads) void norm_rotary_kernel(NormRotaryArgs a
   keep_vector(vectors[1], a.k_weight, 1.f, a.head_dim);
   keep_vector(vectors[2], a.q_bias, 0.f, a.head_dim);
   keep_vector(vectors[3], a.k_bias, 0.f, a.head_dim);
-  form_angles(a, cs, row0, n, 1.f);
+  form_angles<false>(a, cs, row0, n);
   __syncthreads();
   auto turn = [&](uintptr_t src, int64_t ld, uintptr_t dst, int64_t ld_out, Place at, Unit<F32> p, const float* weight,
                   const float* bias, bool has_bias) __attribute__((always_inline)) {
@@ -178,7 +176,7 @@ __global__ __launch_bounds__(kHThreads) void norm_rotary_back_kernel(NormRotaryA
     };
     fetch(p, g);
     __syncthreads();  // (the angles before have been read)
-    form_angles(a, cs, row0, n, -1.f);
+    form_angles<true>(a, cs, row0, n);
     __syncthreads();
     const int turns = (n * heads + step - 1) / step;
     for (int i = 0; i < turns; ++i) {
