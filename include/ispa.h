@@ -750,9 +750,11 @@ size_t ispa_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t n_heads, 
  * A block is 32 neighbouring values of a head: 4-bit numbers (bit 3 the sign, bits 0-2 one of
  * 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(power - 127). The power is the smallest with no value
  * above 7 times it, within 2^-120 .. 2^125, and each value is rounded to the nearest number,
- * ties to the even code, so that it is off by at most half a step (one fifth of the block's
- * largest value at most: a block whose largest is 5 times its power). A block with an infinity
- * or a NaN has power 255 and reads as NaN.
+ * ties to the even code. It is then off by at most half a step, one fifth of the block's largest
+ * value (a block whose largest is 5 times its power), if that lies within 1.25 * 2^-120 ..
+ * 7 * 2^125: in a block below, values are off by up to 2^-122 (what is not larger becomes 0), and
+ * a value above becomes 6 * 2^125, up to a quarter less. A block with an infinity or a NaN has
+ * power 255 and reads as NaN.
  *
  * In all calls
  *   cache       device uint8 [n_pages, n_kv_heads, ispa_kv4_page_bytes], 16-byte aligned

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2607_00712_amd as ispa
+from kv4_format import decode, encode
 
 BF16 = torch.bfloat16
 OTHER = {64: 128, 128: 64}
@@ -55,3 +56,17 @@ def test_calls_for_another_head_dim(d):
     q = row(4, d)
     with pytest.raises(ValueError, match="pages of"):
         ispa.attn_kv4(q, cache, table, start, lens, 2 if d == 64 else 8)
+
+
+def test_how_far_a_number_is_off():
+    """What include/ispa.h says of the rounding, over the whole range of fp32 (the GPU's numbers are
+    the helper's: test_gpu_kv4.py)."""
+    g = torch.Generator().manual_seed(0)
+    for e in range(-149, 128):
+        x = (1 + torch.rand(40, 32, generator=g, dtype=torch.float64)) * 2.0 ** e
+        x[:, 1:] *= 2.0 ** -torch.randint(0, 6, (40, 31), generator=g) * (torch.randint(0, 2, (40, 31), generator=g) * 2 - 1)
+        x = x.float().double()
+        off, top = (decode(*encode(x)) - x).abs(), x.abs().amax(1, keepdim=True).expand(-1, 32)
+        below, above = top < 1.25 * 2.0 ** -120, x.abs() > 7 * 2.0 ** 125
+        assert (off <= torch.where(below, 2.0 ** -122, torch.where(above, x.abs() / 4, top / 5))).all()
+        assert (decode(*encode(x))[above].abs() == 6 * 2.0 ** 125).all()
