@@ -699,7 +699,8 @@ size_t ispa_attn_shared_workspace_bytes(int64_t prefix_len, int64_t capacity, in
  *               may be k (same dtype and row distance), else they must not overlap the inputs
  *               (other columns of the same wider rows do not)
  * Other arguments as for ispa_rotary; n_kv_heads * head_dim <= 2^20 too. Statistics and
- * arithmetic are fp32 (angles fp64), each output is rounded once. Pointers 16-byte aligned,
+ * arithmetic are fp32 (angles, cosine and sine fp64, rounded once with the amplitude), each output
+ * is rounded once. Pointers 16-byte aligned,
  * row distances multiples of 8 and at most 2^24. Asynchronous on `stream`.
  */
 int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
@@ -722,8 +723,9 @@ int ispa_norm_rotary(const void* q, int64_t ld_q, const void* k, int64_t ld_k, i
  *   workspace   device, 256-byte aligned, at least ispa_norm_rotary_backward_workspace_bytes
  *               bytes for the same sizes on the same device; may be NULL where no gradient of
  *               a vector is wanted. Used only during the call's device work.
- * Row distances as for ispa_norm_rotary. Sums over rows and heads are fp32, in an order that depends on the sizes and the device alone:
- * the same call gives the same bits. Asynchronous on `stream`.
+ * Row distances as for ispa_norm_rotary; without rows nothing is done, for the vectors' gradients
+ * too. Sums over rows and heads are fp32, in an order that depends on the sizes and the device
+ * alone: the same call gives the same bits. Asynchronous on `stream`.
  */
 int ispa_norm_rotary_backward(const void* d_q_out, int64_t ld_gq, const void* d_k_out, int64_t ld_gk, int32_t g_dtype,
                               const void* q, int64_t ld_q, const void* k, int64_t ld_k, int32_t x_dtype, int32_t norm,
@@ -817,7 +819,8 @@ int ispa_kv4_read(const void* cache, int64_t n_pages, int64_t page_size, const i
  *   n_req >= 1; n_rows >= 0 (0: nothing is done); n_rows * n_heads <= 2^26 and
  *               n_req * n_kv_heads <= 2^20
  *   max_q       >= 1: most rows of a request, as far as the host knows; the layout of the work
- *               follows it, the result does not depend on it beyond rounding
+ *               follows it, the result does not depend on it beyond rounding. One layout serves
+ *               the call: requests of very different rows take less time in calls of their own
  *   n_heads     a multiple of n_kv_heads: query head i reads key head i / (n_heads / n_kv_heads)
  *   scale       logit scale; <= 0 selects 1/sqrt(head_dim)
  *   out         [n_rows, n_heads * head_dim] of out_dtype, rows ld_out apart; a query without

@@ -1249,7 +1249,7 @@ def kv4_append(q, k, v, positions, slots, freqs, n_heads, cache, page_table, n_k
     max_pages * page_size. Returns q_out (bf16 by default; q_out=q works in place). A row without
     a place (slot -1, a page outside the pool) reaches no cache, its query is turned all the same;
     with q_start (slot_map's, int32 [n_req + 1]) a given q_out keeps what it has in the padding
-    behind q_start[n_req].
+    behind q_start[n_req]. Nothing is recorded for autograd.
     """
     L = lib()
     if norm not in _NORMS:
@@ -1322,9 +1322,11 @@ def attn_kv4(q, cache, page_table, q_start, cache_lens, n_heads, max_q=None, sca
 
     q [n_rows, n_heads * d] bf16, request b's rows from q_start[b] on; cache, page_table and
     page_size as for kv4_append, the key heads are the cache's; q_start int32 [n_req + 1] and cache_lens
-    int32 [n_req] on the device: request b sees its places [0, cache_lens[b]). max_q: most rows
-    of a request, a hint (None: the mean). Returns (out, lse); rows behind q_start[n_req] are
-    left as they were (uninitialised where out or lse is not given).
+    int32 [n_req] on the device: request b sees its places [0, cache_lens[b]), and its tokens see
+    each other. max_q: most rows of a request, a hint (None: the mean); one layout serves the call,
+    so that a long prompt and single tokens take less time in calls of their own. Returns (out,
+    lse); rows behind q_start[n_req] are left as they were (uninitialised where out or lse is not
+    given). Nothing is recorded for autograd.
     """
     L = lib()
     ld_q = _strided_rows(q, "q", None, torch.bfloat16)

@@ -24,12 +24,13 @@
 //
 // Measured, 128 values a head, two kernels and the launches (a large copy runs at 4.9 TB/s, a
 // reader of the same pages without any arithmetic at 5.4, a large bf16 product at 1223 TFLOP/s):
-// 64 tokens of 32 heads on 8 against up to 16384 keys each 115-119 us (5.3 TB/s of pages), three
-// requests of up to 5 tokens against up to 131072 60-75 us (4.7), one token of 12 heads against
-// 32760 23-24 us (18.5 the runs, of which some 6 are the start of a run and its first block's
-// way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 35-39 us
-// (vector issue 0.51 of the busy cycles, matrix cores 0.16): 17 blocks a wave, its start and end as
-// long as half of them; join 8. Wide tiles below.
+// 64 tokens of 32 heads on 8 against up to 16384 keys each 115-129 us as the draw goes (5.3 TB/s of
+// pages), three requests of up to 5 tokens against up to 131072 67-87 (4.4), one token of 12 heads
+// against 32760 23-25 us (19 the runs, of which some 6 are the start of a run and its first block's
+// way, 5 the join). 24 requests of up to 154 rows of 8 heads of 64 values against up to 4128 41-48 us
+// (vector issue 0.51 of the busy cycles, matrix cores 0.22): 17 blocks a wave, its start and end as
+// long as half of them; join 8; of 128 values 64-67. An fp32 output, with three parts of a weight in
+// place of two, takes 10 to 20% longer in these tiles, 28% in wide ones. Wide tiles below.
 #include "attn_rows.h"
 #include "kv4_units.h"
 
@@ -40,9 +41,10 @@ constexpr int kAXcds = 8;
 constexpr int kWideWaves = 8;
 constexpr int kWideRows = kWideWaves * 32;
 constexpr int kJoinThreads = 512;
-// Workgroups of narrow tiles to a compute unit, as many as the registers allow (64 tokens of 32
-// heads of 64 values on 8 against up to 16384 keys: 74 us with three, 89 with two; tiles of 32
-// rows spill with three and gain nothing).
+// Workgroups of narrow tiles to a compute unit (64 tokens of 32 heads of 64 values on 8 against up
+// to 16384 keys: 74 us with three, 89 with two; 24 requests of up to 154 rows, tiles of 32, 43 us with
+// three, which spill 4 registers, and 44 with two). At 128 values a head tiles of 32 rows have all 256
+// registers of two workgroups and spill 1 to 4 of them.
 constexpr int narrow_groups(int head_dim, int tile_rows) { return head_dim == 64 && tile_rows == 16 ? 3 : 2; }
 constexpr int kInFlight = 2;  // blocks that a wave of narrow tiles has on their way
 
@@ -696,9 +698,11 @@ __global__ __launch_bounds__(kShThreads, narrow_groups(D, 16 * RB)) void attn_kv
 // Steps of 64 keys lie in LDS in bf16, four of them in turn; a thread fetches its share of a
 // step's codes (an eighth of a key, and of its values) two steps ahead into registers and converts
 // it one step ahead, between the matrix instructions of the step before. 4680 rows of 12 heads
-// against 32760 keys: 990 us = 951 TFLOP/s; four waves of 64 rows, which read half as much of LDS,
-// were 6% slower. The vector instructions bound it (140 to a wave's block beside 16 matrix
-// instructions, which are busy 0.43 of the cycles, vector issue 0.58, LDS 0.31).
+// against 32760 keys: 1250-1315 us on different cards, 753-716 TFLOP/s of the attention's operations
+// and 1130-1074 of the products that are made with two parts of a weight, which bound it: 0.92-0.88
+// of a large library product's rate (vector issue 0.50 of the cycles, matrix cores 0.51). With one
+// part, 8 bits of a weight, 950 us; four waves of 64 rows, which read half as much of LDS, were 6%
+// slower then.
 template <int D>
 struct WCfg {
   static constexpr int step = 2;  // blocks
@@ -851,7 +855,7 @@ __device__ __forceinline__ void piece_keys(const Kv4AttnArgs& a, SWave<D, 1>& w,
       const int nv = nv_now >> (8 * kb) & 255;
       if (nv < kBlk) mask<RB>(sc, nv, hh);
       f32x16 next[RB];
-      // (not pinned: the compiler's own order is 2 to 4% faster where codes are converted beside)
+      // (not pinned: the compiler's own order is 1% faster where codes are converted beside)
       pipelined<D, RB, F, false>(a, w, vblk, kblk, sc, next, p, v, sum, rounded, [&](int t, int n) __attribute__((always_inline)) {
         constexpr int kPer = kWords / WC::step;  // words beside a block
 #pragma unroll
@@ -1058,12 +1062,18 @@ hipError_t launch_d(const Kv4AttnArgs& a, hipStream_t stream) {
 size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   // Rows of a tile. Up to 16 rows one block of 16 to a wave, up to 128 two: each tile meets the
   // keys again, but few rows give the chip more runs that way, and tiles of 32 fit what a request
-  // has (64 rows of 32 requests against up to 16384 keys 118 us, and 168 in tiles of 64; 16
-  // requests of up to 128 rows 109 us, and 135 in tiles of 128). Beyond, a workgroup takes 256
-  // rows and meets its keys once (one request's 256 rows of 8 heads against 32768 keys 64 us, 73
-  // in tiles of 32; 512 rows 99 and 121). Requests of one batch mostly differ: several keep the
-  // narrow tiles up to 320 rows (24 requests of up to 154 rows 50 us, 70 in tiles of 256; four of
-  // up to 300 53 and 63).
+  // has (32 requests of 32 rows of 8 heads against up to 16384 keys 75 us, 100 in tiles of 16, 322 in
+  // tiles of 256; 64 requests of 16 rows against up to 4096 41, and 48 in tiles of 32; 16 requests of
+  // up to 128 rows 102, and 195 in tiles of 256). Beyond, a workgroup takes 256 rows and meets its
+  // keys once (one request's rows of 8 heads against 32768 keys: 64 rows 38 us in tiles of 32 and 37
+  // in tiles of 256, 128 rows 52.5 and 51, 256 rows 77 and 74, 512 rows 130 and 116). Several requests
+  // keep the narrow tiles up to 320 rows: unequal ones (24 of up to 154 rows 50 us, 75 in tiles of
+  // 256; four of up to 300 64 and 68.5) and equal ones too, the worst of them where a tile of 256 is
+  // nearly full (8 of 8 heads against 4096 keys: 129 rows 58 us, 64 in tiles of 256; 224 rows 74 and
+  // 71; 320 rows 96 and 114; 16 against 32768: 654 and 706, 927 and 763, 1229 and 1376).
+  // One shape serves the call: a prompt of 4680 tokens beside 63 single ones (32 heads on 8, up to
+  // 16384 keys) takes 2444 us in tiles of 256 and 2229 in tiles of 32; in calls of their own they
+  // take 1740 and 119.
   const int64_t rows = (int64_t)(a->max_q < a->n_rows ? a->max_q : a->n_rows) * a->group;
   a->tile_rows = rows <= 16 ? 16 : rows <= (a->c.n_req > 1 ? 320 : 128) ? 32 : kWideRows;
   const int n_cu = attn_cu_count() > 0 ? attn_cu_count() : 256;  // (sizes may be asked for without a device)
@@ -1083,9 +1093,9 @@ size_t attn_kv4_plan(Kv4AttnArgs* a, int head_dim) {
   // Short caches and few items: an item to a workgroup, and no second launch. Narrow tiles (against
   // the same in equal runs with a join): 64 tokens of 32 heads on 8 against up to 512 keys 12.6 us and
   // 19, 1024 16.9 and 21, 1536 20.5 and 23; one row of 12 heads against up to 1536 16.0 and 16.6, 2048
-  // 19 and 16.5; 60 tokens of 16 heads against up to 1024 26.6 and 27.7, 1536 35.5 and 34.5; 120
-  // against up to 512 33.8 and 32. Wide ones: 1000 rows of 8 heads against up to 768 keys 35.1 and 37.4,
-  // 1024 43.2 and 38.9.
+  // 19 and 16.5; 60 rows of 16 heads against 1024 16.2 and 23.7, 1536 20.4 and 24.0, 2048 25.0 and
+  // 24.5; 8 requests of up to 120 rows of 16 heads against up to 1024 19.1 and 30.8, 1536 28.7 and 31.7.
+  // Wide ones: 1000 rows of 8 heads against 512 keys 32.5 and 41.1, 768 42.8 and 42.4, 1024 53.7 and 44.
   const int64_t items = a->most_items;
   a->item_units = 0;
   if (wide ? blocks <= 24 && items <= n_cu : blocks <= 48 && items <= 6 * n_cu && items * blocks <= 128 * n_cu) {

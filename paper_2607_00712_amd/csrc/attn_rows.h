@@ -114,7 +114,7 @@ struct Less {
 // rounding left, rounded again. Up to 128 rows the keys' bytes bound the work and the
 // second product is free: the weights then keep 16 bits, and an output's error is that of
 // its own rounding. Tiles of 256 rows are bound by the products, three in place of two
-// (6240 rows of 12 heads against 37440 keys 1.49 ms with one part, 2.03 with two). There the
+// (6240 rows of 12 heads against 37440 keys 1.49 ms with one part, 1.97 with two). There the
 // output's type decides: an fp32 output has the weights in 16 bits too, a bf16 one the
 // rounded weights alone, normalised by the sum of the rounded weights (2^-8 of a weight at
 // most, as in chunk attention: the output's error is 1.4 times that of its own rounding).

@@ -16,11 +16,11 @@
 // diverges; the angles are formed once for a workgroup's tokens.
 //
 // Measured, bf16, 128 values a head: four requests' 5800 rows (of 6240 with the padding) of 12 +
-// 12 + 12 heads 21.6 us (3.8 TB/s), with rms norms 26; 64 rows of 32 + 8 + 8 heads 6.4. The first is
+// 12 + 12 heads 22 us (3.7 TB/s), with rms norms 26-27; 64 rows of 32 + 8 + 8 heads 6.4. The first is
 // bound by its fp64 steps (vector issue 0.69 of the cycles that a compute unit has waves) as
 // much as by its bytes, and by the registers that these take: a value's loads wait for the run
 // before, and loads ahead of it gained nothing at four waves to a SIMD and lost 6 us at three.
-// Rows read back: 6240 of 12 + 12 heads 11.7 us (4.2 TB/s), bound by the bytes.
+// Rows read back: 6240 of 12 + 12 heads 11.8 us (4.2 TB/s), bound by the bytes.
 #include "head_units.h"
 #include "kv4_units.h"
 

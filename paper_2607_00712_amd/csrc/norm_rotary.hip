@@ -11,14 +11,15 @@
 //
 // Bound by bytes: each tensor is read and written once. A head's values lie in registers, 16
 // to a thread, and its sums go over at most 16 neighbouring lanes; the angles of a token are
-// formed once for all heads, in fp64, while the first heads are on their way. The weights are
-// read from LDS for every head: held in registers they cost the waves that hide the loads
-// (4680 rows of 40 + 40 heads 51 us). The next head's values are on their way during a head.
+// formed once for all heads, with cosine and sine in fp64, while the first heads are on their way.
+// The weights are read from LDS for every head: held in registers they cost the waves that hide the
+// loads (4680 rows of 40 + 40 heads 51 us). The next head's values are on their way during a head.
 //
 // Measured, bf16, 128 values a head: 4680 rows of 40 + 40 heads 36-38 us (5.0-5.3 TB/s; a large
 // copy runs at 4.9), 64 rows of 32 + 8 heads 5.2 (a launch and one chain of loads); backward with
-// the weights' gradients, 4680 rows of 12 + 12 heads 19.1 us (4.5 TB/s) and 3.8 for the launch
-// that adds the workgroups' sums; 1001 rows of 9 + 3 fp32 heads of 96 11.7 and 3.9.
+// the weights' gradients, 4680 rows of 12 + 12 heads 19.9 us (4.3 TB/s) and 3.8 for the launch
+// that adds the workgroups' sums; 4680 fp32 rows with biases 35.6; 1001 rows of 9 + 3 fp32 heads of
+// 96 11.7 and 3.9.
 #include "head_units.h"
 
 namespace ispa {
